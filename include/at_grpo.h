@@ -72,7 +72,9 @@ enum {
   AT_GRPO_DATA_REWARD = 2,       /* non-finite reward (the response then takes no part) */
   AT_GRPO_DATA_TOKEN_RANGE = 4,  /* token_id outside [0, V) on an unmasked row        */
   AT_GRPO_DATA_SEQLENS = 8,      /* cu_seqlens not monotone within [0, n_tok]         */
-  AT_GRPO_DATA_AGENT_RANGE = 16  /* resp_agent / head_of_agent entry out of range     */
+  AT_GRPO_DATA_AGENT_RANGE = 16, /* resp_agent / head_of_agent entry out of range     */
+  AT_GRPO_DATA_PAGE = 32,        /* page id outside the cache, or a token behind its page table */
+  AT_GRPO_DATA_POSITION = 64     /* position outside the rotation table               */
 };
 
 /* Bits of clip_mask[t] (Eq. 2's clip, decided in log space on d = logp - old_logp, one fp32
@@ -93,7 +95,8 @@ typedef enum {
   AT_GRPO_CALL_HEAD_UPDATE = 5,  /* size does not depend on the other arguments */
   AT_GRPO_CALL_DIAGNOSTICS = 6,
   AT_GRPO_CALL_TOKEN_ENTROPY = 7,
-  AT_GRPO_CALL_POLICY_LOSS_FWD_BWD = 8
+  AT_GRPO_CALL_POLICY_LOSS_FWD_BWD = 8,
+  AT_GRPO_CALL_QK_NORM_ROPE_BWD = 9 /* size does not depend on the other arguments */
 } at_grpo_call;
 
 /*
@@ -346,6 +349,149 @@ int at_grpo_head_update(int32_t dtype, int32_t H, int32_t V, int32_t n_heads, vo
                         float* const* W_master, const float* const* dW, float* const* m,
                         float* const* v, const at_grpo_adam* opt, float* grad_norm,
                         void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * ---- In front of the head: queries, keys and the rollout's cache ---------------------------------
+ * Tree sampling (Alg. 1 / "Tree-structured Sampling") draws the K candidates of a group from one prompt,
+ * and the step then trains on all of them.  The calls below are the attention side of such a policy: norms
+ * and rotation of queries and keys (with the gradient that training needs), the same on the way into a
+ * paged cache, and attention that reads a prompt's keys and values once for the candidates that share it.
+ *
+ * They have no error word of their own in a workspace: where `data_error` is not NULL the AT_GRPO_DATA_*
+ * bits of offending elements are or'ed into that int32 in device memory, which the caller clears when it
+ * likes (once per rollout, say).
+ */
+
+/* Rows of heads: element (t, h, d) lies at data + t * token_stride + h * head_stride + d (in elements of the
+ * call's dtype).  Queries, keys and values may therefore be views of one projection's output, or stand head
+ * by head.  data must be 16-byte aligned and both strides multiples of 16 bytes. */
+typedef struct {
+  void* data;
+  int64_t token_stride, head_stride;
+} at_grpo_rows;
+
+/* Which elements of a head are rotated together, for i < rot_dim / 2: (i, i + rot_dim / 2), or (2 i, 2 i + 1). */
+typedef enum { AT_GRPO_ROPE_HALF = 0, AT_GRPO_ROPE_INTERLEAVED = 1 } at_grpo_rope_layout;
+
+/* How frequencies f_i = base^(-2 i / rot_dim) are scaled for contexts longer than `trained` positions. */
+typedef enum {
+  AT_GRPO_ROPE_PLAIN = 0,  /* f_i                                                                        */
+  AT_GRPO_ROPE_LINEAR = 1, /* f_i / factor                                                               */
+  AT_GRPO_ROPE_BASE = 2,   /* base * factor^(rot_dim / (rot_dim - 2)) in place of base; rot_dim > 2       */
+  AT_GRPO_ROPE_PARTS = 3   /* f_i (g + (1 - g) / factor), g = clamp((turns_i - slow) / (fast - slow), 0, 1),
+                              turns_i = trained * f_i / (2 pi): fast turning pairs keep their frequency   */
+} at_grpo_rope_scaling;
+
+typedef struct {
+  int32_t rot_dim;    /* even, > 0                                                                       */
+  int32_t scaling;    /* at_grpo_rope_scaling                                                            */
+  double base;        /* > 0                                                                             */
+  double factor;      /* >= 1 (ignored by PLAIN)                                                         */
+  double trained, slow, fast; /* PARTS: > 0, and slow < fast                                             */
+  double magnitude;   /* cos and sin are multiplied by it; > 0                                           */
+} at_grpo_rope;
+
+/*
+ * The rotation table that the calls below read, computed in 64 bits and rounded once:
+ *   table[n_pos][rot_dim / 2][2] = magnitude * (cos, sin)(p f_i), fp32, 16-byte aligned, p < n_pos
+ */
+int at_grpo_rope_table(const at_grpo_rope* rope, int32_t n_pos, float* table, void* hip_stream);
+
+/* What a layer does to its queries and keys. */
+typedef struct {
+  int32_t dtype, D;         /* at_grpo_dtype of rows and weights; D % 8 == 0, 8 <= D <= 256              */
+  int32_t rot_dim, layout;  /* even, 0 <= rot_dim <= D (0: no rotation); at_grpo_rope_layout             */
+  int32_t n_pos;            /* positions in the table                                                    */
+  float eps;                /* >= 0                                                                      */
+  const float* table;       /* [n_pos][rot_dim / 2][2]; may be NULL where rot_dim == 0                   */
+  const void* q_weight;     /* [D], 16-byte aligned, or NULL: queries are not normed                     */
+  const void* k_weight;     /* [D], or NULL: keys are not normed                                         */
+} at_grpo_norm_rope;
+
+/*
+ * Norm of every head's row and rotation by its token's position, in one pass:
+ *   u = x / sqrt(mean(x^2) + eps) * weight     (u = x without a weight)
+ *   y_a = c u_a - s u_b,  y_b = c u_b + s u_a  for the pairs (a, b) of the layout, (c, s) = table[position[t]]
+ *   y_d = u_d for d >= rot_dim
+ * in fp32, rounded once.  q [n_tok, Hq, D], k [n_tok, Hk, D]; Hk == 0 (or Hq == 0) leaves one of them out.
+ * An output may be its input itself (same data and strides).  A token whose position lies outside the table
+ * raises AT_GRPO_DATA_POSITION and gets rows of zeros.  n_tok == 0 is no error and does nothing.
+ */
+int at_grpo_qk_norm_rope(const at_grpo_norm_rope* layer, int32_t n_tok, int32_t Hq, int32_t Hk,
+                         const at_grpo_rows* q, const at_grpo_rows* k, const int32_t* position,
+                         const at_grpo_rows* q_out, const at_grpo_rows* k_out, int32_t* data_error,
+                         void* hip_stream);
+
+/*
+ * Its gradient.  With g the rotated-back gradient of a row (g_a = c dy_a + s dy_b, g_b = c dy_b - s dy_a),
+ * r = 1 / sqrt(mean(x^2) + eps) and n = x r:
+ *   dx = r (g weight - n mean(g weight n)),   d_weight = sum over all rows of g n     (dx = g without a weight)
+ *   dq, dk as q, k (dq may be dq_out itself, dk dk_out);  dq_weight[D], dk_weight[D] fp32, overwritten, required
+ *   where the layer has the weight.
+ * Tokens whose position lies outside the table get zeros and add nothing.  Sums are taken in a fixed order.
+ * Workspace: AT_GRPO_CALL_QK_NORM_ROPE_BWD.
+ */
+int at_grpo_qk_norm_rope_bwd(const at_grpo_norm_rope* layer, int32_t n_tok, int32_t Hq, int32_t Hk,
+                             const at_grpo_rows* dq_out, const at_grpo_rows* dk_out, const at_grpo_rows* q,
+                             const at_grpo_rows* k, const int32_t* position, const at_grpo_rows* dq,
+                             const at_grpo_rows* dk, float* dq_weight, float* dk_weight, int32_t* data_error,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+
+/*
+ * A paged cache and the sequences of a batch in it.  Sequence s has length[s] tokens of its own; token i of them
+ * lies in page pages[s][i / page_size] at place i % page_size.  With groups, sequences group_seq[g] ..
+ * group_seq[g + 1] - 1 (the candidates of one turn) stand behind the prefix of group g: prefix_len[g] tokens
+ * (the prompt), laid out the same way through prefix_pages[g]; any prefix_len will do, a page that the prefix
+ * does not fill is not shared with what follows.  A sequence in no group has no prefix.
+ * The last cu_q[s + 1] - cu_q[s] own tokens of a sequence are its new ones: rows cu_q[s] .. of the calls' q, k, v.
+ * Token i of sequence s stands at position prefix_len + i.
+ */
+typedef struct {
+  int32_t dtype, Hk, D;          /* of the cache; D as above                                             */
+  int32_t page_size;             /* a power of two, 8 .. 65536                                           */
+  int32_t n_pages;               /* > 0                                                                  */
+  int32_t n_seq, max_pages;      /* rows and columns of pages                                            */
+  int32_t n_group, max_prefix_pages; /* rows and columns of prefix_pages; n_group == 0: no prefixes      */
+  void *k, *v;                   /* [n_pages, Hk, page_size, D], 16-byte aligned                         */
+  const int32_t* pages;          /* [n_seq, max_pages]; entries behind a sequence's length are not read  */
+  const int32_t* length;         /* [n_seq], 0 .. max_pages * page_size                                  */
+  const int32_t* cu_q;           /* [n_seq + 1], not falling; NULL: one new token in every sequence      */
+  const int32_t* group_seq;      /* [n_group + 1], not falling                                           */
+  const int32_t* prefix_len;     /* [n_group], 0 .. max_prefix_pages * page_size                         */
+  const int32_t* prefix_pages;   /* [n_group, max_prefix_pages]                                          */
+} at_grpo_kv;
+
+/*
+ * The new tokens' keys, normed and rotated by their positions as at_grpo_qk_norm_rope does, and their values as
+ * they are go into the cache; their queries, normed and rotated, to q_out (Hq == 0: none).  `length` already
+ * counts the new tokens.  Rows q [n_tok, Hq, D], k and v [n_tok, kv->Hk, D].  A token that belongs to no sequence
+ * (AT_GRPO_DATA_SEQLENS), whose position lies outside the table (AT_GRPO_DATA_POSITION) or whose page is none of
+ * the cache's (AT_GRPO_DATA_PAGE) is left out of the cache, and its q_out rows are zeros.
+ */
+int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* layer, int32_t n_tok, int32_t Hq,
+                      const at_grpo_rows* q, const at_grpo_rows* k, const at_grpo_rows* v,
+                      const at_grpo_rows* q_out, int32_t* data_error, void* hip_stream);
+
+/*
+ * Attention of the new tokens' queries over the cache, Hq a multiple of Hk (query head h reads key head
+ * h / (Hq / Hk)):
+ *   out[t, h] = sum_i p_i v_i,  p = softmax over the visible tokens i of scale <q[t, h], k_i>
+ *   lse[t, h] = ln sum_i exp(scale <q[t, h], k_i>)      (fp32 [n_tok, Hq]; NULL to skip)
+ * Visible are the whole prefix of the sequence's group and its own tokens: with causal != 0 up to and with the
+ * query's own place (length - new tokens + its number among the new ones), with causal == 0 all of them.  The
+ * prefix of a group is read once for all its sequences.  A query that sees nothing gets out 0 and lse -inf.
+ * Tokens in a page that is none of the cache's are not seen (AT_GRPO_DATA_PAGE); a length out of range counts as
+ * 0, and where cu_q or group_seq fall or leave their range no sequence sees anything (AT_GRPO_DATA_SEQLENS).
+ * What lies in the cache behind a sequence's length, NaN included, does not reach its results; the same goes for
+ * tokens that a causal query does not see, if their values are finite.
+ * max_q (host): an upper bound of the new tokens of one sequence; it picks the kernel, results do not depend on
+ * it but for rounding.  scale > 0.  Scores and sums are fp32; bf16 weights are rounded to bf16 for the product
+ * with v.  Workspace: at_grpo_prefix_attention_workspace_bytes (0 on invalid arguments; no pointer in kv is read).
+ */
+int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* q, float scale,
+                             int32_t causal, int32_t max_q, const at_grpo_rows* out, float* lse,
+                             int32_t* data_error, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t at_grpo_prefix_attention_workspace_bytes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q);
 
 /*
  * Bytes of workspace a call needs.  `batch` may be NULL for AT_GRPO_CALL_GROUP_ADVANTAGE; the

@@ -28,8 +28,9 @@ NORM = {"std": 0, "none": 1}
 NORM_FILL = 256      # or'ed into norm: the group buffers are filled behind the last group, so they need not be cleared
 GROUP_BY = {"agent_turn": 0, "trajectory": 1, "parallel": 2}
 CALL_GROUP_ADVANTAGE, CALL_TOKEN_LOGPROB, CALL_POLICY_LOSS_FWD, CALL_POLICY_LOSS_BWD, CALL_SURROGATE, \
-    CALL_HEAD_UPDATE, CALL_DIAGNOSTICS, CALL_TOKEN_ENTROPY, CALL_POLICY_LOSS_FWD_BWD = range(9)
+    CALL_HEAD_UPDATE, CALL_DIAGNOSTICS, CALL_TOKEN_ENTROPY, CALL_POLICY_LOSS_FWD_BWD, CALL_QK_NORM_ROPE_BWD = range(10)
 DTYPE = {torch.float32: 0, torch.bfloat16: 1}
+ROPE_SCALING = {"plain": 0, "linear": 1, "base": 2, "parts": 3}
 
 EXPORTS = [
     "at_grpo_group_advantage", "at_grpo_group_advantage_mixed", "at_grpo_group_advantage_static",
@@ -38,7 +39,8 @@ EXPORTS = [
     "at_grpo_surrogate_diagnostics", "at_grpo_token_entropy",
     "at_grpo_policy_loss_fwd", "at_grpo_policy_loss_bwd", "at_grpo_policy_loss_fwd_bwd", "at_grpo_head_update", "at_grpo_workspace_bytes",
     "at_grpo_status_string", "at_grpo_version", "at_grpo_profile_enable", "at_grpo_profile_classes",
-    "at_grpo_profile_read",
+    "at_grpo_profile_read", "at_grpo_rope_table", "at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append",
+    "at_grpo_prefix_attention", "at_grpo_prefix_attention_workspace_bytes",
 ]
 
 
@@ -50,6 +52,27 @@ class _Adam(C.Structure):
     _fields_ = [("lr", C.c_float), ("beta1", C.c_float), ("beta2", C.c_float), ("eps", C.c_float),
                 ("weight_decay", C.c_float), ("max_grad_norm", C.c_float), ("step", C.c_int32),
                 ("decoupled", C.c_int32)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class _Rope(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("scaling", C.c_int32), ("base", C.c_double), ("factor", C.c_double), ("trained", C.c_double),
+                ("slow", C.c_double), ("fast", C.c_double), ("magnitude", C.c_double)]
+
+
+class _NormRope(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("D", C.c_int32), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("n_pos", C.c_int32),
+                ("eps", C.c_float), ("table", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
+class _KV(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("Hk", C.c_int32), ("D", C.c_int32), ("page_size", C.c_int32), ("n_pages", C.c_int32),
+                ("n_seq", C.c_int32), ("max_pages", C.c_int32), ("n_group", C.c_int32), ("max_prefix_pages", C.c_int32),
+                ("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_void_p), ("length", C.c_void_p), ("cu_q", C.c_void_p),
+                ("group_seq", C.c_void_p), ("prefix_len", C.c_void_p), ("prefix_pages", C.c_void_p)]
 
 
 class _Batch(C.Structure):
@@ -123,6 +146,16 @@ def load_library():
     lib.at_grpo_profile_classes.restype = i32
     lib.at_grpo_profile_read.argtypes = [i32, C.POINTER(C.c_char_p), C.POINTER(C.c_int64),
                                          C.POINTER(C.c_double)]
+    rows, layer, kv = C.POINTER(_Rows), C.POINTER(_NormRope), C.POINTER(_KV)
+    lib.at_grpo_rope_table.argtypes = [C.POINTER(_Rope), i32, vp, vp]
+    lib.at_grpo_qk_norm_rope.argtypes = [layer, i32, i32, i32, rows, rows, vp, rows, rows, vp, vp]
+    lib.at_grpo_qk_norm_rope_bwd.argtypes = [layer, i32, i32, i32, rows, rows, rows, rows, vp, rows, rows, vp, vp, vp, vp, sz, vp]
+    lib.at_grpo_kv_append.argtypes = [kv, layer, i32, i32, rows, rows, rows, rows, vp, vp]
+    lib.at_grpo_prefix_attention.argtypes = [kv, i32, i32, rows, f32, i32, i32, rows, vp, vp, vp, sz, vp]
+    for name in ("at_grpo_rope_table", "at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append", "at_grpo_prefix_attention"):
+        getattr(lib, name).restype = C.c_int
+    lib.at_grpo_prefix_attention_workspace_bytes.argtypes = [kv, i32, i32, i32]
+    lib.at_grpo_prefix_attention_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -595,3 +628,200 @@ def at_grpo_profile_read():
 
 def at_grpo_version() -> int:
     return int(load_library().at_grpo_version())
+
+
+# ---- queries, keys and the rollout's cache ------------------------------------------------------------
+def at_grpo_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, scaling: str = "plain", factor: float = 1.0, trained: float = 0.0,
+                       slow: float = 1.0, fast: float = 32.0, magnitude: float = 1.0, device=None) -> torch.Tensor:
+    """cos and sin of every position's angles, float32 [n_pos, rot_dim / 2, 2]; a program makes it once for all layers.
+
+    `scaling` for contexts longer than the `trained` positions: "plain" (none), "linear" (frequencies / factor), "base" (a larger base),
+    "parts" (pairs that turn more than `fast` times over the trained positions keep their frequency, those that turn less than `slow`
+    times get frequency / factor, a ramp between)."""
+    lib = load_library()
+    table = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device="cuda" if device is None else device)
+    _dev_check(table)
+    c = _Rope(rot_dim, ROPE_SCALING[scaling], base, factor, trained, slow, fast, magnitude)
+    _check(lib.at_grpo_rope_table(C.byref(c), n_pos, _ptr(table), _stream()), "at_grpo_rope_table")
+    return table
+
+
+def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor], heads: Optional[int] = None) -> _Rows:
+    """t [tokens, heads, D] as at_grpo_rows, of the dtype, device, tokens and D of `like`."""
+    if t.dim() != 3 or not t.is_cuda or t.dtype not in DTYPE:
+        raise AtGrpoError(f"{name} must be a [tokens, heads, D] CUDA/HIP tensor of float32 or bfloat16")
+    if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[0] != like.shape[0] or t.shape[2] != like.shape[2]):
+        raise AtGrpoError(f"{name} must have the dtype, device, tokens and head size of the other rows")
+    if heads is not None and t.shape[1] != heads:
+        raise AtGrpoError(f"{name} must have {heads} heads, got {t.shape[1]}")
+    ts, hs, ds = t.stride()
+    step = 16 // t.element_size()
+    if t.numel() and (ds != 1 or ts % step or hs % step or t.data_ptr() % 16):
+        raise AtGrpoError(f"{name}: the elements of a head must be contiguous, heads and tokens multiples of 16 bytes apart, and the data "
+                          "16-byte aligned")
+    return _Rows(t.data_ptr(), ts, hs)
+
+
+def _vector(name: str, t: Optional[torch.Tensor], n: int, dtype: torch.dtype, device):
+    """A contiguous 1-d tensor of n elements (or None) as a pointer."""
+    if t is None:
+        return None
+    if not t.is_cuda or t.device != device or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+        raise AtGrpoError(f"{name} must be a contiguous {dtype} tensor of {n} elements on {device}")
+    return t.data_ptr()
+
+
+def _layer(x: torch.Tensor, rope, q_weight, k_weight, eps: float, interleaved: bool) -> _NormRope:
+    D = x.shape[2]
+    n_pos = half = 0
+    if rope is not None:
+        if rope.dim() != 3 or rope.shape[2] != 2 or rope.dtype != torch.float32 or rope.device != x.device or not rope.is_contiguous():
+            raise AtGrpoError("rope must be a contiguous float32 [positions, rot_dim / 2, 2] tensor on the rows' device")
+        n_pos, half = rope.shape[0], rope.shape[1]
+    return _NormRope(DTYPE[x.dtype], D, 2 * half, 1 if interleaved else 0, n_pos, eps, _ptr(rope),
+                     _vector("q_weight", q_weight, D, x.dtype, x.device), _vector("k_weight", k_weight, D, x.dtype, x.device))
+
+
+def _ref(rows: Optional[_Rows]):
+    return None if rows is None else C.byref(rows)
+
+
+def _word(data_error: Optional[torch.Tensor], device):
+    return _vector("data_error", data_error, 1, torch.int32, device)
+
+
+def at_grpo_qk_norm_rope(q, k, rope, position, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, q_out=None,
+                         k_out=None, data_error=None):
+    """Norm (where there is a weight) and rotation (where there is a table) of queries q [n, Hq, D] and keys k [n, Hk, D]; either may be
+    None.  position int32 [n].  Outputs may be the inputs themselves.  Returns dict(q, k)."""
+    lib = load_library()
+    x = q if q is not None else k
+    cq = _rows("q", q, None) if q is not None else None
+    ck = _rows("k", k, q) if k is not None else None
+    layer = _layer(x, rope, q_weight, k_weight, eps, interleaved)
+    pos = _vector("position", position, x.shape[0], torch.int32, x.device)
+    if q is not None and q_out is None:
+        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and k_out is None:
+        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    oq = _rows("q_out", q_out, q, q.shape[1]) if q is not None else None
+    ok = _rows("k_out", k_out, k, k.shape[1]) if k is not None else None
+    st = lib.at_grpo_qk_norm_rope(C.byref(layer), x.shape[0], q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0,
+                                  _ref(cq), _ref(ck), pos, _ref(oq), _ref(ok), _word(data_error, x.device), _stream())
+    _check(st, "at_grpo_qk_norm_rope")
+    return dict(q=q_out, k=k_out)
+
+
+def at_grpo_qk_norm_rope_bwd(dq_out, dk_out, q, k, rope, position, q_weight=None, k_weight=None, eps: float = 1e-6,
+                             interleaved: bool = False, dq=None, dk=None, data_error=None):
+    """Gradient of at_grpo_qk_norm_rope: from those of its outputs (and its inputs) to those of its inputs, in their dtype, and of the
+    weights, float32 [D].  dq may be dq_out itself, dk dk_out.  Returns dict(dq, dk, dq_weight, dk_weight, workspace)."""
+    lib = load_library()
+    x = q if q is not None else k
+    cq = _rows("q", q, None) if q is not None else None
+    ck = _rows("k", k, q) if k is not None else None
+    layer = _layer(x, rope, q_weight, k_weight, eps, interleaved)
+    pos = _vector("position", position, x.shape[0], torch.int32, x.device)
+    gq = _rows("dq_out", dq_out, q, q.shape[1]) if q is not None else None
+    gk = _rows("dk_out", dk_out, k, k.shape[1]) if k is not None else None
+    if q is not None and dq is None:
+        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and dk is None:
+        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    oq = _rows("dq", dq, q, q.shape[1]) if q is not None else None
+    ok = _rows("dk", dk, k, k.shape[1]) if k is not None else None
+    dqw = torch.empty(x.shape[2], dtype=torch.float32, device=x.device) if q is not None and q_weight is not None else None
+    dkw = torch.empty(x.shape[2], dtype=torch.float32, device=x.device) if k is not None and k_weight is not None else None
+    ws = _workspace(lib.at_grpo_workspace_bytes(CALL_QK_NORM_ROPE_BWD, None, 0, 0, 0, 0), x.device)
+    st = lib.at_grpo_qk_norm_rope_bwd(C.byref(layer), x.shape[0], q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0,
+                                      _ref(gq), _ref(gk), _ref(cq), _ref(ck), pos, _ref(oq), _ref(ok), _ptr(dqw), _ptr(dkw),
+                                      _word(data_error, x.device), _ptr(ws), ws.numel(), _stream())
+    _check(st, "at_grpo_qk_norm_rope_bwd")
+    return dict(dq=dq, dk=dk, dq_weight=dqw, dk_weight=dkw, workspace=ws)
+
+
+@dataclass(frozen=True)
+class KVBatch:
+    """Python-side mirror of at_grpo_kv; keeps the tensors alive.  The tensors' contents may change between calls (lengths grow as
+    tokens are appended), a batch of other tensors is another KVBatch."""
+    cache_k: torch.Tensor                       # [pages, Hk, page_size, D]
+    cache_v: torch.Tensor
+    pages: torch.Tensor                         # int32 [n_seq, max_pages]
+    length: torch.Tensor                        # int32 [n_seq], new tokens counted
+    cu_q: Optional[torch.Tensor] = None         # int32 [n_seq + 1]; None: one new token in every sequence
+    group_seq: Optional[torch.Tensor] = None    # int32 [n_group + 1]; None: no prefixes
+    prefix_len: Optional[torch.Tensor] = None   # int32 [n_group]
+    prefix_pages: Optional[torch.Tensor] = None  # int32 [n_group, max_prefix_pages]
+
+    def __post_init__(self):
+        ck, cv = self.cache_k, self.cache_v
+        _dev_check(ck, cv, self.pages, self.length, self.cu_q, self.group_seq, self.prefix_len, self.prefix_pages)
+        _i32_check(pages=self.pages, length=self.length, cu_q=self.cu_q, group_seq=self.group_seq, prefix_len=self.prefix_len,
+                   prefix_pages=self.prefix_pages)
+        if ck.dim() != 4 or ck.dtype not in DTYPE or cv.shape != ck.shape or cv.dtype != ck.dtype:
+            raise AtGrpoError("cache_k and cache_v must be [pages, heads, page_size, D] tensors of one shape, float32 or bfloat16")
+        n_seq = self.length.numel()
+        if self.pages.dim() != 2 or self.pages.shape[0] != n_seq:
+            raise AtGrpoError("pages must be [n_seq, max_pages]")
+        if self.cu_q is not None and self.cu_q.numel() != n_seq + 1:
+            raise AtGrpoError("cu_q must have n_seq + 1 elements")
+        n_group = 0
+        if self.group_seq is not None:
+            n_group = self.group_seq.numel() - 1
+            if self.prefix_len is None or self.prefix_pages is None or n_group < 0 or self.prefix_len.numel() != n_group or \
+                    self.prefix_pages.dim() != 2 or self.prefix_pages.shape[0] != n_group:
+                raise AtGrpoError("groups need prefix_len [n_group] and prefix_pages [n_group, max_prefix_pages]")
+        for t in (cv, self.pages, self.length, self.cu_q, self.group_seq, self.prefix_len, self.prefix_pages):
+            if t is not None and t.device != ck.device:
+                raise AtGrpoError("the tensors of a KVBatch must be on one device")
+        object.__setattr__(self, "c", _KV(
+            DTYPE[ck.dtype], ck.shape[1], ck.shape[3], ck.shape[2], ck.shape[0], n_seq, self.pages.shape[1], n_group,
+            self.prefix_pages.shape[1] if n_group else 0, ck.data_ptr(), cv.data_ptr(), self.pages.data_ptr(), self.length.data_ptr(),
+            _ptr(self.cu_q), _ptr(self.group_seq) if n_group else None, _ptr(self.prefix_len) if n_group else None,
+            _ptr(self.prefix_pages) if n_group else None))
+
+    def _rows(self, name: str, t: torch.Tensor, like: Optional[torch.Tensor], heads: Optional[int] = None) -> _Rows:
+        r = _rows(name, t, like, heads)
+        if t.dtype != self.cache_k.dtype or t.shape[2] != self.cache_k.shape[3] or t.device != self.cache_k.device:
+            raise AtGrpoError(f"{name} must have the cache's dtype, head size and device")
+        return r
+
+
+def at_grpo_kv_append(kv: KVBatch, q, k, v, rope, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, q_out=None,
+                      data_error=None):
+    """Normed and rotated keys k [n, Hk, D] and values v of the new tokens go into the cache; queries q [n, Hq, D] (or None), normed and
+    rotated, to q_out, which may be q itself.  Returns dict(q)."""
+    lib = load_library()
+    ck, cv = kv._rows("k", k, None, kv.c.Hk), kv._rows("v", v, k, kv.c.Hk)
+    cq = oq = None
+    if q is not None:
+        cq = kv._rows("q", q, k)
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        oq = kv._rows("q_out", q_out, q, q.shape[1])
+    layer = _layer(k, rope, q_weight, k_weight, eps, interleaved)
+    st = lib.at_grpo_kv_append(C.byref(kv.c), C.byref(layer), k.shape[0], q.shape[1] if q is not None else 0, _ref(cq), C.byref(ck),
+                               C.byref(cv), _ref(oq), _word(data_error, k.device), _stream())
+    _check(st, "at_grpo_kv_append")
+    return dict(q=q_out)
+
+
+def at_grpo_prefix_attention(kv: KVBatch, q, scale: Optional[float] = None, causal: bool = True, max_q: int = 1, out=None,
+                             want_lse: bool = False, data_error=None):
+    """Attention of the new tokens' queries q [n, Hq, D] over their sequences' tokens and their groups' prefixes (1 / sqrt(D) where no
+    scale is given).  max_q: an upper bound of the new tokens of one sequence.  out may not be q.  Returns dict(out, lse, workspace)."""
+    lib = load_library()
+    cq = kv._rows("q", q, None)
+    n, Hq, D = q.shape
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    co = kv._rows("out", out, q, Hq)
+    lse = torch.empty((n, Hq), dtype=torch.float32, device=q.device) if want_lse else None
+    nbytes = lib.at_grpo_prefix_attention_workspace_bytes(C.byref(kv.c), n, Hq, max_q)
+    if nbytes == 0:
+        raise AtGrpoError("at_grpo_prefix_attention: heads, head size, page size or max_q that it does not cover")
+    ws = _workspace(nbytes, q.device)
+    st = lib.at_grpo_prefix_attention(C.byref(kv.c), n, Hq, C.byref(cq), D ** -0.5 if scale is None else scale, 1 if causal else 0, max_q,
+                                      C.byref(co), _ptr(lse), _word(data_error, q.device), _ptr(ws), ws.numel(), _stream())
+    _check(st, "at_grpo_prefix_attention")
+    return dict(out=out, lse=lse, workspace=ws)

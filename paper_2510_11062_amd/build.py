@@ -14,7 +14,7 @@ CLIENT = os.path.join(PKG, "abi_client")
 PROBE = os.path.join(PKG, "gemm_probe")
 BINDING = os.path.join(PKG, "_binding.so")
 SOURCES = ["head_bf16.hip", "head_f32.hip", "group_advantage.hip", "api.hip", "token_kernels.hip", "head_kernels.hip",
-           "optimizer.hip"]      # the longest first
+           "optimizer.hip", "rope.hip", "prefix_attention.hip"]      # the longest first
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -11,6 +11,7 @@ namespace atg {
 
 size_t group_advantage_workspace(int32_t n_resp, int32_t n_env, int32_t n_agent, int32_t n_turn);
 size_t head_update_workspace();
+size_t qk_norm_rope_bwd_workspace();
 
 // ---- timing aid --------------------------------------------------------------------------------
 namespace {
@@ -21,7 +22,7 @@ struct ProfState {
 ProfState g_prof;
 const char* const kProfNames[PROF_N] = {"group_advantage", "token_prep", "head_fwd", "lse_combine",
                                         "surrogate", "coef", "transpose", "head_dz", "head_dh",
-                                        "head_dw", "fill", "grad_norm", "adam", "head_fe"};
+                                        "head_dw", "fill", "grad_norm", "adam", "head_fe", "rope", "attention"};
 }  // namespace
 
 void prof_begin(int cls, hipStream_t s) {
@@ -296,6 +297,7 @@ extern "C" size_t at_grpo_workspace_bytes(int32_t which_call, const at_grpo_batc
   if (which_call == AT_GRPO_CALL_GROUP_ADVANTAGE)
     return group_advantage_workspace(n_resp, n_env, n_agent, n_turn);
   if (which_call == AT_GRPO_CALL_HEAD_UPDATE) return head_update_workspace();
+  if (which_call == AT_GRPO_CALL_QK_NORM_ROPE_BWD) return qk_norm_rope_bwd_workspace();
   if (which_call == AT_GRPO_CALL_DIAGNOSTICS) {
     if (check_layout(batch, false) != AT_GRPO_OK) return 0;
     return diagnostics_workspace(batch->n_resp);

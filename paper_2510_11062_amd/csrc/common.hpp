@@ -65,6 +65,8 @@ enum ProfClass {
   PROF_GRAD_NORM,      // global gradient norm of the head update
   PROF_ADAM,           // fused clip + Adam step
   PROF_HEAD_FE,        // head contraction that writes the exponentials (one-pass forward + backward)
+  PROF_ROPE,           // norms and rotation of queries and keys, their gradient, appending to a cache
+  PROF_ATTENTION,      // attention over a paged cache
   PROF_N
 };
 

@@ -1,0 +1,91 @@
+// What the calls on a paged cache share: the cache and its sequences as the kernels see them, and the checks on the host.
+#pragma once
+
+#include "common.hpp"
+
+namespace atg {
+
+constexpr int kMaxHeadDim = 256;
+
+// at_grpo_rows as the kernels see it
+struct Rows {
+  void* data;
+  int64_t ts, hs;
+};
+
+inline Rows rows_of(const at_grpo_rows* r) { return r ? Rows{r->data, r->token_stride, r->head_stride} : Rows{}; }
+
+struct KvView {
+  int Hk, D, page_shift, n_pages, n_seq, max_pages, n_group, max_prefix_pages;
+  void *k, *v;
+  const int32_t *pages, *length, *cu_q, *group_seq, *prefix_len, *prefix_pages;
+};
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+inline int elem_size(int32_t dtype) { return dtype == AT_GRPO_BF16 ? 2 : 4; }
+
+inline int check_head_dim(int32_t dtype, int32_t D) {
+  if (dtype != AT_GRPO_F32 && dtype != AT_GRPO_BF16) return AT_GRPO_EUNSUPPORTED;
+  if (D <= 0) return AT_GRPO_EINVAL;
+  return D % 8 == 0 && D <= kMaxHeadDim ? AT_GRPO_OK : AT_GRPO_EUNSUPPORTED;
+}
+
+// 16-byte loads of a row's elements need its address and both strides to be multiples of 16 bytes.
+inline int check_rows(const at_grpo_rows* r, int32_t dtype) {
+  if (!r || !r->data || !aligned16(r->data)) return AT_GRPO_EINVAL;
+  const int64_t step = 16 / elem_size(dtype);
+  return r->token_stride % step == 0 && r->head_stride % step == 0 ? AT_GRPO_OK : AT_GRPO_EINVAL;
+}
+
+inline int check_kv_sizes(const at_grpo_kv* kv, int32_t n_tok) {
+  if (!kv) return AT_GRPO_EINVAL;
+  ATG_TRY(check_head_dim(kv->dtype, kv->D));
+  if (kv->Hk <= 0 || kv->n_pages <= 0 || kv->n_seq < 0 || kv->max_pages < 0 || kv->n_group < 0 || kv->max_prefix_pages < 0 || n_tok < 0)
+    return AT_GRPO_EINVAL;
+  if (kv->page_size < 8 || kv->page_size > 65536 || (kv->page_size & (kv->page_size - 1))) return AT_GRPO_EUNSUPPORTED;
+  const int64_t most = 0x7fffff00;       // places, rows of a call and units of the schedule are counted in 32 bits
+  if (static_cast<int64_t>(kv->max_pages) * kv->page_size > most / 2 || static_cast<int64_t>(kv->max_prefix_pages) * kv->page_size > most / 2 ||
+      static_cast<int64_t>(kv->n_seq) + kv->n_group > most / 2)
+    return AT_GRPO_EUNSUPPORTED;
+  return AT_GRPO_OK;
+}
+
+// Pointers are looked at only where there is something behind them.
+inline int check_kv(const at_grpo_kv* kv, int32_t n_tok, KvView* out) {
+  ATG_TRY(check_kv_sizes(kv, n_tok));
+  if (!kv->k || !kv->v || !aligned16(kv->k) || !aligned16(kv->v)) return AT_GRPO_EINVAL;
+  if (kv->n_seq > 0 && (!kv->length || (kv->max_pages > 0 && !kv->pages))) return AT_GRPO_EINVAL;
+  if (!kv->cu_q && n_tok != kv->n_seq) return AT_GRPO_EINVAL;
+  if (kv->n_group > 0 && (!kv->group_seq || !kv->prefix_len || (kv->max_prefix_pages > 0 && !kv->prefix_pages))) return AT_GRPO_EINVAL;
+  int shift = 0;
+  while ((1 << shift) < kv->page_size) ++shift;
+  *out = KvView{kv->Hk, kv->D, shift, kv->n_pages, kv->n_seq, kv->max_pages, kv->n_group, kv->max_prefix_pages,
+                kv->k, kv->v, kv->pages, kv->length, kv->cu_q, kv->group_seq, kv->prefix_len, kv->prefix_pages};
+  return AT_GRPO_OK;
+}
+
+#ifdef __HIPCC__
+__device__ __forceinline__ float to_f32(float x) { return x; }
+__device__ __forceinline__ float to_f32(bf16_t x) { return bf16_to_f32(x); }
+
+// How many of the rising a[0 .. n) are <= key, found by a whole wavefront, 64 entries at a time; between 0 and n whatever a holds.
+__device__ __forceinline__ int wave_upper_bound(const int32_t* __restrict__ a, int n, int key) {
+  const int lane = threadIdx.x & 63;
+  int base = 0;
+  while (n > 64) {
+    const int step = (n + 63) >> 6, at = lane * step;
+    const int c = __popcll(__ballot(at < n && a[base + (at < n ? at : 0)] <= key));
+    if (c == 0) return base;
+    base += (c - 1) * step;
+    n = min(step, n - (c - 1) * step);
+  }
+  return base + __popcll(__ballot(lane < n && a[base + (lane < n ? lane : 0)] <= key));
+}
+
+__device__ __forceinline__ void raise_data_error(int32_t* word, int bits) {
+  if (word && bits) atomicOr(word, bits);
+}
+#endif
+
+}  // namespace atg

@@ -1,0 +1,305 @@
+"""Attention over a paged cache and shared prefixes against the oracle in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import rollout_oracle as oracle
+from paper_2510_11062_amd import api
+from tests.rollout_case import DTYPES, Paged, assert_within, attention_bounds, host64, i32, rounded, to_dev
+
+EDGES = [1, 15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129]
+
+# Hq, Hk, D, page, lengths, new (None: one each), group sizes, prefixes
+CASES = {
+    "one token": (1, 1, 64, 16, [1], None, [], []),
+    "decode, edges": (4, 2, 128, 16, EDGES, None, [], []),
+    "decode, small pages": (2, 1, 64, 8, EDGES, None, [13], [45]),
+    "group": (16, 8, 128, 16, [1, 9, 30, 64], None, [4], [197]),
+    "groups of all sizes": (8, 2, 128, 32, [5] * 24, None, [1, 2, 0, 8, 3, 10], [1, 64, 50, 333, 0, 129]),
+    "some without a prefix": (4, 4, 64, 16, [40, 3, 70], None, [2], [31]),
+    "nothing of their own": (4, 2, 128, 16, [0, 0, 6], [0, 0, 3], [2, 1], [20, 0]),
+    "wide groups": (32, 2, 128, 16, [3, 33, 7, 20, 1, 2, 90, 12, 45], None, [8, 1], [700, 90]),
+    "many heads on one": (24, 1, 128, 64, [130, 5], None, [2], [260]),
+    "message": (8, 2, 64, 16, [61, 37, 40, 1, 20], [37, 5, 40, 1, 0], [3, 2], [300, 17]),
+    "prompt": (4, 2, 128, 64, [300, 77], [300, 77], [], []),
+    "prompts, odd": (3, 3, 128, 16, [65, 1, 130], [65, 1, 130], [1, 2], [10, 33]),
+    "head of 256": (4, 2, 256, 16, [50, 130, 17], None, [3], [100]),
+    "head of 256, message": (8, 1, 256, 16, [50, 130], [20, 9], [2], [77]),
+    "head of 80": (6, 2, 80, 16, [50, 33, 1], None, [3], [100]),
+    "head of 96, message": (4, 4, 96, 32, [50, 130, 17], [8, 100, 1], [], []),
+    "head of 200": (2, 1, 200, 16, [50, 130, 17], [8, 100, 1], [2], [40]),
+    "head of 8": (2, 2, 8, 8, [50, 3], None, [2], [20]),
+    "long": (4, 1, 128, 64, [2100, 900, 1, 4000], None, [3], [9000]),
+    "long, wide pages": (2, 1, 64, 1024, [1500, 10], [70, 10], [2], [5000]),
+    "many short": (4, 2, 64, 16, [1 + i % 40 for i in range(300)], None, [3] * 100, [i % 50 for i in range(100)]),
+}
+
+
+def attend(kv, q, **kw):
+    return api.at_grpo_prefix_attention(kv, q, **kw)
+
+
+def check(p, q64, out, ref, what=""):
+    o, lse, mag, big, n = ref
+    bo, bl = attention_bounds(p.dtype, p.D, o, mag, big, n)
+    assert_within(host64(out["out"]), o, bo, what + " out")
+    if out["lse"] is not None:
+        got = host64(out["lse"])
+        seen = np.isfinite(lse)
+        assert np.array_equal(np.isneginf(got), ~seen), what
+        assert_within(np.where(seen, got, 0), np.where(seen, lse, 0), bl + 2.0 ** -22 * np.abs(np.where(seen, lse, 0)), what + " lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("name", CASES)
+def test_against_the_oracle(gpu_device, dtype, name):
+    Hq, Hk, D, page, length, new, size, prefix = CASES[name]
+    p = Paged(dtype, Hk, D, page, length, new, size, prefix, seed=len(name))
+    q64 = p.queries(Hq, 1.5)
+    q, kv = to_dev(q64, p.dtype, gpu_device), p.device(gpu_device)
+    word = torch.zeros(1, dtype=torch.int32, device=gpu_device)
+    for causal in (True, False):
+        ref = p.attention(q64, D ** -0.5, causal)
+        out = attend(kv, q, causal=causal, max_q=int(p.new.max()), want_lse=True, data_error=word)
+        check(p, q64, out, ref, f"causal={causal}")
+        again = attend(kv, q, causal=causal, max_q=int(p.new.max()))
+        assert again["lse"] is None and torch.equal(again["out"], out["out"])
+    assert int(word) == 0
+    # whichever kernel a bound of the new tokens picks
+    for max_q in {1, 7, 64, 4096}:
+        check(p, q64, attend(kv, q, causal=False, max_q=max_q, want_lse=True), ref, f"max_q={max_q}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("scale", [0.02, 0.5, 3.0])
+def test_scores_near_and_far_from_each_other(gpu_device, dtype, scale):
+    """From even weights to one token that takes all, with the largest score first, last and in between."""
+    for order in ("rising", "falling", "mixed"):
+        p = Paged(dtype, 1, 64, 16, [150, 70], None, [2], [200], seed=3)
+        q64 = p.queries(4, 2.0)
+        for table, n in ((p.pages[0], 150), (p.pages[1], 70), (p.prefix_pages[0], 200)):
+            for i in range(n):
+                f = {"rising": i / n, "falling": 1 - i / n, "mixed": (i * 37 % n) / n}[order]
+                p.k[table[i // 16], :, i % 16] = torch.from_numpy(q64[0, 0] * 2 * f).to(p.dtype).double().numpy()
+        out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), scale=scale, want_lse=True)
+        check(p, q64, out, p.attention(q64, scale), f"{order} {scale}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_numbers_at_the_ends_of_the_range(gpu_device, dtype):
+    """Keys of the type's lowest and highest values, infinite scores, NaN in a visible place: what the formula says, for the sequences that
+    see it, and nothing for the others."""
+    p = Paged(dtype, 2, 64, 16, [40, 40, 40, 40, 40], None, [2], [30], seed=4)
+    q64 = rounded(np.abs(p.queries(2)) + 0.5, p.dtype)
+    low = float(torch.finfo(p.dtype).min)
+    p.k[p.pages[0][0], :, 3] = low                  # scores of -inf: weight 0, as if masked
+    p.k[p.pages[1][:3]] = low                        # sequence 1: all of its own tokens
+    p.k[p.pages[2][:3]] = low                        # sequence 2: everything that it sees
+    p.k[p.pages[3][1], :, 5] = np.inf
+    p.v[p.pages[4][1], 0, 2, 7] = np.nan
+    kv, q = p.device(gpu_device), to_dev(q64, p.dtype, gpu_device)
+    out = attend(kv, q, want_lse=True)
+    o, lse = host64(out["out"]), host64(out["lse"])
+    # scale * <q, k> of the lowest bf16 value is -inf or a finite number beyond any other score, by the sizes of q: either has no weight
+    for s in (0, 1):
+        keep = [i for i in range(40) if not (s == 0 and i == 3) and s == 0]
+        k = np.concatenate([oracle.rows(p.k, p.prefix_pages[0], 30), oracle.rows(p.k, p.pages[s], 40)[keep]])
+        v = np.concatenate([oracle.rows(p.v, p.prefix_pages[0], 30), oracle.rows(p.v, p.pages[s], 40)[keep]])
+        r = oracle.attention(q64[s:s + 1], k, v, 0.125, [len(k)])
+        bo, bl = attention_bounds(p.dtype, 64, r[0], r[2], r[3], np.array([len(k)]))
+        assert_within(o[s:s + 1], r[0], bo, f"sequence {s}")
+        assert_within(lse[s:s + 1], r[1], bl + 1e-6, f"lse {s}")
+    assert np.isnan(o[3]).all() and np.isnan(lse[3]).all()
+    bad = np.zeros((2, 64), dtype=bool)
+    bad[0, 7] = True
+    assert np.array_equal(np.isnan(o[4]), bad) and np.isfinite(lse[4]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_strides(gpu_device, dtype):
+    p = Paged(dtype, 2, 128, 16, [61, 37, 40], [37, 5, 40], [3], [90], seed=6)
+    q64 = p.queries(4)
+    q, kv, n = to_dev(q64, p.dtype, gpu_device), p.device(gpu_device), p.n_tok
+    ref = attend(kv, q, max_q=40, want_lse=True)
+    fused = torch.zeros(n, 9, 128, dtype=p.dtype, device=gpu_device)
+    fused[:, 2:6] = q
+    heads_first = torch.full((6, n, 128), 7.0, dtype=p.dtype, device=gpu_device)
+    out = attend(kv, fused[:, 2:6], max_q=40, want_lse=True, out=heads_first[1:5].transpose(0, 1))
+    assert torch.equal(heads_first[1:5].transpose(0, 1), ref["out"]) and torch.equal(out["lse"], ref["lse"])
+    assert (heads_first[0] == 7).all() and (heads_first[5] == 7).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [None, [3, 9, 1, 20]])
+def test_data_errors(gpu_device, dtype, new):
+    p = Paged(dtype, 2, 64, 16, [50, 90, 33, 20], new, [2, 2], [40, 70], seed=8)
+    q64 = p.queries(4)
+    q = to_dev(q64, p.dtype, gpu_device)
+    max_q = int(p.new.max())
+
+    def run(**over):
+        word = torch.zeros(1, dtype=torch.int32, device=gpu_device)
+        out = attend(p.device(gpu_device, **over), q, max_q=max_q, want_lse=True, causal=False, data_error=word)
+        return int(word), out
+
+    def refer(drop):
+        """The oracle without the dropped (table, first, last) tokens."""
+        o, mag = np.zeros(q64.shape), np.zeros(q64.shape)
+        lse, big, n = np.full(q64.shape[:2], -np.inf), np.zeros(q64.shape[:2]), np.zeros(len(q64), dtype=np.int64)
+        for s in range(4):
+            g, ks, vs = int(p.group[s]), [], []
+            for table, L, tag in ((p.prefix_pages[g], p.prefix[g], ("prefix", g)), (p.pages[s], p.length[s], ("own", s))):
+                keep = [i for i in range(int(L)) if not any(tag == d[0] and d[1] <= i < d[2] for d in drop)]
+                ks.append(oracle.rows(p.k, table, int(L))[keep])
+                vs.append(oracle.rows(p.v, table, int(L))[keep])
+            k, v = np.concatenate(ks), np.concatenate(vs)
+            a, b = p.cu_q[s], p.cu_q[s + 1]
+            o[a:b], lse[a:b], mag[a:b], big[a:b] = oracle.attention(q64[a:b], k, v, 0.125, [len(k)] * (b - a))
+            n[a:b] = len(k)
+        return o, lse, mag, big, n
+
+    pages = p.pages.copy()
+    pages[1, 2], pages[3, 0], pages[3, 1] = p.n_pages, -1, 1 << 30
+    bits, out = run(pages=i32(pages, gpu_device))
+    assert bits == 32
+    check(p, q64, out, refer([(("own", 1), 32, 48), (("own", 3), 0, 20)]), "pages")
+    tables = p.prefix_pages.copy()
+    tables[0, :] = -5
+    tables[1, 4] = p.n_pages + 7
+    bits, out = run(prefix_pages=i32(tables, gpu_device))
+    assert bits == 32
+    check(p, q64, out, refer([(("prefix", 0), 0, 40), (("prefix", 1), 64, 70)]), "prefix pages")
+    for wrong in (-1, 1 << 20):
+        length, prefix = p.length.copy(), p.prefix.copy()
+        length[0], prefix[1] = wrong, wrong
+        bits, out = run(length=i32(length, gpu_device), prefix_len=i32(prefix, gpu_device))
+        assert bits == 8
+        check(p, q64, out, refer([(("own", 0), 0, 50), (("prefix", 1), 0, 70)]), "lengths")
+    falls = [dict(group_seq=i32(x, gpu_device)) for x in ([0, 3, 2], [-1, 2, 4], [0, 2, 5])]
+    if new:
+        falls += [dict(cu_q=i32(x, gpu_device)) for x in ([0, 12, 3, 13, 33], [-2, 3, 12, 13, 33], [0, 3, 12, 13, 34])]
+    for over in falls:
+        bits, out = run(**over)
+        assert bits == 8 and not out["out"].any() and torch.isneginf(out["lse"]).all(), over
+
+
+@pytest.mark.gpu
+def test_tokens_of_no_sequence(gpu_device):
+    """Rows in front of cu_q[0] and behind its last entry see nothing."""
+    p = Paged("bf16", 2, 64, 16, [50, 30], [3, 2], [2], [40], seed=8)
+    q64 = p.queries(4)
+    q = torch.cat([torch.ones(2, 4, 64, dtype=p.dtype, device=gpu_device), to_dev(q64, p.dtype, gpu_device), torch.ones(1, 4, 64, dtype=p.dtype, device=gpu_device)])
+    out = attend(p.device(gpu_device, cu_q=i32(p.cu_q + 2, gpu_device)), q, max_q=3, want_lse=True)
+    inner = dict(out=out["out"][2:-1], lse=out["lse"][2:-1])
+    check(p, q64, inner, p.attention(q64, 0.125))
+    for rows in (out["out"][:2], out["out"][-1:]):
+        assert not rows.any()
+    assert torch.isneginf(out["lse"][:2]).all() and torch.isneginf(out["lse"][-1:]).all()
+
+
+@pytest.mark.gpu
+def test_cache_past_two_gibielements(gpu_device):
+    Hk, page, D = 8, 64, 128
+    n_pages = (1 << 31) // (Hk * page * D) + 3
+    cache = [torch.zeros(n_pages, Hk, page, D, dtype=torch.bfloat16, device=gpu_device) for _ in range(2)]
+    small = [torch.randn(4, Hk, page, D, device=gpu_device).bfloat16() for _ in range(2)]
+    last = [n_pages - 1, n_pages - 3, n_pages - 2, n_pages - 4]
+    for c, s in zip(cache, small):
+        c[last] = s
+    q = torch.randn(2, 16, D, device=gpu_device).bfloat16()
+    kw = dict(length=i32([60, 100], gpu_device), group_seq=i32([0, 2], gpu_device), prefix_len=i32([50], gpu_device))
+    far = api.KVBatch(*cache, pages=i32([[last[0], 0], [last[1], last[2]]], gpu_device), prefix_pages=i32([[last[3]]], gpu_device), **kw)
+    near = api.KVBatch(*small, pages=i32([[0, 0], [1, 2]], gpu_device), prefix_pages=i32([[3]], gpu_device), **kw)
+    assert torch.equal(attend(far, q)["out"], attend(near, q)["out"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_side_stream_and_graph(gpu_device, dtype):
+    """The same bits on another stream, and from a captured graph with eager work between its replays; lengths that grow in place are read
+    by every replay."""
+    p = Paged(dtype, 2, 128, 16, [40, 100, 7, 64], None, [2, 2], [300, 90], seed=9, spare_columns=0)
+    q64 = p.queries(8)
+    q, kv = to_dev(q64, p.dtype, gpu_device), p.device(gpu_device)
+    want = attend(kv, q, want_lse=True)
+    want = want["out"].clone(), want["lse"].clone()
+    side = torch.cuda.Stream(device=gpu_device)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = attend(kv, q, want_lse=True)
+        attend(kv, q, want_lse=True)
+    side.synchronize()
+    assert torch.equal(got["out"], want[0]) and torch.equal(got["lse"], want[1])
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(g, stream=side):
+            out = attend(kv, q, want_lse=True)
+    for step in range(3):
+        kv.length.copy_(i32(p.length - 3 * step, gpu_device))
+        eager = attend(kv, q, want_lse=True)
+        eager = eager["out"].clone(), eager["lse"].clone()
+        out["out"].fill_(9)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out["out"], eager[0]) and torch.equal(out["lse"], eager[1])
+
+
+@pytest.mark.gpu
+def test_a_used_workspace_changes_nothing(gpu_device):
+    p = Paged("bf16", 2, 128, 16, [40, 100, 7, 64], None, [2, 2], [3000, 90], seed=10)
+    q = to_dev(p.queries(8), p.dtype, gpu_device)
+    kv = p.device(gpu_device)
+    out = attend(kv, q, want_lse=True)
+    out["workspace"].fill_(255)
+    again = attend(kv, q, want_lse=True)
+    assert torch.equal(out["out"], again["out"]) and torch.equal(out["lse"], again["lse"])
+
+
+@pytest.mark.gpu
+def test_no_tokens_and_refusals(gpu_device):
+    p = Paged("bf16", 2, 64, 16, [5, 7], [2, 1], [2], [9])
+    kv, q = p.device(gpu_device), to_dev(p.queries(4), DTYPES["bf16"], gpu_device)
+    none = p.device(gpu_device, cu_q=i32([0, 0, 0], gpu_device))
+    assert attend(none, q[:0])["out"].shape == (0, 4, 64)
+    empty = api.KVBatch(kv.cache_k, kv.cache_v, kv.pages[:0], kv.length[:0])
+    assert attend(empty, q[:0])["out"].shape == (0, 4, 64)
+    for args in (dict(q=q[:, :3]), dict(q=q.float()), dict(q=q[..., :32].contiguous()), dict(max_q=0), dict(scale=0.0), dict(scale=-1.0),
+                 dict(scale=float("nan")), dict(out=torch.empty_like(q)[:, :2]), dict(out=q.float()), dict(q=q.cpu()),
+                 dict(data_error=torch.zeros(2, dtype=torch.int32, device=gpu_device))):
+        with pytest.raises(api.AtGrpoError):
+            attend(kv, **{"q": q, "max_q": 2, **args})
+    with pytest.raises(api.AtGrpoError):
+        attend(p.device(gpu_device, cu_q=None), q, max_q=2)        # three tokens for two sequences
+
+
+def test_workspace_sizes_and_refusals_on_the_host():
+    lib, C = api.load_library(), api.C
+    base = dict(dtype=1, Hk=2, D=64, page_size=16, n_pages=9, n_seq=4, max_pages=3, n_group=1, max_prefix_pages=2, k=4096, v=4096, pages=4096,
+                length=4096, cu_q=None, group_seq=4096, prefix_len=4096, prefix_pages=4096)
+
+    def size(n=4, hq=4, max_q=1, **kw):
+        return lib.at_grpo_prefix_attention_workspace_bytes(C.byref(api._KV(*{**base, **kw}.values())), n, hq, max_q)
+
+    def call(n=4, hq=4, scale=1.0, max_q=1, rows=(4096, 64, 64), ws=4096, nbytes=1 << 40, **kw):
+        r = C.byref(api._Rows(*rows))
+        return lib.at_grpo_prefix_attention(C.byref(api._KV(*{**base, **kw}.values())), n, hq, r, scale, 1, max_q, r, None, None, ws, nbytes, None)
+
+    assert size() > 0 and size(n=0) > 0
+    for kw, status in [(dict(dtype=3), 2), (dict(D=60), 2), (dict(D=264), 2), (dict(page_size=4), 2), (dict(page_size=24), 2), (dict(hq=3), 1),
+                       (dict(hq=0), 1), (dict(max_q=0), 1), (dict(n=-1), 1), (dict(n_pages=0), 1), (dict(n=1 << 30, hq=4), 2)]:
+        assert size(**kw) == 0 and call(**kw) == status, kw
+    for kw, status in [(dict(scale=0.0), 1), (dict(scale=float("inf")), 1), (dict(n=3), 1), (dict(length=None), 1), (dict(group_seq=None), 1),
+                       (dict(rows=(4100, 64, 64)), 1), (dict(rows=(4096, 63, 64)), 1), (dict(ws=None), 3), (dict(ws=4097), 3), (dict(nbytes=size() - 1), 3),
+                       (dict(k=None), 1)]:
+        assert call(**kw) == status, kw
+    # scratch memory for more tokens, sequences or groups serves fewer
+    for key, values in (("n", [0, 1, 4, 100, 5000, 100000]), ("n_seq", [0, 1, 4, 700, 5000]), ("n_group", [1, 2, 700])):
+        got = [size(**{key: v, "cu_q": 4096}) for v in values]
+        assert got == sorted(got) and got[0] > 0, key
+    assert size(n_group=0) <= size(n_group=1)
