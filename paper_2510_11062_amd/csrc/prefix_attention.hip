@@ -1,119 +1,635 @@
 // Attention of new tokens over a paged cache, the prompts of groups of candidates among it (gfx950).
 //
-//   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale <q, k_i> - m)  over the visible tokens, with the running maximum m and sum of one pass.
+//   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale <q, k_i> - m)  over the visible tokens i
 //
-// One wavefront per query and head: a lane scores a token, then the lanes own elements of the output.
+// in one pass with a running maximum m.  What there is to read is the keys and values, and where few queries read them their passage
+// from memory bounds the call.  Hence units of work that read a token once for all queries that see it: the prefix of a group with the
+// queries of all its sequences, and a sequence's own tokens with its queries.  A unit's rows are its queries times the Hq / Hk heads
+// that share a key head; rows are cut into tiles of 16 to 64, tokens into chunks of equal length over the whole batch, so that long
+// prompts and ragged responses fill the chip alike, and the chunks' results are joined by a second kernel.
+//
+// A wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
+//   S^T = K Q^T     MFMA 16x16: tokens down, queries across, so that a lane has four consecutive tokens of one query
+//   P^T             is at once the second product's operand: no lane needs a weight that another one computed
+//   O^T += V^T P^T  a lane loads whole rows of V, eight elements of eight tokens, and transposes that block by itself
+// The four wavefronts of a workgroup take turns in a chunk's tokens and add up at its end.
 #include "kv_common.hpp"
 
 #include <math.h>
+
+#include <type_traits>
 
 namespace atg {
 
 namespace {
 
-template <typename T>
-__global__ __launch_bounds__(256) void k_attend(KvView kv, int n_tok, int Hq, Rows q, float scale, int causal, Rows out, float* __restrict__ lse,
-                                                int32_t* data_error) {
-  __shared__ float q_lds[4][kMaxHeadDim];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + wave;
-  if (unit >= static_cast<int64_t>(n_tok) * Hq) return;
-  const int t = static_cast<int>(unit / Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * Hq), hk = h / (Hq / kv.Hk), D = kv.D;
-  int error = 0, s = t, q0 = t, q1 = t + 1;
-  // an index that falls anywhere leaves nothing visible anywhere
-  bool falls = false;
-  if (kv.cu_q)
-    for (int i = lane; i < kv.n_seq; i += 64) falls |= kv.cu_q[i] < 0 || kv.cu_q[i + 1] < kv.cu_q[i] || kv.cu_q[i + 1] > n_tok;
-  if (kv.n_group)
-    for (int i = lane; i < kv.n_group; i += 64)
-      falls |= kv.group_seq[i] < 0 || kv.group_seq[i + 1] < kv.group_seq[i] || kv.group_seq[i + 1] > kv.n_seq;
-  int own = 0, prefix = 0, g = 0;
-  if (__any(falls)) {
-    error = AT_GRPO_DATA_SEQLENS;
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kTarget = 1024;        // items that the chunks' length aims at: four for each compute unit
+constexpr int kMinBlocks = 2;        // shortest chunk, in blocks of 64 tokens: 32 for each wavefront
+constexpr int kPageSlots = 1024;     // page ids of a chunk in LDS at a time
+constexpr int kMaxRows = 64;         // rows of the largest tile
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// The running maximum is raised where a score passes it by more than this (in powers of two): weights of at most 2^8 lose nothing in
+// fp32 sums, nor in bf16, whose error is relative, and most tokens then leave the sums as they are.
+constexpr float kSlack = 8.f;
+
+struct Args {
+  int n_tok, Hq, share;      // share: Hq / Hk
+  int causal;
+  float scale;
+  Rows q, out;
+  float* lse;                // [n_tok, Hq] or null
+  int32_t* data_error;
+  int4* units;               // workspace: [n_group + n_seq] first row of parts, chunks, first token, tokens
+  float* part_lse;           // [rows of parts]
+  float* part_out;           // [rows of parts, D], each divided by its own sum
+};
+
+// A unit: queries tok0 .. tok0 + ntok - 1 over the first `len` tokens of a page table.  Units 0 .. n_group - 1 are the prefixes.
+struct Unit {
+  int tok0, ntok, len;
+};
+
+__device__ __forceinline__ Unit unit_of(const KvView& kv, int u, int n_tok, int* error, bool* falls) {
+  int s0 = u - kv.n_group, s1 = s0 + 1, len, most;
+  if (u < kv.n_group) {
+    s0 = kv.group_seq[u];
+    s1 = kv.group_seq[u + 1];
+    if (s0 < 0 || s1 < s0 || s1 > kv.n_seq) {
+      *falls = true;
+      return Unit{0, 0, 0};
+    }
+    len = kv.prefix_len[u];
+    most = kv.max_prefix_pages << kv.page_shift;
   } else {
-    if (kv.cu_q) {
-      s = wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1;
-      if (s >= 0 && s < kv.n_seq) {
-        q0 = kv.cu_q[s];
-        q1 = kv.cu_q[s + 1];
+    len = kv.length[s0];
+    most = kv.max_pages << kv.page_shift;
+  }
+  const int t0 = kv.cu_q ? kv.cu_q[s0] : s0, t1 = kv.cu_q ? kv.cu_q[s1] : s1;
+  if (t0 < 0 || t1 < t0 || t1 > n_tok) {
+    *falls = true;
+    return Unit{0, 0, 0};
+  }
+  if (len < 0 || len > most) {
+    *error |= AT_GRPO_DATA_SEQLENS;
+    len = 0;
+  }
+  return Unit{t0, t1 - t0, len};
+}
+
+// The batch cut into items, the same in every workgroup: an item is a chunk of a unit's tokens, a key head and a tile of rows.
+struct Schedule {
+  int first[257];     // items in front of each thread's units, and all
+  int part[256];      // rows of parts in front of them
+  int chunk;          // tokens of a chunk
+  int unit, index, chunks, part0;     // the item at hand: its unit, its number there
+  Unit at;
+  int64_t cost[4];
+};
+
+__device__ __forceinline__ int tiles_of(const Unit& u, int share, int rows) { return static_cast<int>((static_cast<int64_t>(u.ntok) * share + rows - 1) / rows); }
+
+template <int RP, int RO>
+__device__ void make_schedule(const KvView& kv, const Args& a, Schedule& S, int* scan_lds) {
+  const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, u0 = min(n, tid * per), u1 = min(n, u0 + per);
+  int error = 0;
+  bool falls = false;
+  int64_t cost = 0;
+  for (int u = u0; u < u1; ++u) {
+    const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
+    cost += static_cast<int64_t>(tiles_of(x, a.share, u < kv.n_group ? RP : RO)) * ((x.len + 63) >> 6);
+  }
+  const bool none = __syncthreads_or(falls);
+  if (none) error |= AT_GRPO_DATA_SEQLENS;
+  if (blockIdx.x == 0) raise_data_error(a.data_error, error);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) cost += __shfl_xor(cost, o, 64);
+  if ((tid & 63) == 0) S.cost[tid >> 6] = cost;
+  __syncthreads();
+  cost = (S.cost[0] + S.cost[1] + S.cost[2] + S.cost[3]) * kv.Hk;
+  int64_t blocks = (cost + kTarget - 1) / kTarget;
+  blocks = blocks < kMinBlocks ? kMinBlocks : blocks > (1 << 24) ? (1 << 24) : blocks;
+  const int chunk = static_cast<int>(blocks) << 6;
+  int items = 0, parts = 0;
+  if (!none)
+    for (int u = u0; u < u1; ++u) {
+      const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
+      const int chunks = (x.len + chunk - 1) / chunk;
+      items += tiles_of(x, a.share, u < kv.n_group ? RP : RO) * chunks * kv.Hk;
+      parts += x.ntok * a.Hq * chunks;
+    }
+  int total_items, total_parts;
+  const int item0 = block_exclusive_scan<256>(items, scan_lds, &total_items);
+  int part0 = block_exclusive_scan<256>(parts, scan_lds, &total_parts);
+  S.first[tid] = item0;
+  S.part[tid] = part0;
+  if (tid == 0) {
+    S.first[256] = total_items;
+    S.chunk = chunk;
+  }
+  if (blockIdx.x == 0)       // for the kernel that joins the parts
+    for (int u = u0; u < u1; ++u) {
+      Unit x{0, 0, 0};
+      if (!none) x = unit_of(kv, u, a.n_tok, &error, &falls);
+      const int chunks = (x.len + chunk - 1) / chunk;
+      a.units[u] = make_int4(part0, chunks, x.tok0, x.ntok);
+      part0 += x.ntok * a.Hq * chunks;
+    }
+  __syncthreads();
+}
+
+// Puts item `item` into S.
+template <int RP, int RO>
+__device__ void find_item(const KvView& kv, const Args& a, Schedule& S, int item) {
+  const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x;
+  __syncthreads();
+  if (S.first[tid] <= item && item < S.first[tid + 1]) {
+    int left = item - S.first[tid], part0 = S.part[tid], error = 0;
+    bool falls = false;
+    for (int u = tid * per; u < n; ++u) {
+      const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
+      const int chunks = (x.len + S.chunk - 1) / S.chunk, items = tiles_of(x, a.share, u < kv.n_group ? RP : RO) * chunks * kv.Hk;
+      if (left < items) {
+        S.unit = u;
+        S.index = left;
+        S.chunks = chunks;
+        S.part0 = part0;
+        S.at = x;
+        break;
+      }
+      left -= items;
+      part0 += x.ntok * a.Hq * chunks;
+    }
+  }
+  __syncthreads();
+}
+
+// What a lane (m, g) = (lane & 15, lane >> 4) holds of a tile of TOK tokens.
+//   bf16: K elements 32 c + 8 g .. + 7 of tokens m and 16 + m; V elements 128 b + 8 m .. + 7 (64-wide heads: 4 m .. + 3) of the tokens
+//         4 g .. + 3 and 16 + 4 g .. + 3.
+//   fp32: K elements 16 c + 4 g .. + 3 of token m; V elements 64 b + 4 m .. + 3 of tokens 4 g .. + 3.
+// E: elements of V in a lane's row; NB: blocks of 16 E in a head.
+template <typename T, int D>
+struct Shape;
+template <int D>
+struct Shape<bf16_t, D> {
+  static constexpr int TOK = 32, SUB = 2, KC = D / 32, KE = 8, E = D >= 128 ? 8 : 4, NB = D / (16 * E);
+  typedef uint4 KV;
+  typedef typename std::conditional<E == 8, uint4, uint2>::type VV;
+};
+template <int D>
+struct Shape<float, D> {
+  static constexpr int TOK = 16, SUB = 1, KC = D / 16, KE = 4, E = 4, NB = D / 64;
+  typedef f32x4 KV;
+  typedef f32x4 VV;
+};
+
+__device__ __forceinline__ uint32_t dword(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ uint32_t dword(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
+
+// Element e of eight tokens' rows, side by side: an operand of V^T.
+template <typename VV>
+__device__ __forceinline__ bf16x8 transposed(const VV (&v)[8], int e) {
+  uint32_t o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) o[j] = __builtin_amdgcn_perm(dword(v[2 * j + 1], e >> 1), dword(v[2 * j], e >> 1), e & 1 ? 0x07060302u : 0x05040100u);
+  return __builtin_bit_cast(bf16x8, make_uint4(o[0], o[1], o[2], o[3]));
+}
+
+struct Lds {
+  Schedule S;
+  int scan[4];
+  int pages[kPageSlots];
+  float ml[4][kMaxRows][2];
+  float slab[4][16][128 + 4];
+};
+
+// One item: the rows of one tile over one chunk.
+template <typename T, int D, int NR, bool EXACT>
+__device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int32_t* table) {
+  typedef Shape<T, D> Z;
+  constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, R = 16 * NR;
+  constexpr bool kBf16 = sizeof(T) == 2;
+  const Schedule& S = lds.S;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
+  const Unit u = S.at;
+  const bool own = S.unit >= kv.n_group;
+  const int rows = u.ntok * a.share, tiles = (rows + R - 1) / R;
+  // row tiles turn fastest, so that workgroups that read the same tokens run together; the last ones, which see most, go first
+  const int tile = tiles - 1 - S.index % tiles, hc = S.index / tiles, c = hc % S.chunks, hk = hc / S.chunks;
+  const int r0 = tile * R;
+  const int dim = EXACT ? D : kv.D;
+  // A causal query sees the own tokens in front of `first + its number among the new tokens`.
+  const bool steps = own && a.causal;
+  const int first = u.len - u.ntok + 1;
+  const int last_tok = (min(rows, r0 + R) - 1) / a.share, first_tok = r0 / a.share;
+  const int k0 = c * S.chunk, k1 = min(min(u.len, k0 + S.chunk), steps ? first + last_tok : u.len), all_see = steps ? first + first_tok : k1;
+
+  typename Z::KV q[NR][KC];
+  int limit[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int r = r0 + 16 * n + m, tq = min(r, rows - 1) / a.share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
+    const T* from = static_cast<const T*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
+    limit[n] = steps ? min(k1, first + tq) : k1;
+#pragma unroll
+    for (int x = 0; x < KC; ++x) {
+      const int d = 4 * Z::KE * x + Z::KE * g;
+      typename Z::KV z{};
+      if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(from + d);
+      q[n][x] = z;
+    }
+  }
+  const float to_log2 = a.scale * kLog2e;
+  f32x4 acc[NR][NB][E];
+  float top[NR], ref[NR], sum[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    top[n] = -INFINITY;
+    ref[n] = 0.f;
+    sum[n] = 0.f;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[n][b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  const int64_t page_step = (static_cast<int64_t>(kv.Hk) * dim) << kv.page_shift;
+  const int in_page = (1 << kv.page_shift) - 1;
+  const T* const kbase = static_cast<const T*>(kv.k) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+  const T* const vbase = static_cast<const T*>(kv.v) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+
+  for (int from = k0; from < k1;) {
+    const int page0 = from >> kv.page_shift, to = min(k1, (page0 + kPageSlots) << kv.page_shift);
+    const int n_slots = ((to - 1) >> kv.page_shift) - page0 + 1;
+    bool missing = false;
+    __syncthreads();
+    for (int i = tid; i < n_slots; i += 256) {
+      int id = table[page0 + i];
+      if (static_cast<unsigned>(id) >= static_cast<unsigned>(kv.n_pages)) {
+        id = -1;
+        missing = true;
+      }
+      lds.pages[i] = id;
+    }
+    const bool holes = __syncthreads_or(missing);
+    if (missing) raise_data_error(a.data_error, AT_GRPO_DATA_PAGE);
+
+    typename Z::KV k[SUB][KC];
+    typename Z::VV v[NB][VJ];
+    auto row_of = [&](int token) {      // a token behind the last stands for it
+      const int i = min(token, to - 1), id = max(0, lds.pages[(i >> kv.page_shift) - page0]);
+      return id * page_step + static_cast<int64_t>(i & in_page) * dim;
+    };
+    auto load_k = [&](int t) {
+#pragma unroll
+      for (int s = 0; s < SUB; ++s) {
+        const T* p = kbase + row_of(t + 16 * s + m);
+#pragma unroll
+        for (int x = 0; x < KC; ++x) {
+          const int d = 4 * Z::KE * x + Z::KE * g;
+          typename Z::KV z{};
+          if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(p + d);
+          k[s][x] = z;
+        }
+      }
+    };
+    auto load_v = [&](int t) {
+#pragma unroll
+      for (int s = 0; s < SUB; ++s) {
+        const T* p = vbase + row_of(min(t + 16 * s + 4 * g, (to - 1) & ~3));      // four tokens that start at a multiple of four share a page
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          const int d = 16 * E * b + E * m;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            typename Z::VV z{};
+            if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::VV*>(p + static_cast<int64_t>(j) * dim + d);
+            v[b][4 * s + j] = z;
+          }
+        }
+      }
+    };
+
+    int t = from + TOK * wave;
+    if (t < to) {
+      load_k(t);
+      load_v(t);
+    }
+    for (; t < to; t += 4 * TOK) {
+      f32x4 s[NR][SUB];
+#pragma unroll
+      for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int y = 0; y < SUB; ++y) {
+          s[n][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int x = 0; x < KC; ++x) {
+            if constexpr (kBf16) {
+              s[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][x]), __builtin_bit_cast(bf16x8, q[n][x]), s[n][y], 0, 0, 0);
+            } else {
+#pragma unroll
+              for (int z = 0; z < 4; ++z) s[n][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[y][x][z], q[n][x][z], s[n][y], 0, 0, 0);
+            }
+          }
+        }
+      const int next = t + 4 * TOK;
+      if (next < to) load_k(next);
+      if (t + TOK > min(to, all_see) || holes) {
+        // tokens that a row does not see, and what lies in the cache behind the last or in no page: no weight, and no value
+#pragma unroll
+        for (int y = 0; y < SUB; ++y) {
+          const int t4 = t + 16 * y + 4 * g;
+          const bool there = t4 < to && lds.pages[(t4 >> kv.page_shift) - page0] >= 0;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+              if (!there || t4 + i >= limit[n]) s[n][y][i] = -INFINITY;
+            if (!there || t4 + i >= to)
+#pragma unroll
+              for (int b = 0; b < NB; ++b) v[b][4 * y + i] = typename Z::VV{};
+          }
+        }
+      }
+      uint32_t w16[NR][4];
+      float w32[NR][4];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        float high = -INFINITY;
+#pragma unroll
+        for (int y = 0; y < SUB; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) high = fmaxf(high, s[n][y][i]);
+        high *= to_log2;
+        if (__any(high > top[n] + kSlack)) {
+          high = fmaxf(high, __shfl_xor(high, 16, 64));
+          high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top[n]);
+          const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top[n] - now);
+          top[n] = high;
+          ref[n] = now;
+          sum[n] *= keep;
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[n][b][e] *= keep;
+        }
+        float p[4 * SUB];
+#pragma unroll
+        for (int y = 0; y < SUB; ++y)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            p[4 * y + i] = __builtin_amdgcn_exp2f(fmaf(s[n][y][i], to_log2, -ref[n]));
+            sum[n] += p[4 * y + i];
+          }
+        if constexpr (kBf16) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w16[n][j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) w32[n][j] = p[j];
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          if constexpr (kBf16) {
+            const bf16x8 vt = transposed(v[b], e);
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+              acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])),
+                                                                     acc[n][b][e], 0, 0, 0);
+          } else {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], acc[n][b][e], 0, 0, 0);
+          }
+        }
+      if (next < to) load_v(next);
+    }
+    from = to;
+  }
+
+  // The wavefronts' maxima and sums, then their products, each divided by the sum of all.
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    sum[n] += __shfl_xor(sum[n], 16, 64);
+    sum[n] += __shfl_xor(sum[n], 32, 64);
+    if (g == 0) {
+      lds.ml[wave][16 * n + m][0] = top[n];
+      lds.ml[wave][16 * n + m][1] = sum[n];
+    }
+  }
+  __syncthreads();
+  const bool direct = kv.n_group == 0 && S.chunks == 1;
+  float high[NR], total[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    high[n] = -INFINITY;
+    total[n] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) high[n] = fmaxf(high[n], lds.ml[w][16 * n + m][0]);
+    const float now = high[n] == -INFINITY ? 0.f : high[n];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) total[n] += lds.ml[w][16 * n + m][1] * __builtin_amdgcn_exp2f(lds.ml[w][16 * n + m][0] - now);
+    const float f = total[n] == 0.f ? 0.f : __builtin_amdgcn_exp2f(top[n] - now) / total[n];
+    const int r = r0 + 16 * n + m;
+    if (wave == 0 && g == 0 && r < rows) {
+      const int tq = r / a.share, h = hk * a.share + r - tq * a.share;
+      const float x = total[n] == 0.f ? -INFINITY : fmaf(now, kLn2, logf(total[n]));
+      if (!direct) a.part_lse[S.part0 + (static_cast<int64_t>(c) * u.ntok + tq) * a.Hq + h] = x;
+      else if (a.lse) a.lse[static_cast<int64_t>(u.tok0 + tq) * a.Hq + h] = x;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+          *reinterpret_cast<f32x4*>(&lds.slab[wave][m][E * (4 * g + i) + e]) =
+              f32x4{acc[n][b][e][i] * f, acc[n][b][e + 1][i] * f, acc[n][b][e + 2][i] * f, acc[n][b][e + 3][i] * f};
+      __syncthreads();
+      const int row = tid >> 4, rr = r0 + 16 * n + row, d = E * (tid & 15);
+      if (rr < rows && (EXACT || 16 * E * b + d < dim)) {
+        f32x4 o[E / 4];
+#pragma unroll
+        for (int e = 0; e < E / 4; ++e) {
+          f32x4 x[4];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&lds.slab[w][row][d + 4 * e]);
+          o[e] = (x[0] + x[1]) + (x[2] + x[3]);
+        }
+        const int tq = rr / a.share, h = hk * a.share + rr - tq * a.share;
+        if (direct) {
+          T* to = static_cast<T*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 16 * E * b + d;
+#pragma unroll
+          for (int e = 0; e < E / 4; ++e) {
+            if constexpr (kBf16) *reinterpret_cast<uint2*>(to + 4 * e) = make_uint2(pack_bf16x2(o[e][0], o[e][1]), pack_bf16x2(o[e][2], o[e][3]));
+            else *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
+          }
+        } else {
+          float* to = a.part_out + (S.part0 + (static_cast<int64_t>(c) * u.ntok + tq) * a.Hq + h) * dim + 16 * E * b + d;
+#pragma unroll
+          for (int e = 0; e < E / 4; ++e) *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
+        }
       }
     }
-    if (s >= 0 && s < kv.n_seq) {
-      own = kv.length[s];
-      if (own < 0 || own > (kv.max_pages << kv.page_shift)) {
-        own = 0;
-        error |= AT_GRPO_DATA_SEQLENS;
-      }
-      if (causal) own = max(0, own - (q1 - 1 - t));
-      if (kv.n_group) {
-        g = wave_upper_bound(kv.group_seq, kv.n_group + 1, s) - 1;
-        if (g >= 0 && g < kv.n_group) {
-          prefix = kv.prefix_len[g];
-          if (prefix < 0 || prefix > (kv.max_prefix_pages << kv.page_shift)) {
-            prefix = 0;
-            error |= AT_GRPO_DATA_SEQLENS;
+  }
+}
+
+template <typename T, int D, int NRP, int NRO, bool EXACT>
+__global__ __launch_bounds__(256, NRP == 1 ? 3 : NRP == 2 && D <= 128 ? 2 : 1) void k_attend(KvView kv, Args a) {
+  __shared__ Lds lds;
+  make_schedule<16 * NRP, 16 * NRO>(kv, a, lds.S, lds.scan);
+  // neighbouring items go to one XCD
+  const int per_xcd = gridDim.x >> 3, w = per_xcd << 3 == gridDim.x ? (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3) : blockIdx.x;
+  for (int item = w; item < lds.S.first[256]; item += gridDim.x) {
+    find_item<16 * NRP, 16 * NRO>(kv, a, lds.S, item);
+    const int u = lds.S.unit;
+    if (u < kv.n_group) attend_item<T, D, NRP, EXACT>(kv, a, lds, kv.prefix_pages + static_cast<int64_t>(u) * kv.max_prefix_pages);
+    else attend_item<T, D, NRO, EXACT>(kv, a, lds, kv.pages + static_cast<int64_t>(u - kv.n_group) * kv.max_pages);
+  }
+}
+
+// out = sum_c exp(lse_c - lse) out_c over the chunks of the prefix and of the own tokens.  A wavefront per query and head: four chunks at
+// a time, sixteen lanes for the elements of one.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join(KvView kv, Args a) {
+  const int lane = threadIdx.x & 63, l = lane & 15, slot = lane >> 4, D = kv.D;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  if (unit >= static_cast<int64_t>(a.n_tok) * a.Hq) return;
+  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * a.Hq);
+  const int s = kv.cu_q ? wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1 : t;
+  int4 of[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+  if (s >= 0 && s < kv.n_seq) {
+    of[1] = a.units[kv.n_group + s];
+    if (kv.n_group) {
+      const int g = wave_upper_bound(kv.group_seq, kv.n_group + 1, s) - 1;
+      if (g >= 0 && g < kv.n_group) of[0] = a.units[g];
+    }
+  }
+  if (kv.n_group == 0 && of[1].y == 1) return;      // in its place already
+  const int n0 = of[0].y, n = n0 + of[1].y;
+  auto part_of = [&](int c) {
+    const int4 x = c < n0 ? of[0] : of[1];
+    return x.x + (static_cast<int64_t>(c < n0 ? c : c - n0) * x.w + (t - x.z)) * a.Hq + h;
+  };
+  float high = -INFINITY;
+  for (int c = lane; c < n; c += 64) {
+    const float x = a.part_lse[part_of(c)];
+    high = x > high || x != x ? x : high;      // NaN stays
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float x = __shfl_xor(high, o, 64);
+    high = x > high || x != x ? x : high;
+  }
+  const float now = high == -INFINITY ? 0.f : high;
+  float total = 0.f, acc[kMaxHeadDim / 16] = {};
+  for (int c0 = 0; c0 < n; c0 += 4) {
+    const int c = c0 + slot;
+    float w = 0.f;
+    if (c < n) {
+      const int64_t p = part_of(c);
+      w = __builtin_amdgcn_exp2f((a.part_lse[p] - now) * kLog2e);
+      const float* from = a.part_out + p * D;
+#pragma unroll
+      for (int x = 0; x < kMaxHeadDim / 128; ++x) {
+        const int d = 128 * x + 8 * l;
+        if (d < D) {
+          const f32x4 y0 = *reinterpret_cast<const f32x4*>(from + d), y1 = *reinterpret_cast<const f32x4*>(from + d + 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            acc[8 * x + i] = fmaf(w, y0[i], acc[8 * x + i]);
+            acc[8 * x + 4 + i] = fmaf(w, y1[i], acc[8 * x + 4 + i]);
           }
         }
       }
     }
+    total += w;
   }
-  const T* qr = static_cast<const T*>(q.data) + t * q.ts + h * q.hs;
-  for (int d = lane; d < D; d += 64) q_lds[wave][d] = to_f32(qr[d]) * scale;
-  __builtin_amdgcn_wave_barrier();
-  float acc[kMaxHeadDim / 64] = {}, m = -INFINITY, l = 0.f;
-  for (int seg = 0; seg < 2; ++seg) {
-    const int n = seg ? own : prefix;
-    const int32_t* table = seg ? kv.pages + static_cast<int64_t>(s) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(g) * kv.max_prefix_pages;
-    for (int i0 = 0; i0 < n; i0 += 64) {
-      const int i = i0 + lane;
-      int64_t row = -1;
-      float z = -INFINITY;
-      if (i < n) {
-        const int page = table[i >> kv.page_shift];
-        if (static_cast<unsigned>(page) < static_cast<unsigned>(kv.n_pages)) {
-          row = (((static_cast<int64_t>(page) * kv.Hk + hk) << kv.page_shift) + (i & ((1 << kv.page_shift) - 1))) * D;
-          const T* kr = static_cast<const T*>(kv.k) + row;
-          z = 0.f;
-          for (int d = 0; d < D; ++d) z = fmaf(q_lds[wave][d], to_f32(kr[d]), z);
-        } else {
-          error |= AT_GRPO_DATA_PAGE;
+  total += __shfl_xor(total, 16, 64);
+  total += __shfl_xor(total, 32, 64);
+#pragma unroll
+  for (int i = 0; i < kMaxHeadDim / 16; ++i) {
+    acc[i] += __shfl_xor(acc[i], 16, 64);
+    acc[i] += __shfl_xor(acc[i], 32, 64);
+  }
+  if (slot == 0) {
+    const float f = total == 0.f ? 0.f : 1.f / total;
+    T* to = static_cast<T*>(a.out.data) + t * a.out.ts + h * a.out.hs;
+#pragma unroll
+    for (int x = 0; x < kMaxHeadDim / 128; ++x) {
+      const int d = 128 * x + 8 * l;
+      if (d < D)
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+          const float* y = acc + 8 * x + i;
+          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to + d + i) = make_uint2(pack_bf16x2(y[0] * f, y[1] * f), pack_bf16x2(y[2] * f, y[3] * f));
+          else *reinterpret_cast<f32x4*>(to + d + i) = f32x4{y[0] * f, y[1] * f, y[2] * f, y[3] * f};
         }
-      }
-      float top = z;
-      for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-      const float now = fmaxf(m, top), ref = now == -INFINITY ? 0.f : now, keep = expf(m - ref), p = row >= 0 ? expf(z - ref) : 0.f;
-      float sum = p;
-      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
-      l = l * keep + sum;
-      m = now;
-      for (int e = 0; e < kMaxHeadDim / 64; ++e) acc[e] *= keep;
-      for (int j = 0; j < min(64, n - i0); ++j) {
-        const int64_t r = __shfl(row, j, 64);
-        const float pj = __shfl(p, j, 64);
-        if (r < 0) continue;
-        const T* vr = static_cast<const T*>(kv.v) + r;
-        for (int e = 0; e < kMaxHeadDim / 64; ++e)
-          if (e * 64 + lane < D) acc[e] = fmaf(pj, to_f32(vr[e * 64 + lane]), acc[e]);
-      }
     }
+    if (a.lse && l == 0) a.lse[unit] = total == 0.f ? -INFINITY : now + logf(total);
   }
-  raise_data_error(data_error, error);
-  T* o = static_cast<T*>(out.data) + t * out.ts + h * out.hs;
-  for (int e = 0; e < kMaxHeadDim / 64; ++e)
-    if (e * 64 + lane < D) o[e * 64 + lane] = from_f32<T>(l == 0.f ? 0.f : acc[e] / l);
-  if (lse && lane == 0) lse[unit] = l == 0.f ? -INFINITY : m + logf(l);
 }
 
-size_t workspace_of(const at_grpo_kv*, int32_t, int32_t, int32_t) {
-  WsAlloc ws(nullptr);
-  ws.take<int32_t>(64);
-  return ws.bytes();
-}
-
+// ---- host -------------------------------------------------------------------------------------------
 int check_sizes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q) {
   ATG_TRY(check_kv_sizes(kv, n_tok));
   if (Hq <= 0 || Hq % kv->Hk || max_q < 1) return AT_GRPO_EINVAL;
-  return static_cast<int64_t>(n_tok) * Hq <= 0x7fffff00 ? AT_GRPO_OK : AT_GRPO_EUNSUPPORTED;
+  // rows of parts and items are counted in 32 bits
+  const int64_t units = static_cast<int64_t>(kv->n_seq) + kv->n_group;
+  return static_cast<int64_t>(n_tok) * Hq <= 0x3f000000 && units * kv->Hk <= 0x3f000000 ? AT_GRPO_OK : AT_GRPO_EUNSUPPORTED;
+}
+
+// Chunks are ceil(cost / kTarget) blocks of 64 tokens long or longer (cost: blocks times tiles times key heads), so they cut the rows of
+// all units into at most kTarget * kMaxRows rows of parts more than one for each query, head and kind of unit.
+struct Scratch {
+  int4* units;
+  float *part_lse, *part_out;
+};
+
+Scratch lay_out(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, WsAlloc& ws) {
+  const size_t rows = static_cast<size_t>(kTarget) * kMaxRows + static_cast<size_t>(n_tok) * Hq * (kv->n_group > 0 ? 2 : 1);
+  Scratch s;
+  s.units = ws.take<int4>(static_cast<size_t>(kv->n_seq) + kv->n_group);
+  s.part_lse = ws.take<float>(rows);
+  s.part_out = ws.take<float>(rows * kv->D);
+  return s;
+}
+
+typedef void (*Kernel)(KvView, Args);
+struct Choice {
+  Kernel kernel;
+  int rows_p, rows_o;
+};
+
+template <typename T, int D, bool EXACT>
+Choice choose_of(int rows_p, int rows_o) {
+  constexpr int kMost = sizeof(T) == 4 || D == 256 ? 2 : 4;
+  if constexpr (!EXACT) {
+    return {k_attend<T, D, kMost, kMost, false>, 16 * kMost, 16 * kMost};
+  } else {
+    if (rows_o > 16) return {k_attend<T, D, kMost, kMost, true>, 16 * kMost, 16 * kMost};
+    if (rows_p > 32 && kMost == 4) return {k_attend<T, D, kMost, 1, true>, 16 * kMost, 16};
+    if (rows_p > 16) return {k_attend<T, D, 2, 1, true>, 32, 16};
+    return {k_attend<T, D, 1, 1, true>, 16, 16};
+  }
+}
+
+template <typename T>
+Choice choose(int D, int rows_p, int rows_o) {
+  if (D == 64) return choose_of<T, 64, true>(rows_p, rows_o);
+  if (D == 128) return choose_of<T, 128, true>(rows_p, rows_o);
+  if (D == 256) return choose_of<T, 256, true>(rows_p, rows_o);
+  if (D < 64) return choose_of<T, 64, false>(rows_p, rows_o);
+  if (D < 128) return choose_of<T, 128, false>(rows_p, rows_o);
+  return choose_of<T, 256, false>(rows_p, rows_o);
 }
 
 }  // namespace
@@ -122,7 +638,10 @@ int check_sizes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q) 
 using namespace atg;
 
 extern "C" size_t at_grpo_prefix_attention_workspace_bytes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q) {
-  return check_sizes(kv, n_tok, Hq, max_q) == AT_GRPO_OK ? workspace_of(kv, n_tok, Hq, max_q) : 0;
+  if (check_sizes(kv, n_tok, Hq, max_q) != AT_GRPO_OK) return 0;
+  WsAlloc ws(nullptr);
+  lay_out(kv, n_tok, Hq, ws);
+  return ws.bytes();
 }
 
 extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* q, float scale, int32_t causal,
@@ -135,12 +654,25 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   if (n_tok == 0) return AT_GRPO_OK;
   ATG_TRY(check_rows(q, kv->dtype));
   ATG_TRY(check_rows(out, kv->dtype));
-  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < workspace_of(kv, n_tok, Hq, max_q)) return AT_GRPO_EWORKSPACE;
+  WsAlloc ws(workspace);
+  const Scratch scratch = lay_out(kv, n_tok, Hq, ws);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < ws.bytes()) return AT_GRPO_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const unsigned blocks = static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * Hq, 4));
+  const int share = Hq / kv->Hk;
+  const Args args{n_tok, Hq, share, causal != 0, scale, rows_of(q), rows_of(out), lse, data_error, scratch.units, scratch.part_lse, scratch.part_out};
+  const int64_t all_rows = static_cast<int64_t>(n_tok) * share;
+  const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
+  auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
+  const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, small(rows_p), small(rows_o)) : choose<float>(kv->D, small(rows_p), small(rows_o));
+  // as many workgroups as there can be items, to whole rounds over the XCDs; beyond that they loop
+  const int64_t tiles = (kv->n_group ? all_rows / k.rows_p + kv->n_group : 0) + all_rows / k.rows_o + kv->n_seq;
+  const int64_t items = kTarget + tiles * kv->Hk;
+  const unsigned blocks = static_cast<unsigned>(items < 16384 ? round_up(items, 8) : 16384);
   ProfScope ps(PROF_ATTENTION, s);
-  auto k = kv->dtype == AT_GRPO_BF16 ? k_attend<bf16_t> : k_attend<float>;
-  hipLaunchKernelGGL(k, dim3(blocks), dim3(256), 0, s, view, n_tok, Hq, rows_of(q), scale, causal, rows_of(out), lse, data_error);
+  hipLaunchKernelGGL(k.kernel, dim3(blocks), dim3(256), 0, s, view, args);
+  ATG_LAUNCH_CHECK();
+  auto join = kv->dtype == AT_GRPO_BF16 ? k_join<bf16_t> : k_join<float>;
+  hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * Hq, 4))), dim3(256), 0, s, view, args);
   ATG_LAUNCH_CHECK();
   return AT_GRPO_OK;
 }
