@@ -11,13 +11,15 @@
 
 #include <math.h>
 
+#include <type_traits>
+
 namespace atg {
 
 namespace {
 
 struct Layer {
   int D, half, interleaved, n_pos;   // half: pairs that turn
-  float eps;
+  float eps, inv_D;
   const float* table;
   const void *qw, *kw;
 };
@@ -26,53 +28,107 @@ struct Pairs {
   float a[4], b[4];
 };
 
-// Where the pairs 4 l .. 4 l + 3 of a row lie.
+// A lane's eight elements of a row as they lie in memory: four from `lo` on and four from `hi` on, or, where rot_dim is no multiple of
+// eight (VEC false), the first and second elements of its four pairs one by one.
 struct Places {
-  int at_a[4], at_b[4];
+  int at[8];
+  bool apart;      // lo holds the pairs' first elements and hi their second; otherwise pairs lie side by side
 };
 
+template <bool VEC>
 __device__ __forceinline__ Places places_of(const Layer& L, int l) {
   Places p;
+  p.apart = !VEC || (!L.interleaved && 4 * l < L.half);
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int pair = 4 * l + i;
-    const bool apart = !L.interleaved && pair < L.half;
-    p.at_a[i] = apart ? pair : 2 * pair;
-    p.at_b[i] = apart ? pair + L.half : 2 * pair + 1;
+    const bool far = !L.interleaved && pair < L.half;
+    p.at[i] = far ? pair : VEC ? 8 * l + i : 2 * pair;
+    p.at[4 + i] = far ? pair + L.half : VEC ? 8 * l + 4 + i : 2 * pair + 1;
   }
   return p;
 }
 
 template <typename T>
-__device__ __forceinline__ Pairs load_pairs(const T* row, const Places& p) {
-  Pairs x;
+struct Raw;
+template <>
+struct Raw<bf16_t> {
+  uint2 lo, hi;
+};
+template <>
+struct Raw<float> {
+  float4 lo, hi;
+};
+
+template <bool VEC, typename T>
+__device__ __forceinline__ Raw<T> load_raw(const T* row, const Places& p) {
+  Raw<T> r;
+  if constexpr (VEC) {
+    r.lo = *reinterpret_cast<const decltype(r.lo)*>(row + p.at[0]);
+    r.hi = *reinterpret_cast<const decltype(r.hi)*>(row + p.at[4]);
+  } else {
+    T* x = reinterpret_cast<T*>(&r);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    x.a[i] = to_f32(row[p.at_a[i]]);
-    x.b[i] = to_f32(row[p.at_b[i]]);
+    for (int i = 0; i < 8; ++i) x[i] = row[p.at[i]];
   }
-  return x;
+  return r;
 }
 
-template <typename T>
-__device__ __forceinline__ void store_pairs(T* row, const Places& p, const Pairs& x) {
+template <bool VEC, typename T>
+__device__ __forceinline__ void store_raw(T* row, const Places& p, const Raw<T>& r) {
+  if constexpr (VEC) {
+    *reinterpret_cast<decltype(Raw<T>::lo)*>(row + p.at[0]) = r.lo;
+    *reinterpret_cast<decltype(Raw<T>::hi)*>(row + p.at[4]) = r.hi;
+  } else {
+    const T* x = reinterpret_cast<const T*>(&r);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    row[p.at_a[i]] = from_f32<T>(x.a[i]);
-    row[p.at_b[i]] = from_f32<T>(x.b[i]);
+    for (int i = 0; i < 8; ++i) row[p.at[i]] = x[i];
   }
+}
+
+__device__ __forceinline__ Pairs sorted(const float (&lo)[4], const float (&hi)[4], bool apart) {
+  return Pairs{{lo[0], apart ? lo[1] : lo[2], apart ? lo[2] : hi[0], apart ? lo[3] : hi[2]},
+               {apart ? hi[0] : lo[1], apart ? hi[1] : lo[3], apart ? hi[2] : hi[1], hi[3]}};
+}
+
+__device__ __forceinline__ Pairs pairs_of(const Raw<float>& r, const Places& p) {
+  const float lo[4] = {r.lo.x, r.lo.y, r.lo.z, r.lo.w}, hi[4] = {r.hi.x, r.hi.y, r.hi.z, r.hi.w};
+  return sorted(lo, hi, p.apart);
+}
+__device__ __forceinline__ Pairs pairs_of(const Raw<bf16_t>& r, const Places& p) {
+  const auto low = [](uint32_t x) { return __uint_as_float(x << 16); };
+  const auto high = [](uint32_t x) { return __uint_as_float(x & 0xffff0000u); };
+  const float lo[4] = {low(r.lo.x), high(r.lo.x), low(r.lo.y), high(r.lo.y)}, hi[4] = {low(r.hi.x), high(r.hi.x), low(r.hi.y), high(r.hi.y)};
+  return sorted(lo, hi, p.apart);
+}
+
+// pairs_of backwards
+template <typename T>
+__device__ __forceinline__ Raw<T> raw_of(const Pairs& x, const Places& p) {
+  const float lo[4] = {x.a[0], p.apart ? x.a[1] : x.b[0], p.apart ? x.a[2] : x.a[1], p.apart ? x.a[3] : x.b[1]};
+  const float hi[4] = {p.apart ? x.b[0] : x.a[2], p.apart ? x.b[1] : x.b[2], p.apart ? x.b[2] : x.a[3], x.b[3]};
+  if constexpr (sizeof(T) == 4) return Raw<T>{make_float4(lo[0], lo[1], lo[2], lo[3]), make_float4(hi[0], hi[1], hi[2], hi[3])};
+  else
+    return Raw<T>{make_uint2(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3])), make_uint2(pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3]))};
 }
 
 // Cosines and sines of a lane's pairs; 1 and 0 behind the last that turns.
+template <bool VEC>
 __device__ __forceinline__ Pairs load_turn(const Layer& L, int l, int position) {
-  Pairs t;
+  Pairs t{{1.f, 1.f, 1.f, 1.f}, {}};
+  const float* e = L.table + 2 * (static_cast<int64_t>(position) * L.half + 4 * l);
+  if constexpr (VEC) {
+    if (4 * l < L.half) {
+      const float4 x = *reinterpret_cast<const float4*>(e), y = *reinterpret_cast<const float4*>(e + 4);
+      t = Pairs{{x.x, x.z, y.x, y.z}, {x.y, x.w, y.y, y.w}};
+    }
+  } else {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int pair = 4 * l + i;
-    const bool turns = pair < L.half;
-    const float* e = L.table + 2 * (static_cast<int64_t>(position) * L.half + pair);
-    t.a[i] = turns ? e[0] : 1.f;
-    t.b[i] = turns ? e[1] : 0.f;
+    for (int i = 0; i < 4; ++i)
+      if (4 * l + i < L.half) {
+        t.a[i] = e[2 * i];
+        t.b[i] = e[2 * i + 1];
+      }
   }
   return t;
 }
@@ -89,7 +145,7 @@ __device__ __forceinline__ float inverse_size(const Pairs& x, const Layer& L) {
   float ss = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) ss = fmaf(x.a[i], x.a[i], fmaf(x.b[i], x.b[i], ss));
-  return 1.f / sqrtf(row_sum<LANES>(ss) / static_cast<float>(L.D) + L.eps);
+  return rsqrtf(fmaf(row_sum<LANES>(ss), L.inv_D, L.eps));
 }
 
 // Where a new token belongs: its position, and its place in the cache (rows between its heads are page_size * D apart).
@@ -140,137 +196,202 @@ __device__ __forceinline__ Spot find_spot(const KvView& kv, int n_pos, int t, in
   return spot;
 }
 
-// The heads of one token that a wavefront takes: part, part + parts, .. of groups of 64 / LANES heads.
-template <typename T, int LANES>
-__device__ void rotate_rows(const Layer& L, const T* src, int64_t src_hs, T* dst, int64_t dst_hs, int H, const void* weight, const Pairs& turn,
-                            const Places& p, bool zero, int part, int parts) {
-  constexpr int G = 64 / LANES;
-  const int l = threadIdx.x & (LANES - 1), grp = (threadIdx.x & 63) / LANES;
-  const bool mine = 8 * l < L.D;
-  Pairs w{{1.f, 1.f, 1.f, 1.f}, {1.f, 1.f, 1.f, 1.f}};
-  if (weight && mine) w = load_pairs(static_cast<const T*>(weight), p);
-  for (int h0 = part * G; h0 < H; h0 += parts * G) {
-    const int h = h0 + grp;
-    const bool on = mine && h < H;
-    Pairs x{};
-    if (on && !zero) x = load_pairs(src + h * src_hs, p);
-    if (weight) {
-      const float r = inverse_size<LANES>(x, L);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x.a[i] *= r * w.a[i];
-        x.b[i] *= r * w.b[i];
-      }
-    }
-    Pairs y;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y.a[i] = fmaf(x.a[i], turn.a[i], -x.b[i] * turn.b[i]);
-      y.b[i] = fmaf(x.b[i], turn.a[i], x.a[i] * turn.b[i]);
-    }
-    if (zero) y = Pairs{};
-    if (on) store_pairs(dst + h * dst_hs, p, y);
-  }
+// The rows of one token are its queries' heads, then its keys', then (appending) its values'; a wavefront takes every parts-th group of
+// 64 / LANES of them, kBatch groups in flight at a time.  Where a row lies: element 0 of head j of its kind.
+constexpr int kBatch = 4;
+
+template <typename T>
+struct Token {
+  const T* src[3];
+  T* dst[3];
+  int64_t src_hs[3], dst_hs[3];
+  int end[3];        // first row behind the kind
+};
+
+template <typename T>
+__device__ __forceinline__ const T* source_of(const Token<T>& t, int j) {
+  return j < t.end[0] ? t.src[0] + j * t.src_hs[0] : j < t.end[1] ? t.src[1] + (j - t.end[0]) * t.src_hs[1] : t.src[2] + (j - t.end[1]) * t.src_hs[2];
+}
+template <typename T>
+__device__ __forceinline__ T* target_of(const Token<T>& t, int j) {
+  return j < t.end[0] ? t.dst[0] + j * t.dst_hs[0] : j < t.end[1] ? t.dst[1] + (j - t.end[0]) * t.dst_hs[1] : t.dst[2] + (j - t.end[1]) * t.dst_hs[2];
 }
 
-template <typename T, int LANES>
+template <typename T, int LANES, bool VEC>
+struct Rotator {
+  static constexpr int G = 64 / LANES;
+  const Layer& L;
+  const Places p;
+  const int l, grp;
+  const bool mine;
+  Pairs wq{{1.f, 1.f, 1.f, 1.f}, {1.f, 1.f, 1.f, 1.f}}, wk = wq;
+  Raw<T> x[kBatch];
+
+  __device__ __forceinline__ explicit Rotator(const Layer& layer)
+      : L(layer), p(places_of<VEC>(layer, threadIdx.x & (LANES - 1))), l(threadIdx.x & (LANES - 1)), grp((threadIdx.x & 63) / LANES), mine(8 * l < layer.D) {
+    if (mine && L.qw) wq = pairs_of(load_raw<VEC>(static_cast<const T*>(L.qw), p), p);
+    if (mine && L.kw) wk = pairs_of(load_raw<VEC>(static_cast<const T*>(L.kw), p), p);
+  }
+
+  __device__ __forceinline__ void load(const Token<T>& t, int j0, int step) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int j = j0 + i * step + grp;
+      x[i] = Raw<T>{};
+      if (mine && j < t.end[2]) x[i] = load_raw<VEC>(source_of(t, j), p);
+    }
+  }
+
+  // zero: queries get zeros, and there is no place for the rest
+  __device__ __forceinline__ void store(const Token<T>& t, int j0, int step, const Pairs& turn, bool zero) {
+#pragma unroll
+    for (int i = 0; i < kBatch; ++i) {
+      const int j = j0 + i * step + grp;
+      if (j0 + i * step >= t.end[2]) break;
+      const bool is_q = j < t.end[0], value = j >= t.end[1], norm = is_q ? L.qw != nullptr : !value && L.kw != nullptr;
+      Pairs u = pairs_of(x[i], p);
+      const float r = inverse_size<LANES>(u, L);
+      Raw<T> y = x[i];
+      if (!value) {
+        Pairs v;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (norm) {
+            u.a[e] *= r * (is_q ? wq.a[e] : wk.a[e]);
+            u.b[e] *= r * (is_q ? wq.b[e] : wk.b[e]);
+          }
+          v.a[e] = fmaf(u.a[e], turn.a[e], -u.b[e] * turn.b[e]);
+          v.b[e] = fmaf(u.b[e], turn.a[e], u.a[e] * turn.b[e]);
+        }
+        y = raw_of<T>(v, p);
+      }
+      if (zero) y = Raw<T>{};
+      if (mine && j < t.end[2]) store_raw<VEC>(target_of(t, j), p, y);
+    }
+  }
+};
+
+template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts, int Hq, int Hk, Rows q, Rows k, const int32_t* __restrict__ position,
                                                    Rows q_out, Rows k_out, int32_t* data_error) {
   const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int t = unit / parts, part = unit - t * parts, l = threadIdx.x & (LANES - 1);
+  const int t = unit / parts, part = unit - t * parts;
   if (t >= n_tok) return;
+  const Token<T> token{{static_cast<const T*>(q.data) + t * q.ts, static_cast<const T*>(k.data) + t * k.ts, nullptr},
+                       {static_cast<T*>(q_out.data) + t * q_out.ts, static_cast<T*>(k_out.data) + t * k_out.ts, nullptr},
+                       {q.hs, k.hs, 0}, {q_out.hs, k_out.hs, 0}, {Hq, Hq + Hk, Hq + Hk}};
+  Rotator<T, LANES, VEC> R(L);
+  const int step = parts * R.G;
+  int j0 = part * R.G;
   const int pos = L.half ? position[t] : 0;
+  R.load(token, j0, step);
   const bool bad = L.half && static_cast<unsigned>(pos) >= static_cast<unsigned>(L.n_pos);
-  if (bad && (threadIdx.x & 63) == 0) raise_data_error(data_error, AT_GRPO_DATA_POSITION);
-  const Places p = places_of(L, l);
+  if (bad && part == 0 && (threadIdx.x & 63) == 0) raise_data_error(data_error, AT_GRPO_DATA_POSITION);
   Pairs turn{{1.f, 1.f, 1.f, 1.f}, {}};
-  if (!bad && L.half) turn = load_turn(L, l, pos);
-  if (Hq) rotate_rows<T, LANES>(L, static_cast<const T*>(q.data) + t * q.ts, q.hs, static_cast<T*>(q_out.data) + t * q_out.ts, q_out.hs, Hq, L.qw, turn, p,
-                                bad, part, parts);
-  if (Hk) rotate_rows<T, LANES>(L, static_cast<const T*>(k.data) + t * k.ts, k.hs, static_cast<T*>(k_out.data) + t * k_out.ts, k_out.hs, Hk, L.kw, turn, p,
-                                bad, part, parts);
+  if (!bad && L.half) turn = load_turn<VEC>(L, R.l, pos);
+  for (;;) {
+    R.store(token, j0, step, turn, bad);
+    j0 += kBatch * step;
+    if (j0 >= Hq + Hk) break;
+    R.load(token, j0, step);
+  }
 }
 
-template <typename T, int LANES>
+template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_kv_append(KvView kv, Layer L, int n_tok, int parts, int Hq, Rows q, Rows k, Rows v, Rows q_out,
                                                    int32_t* data_error) {
-  constexpr int G = 64 / LANES;
   const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int t = unit / parts, part = unit - t * parts, l = threadIdx.x & (LANES - 1), grp = (threadIdx.x & 63) / LANES;
+  const int t = unit / parts, part = unit - t * parts;
   if (t >= n_tok) return;
+  const int64_t hs = static_cast<int64_t>(kv.D) << kv.page_shift;
+  Token<T> token{{static_cast<const T*>(q.data) + t * q.ts, static_cast<const T*>(k.data) + t * k.ts, static_cast<const T*>(v.data) + t * v.ts},
+                 {static_cast<T*>(q_out.data) + t * q_out.ts, static_cast<T*>(kv.k), static_cast<T*>(kv.v)},
+                 {q.hs, k.hs, v.hs}, {q_out.hs, hs, hs}, {Hq, Hq + kv.Hk, Hq + 2 * kv.Hk}};
+  Rotator<T, LANES, VEC> R(L);
+  const int step = parts * R.G;
+  int j0 = part * R.G;
+  R.load(token, j0, step);      // rows do not wait for where they go
   const Spot spot = find_spot(kv, L.half ? L.n_pos : -1, t, part == 0 ? data_error : nullptr);
   const bool bad = spot.position < 0;
-  const Places p = places_of(L, l);
   Pairs turn{{1.f, 1.f, 1.f, 1.f}, {}};
-  if (!bad && L.half) turn = load_turn(L, l, spot.position);
-  if (Hq) rotate_rows<T, LANES>(L, static_cast<const T*>(q.data) + t * q.ts, q.hs, static_cast<T*>(q_out.data) + t * q_out.ts, q_out.hs, Hq, L.qw, turn, p,
-                                bad, part, parts);
-  if (bad) return;
-  const int64_t hs = static_cast<int64_t>(kv.D) << kv.page_shift;
-  rotate_rows<T, LANES>(L, static_cast<const T*>(k.data) + t * k.ts, k.hs, static_cast<T*>(kv.k) + spot.at, hs, kv.Hk, L.kw, turn, p, false, part, parts);
-  if (8 * l >= L.D) return;
-  for (int h = part * G + grp; h < kv.Hk; h += parts * G) {
-    const uint4* from = reinterpret_cast<const uint4*>(static_cast<const T*>(v.data) + t * v.ts + h * v.hs + 8 * l);
-    uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(kv.v) + spot.at + h * hs + 8 * l);
-#pragma unroll
-    for (int i = 0; i < static_cast<int>(sizeof(T)) / 2; ++i) to[i] = from[i];
+  if (!bad && L.half) turn = load_turn<VEC>(L, R.l, spot.position);
+  token.dst[1] += spot.at;
+  token.dst[2] += spot.at;
+  if (bad) token.end[1] = token.end[2] = Hq;
+  for (;;) {
+    R.store(token, j0, step, turn, bad);
+    j0 += kBatch * step;
+    if (j0 >= token.end[2]) break;
+    R.load(token, j0, step);
   }
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------
 constexpr int kGradBlocks = 1024;
 
-template <typename T, int LANES>
-__device__ void rotate_rows_back(const Layer& L, const T* dy, int64_t dy_hs, const T* src, int64_t src_hs, T* dst, int64_t dst_hs, int H, const void* weight,
-                                 const Pairs& turn, const Places& p, bool zero, int part, int parts, Pairs& dw) {
+constexpr int kGradBatch = 2;
+
+template <typename T, int LANES, bool VEC>
+__device__ __forceinline__ void rotate_rows_back(const Layer& L, const T* dy, int64_t dy_hs, const T* src, int64_t src_hs, T* dst, int64_t dst_hs, int H,
+                                                 const Pairs& w, bool norm, const Pairs& turn, const Places& p, bool zero, int part, int parts, Pairs& dw) {
   constexpr int G = 64 / LANES;
   const int l = threadIdx.x & (LANES - 1), grp = (threadIdx.x & 63) / LANES;
   const bool mine = 8 * l < L.D;
-  Pairs w{};
-  if (weight && mine) w = load_pairs(static_cast<const T*>(weight), p);
-  for (int h0 = part * G; h0 < H; h0 += parts * G) {
-    const int h = h0 + grp;
-    const bool on = mine && h < H;
-    Pairs x{}, g{};
-    if (on && !zero) {
-      const Pairs d = load_pairs(dy + h * dy_hs, p);
+  for (int h0 = part * G; h0 < H; h0 += kGradBatch * parts * G) {
+    Raw<T> rx[kGradBatch], rg[kGradBatch];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        g.a[i] = fmaf(d.a[i], turn.a[i], d.b[i] * turn.b[i]);
-        g.b[i] = fmaf(d.b[i], turn.a[i], -d.a[i] * turn.b[i]);
+    for (int i = 0; i < kGradBatch; ++i) {
+      const int h = h0 + i * parts * G + grp;
+      rx[i] = rg[i] = Raw<T>{};
+      if (mine && h < H && !zero) {
+        rg[i] = load_raw<VEC>(dy + h * dy_hs, p);
+        if (norm) rx[i] = load_raw<VEC>(src + h * src_hs, p);
       }
-      if (weight) x = load_pairs(src + h * src_hs, p);
     }
-    if (weight) {
-      const float r = inverse_size<LANES>(x, L);
-      float dot = 0.f;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x.a[i] *= r;
-        x.b[i] *= r;
-        if (on && !zero) {      // lanes without a row would add 0 times the size of no row
-          dw.a[i] = fmaf(g.a[i], x.a[i], dw.a[i]);
-          dw.b[i] = fmaf(g.b[i], x.b[i], dw.b[i]);
+    for (int i = 0; i < kGradBatch; ++i) {
+      const int h = h0 + i * parts * G + grp;
+      if (h0 + i * parts * G >= H) break;
+      const bool on = mine && h < H;
+      const Pairs d = pairs_of(rg[i], p);
+      Pairs x = pairs_of(rx[i], p), g;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        g.a[e] = fmaf(d.a[e], turn.a[e], d.b[e] * turn.b[e]);
+        g.b[e] = fmaf(d.b[e], turn.a[e], -d.a[e] * turn.b[e]);
+      }
+      if (norm) {
+        const float r = inverse_size<LANES>(x, L);
+        float dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          x.a[e] *= r;
+          x.b[e] *= r;
+          if (on && !zero) {      // a lane without a row would add 0 times the size of no row
+            dw.a[e] = fmaf(g.a[e], x.a[e], dw.a[e]);
+            dw.b[e] = fmaf(g.b[e], x.b[e], dw.b[e]);
+          }
+          g.a[e] *= w.a[e];
+          g.b[e] *= w.b[e];
+          dot = fmaf(g.a[e], x.a[e], fmaf(g.b[e], x.b[e], dot));
         }
-        g.a[i] *= w.a[i];
-        g.b[i] *= w.b[i];
-        dot = fmaf(g.a[i], x.a[i], fmaf(g.b[i], x.b[i], dot));
-      }
-      const float mean = row_sum<LANES>(dot) / static_cast<float>(L.D);
+        const float mean = row_sum<LANES>(dot) * L.inv_D;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        g.a[i] = r * fmaf(-x.a[i], mean, g.a[i]);
-        g.b[i] = r * fmaf(-x.b[i], mean, g.b[i]);
+        for (int e = 0; e < 4; ++e) {
+          g.a[e] = r * fmaf(-x.a[e], mean, g.a[e]);
+          g.b[e] = r * fmaf(-x.b[e], mean, g.b[e]);
+        }
       }
+      Raw<T> y = raw_of<T>(g, p);
+      if (zero) y = Raw<T>{};
+      if (on) store_raw<VEC>(dst + h * dst_hs, p, y);
     }
-    if (zero) g = Pairs{};
-    if (on) store_pairs(dst + h * dst_hs, p, g);
   }
 }
 
 // The rows of one kind (0 queries, 1 keys) that a workgroup's lanes added up, as one row of partial sums.
-template <int LANES>
-__device__ void store_partial(const Layer& L, Pairs dw, const Places& p, float* lds, float* __restrict__ partial) {
+template <int LANES, bool VEC>
+__device__ void store_partial(const Layer& L, Pairs dw, float* lds, float* __restrict__ partial) {
   const int l = threadIdx.x & (LANES - 1), lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -283,8 +404,10 @@ __device__ void store_partial(const Layer& L, Pairs dw, const Places& p, float* 
   if (lane < LANES && 8 * l < L.D) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      lds[wave * kMaxHeadDim + p.at_a[i]] = dw.a[i];
-      lds[wave * kMaxHeadDim + p.at_b[i]] = dw.b[i];
+      const int pair = 4 * l + i;
+      const bool far = !L.interleaved && pair < L.half;
+      lds[wave * kMaxHeadDim + (far ? pair : 2 * pair)] = dw.a[i];
+      lds[wave * kMaxHeadDim + (far ? pair + L.half : 2 * pair + 1)] = dw.b[i];
     }
   }
   __syncthreads();
@@ -292,14 +415,16 @@ __device__ void store_partial(const Layer& L, Pairs dw, const Places& p, float* 
   if (d < L.D) partial[d] = (lds[d] + lds[kMaxHeadDim + d]) + (lds[2 * kMaxHeadDim + d] + lds[3 * kMaxHeadDim + d]);
 }
 
-template <typename T, int LANES>
+template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_norm_rope_bwd(Layer L, int n_tok, int parts, int Hq, int Hk, Rows dq_out, Rows dk_out, Rows q, Rows k,
                                                        const int32_t* __restrict__ position, Rows dq, Rows dk, float* __restrict__ partial,
                                                        int32_t* data_error) {
   __shared__ float lds[4 * kMaxHeadDim];
   const int l = threadIdx.x & (LANES - 1);
-  const Places p = places_of(L, l);
-  Pairs dwq{}, dwk{};
+  const Places p = places_of<VEC>(L, l);
+  Pairs dwq{}, dwk{}, wq{}, wk{};
+  if (8 * l < L.D && L.qw) wq = pairs_of(load_raw<VEC>(static_cast<const T*>(L.qw), p), p);
+  if (8 * l < L.D && L.kw) wk = pairs_of(load_raw<VEC>(static_cast<const T*>(L.kw), p), p);
   const int64_t units = static_cast<int64_t>(n_tok) * parts;
   for (int64_t unit = blockIdx.x * 4 + (threadIdx.x >> 6); unit < units; unit += gridDim.x * 4) {
     const int64_t t = unit / parts;
@@ -308,34 +433,37 @@ __global__ __launch_bounds__(256) void k_norm_rope_bwd(Layer L, int n_tok, int p
     const bool bad = L.half && static_cast<unsigned>(pos) >= static_cast<unsigned>(L.n_pos);
     if (bad && part == 0 && (threadIdx.x & 63) == 0) raise_data_error(data_error, AT_GRPO_DATA_POSITION);
     Pairs turn{{1.f, 1.f, 1.f, 1.f}, {}};
-    if (!bad && L.half) turn = load_turn(L, l, pos);
+    if (!bad && L.half) turn = load_turn<VEC>(L, l, pos);
     if (Hq)
-      rotate_rows_back<T, LANES>(L, static_cast<const T*>(dq_out.data) + t * dq_out.ts, dq_out.hs, static_cast<const T*>(q.data) + t * q.ts, q.hs,
-                                 static_cast<T*>(dq.data) + t * dq.ts, dq.hs, Hq, L.qw, turn, p, bad, part, parts, dwq);
+      rotate_rows_back<T, LANES, VEC>(L, static_cast<const T*>(dq_out.data) + t * dq_out.ts, dq_out.hs, static_cast<const T*>(q.data) + t * q.ts, q.hs,
+                                      static_cast<T*>(dq.data) + t * dq.ts, dq.hs, Hq, wq, L.qw != nullptr, turn, p, bad, part, parts, dwq);
     if (Hk)
-      rotate_rows_back<T, LANES>(L, static_cast<const T*>(dk_out.data) + t * dk_out.ts, dk_out.hs, static_cast<const T*>(k.data) + t * k.ts, k.hs,
-                                 static_cast<T*>(dk.data) + t * dk.ts, dk.hs, Hk, L.kw, turn, p, bad, part, parts, dwk);
+      rotate_rows_back<T, LANES, VEC>(L, static_cast<const T*>(dk_out.data) + t * dk_out.ts, dk_out.hs, static_cast<const T*>(k.data) + t * k.ts, k.hs,
+                                      static_cast<T*>(dk.data) + t * dk.ts, dk.hs, Hk, wk, L.kw != nullptr, turn, p, bad, part, parts, dwk);
   }
-  if (L.qw) store_partial<LANES>(L, dwq, p, lds, partial + static_cast<int64_t>(blockIdx.x) * L.D);
-  if (L.kw) store_partial<LANES>(L, dwk, p, lds, partial + (static_cast<int64_t>(kGradBlocks) + blockIdx.x) * L.D);
+  if (L.qw) store_partial<LANES, VEC>(L, dwq, lds, partial + static_cast<int64_t>(blockIdx.x) * L.D);
+  if (L.kw) store_partial<LANES, VEC>(L, dwk, lds, partial + (static_cast<int64_t>(kGradBlocks) + blockIdx.x) * L.D);
 }
 
-// d_weight[d] = sum over the workgroups' rows, 16 elements a workgroup, in 64 bits
-__global__ __launch_bounds__(256) void k_weight_grad(int D, int blocks, const float* __restrict__ partial, float* dq_weight, float* dk_weight) {
-  __shared__ double red[16][17];
-  const int c = threadIdx.x & 15, slice = threadIdx.x >> 4, d = blockIdx.x * 16 + c;
+// d_weight[d] = sum over the workgroups' rows, eight elements a workgroup, in 64 bits
+__global__ __launch_bounds__(1024) void k_weight_grad(int D, int blocks, const float* __restrict__ partial, float* dq_weight, float* dk_weight) {
+  __shared__ double red[128][8];
+  const int c = threadIdx.x & 7, slice = threadIdx.x >> 3, d = blockIdx.x * 8 + c;      // D is a multiple of 8
   float* out = blockIdx.y ? dk_weight : dq_weight;
   if (!out) return;
-  const float* rows = partial + static_cast<int64_t>(blockIdx.y) * kGradBlocks * D;
+  const float* rows = partial + static_cast<int64_t>(blockIdx.y) * kGradBlocks * D + d;
+  float x[kGradBlocks / 128];
+#pragma unroll
+  for (int i = 0; i < kGradBlocks / 128; ++i) x[i] = slice + 128 * i < blocks ? rows[static_cast<int64_t>(slice + 128 * i) * D] : 0.f;
   double s = 0.0;
-  if (d < D)
-    for (int b = slice; b < blocks; b += 16) s += static_cast<double>(rows[static_cast<int64_t>(b) * D + d]);
+#pragma unroll
+  for (int i = 0; i < kGradBlocks / 128; ++i) s += static_cast<double>(x[i]);
   red[slice][c] = s;
-  __syncthreads();
-  if (slice == 0 && d < D) {
-    for (int i = 1; i < 16; ++i) s += red[i][c];
-    out[d] = static_cast<float>(s);
+  for (int o = 64; o > 0; o >>= 1) {
+    __syncthreads();
+    if (slice < o) red[slice][c] += red[slice + o][c];
   }
+  if (slice == 0) out[d] = static_cast<float>(red[0][c]);
 }
 
 // ---- table ------------------------------------------------------------------------------------------
@@ -368,23 +496,30 @@ int check_layer(const at_grpo_norm_rope* a, Layer* out) {
   if (a->layout != AT_GRPO_ROPE_HALF && a->layout != AT_GRPO_ROPE_INTERLEAVED) return AT_GRPO_EINVAL;
   if (a->rot_dim > 0 && (!a->table || a->n_pos <= 0 || !aligned16(a->table))) return AT_GRPO_EINVAL;
   if ((a->q_weight && !aligned16(a->q_weight)) || (a->k_weight && !aligned16(a->k_weight))) return AT_GRPO_EINVAL;
-  *out = Layer{a->D, a->rot_dim / 2, a->layout, a->n_pos, a->eps, a->table, a->q_weight, a->k_weight};
+  *out = Layer{a->D, a->rot_dim / 2, a->layout, a->n_pos, a->eps, 1.f / static_cast<float>(a->D), a->table, a->q_weight, a->k_weight};
   return AT_GRPO_OK;
 }
 
 int lanes_of(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : 32; }
 
 // Few tokens are shared by several wavefronts each, so that the chip has work: about 4096 wavefronts, or all groups of heads.
-int parts_of(int n_tok, int most_heads, int lanes) {
-  const int groups = static_cast<int>(ceil_div(most_heads, 64 / lanes));
+int parts_of(int n_tok, int rows, int lanes) {
+  const int groups = static_cast<int>(ceil_div(rows, 64 / lanes));
   const int64_t want = ceil_div(4096, n_tok > 0 ? n_tok : 1);
   return static_cast<int>(want < groups ? want : groups);
 }
 
+// f(element, integral constant of the lanes of a row, whether pairs come in whole vectors)
 template <typename F>
-int by_type_and_lanes(int32_t dtype, int lanes, F f) {
-  if (dtype == AT_GRPO_BF16) return lanes == 8 ? f(bf16_t{}, std::integral_constant<int, 8>{}) : lanes == 16 ? f(bf16_t{}, std::integral_constant<int, 16>{}) : f(bf16_t{}, std::integral_constant<int, 32>{});
-  return lanes == 8 ? f(0.f, std::integral_constant<int, 8>{}) : lanes == 16 ? f(0.f, std::integral_constant<int, 16>{}) : f(0.f, std::integral_constant<int, 32>{});
+int by_shape(int32_t dtype, const Layer& L, F f) {
+  const auto by_lanes = [&](auto t, auto vec) -> int {
+    const int lanes = lanes_of(L.D);
+    if (lanes == 8) return f(t, std::integral_constant<int, 8>{}, vec);
+    return lanes == 16 ? f(t, std::integral_constant<int, 16>{}, vec) : f(t, std::integral_constant<int, 32>{}, vec);
+  };
+  const bool vec = L.half % 4 == 0;
+  if (dtype == AT_GRPO_BF16) return vec ? by_lanes(bf16_t{}, std::true_type{}) : by_lanes(bf16_t{}, std::false_type{});
+  return vec ? by_lanes(0.f, std::true_type{}) : by_lanes(0.f, std::false_type{});
 }
 
 }  // namespace
@@ -441,12 +576,12 @@ extern "C" int at_grpo_qk_norm_rope(const at_grpo_norm_rope* layer, int32_t n_to
   if (Hk) ATG_TRY(check_rows(k, layer->dtype));
   if (Hk) ATG_TRY(check_rows(k_out, layer->dtype));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const int lanes = lanes_of(L.D), parts = parts_of(n_tok, Hq > Hk ? Hq : Hk, lanes);
+  const int parts = parts_of(n_tok, Hq + Hk, lanes_of(L.D));
   const int64_t blocks = ceil_div(static_cast<int64_t>(n_tok) * parts, 4);
   if (blocks > 0x7fffffff || static_cast<int64_t>(n_tok) * parts > 0x7fffffff) return AT_GRPO_EUNSUPPORTED;
   ProfScope ps(PROF_ROPE, s);
-  return by_type_and_lanes(layer->dtype, lanes, [&](auto t, auto n) -> int {
-    hipLaunchKernelGGL((k_norm_rope<decltype(t), decltype(n)::value>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, L, n_tok, parts, Hq, Hk,
+  return by_shape(layer->dtype, L, [&](auto t, auto n, auto vec) -> int {
+    hipLaunchKernelGGL((k_norm_rope<decltype(t), decltype(n)::value, decltype(vec)::value>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, L, n_tok, parts, Hq, Hk,
                        Hq ? rows_of(q) : Rows{}, Hk ? rows_of(k) : Rows{}, position, Hq ? rows_of(q_out) : Rows{}, Hk ? rows_of(k_out) : Rows{}, data_error);
     ATG_LAUNCH_CHECK();
     return AT_GRPO_OK;
@@ -479,13 +614,13 @@ extern "C" int at_grpo_qk_norm_rope_bwd(const at_grpo_norm_rope* layer, int32_t 
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < qk_norm_rope_bwd_workspace()) return AT_GRPO_EWORKSPACE;
   float* partial = static_cast<float*>(workspace);
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const int lanes = lanes_of(L.D), parts = parts_of(n_tok, Hq > Hk ? Hq : Hk, lanes);
+  const int parts = parts_of(n_tok, Hq > Hk ? Hq : Hk, lanes_of(L.D));
   const int64_t want = ceil_div(static_cast<int64_t>(n_tok) * parts, 4);
   const unsigned blocks = static_cast<unsigned>(want > kGradBlocks ? kGradBlocks : want < 1 ? 1 : want);
   const bool rows = n_tok > 0;
   ProfScope ps(PROF_ROPE, s);
-  ATG_TRY(by_type_and_lanes(layer->dtype, lanes, [&](auto t, auto n) -> int {
-    hipLaunchKernelGGL((k_norm_rope_bwd<decltype(t), decltype(n)::value>), dim3(blocks), dim3(256), 0, s, L, n_tok, parts, Hq, Hk,
+  ATG_TRY(by_shape(layer->dtype, L, [&](auto t, auto n, auto vec) -> int {
+    hipLaunchKernelGGL((k_norm_rope_bwd<decltype(t), decltype(n)::value, decltype(vec)::value>), dim3(blocks), dim3(256), 0, s, L, n_tok, parts, Hq, Hk,
                        rows && Hq ? rows_of(dq_out) : Rows{}, rows && Hk ? rows_of(dk_out) : Rows{}, rows && L.qw ? rows_of(q) : Rows{},
                        rows && L.kw ? rows_of(k) : Rows{}, position, rows && Hq ? rows_of(dq) : Rows{}, rows && Hk ? rows_of(dk) : Rows{}, partial,
                        data_error);
@@ -493,7 +628,7 @@ extern "C" int at_grpo_qk_norm_rope_bwd(const at_grpo_norm_rope* layer, int32_t 
     return AT_GRPO_OK;
   }));
   if (L.qw || L.kw) {
-    hipLaunchKernelGGL(k_weight_grad, dim3(static_cast<unsigned>(ceil_div(L.D, 16)), 2), dim3(256), 0, s, L.D, static_cast<int>(blocks), partial,
+    hipLaunchKernelGGL(k_weight_grad, dim3(static_cast<unsigned>(L.D / 8), 2), dim3(1024), 0, s, L.D, static_cast<int>(blocks), partial,
                        L.qw ? dq_weight : nullptr, L.kw ? dk_weight : nullptr);
     ATG_LAUNCH_CHECK();
   }
@@ -513,12 +648,12 @@ extern "C" int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* 
   if (Hq) ATG_TRY(check_rows(q, layer->dtype));
   if (Hq) ATG_TRY(check_rows(q_out, layer->dtype));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
-  const int lanes = lanes_of(L.D), parts = parts_of(n_tok, Hq > kv->Hk ? Hq : kv->Hk, lanes);
+  const int parts = parts_of(n_tok, Hq + 2 * kv->Hk, lanes_of(L.D));
   if (static_cast<int64_t>(n_tok) * parts > 0x7fffffff) return AT_GRPO_EUNSUPPORTED;
   const unsigned blocks = static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * parts, 4));
   ProfScope ps(PROF_ROPE, s);
-  return by_type_and_lanes(layer->dtype, lanes, [&](auto t, auto n) -> int {
-    hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(n)::value>), dim3(blocks), dim3(256), 0, s, view, L, n_tok, parts, Hq,
+  return by_shape(layer->dtype, L, [&](auto t, auto n, auto vec) -> int {
+    hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(n)::value, decltype(vec)::value>), dim3(blocks), dim3(256), 0, s, view, L, n_tok, parts, Hq,
                        Hq ? rows_of(q) : Rows{}, rows_of(k), rows_of(v), Hq ? rows_of(q_out) : Rows{}, data_error);
     ATG_LAUNCH_CHECK();
     return AT_GRPO_OK;
