@@ -1,4 +1,4 @@
-"""Thin Python binding of libat_grpo.so: argument marshalling only (for the grouping calls, whose kernels are short, in csrc/binding.cpp).
+"""Thin Python binding of libat_grpo.so: argument marshalling only (for the calls whose kernels are short in csrc/binding.cpp).
 
 Every function has the name of the C entry point it calls (see include/at_grpo.h) and takes
 torch tensors that already live on the GPU; outputs and the workspace are allocated here with
@@ -22,6 +22,7 @@ _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libat_grpo
 _lib = None
 _binding = None             # csrc/binding.cpp, loaded by the first call that goes through it
 _group_fn = _mixed_fn = 0   # addresses of the library's grouping calls
+_fn = {}                    # and of the others that go through it
 
 AGG = {"token_mean": 0, "seq_mean_token_mean": 1}
 NORM = {"std": 0, "none": 1}
@@ -161,8 +162,8 @@ def load_library():
 
 
 def load_binding():
-    """Loads _binding.so (built in-tree with the library) for the two grouping calls that go through it; raises if it is missing or was
-    built for another torch.  Every other call does without."""
+    """Loads _binding.so (built in-tree with the library) for the calls that go through it: two that group responses, and those on
+    queries, keys and the rollout's cache; raises if it is missing or was built for another torch.  Every other call does without."""
     global _binding, _group_fn, _mixed_fn
     if _binding is None:
         lib = load_library()
@@ -172,6 +173,9 @@ def load_binding():
             raise AtGrpoError(f"_binding.so is missing or does not load ({e}): run `python -m paper_2510_11062_amd.build`") from e
         _group_fn = C.cast(lib.at_grpo_group_advantage, C.c_void_p).value
         _mixed_fn = C.cast(lib.at_grpo_group_advantage_mixed, C.c_void_p).value
+        for name in ("at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append", "at_grpo_prefix_attention",
+                     "at_grpo_prefix_attention_workspace_bytes"):
+            _fn[name] = C.cast(getattr(lib, name), C.c_void_p).value
         _binding = binding
     return _binding
 
@@ -646,9 +650,9 @@ def at_grpo_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, scaling:
     return table
 
 
-def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor], heads: Optional[int] = None) -> _Rows:
-    """t [tokens, heads, D] as at_grpo_rows, of the dtype, device, tokens and D of `like`."""
-    if t.dim() != 3 or not t.is_cuda or t.dtype not in DTYPE:
+def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor], heads: Optional[int] = None):
+    """Raises unless t is [tokens, heads, D] of the dtype, device, tokens and D of `like`, as at_grpo_rows can hold it."""
+    if not isinstance(t, torch.Tensor) or t.dim() != 3 or not t.is_cuda or t.dtype not in DTYPE:
         raise AtGrpoError(f"{name} must be a [tokens, heads, D] CUDA/HIP tensor of float32 or bfloat16")
     if like is not None and (t.dtype != like.dtype or t.device != like.device or t.shape[0] != like.shape[0] or t.shape[2] != like.shape[2]):
         raise AtGrpoError(f"{name} must have the dtype, device, tokens and head size of the other rows")
@@ -659,31 +663,20 @@ def _rows(name: str, t: torch.Tensor, like: Optional[torch.Tensor], heads: Optio
     if t.numel() and (ds != 1 or ts % step or hs % step or t.data_ptr() % 16):
         raise AtGrpoError(f"{name}: the elements of a head must be contiguous, heads and tokens multiples of 16 bytes apart, and the data "
                           "16-byte aligned")
-    return _Rows(t.data_ptr(), ts, hs)
 
 
 def _vector(name: str, t: Optional[torch.Tensor], n: int, dtype: torch.dtype, device):
-    """A contiguous 1-d tensor of n elements (or None) as a pointer."""
-    if t is None:
-        return None
-    if not t.is_cuda or t.device != device or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous():
+    """Raises unless t is a contiguous 1-d tensor of n elements, or None."""
+    if t is not None and (not isinstance(t, torch.Tensor) or t.device != device or t.dtype != dtype or t.dim() != 1 or t.shape[0] != n or not t.is_contiguous()):
         raise AtGrpoError(f"{name} must be a contiguous {dtype} tensor of {n} elements on {device}")
-    return t.data_ptr()
 
 
-def _layer(x: torch.Tensor, rope, q_weight, k_weight, eps: float, interleaved: bool) -> _NormRope:
-    D = x.shape[2]
-    n_pos = half = 0
-    if rope is not None:
-        if rope.dim() != 3 or rope.shape[2] != 2 or rope.dtype != torch.float32 or rope.device != x.device or not rope.is_contiguous():
-            raise AtGrpoError("rope must be a contiguous float32 [positions, rot_dim / 2, 2] tensor on the rows' device")
-        n_pos, half = rope.shape[0], rope.shape[1]
-    return _NormRope(DTYPE[x.dtype], D, 2 * half, 1 if interleaved else 0, n_pos, eps, _ptr(rope),
-                     _vector("q_weight", q_weight, D, x.dtype, x.device), _vector("k_weight", k_weight, D, x.dtype, x.device))
-
-
-def _ref(rows: Optional[_Rows]):
-    return None if rows is None else C.byref(rows)
+def _layer(x: torch.Tensor, rope, q_weight, k_weight, eps: float, interleaved: bool):
+    if rope is not None and (rope.dim() != 3 or rope.shape[2] != 2 or rope.dtype != torch.float32 or rope.device != x.device
+                             or not rope.is_contiguous()):
+        raise AtGrpoError("rope must be a contiguous float32 [positions, rot_dim / 2, 2] tensor on the rows' device")
+    _vector("q_weight", q_weight, x.shape[2], x.dtype, x.device)
+    _vector("k_weight", k_weight, x.shape[2], x.dtype, x.device)
 
 
 def _word(data_error: Optional[torch.Tensor], device):
@@ -694,56 +687,74 @@ def at_grpo_qk_norm_rope(q, k, rope, position, q_weight=None, k_weight=None, eps
                          k_out=None, data_error=None):
     """Norm (where there is a weight) and rotation (where there is a table) of queries q [n, Hq, D] and keys k [n, Hk, D]; either may be
     None.  position int32 [n].  Outputs may be the inputs themselves.  Returns dict(q, k)."""
-    lib = load_library()
+    if _binding is None:
+        load_binding()
     x = q if q is not None else k
-    cq = _rows("q", q, None) if q is not None else None
-    ck = _rows("k", k, q) if k is not None else None
-    layer = _layer(x, rope, q_weight, k_weight, eps, interleaved)
-    pos = _vector("position", position, x.shape[0], torch.int32, x.device)
-    if q is not None and q_out is None:
-        q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k is not None and k_out is None:
-        k_out = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    oq = _rows("q_out", q_out, q, q.shape[1]) if q is not None else None
-    ok = _rows("k_out", k_out, k, k.shape[1]) if k is not None else None
-    st = lib.at_grpo_qk_norm_rope(C.byref(layer), x.shape[0], q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0,
-                                  _ref(cq), _ref(ck), pos, _ref(oq), _ref(ok), _word(data_error, x.device), _stream())
-    _check(st, "at_grpo_qk_norm_rope")
-    return dict(q=q_out, k=k_out)
+    out = None
+    if x is not None and x.is_cuda:
+        out = _binding.qk_norm_rope(_fn["at_grpo_qk_norm_rope"], q, k, rope, position, q_weight, k_weight, eps, interleaved, q_out, k_out,
+                                    data_error, _stream())
+    if type(out) is dict:
+        return out
+    x = _explain_qk(q, k, rope, position, q_weight, k_weight, eps, interleaved, dict(q_out=q_out), dict(k_out=k_out))
+    _word(data_error, x.device)
+    _refused(out, "at_grpo_qk_norm_rope")
 
 
 def at_grpo_qk_norm_rope_bwd(dq_out, dk_out, q, k, rope, position, q_weight=None, k_weight=None, eps: float = 1e-6,
                              interleaved: bool = False, dq=None, dk=None, data_error=None):
     """Gradient of at_grpo_qk_norm_rope: from those of its outputs (and its inputs) to those of its inputs, in their dtype, and of the
     weights, float32 [D].  dq may be dq_out itself, dk dk_out.  Returns dict(dq, dk, dq_weight, dk_weight, workspace)."""
-    lib = load_library()
+    if _binding is None:
+        load_binding()
     x = q if q is not None else k
-    cq = _rows("q", q, None) if q is not None else None
-    ck = _rows("k", k, q) if k is not None else None
-    layer = _layer(x, rope, q_weight, k_weight, eps, interleaved)
-    pos = _vector("position", position, x.shape[0], torch.int32, x.device)
-    gq = _rows("dq_out", dq_out, q, q.shape[1]) if q is not None else None
-    gk = _rows("dk_out", dk_out, k, k.shape[1]) if k is not None else None
-    if q is not None and dq is None:
-        dq = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    if k is not None and dk is None:
-        dk = torch.empty(k.shape, dtype=k.dtype, device=k.device)
-    oq = _rows("dq", dq, q, q.shape[1]) if q is not None else None
-    ok = _rows("dk", dk, k, k.shape[1]) if k is not None else None
-    dqw = torch.empty(x.shape[2], dtype=torch.float32, device=x.device) if q is not None and q_weight is not None else None
-    dkw = torch.empty(x.shape[2], dtype=torch.float32, device=x.device) if k is not None and k_weight is not None else None
-    ws = _workspace(lib.at_grpo_workspace_bytes(CALL_QK_NORM_ROPE_BWD, None, 0, 0, 0, 0), x.device)
-    st = lib.at_grpo_qk_norm_rope_bwd(C.byref(layer), x.shape[0], q.shape[1] if q is not None else 0, k.shape[1] if k is not None else 0,
-                                      _ref(gq), _ref(gk), _ref(cq), _ref(ck), pos, _ref(oq), _ref(ok), _ptr(dqw), _ptr(dkw),
-                                      _word(data_error, x.device), _ptr(ws), ws.numel(), _stream())
-    _check(st, "at_grpo_qk_norm_rope_bwd")
-    return dict(dq=dq, dk=dk, dq_weight=dqw, dk_weight=dkw, workspace=ws)
+    out = None
+    if x is not None and x.is_cuda:
+        ws = _workspace(_rope_bwd_bytes(), x.device)
+        out = _binding.qk_norm_rope_bwd(_fn["at_grpo_qk_norm_rope_bwd"], dq_out, dk_out, q, k, rope, position, q_weight, k_weight, eps, interleaved,
+                                        dq, dk, data_error, ws.data_ptr(), ws.numel(), _stream())
+    if type(out) is dict:
+        out["workspace"] = ws
+        return out
+    if q is not None and dq_out is None or k is not None and dk_out is None:
+        raise AtGrpoError("the gradients of both outputs are needed")
+    x = _explain_qk(q, k, rope, position, q_weight, k_weight, eps, interleaved, dict(dq_out=dq_out, dq=dq), dict(dk_out=dk_out, dk=dk))
+    _word(data_error, x.device)
+    _refused(out, "at_grpo_qk_norm_rope_bwd")
 
 
-@dataclass(frozen=True)
+@functools.lru_cache(maxsize=1)
+def _rope_bwd_bytes() -> int:
+    return int(load_library().at_grpo_workspace_bytes(CALL_QK_NORM_ROPE_BWD, None, 0, 0, 0, 0))
+
+
+def _explain_qk(q, k, rope, position, q_weight, k_weight, eps, interleaved, of_q, of_k):
+    """Raises for the argument that the extension did not take, if there is one; returns the rows that the others go by."""
+    x = q if q is not None else k
+    if x is None:
+        raise AtGrpoError("queries or keys are needed")
+    if q is not None:
+        _rows("q", q, None)
+    if k is not None:
+        _rows("k", k, q)
+    _layer(x, rope, q_weight, k_weight, eps, interleaved)
+    _vector("position", position, x.shape[0], torch.int32, x.device)
+    for like, given in ((q, of_q), (k, of_k)):
+        for name, t in given.items():
+            if like is not None and t is not None:
+                _rows(name, t, like, like.shape[1])
+    return x
+
+
+def _refused(out, what: str):
+    if out is not None:
+        _check(out, what)
+    raise AtGrpoError(f"{what}: arguments that it does not take")
+
+
+@dataclass
 class KVBatch:
-    """Python-side mirror of at_grpo_kv; keeps the tensors alive.  The tensors' contents may change between calls (lengths grow as
-    tokens are appended), a batch of other tensors is another KVBatch."""
+    """Python-side mirror of at_grpo_kv.  The tensors' contents may change between calls (lengths grow as tokens are appended)."""
     cache_k: torch.Tensor                       # [pages, Hk, page_size, D]
     cache_v: torch.Tensor
     pages: torch.Tensor                         # int32 [n_seq, max_pages]
@@ -754,6 +765,13 @@ class KVBatch:
     prefix_pages: Optional[torch.Tensor] = None  # int32 [n_group, max_prefix_pages]
 
     def __post_init__(self):
+        if _binding is None:
+            load_binding()
+        if not _binding.check_kv(self):
+            self._explain()
+
+    def _explain(self):
+        """Raises for the tensor that does not belong with the others."""
         ck, cv = self.cache_k, self.cache_v
         _dev_check(ck, cv, self.pages, self.length, self.cu_q, self.group_seq, self.prefix_len, self.prefix_pages)
         _i32_check(pages=self.pages, length=self.length, cu_q=self.cu_q, group_seq=self.group_seq, prefix_len=self.prefix_len,
@@ -765,63 +783,65 @@ class KVBatch:
             raise AtGrpoError("pages must be [n_seq, max_pages]")
         if self.cu_q is not None and self.cu_q.numel() != n_seq + 1:
             raise AtGrpoError("cu_q must have n_seq + 1 elements")
-        n_group = 0
         if self.group_seq is not None:
             n_group = self.group_seq.numel() - 1
             if self.prefix_len is None or self.prefix_pages is None or n_group < 0 or self.prefix_len.numel() != n_group or \
                     self.prefix_pages.dim() != 2 or self.prefix_pages.shape[0] != n_group:
                 raise AtGrpoError("groups need prefix_len [n_group] and prefix_pages [n_group, max_prefix_pages]")
-        for t in (cv, self.pages, self.length, self.cu_q, self.group_seq, self.prefix_len, self.prefix_pages):
-            if t is not None and t.device != ck.device:
-                raise AtGrpoError("the tensors of a KVBatch must be on one device")
-        object.__setattr__(self, "c", _KV(
-            DTYPE[ck.dtype], ck.shape[1], ck.shape[3], ck.shape[2], ck.shape[0], n_seq, self.pages.shape[1], n_group,
-            self.prefix_pages.shape[1] if n_group else 0, ck.data_ptr(), cv.data_ptr(), self.pages.data_ptr(), self.length.data_ptr(),
-            _ptr(self.cu_q), _ptr(self.group_seq) if n_group else None, _ptr(self.prefix_len) if n_group else None,
-            _ptr(self.prefix_pages) if n_group else None))
+        raise AtGrpoError("the tensors of a KVBatch must be on one device, with fewer than 2^31 rows and columns")
 
-    def _rows(self, name: str, t: torch.Tensor, like: Optional[torch.Tensor], heads: Optional[int] = None) -> _Rows:
-        r = _rows(name, t, like, heads)
+    def _rows(self, name: str, t: torch.Tensor, like: Optional[torch.Tensor], heads: Optional[int] = None):
+        _rows(name, t, like, heads)
         if t.dtype != self.cache_k.dtype or t.shape[2] != self.cache_k.shape[3] or t.device != self.cache_k.device:
             raise AtGrpoError(f"{name} must have the cache's dtype, head size and device")
-        return r
 
 
 def at_grpo_kv_append(kv: KVBatch, q, k, v, rope, q_weight=None, k_weight=None, eps: float = 1e-6, interleaved: bool = False, q_out=None,
                       data_error=None):
     """Normed and rotated keys k [n, Hk, D] and values v of the new tokens go into the cache; queries q [n, Hq, D] (or None), normed and
     rotated, to q_out, which may be q itself.  Returns dict(q)."""
-    lib = load_library()
-    ck, cv = kv._rows("k", k, None, kv.c.Hk), kv._rows("v", v, k, kv.c.Hk)
-    cq = oq = None
+    if _binding is None:
+        load_binding()
+    out = _binding.kv_append(_fn["at_grpo_kv_append"], kv, q, k, v, rope, q_weight, k_weight, eps, interleaved, q_out, data_error, _stream())
+    if type(out) is dict:
+        return out
+    kv.__post_init__()
+    heads = kv.cache_k.shape[1]
+    kv._rows("k", k, None, heads)
+    kv._rows("v", v, k, heads)
     if q is not None:
-        cq = kv._rows("q", q, k)
-        if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        oq = kv._rows("q_out", q_out, q, q.shape[1])
-    layer = _layer(k, rope, q_weight, k_weight, eps, interleaved)
-    st = lib.at_grpo_kv_append(C.byref(kv.c), C.byref(layer), k.shape[0], q.shape[1] if q is not None else 0, _ref(cq), C.byref(ck),
-                               C.byref(cv), _ref(oq), _word(data_error, k.device), _stream())
-    _check(st, "at_grpo_kv_append")
-    return dict(q=q_out)
+        kv._rows("q", q, k)
+        if q_out is not None:
+            kv._rows("q_out", q_out, q, q.shape[1])
+    _layer(k, rope, q_weight, k_weight, eps, interleaved)
+    _word(data_error, k.device)
+    _refused(out, "at_grpo_kv_append")
 
 
 def at_grpo_prefix_attention(kv: KVBatch, q, scale: Optional[float] = None, causal: bool = True, max_q: int = 1, out=None,
                              want_lse: bool = False, data_error=None):
     """Attention of the new tokens' queries q [n, Hq, D] over their sequences' tokens and their groups' prefixes (1 / sqrt(D) where no
     scale is given).  max_q: an upper bound of the new tokens of one sequence.  out may not be q.  Returns dict(out, lse, workspace)."""
-    lib = load_library()
-    cq = kv._rows("q", q, None)
-    n, Hq, D = q.shape
-    if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-    co = kv._rows("out", out, q, Hq)
-    lse = torch.empty((n, Hq), dtype=torch.float32, device=q.device) if want_lse else None
-    nbytes = lib.at_grpo_prefix_attention_workspace_bytes(C.byref(kv.c), n, Hq, max_q)
-    if nbytes == 0:
-        raise AtGrpoError("at_grpo_prefix_attention: heads, head size, page size or max_q that it does not cover")
-    ws = _workspace(nbytes, q.device)
-    st = lib.at_grpo_prefix_attention(C.byref(kv.c), n, Hq, C.byref(cq), D ** -0.5 if scale is None else scale, 1 if causal else 0, max_q,
-                                      C.byref(co), _ptr(lse), _word(data_error, q.device), _ptr(ws), ws.numel(), _stream())
-    _check(st, "at_grpo_prefix_attention")
-    return dict(out=out, lse=lse, workspace=ws)
+    if _binding is None:
+        load_binding()
+    res = None
+    if q.is_cuda:
+        stream = _stream()
+        ws = _workspace_cache.get((q.device.index, stream))
+        call = lambda: _binding.prefix_attention(_fn["at_grpo_prefix_attention"], _fn["at_grpo_prefix_attention_workspace_bytes"], kv, q, scale,
+                                                 causal, max_q, out, want_lse, data_error, ws, stream)
+        res = call()
+        if type(res) is tuple:
+            ws = _workspace(res[0], q.device)
+            res = call()
+    if type(res) is dict:
+        res["workspace"] = ws
+        return res
+    kv.__post_init__()
+    kv._rows("q", q, None)
+    if out is not None:
+        kv._rows("out", out, q, q.shape[1])
+    _word(data_error, q.device)
+    if res is None:
+        raise AtGrpoError("at_grpo_prefix_attention: heads, head size, page size, tokens or max_q that it does not cover")
+    _refused(res, "at_grpo_prefix_attention")
