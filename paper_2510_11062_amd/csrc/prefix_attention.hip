@@ -5,14 +5,16 @@
 // in one pass with a running maximum m.  What there is to read is the keys and values, and where few queries read them their passage
 // from memory bounds the call.  Hence units of work that read a token once for all queries that see it: the prefix of a group with the
 // queries of all its sequences, and a sequence's own tokens with its queries.  A unit's rows are its queries times the Hq / Hk heads
-// that share a key head; rows are cut into tiles of 16 to 64, tokens into chunks of equal length over the whole batch, so that long
-// prompts and ragged responses fill the chip alike, and the chunks' results are joined by a second kernel.
+// that share a key head, cut into tiles of 16 to 64; a tile's passage over a unit's tokens for one key head is a run.  The runs of the
+// whole batch, one behind the other, are dealt to the workgroups in equal shares of 64-token blocks, wherever that cuts a run: long
+// prompts and ragged responses fill the chip alike, whatever their lengths, which only the device knows.  A second kernel joins the
+// parts of a row: that of its prefix, that of its own tokens, and those of the workgroups that began in the middle of its run.
 //
 // A wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
 //   S^T = K Q^T     MFMA 16x16: tokens down, queries across, so that a lane has four consecutive tokens of one query
 //   P^T             is at once the second product's operand: no lane needs a weight that another one computed
 //   O^T += V^T P^T  a lane loads whole rows of V, eight elements of eight tokens, and transposes that block by itself
-// The four wavefronts of a workgroup take turns in a chunk's tokens and add up at its end.
+// The four wavefronts of a workgroup take turns in a run's tokens and add up at its end.
 #include "kv_common.hpp"
 
 #include <math.h>
@@ -26,8 +28,11 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
-constexpr int kTarget = 1024;        // items that the chunks' length aims at: four for each compute unit
-constexpr int kMinBlocks = 2;        // shortest chunk, in blocks of 64 tokens: 32 for each wavefront
+constexpr int kMostGroups = 1024;     // workgroups of a launch
+constexpr int kCachedUnits = 512;     // units whose sizes are kept in LDS
+// A run's beginning and end (page ids, queries, adding up) take about as long as a block of 64 tokens, and count as one.  Shares are
+// three blocks at least, so that every wavefront has a tile to begin with.
+constexpr int kRunCost = 1, kMinShare = 3;
 constexpr int kPageSlots = 1024;     // page ids of a chunk in LDS at a time
 constexpr int kMaxRows = 64;         // rows of the largest tile
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -42,14 +47,16 @@ struct Args {
   Rows q, out;
   float* lse;                // [n_tok, Hq] or null
   int32_t* data_error;
-  int4* units;               // workspace: [n_group + n_seq] first row of parts, chunks, first token, tokens
-  float* part_lse;           // [rows of parts]
-  float* part_out;           // [rows of parts, D], each divided by its own sum
+  int4* units;               // workspace: [n_group + n_seq] cost in front of the unit, cost of a run, first token, tokens; then {share, ..}
+  // Parts, each divided by its own sum.  A run's first part lies by its query and head, those of prefixes first: [2 or 1][n_tok][Hq].
+  // A workgroup's first part, where it begins inside a run, lies behind them: [workgroup][row of the tile].
+  float* part_lse;
+  float* part_out;           // .. [D]
 };
 
 // A unit: queries tok0 .. tok0 + ntok - 1 over the first `len` tokens of a page table.  Units 0 .. n_group - 1 are the prefixes.
 struct Unit {
-  int tok0, ntok, len;
+  int tok0, ntok, len, row;      // row: of the page table
 };
 
 __device__ __forceinline__ Unit unit_of(const KvView& kv, int u, int n_tok, int* error, bool* falls) {
@@ -59,7 +66,7 @@ __device__ __forceinline__ Unit unit_of(const KvView& kv, int u, int n_tok, int*
     s1 = kv.group_seq[u + 1];
     if (s0 < 0 || s1 < s0 || s1 > kv.n_seq) {
       *falls = true;
-      return Unit{0, 0, 0};
+      return Unit{0, 0, 0, 0};
     }
     len = kv.prefix_len[u];
     most = kv.max_prefix_pages << kv.page_shift;
@@ -70,26 +77,42 @@ __device__ __forceinline__ Unit unit_of(const KvView& kv, int u, int n_tok, int*
   const int t0 = kv.cu_q ? kv.cu_q[s0] : s0, t1 = kv.cu_q ? kv.cu_q[s1] : s1;
   if (t0 < 0 || t1 < t0 || t1 > n_tok) {
     *falls = true;
-    return Unit{0, 0, 0};
+    return Unit{0, 0, 0, 0};
   }
   if (len < 0 || len > most) {
     *error |= AT_GRPO_DATA_SEQLENS;
     len = 0;
   }
-  return Unit{t0, t1 - t0, len};
+  return Unit{t0, t1 - t0, len, u < kv.n_group ? u : s0};
 }
 
-// The batch cut into items, the same in every workgroup: an item is a chunk of a unit's tokens, a key head and a tile of rows.
-struct Schedule {
-  int first[257];     // items in front of each thread's units, and all
-  int part[256];      // rows of parts in front of them
-  int chunk;          // tokens of a chunk
-  int unit, index, chunks, part0;     // the item at hand: its unit, its number there
-  Unit at;
-  int64_t cost[4];
-};
+__device__ __forceinline__ int tiles_of(int ntok, int share, int rows) { return (ntok * share + rows - 1) / rows; }
 
-__device__ __forceinline__ int tiles_of(const Unit& u, int share, int rows) { return static_cast<int>((static_cast<int64_t>(u.ntok) * share + rows - 1) / rows); }
+// Tiles of a causal unit see more tokens the later they come.  They take turns from both ends, so that any two neighbours see as many as
+// others, and the mean stands for each.
+__device__ __forceinline__ int tile_at(int turn, int tiles) { return turn & 1 ? turn >> 1 : tiles - 1 - (turn >> 1); }
+__device__ __forceinline__ int turn_of(int tile, int tiles) { return tile < tiles / 2 ? 2 * tile + 1 : 2 * (tiles - 1 - tile); }
+
+// Cost of each run of a unit, in blocks of 64 << coarse tokens.
+__device__ __forceinline__ int run_cost(const Unit& u, bool steps, int coarse) {
+  const int mean = steps ? max(1, u.len - (u.ntok - 1) / 2) : u.len;
+  return u.len == 0 || u.ntok == 0 ? 0 : static_cast<int>(((static_cast<int64_t>(mean) + 63) >> 6 >> coarse) + kRunCost);
+}
+
+// Where a run of `cost` over tokens 0 .. end - 1 is cut: the token that stands at `at` of its cost.
+__device__ __forceinline__ int cut(int at, int cost, int end) {
+  return at <= 0 ? 0 : at >= cost ? end : static_cast<int>(static_cast<int64_t>(end) * at / cost) & ~63;
+}
+
+// The same in every workgroup.
+struct Schedule {
+  int first[257];      // cost in front of each thread's units, and all
+  int share;           // cost of a workgroup
+  int coarse;
+  int unit, base;      // the unit that a workgroup begins in, and the cost in front of it
+  int64_t cost[4];
+  Unit cache[kCachedUnits];
+};
 
 template <int RP, int RO>
 __device__ void make_schedule(const KvView& kv, const Args& a, Schedule& S, int* scan_lds) {
@@ -99,7 +122,8 @@ __device__ void make_schedule(const KvView& kv, const Args& a, Schedule& S, int*
   int64_t cost = 0;
   for (int u = u0; u < u1; ++u) {
     const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
-    cost += static_cast<int64_t>(tiles_of(x, a.share, u < kv.n_group ? RP : RO)) * ((x.len + 63) >> 6);
+    if (u < kCachedUnits) S.cache[u] = x;
+    cost += static_cast<int64_t>(tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO)) * run_cost(x, a.causal && u >= kv.n_group, 0);
   }
   const bool none = __syncthreads_or(falls);
   if (none) error |= AT_GRPO_DATA_SEQLENS;
@@ -109,59 +133,32 @@ __device__ void make_schedule(const KvView& kv, const Args& a, Schedule& S, int*
   if ((tid & 63) == 0) S.cost[tid >> 6] = cost;
   __syncthreads();
   cost = (S.cost[0] + S.cost[1] + S.cost[2] + S.cost[3]) * kv.Hk;
-  int64_t blocks = (cost + kTarget - 1) / kTarget;
-  blocks = blocks < kMinBlocks ? kMinBlocks : blocks > (1 << 24) ? (1 << 24) : blocks;
-  const int chunk = static_cast<int>(blocks) << 6;
-  int items = 0, parts = 0;
+  int coarse = 0;      // costs are counted in 32 bits
+  while (cost >> coarse > (1 << 29)) ++coarse;
+  int mine = 0;
   if (!none)
     for (int u = u0; u < u1; ++u) {
-      const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
-      const int chunks = (x.len + chunk - 1) / chunk;
-      items += tiles_of(x, a.share, u < kv.n_group ? RP : RO) * chunks * kv.Hk;
-      parts += x.ntok * a.Hq * chunks;
+      const Unit x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
+      mine += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * run_cost(x, a.causal && u >= kv.n_group, coarse) * kv.Hk;
     }
-  int total_items, total_parts;
-  const int item0 = block_exclusive_scan<256>(items, scan_lds, &total_items);
-  int part0 = block_exclusive_scan<256>(parts, scan_lds, &total_parts);
-  S.first[tid] = item0;
-  S.part[tid] = part0;
+  int total;
+  int at = block_exclusive_scan<256>(mine, scan_lds, &total);
+  const int share = max(kMinShare, (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x));
+  S.first[tid] = at;
   if (tid == 0) {
-    S.first[256] = total_items;
-    S.chunk = chunk;
+    S.first[256] = total;
+    S.share = share;
+    S.coarse = coarse;
   }
-  if (blockIdx.x == 0)       // for the kernel that joins the parts
+  if (blockIdx.x == 0) {       // for the kernel that joins the parts
     for (int u = u0; u < u1; ++u) {
-      Unit x{0, 0, 0};
-      if (!none) x = unit_of(kv, u, a.n_tok, &error, &falls);
-      const int chunks = (x.len + chunk - 1) / chunk;
-      a.units[u] = make_int4(part0, chunks, x.tok0, x.ntok);
-      part0 += x.ntok * a.Hq * chunks;
+      Unit x{0, 0, 0, 0};
+      if (!none) x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
+      const int c = run_cost(x, a.causal && u >= kv.n_group, coarse);
+      a.units[u] = make_int4(at, c, x.tok0, x.ntok);
+      at += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * c * kv.Hk;
     }
-  __syncthreads();
-}
-
-// Puts item `item` into S.
-template <int RP, int RO>
-__device__ void find_item(const KvView& kv, const Args& a, Schedule& S, int item) {
-  const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x;
-  __syncthreads();
-  if (S.first[tid] <= item && item < S.first[tid + 1]) {
-    int left = item - S.first[tid], part0 = S.part[tid], error = 0;
-    bool falls = false;
-    for (int u = tid * per; u < n; ++u) {
-      const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
-      const int chunks = (x.len + S.chunk - 1) / S.chunk, items = tiles_of(x, a.share, u < kv.n_group ? RP : RO) * chunks * kv.Hk;
-      if (left < items) {
-        S.unit = u;
-        S.index = left;
-        S.chunks = chunks;
-        S.part0 = part0;
-        S.at = x;
-        break;
-      }
-      left -= items;
-      part0 += x.ntok * a.Hq * chunks;
-    }
+    if (tid == 0) a.units[n] = make_int4(share, 0, 0, 0);
   }
   __syncthreads();
 }
@@ -206,26 +203,20 @@ struct Lds {
   float slab[4][16][128 + 4];
 };
 
-// One item: the rows of one tile over one chunk.
+// Costs `from` to `to` of run `run` (key head, tile) of unit u: a part of each of its rows.
 template <typename T, int D, int NR, bool EXACT>
-__device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int32_t* table) {
+__device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
   typedef Shape<T, D> Z;
   constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, R = 16 * NR;
   constexpr bool kBf16 = sizeof(T) == 2;
-  const Schedule& S = lds.S;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, m = lane & 15, g = lane >> 4;
-  const Unit u = S.at;
-  const bool own = S.unit >= kv.n_group;
-  const int rows = u.ntok * a.share, tiles = (rows + R - 1) / R;
-  // row tiles turn fastest, so that workgroups that read the same tokens run together; the last ones, which see most, go first
-  const int tile = tiles - 1 - S.index % tiles, hc = S.index / tiles, c = hc % S.chunks, hk = hc / S.chunks;
-  const int r0 = tile * R;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+  const int rows = u.ntok * a.share, tiles = tiles_of(u.ntok, a.share, R), hk = run / tiles, tile = tile_at(run - hk * tiles, tiles), r0 = tile * R;
   const int dim = EXACT ? D : kv.D;
   // A causal query sees the own tokens in front of `first + its number among the new tokens`.
   const bool steps = own && a.causal;
   const int first = u.len - u.ntok + 1;
-  const int last_tok = (min(rows, r0 + R) - 1) / a.share, first_tok = r0 / a.share;
-  const int k0 = c * S.chunk, k1 = min(min(u.len, k0 + S.chunk), steps ? first + last_tok : u.len), all_see = steps ? first + first_tok : k1;
+  const int last_tok = (min(rows, r0 + R) - 1) / a.share, first_tok = r0 / a.share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
+  const int k0 = cut(cost0, cost, end), k1 = cut(cost1, cost, end), all_see = steps ? first + first_tok : k1;
 
   typename Z::KV q[NR][KC];
   int limit[NR];
@@ -256,6 +247,7 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
       for (int e = 0; e < E; ++e) acc[n][b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
 
+  const int32_t* const table = own ? kv.pages + static_cast<int64_t>(u.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(u.row) * kv.max_prefix_pages;
   const int64_t page_step = (static_cast<int64_t>(kv.Hk) * dim) << kv.page_shift;
   const int in_page = (1 << kv.page_shift) - 1;
   const T* const kbase = static_cast<const T*>(kv.k) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
@@ -313,12 +305,13 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
       }
     };
 
-    int t = from + TOK * wave;
-    if (t < to) {
-      load_k(t);
-      load_v(t);
-    }
-    for (; t < to; t += 4 * TOK) {
+    // Loads are never behind a branch: the compiler could not tell then which of them are still on their way, and would wait for all.
+    // What is asked for behind the last tile is the last token's row.
+    load_k(from + TOK * wave);
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+    load_v(from + TOK * wave);
+    for (int t = from + TOK * wave; t < to; t += 4 * TOK) {
       f32x4 s[NR][SUB];
 #pragma unroll
       for (int n = 0; n < NR; ++n)
@@ -335,8 +328,7 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
             }
           }
         }
-      const int next = t + 4 * TOK;
-      if (next < to) load_k(next);
+      load_k(t + 4 * TOK);
       if (t + TOK > min(to, all_see) || holes) {
         // tokens that a row does not see, and what lies in the cache behind the last or in no page: no weight, and no value
 #pragma unroll
@@ -409,7 +401,8 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
               for (int i = 0; i < 4; ++i) acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], acc[n][b][e], 0, 0, 0);
           }
         }
-      if (next < to) load_v(next);
+      load_v(t + 4 * TOK);
+      asm volatile("" ::: "memory");      // the loads stay on this side of the jump back
     }
     from = to;
   }
@@ -425,7 +418,12 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
     }
   }
   __syncthreads();
-  const bool direct = kv.n_group == 0 && S.chunks == 1;
+  const bool direct = kv.n_group == 0 && cost0 == 0 && cost1 == cost;
+  // where a row's part lies: by its query and head, or with the workgroup's
+  const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq, by_group = static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1);
+  auto part_of = [&](int r, int tq, int h) {
+    return cost0 == 0 ? by_query + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h : by_group + static_cast<int64_t>(group) * kMaxRows + (r - r0);
+  };
   float high[NR], total[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -441,7 +439,7 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
     if (wave == 0 && g == 0 && r < rows) {
       const int tq = r / a.share, h = hk * a.share + r - tq * a.share;
       const float x = total[n] == 0.f ? -INFINITY : fmaf(now, kLn2, logf(total[n]));
-      if (!direct) a.part_lse[S.part0 + (static_cast<int64_t>(c) * u.ntok + tq) * a.Hq + h] = x;
+      if (!direct) a.part_lse[part_of(r, tq, h)] = x;
       else if (a.lse) a.lse[static_cast<int64_t>(u.tok0 + tq) * a.Hq + h] = x;
     }
 #pragma unroll
@@ -473,7 +471,7 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
             else *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
           }
         } else {
-          float* to = a.part_out + (S.part0 + (static_cast<int64_t>(c) * u.ntok + tq) * a.Hq + h) * dim + 16 * E * b + d;
+          float* to = a.part_out + part_of(rr, tq, h) * dim + 16 * E * b + d;
 #pragma unroll
           for (int e = 0; e < E / 4; ++e) *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
         }
@@ -482,42 +480,90 @@ __device__ void attend_item(const KvView& kv, const Args& a, Lds& lds, const int
   }
 }
 
+// Workgroups on a compute unit, by the registers of a wavefront.
+template <int D, int NRP>
+constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
+
 template <typename T, int D, int NRP, int NRO, bool EXACT>
-__global__ __launch_bounds__(256, NRP == 1 ? 3 : NRP == 2 && D <= 128 ? 2 : 1) void k_attend(KvView kv, Args a) {
+__global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
   __shared__ Lds lds;
-  make_schedule<16 * NRP, 16 * NRO>(kv, a, lds.S, lds.scan);
-  // neighbouring items go to one XCD
+  Schedule& S = lds.S;
+  make_schedule<16 * NRP, 16 * NRO>(kv, a, S, lds.scan);
+  // neighbouring shares go to one XCD
   const int per_xcd = gridDim.x >> 3, w = per_xcd << 3 == gridDim.x ? (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3) : blockIdx.x;
-  for (int item = w; item < lds.S.first[256]; item += gridDim.x) {
-    find_item<16 * NRP, 16 * NRO>(kv, a, lds.S, item);
-    const int u = lds.S.unit;
-    if (u < kv.n_group) attend_item<T, D, NRP, EXACT>(kv, a, lds, kv.prefix_pages + static_cast<int64_t>(u) * kv.max_prefix_pages);
-    else attend_item<T, D, NRO, EXACT>(kv, a, lds, kv.pages + static_cast<int64_t>(u - kv.n_group) * kv.max_pages);
+  const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, total = S.first[256];
+  const int64_t begin = static_cast<int64_t>(w) * S.share;
+  if (begin >= total) return;
+  int at = static_cast<int>(begin);
+  const int stop = min(total, at + S.share);
+  auto unit_at = [&](int u) {
+    int error = 0;
+    bool falls = false;
+    return u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
+  };
+  auto runs_of = [&](const Unit& x, bool own) { return tiles_of(x.ntok, a.share, own ? 16 * NRO : 16 * NRP) * kv.Hk; };
+  if (S.first[tid] <= at && at < S.first[tid + 1]) {
+    int base = S.first[tid], u = tid * per;
+    for (;; ++u) {
+      const Unit x = unit_at(u);
+      const bool own = u >= kv.n_group;
+      const int c = runs_of(x, own) * run_cost(x, own && a.causal, S.coarse);
+      if (at < base + c) break;
+      base += c;
+    }
+    S.unit = u;
+    S.base = base;
+  }
+  __syncthreads();
+  int u = S.unit, base = S.base;
+  while (at < stop) {
+    const Unit x = unit_at(u);
+    const bool own = u >= kv.n_group;
+    const int cost = run_cost(x, own && a.causal, S.coarse), all = runs_of(x, own) * cost;
+    while (at < min(stop, base + all)) {
+      const int run = (at - base) / cost, run0 = base + run * cost, to = min(stop, run0 + cost);
+      if (own) attend_run<T, D, NRO, EXACT>(kv, a, lds, x, true, run, cost, at - run0, to - run0, w);
+      else attend_run<T, D, NRP, EXACT>(kv, a, lds, x, false, run, cost, at - run0, to - run0, w);
+      at = to;
+    }
+    base += all;
+    ++u;
   }
 }
 
-// out = sum_c exp(lse_c - lse) out_c over the chunks of the prefix and of the own tokens.  A wavefront per query and head: four chunks at
-// a time, sixteen lanes for the elements of one.
+// out = sum_p exp(lse_p - lse) out_p over the parts of a row.  A wavefront per query and head: four parts at a time, sixteen lanes for the
+// elements of one.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join(KvView kv, Args a) {
+__global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int rows_o) {
   const int lane = threadIdx.x & 63, l = lane & 15, slot = lane >> 4, D = kv.D;
   const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
   if (unit >= static_cast<int64_t>(a.n_tok) * a.Hq) return;
-  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * a.Hq);
-  const int s = kv.cu_q ? wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1 : t;
-  int4 of[2] = {make_int4(0, 0, 0, 0), make_int4(0, 0, 0, 0)};
+  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * a.Hq), hk = h / a.share;
+  const int s = kv.cu_q ? wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1 : t, share = a.units[kv.n_group + kv.n_seq].x;
+  int group0[2] = {0, 0}, count[2] = {0, 0}, row[2] = {0, 0};      // the run's first workgroup, its workgroups, the row in its tile
+  auto look_up = [&](int which, int u, int rows) {
+    const int4 x = a.units[u];
+    if (x.y == 0 || t < x.z || t - x.z >= x.w) return;
+    const int tiles = tiles_of(x.w, a.share, rows), r = (t - x.z) * a.share + h - hk * a.share, tile = r / rows;
+    const int run0 = x.x + (hk * tiles + turn_of(tile, tiles)) * x.y;
+    group0[which] = run0 / share;
+    count[which] = (run0 + x.y - 1) / share - group0[which] + 1;
+    row[which] = r - tile * rows;
+  };
   if (s >= 0 && s < kv.n_seq) {
-    of[1] = a.units[kv.n_group + s];
+    look_up(1, kv.n_group + s, rows_o);
     if (kv.n_group) {
       const int g = wave_upper_bound(kv.group_seq, kv.n_group + 1, s) - 1;
-      if (g >= 0 && g < kv.n_group) of[0] = a.units[g];
+      if (g >= 0 && g < kv.n_group) look_up(0, g, rows_p);
     }
   }
-  if (kv.n_group == 0 && of[1].y == 1) return;      // in its place already
-  const int n0 = of[0].y, n = n0 + of[1].y;
-  auto part_of = [&](int c) {
-    const int4 x = c < n0 ? of[0] : of[1];
-    return x.x + (static_cast<int64_t>(c < n0 ? c : c - n0) * x.w + (t - x.z)) * a.Hq + h;
+  if (kv.n_group == 0 && count[1] == 1) return;      // in its place already
+  const int n0 = count[0], n = n0 + count[1];
+  const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq, by_group = queries * (kv.n_group ? 2 : 1);
+  auto part_of = [&](int p) {
+    const bool own = p >= n0;
+    const int i = own ? p - n0 : p;
+    return i == 0 ? (own && kv.n_group ? queries : 0) + unit : by_group + static_cast<int64_t>((own ? group0[1] : group0[0]) + i) * kMaxRows + (own ? row[1] : row[0]);
   };
   float high = -INFINITY;
   for (int c = lane; c < n; c += 64) {
@@ -582,22 +628,20 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a) {
 int check_sizes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q) {
   ATG_TRY(check_kv_sizes(kv, n_tok));
   if (Hq <= 0 || Hq % kv->Hk || max_q < 1) return AT_GRPO_EINVAL;
-  // rows of parts and items are counted in 32 bits
+  // rows of all units and runs are counted in 32 bits
   const int64_t units = static_cast<int64_t>(kv->n_seq) + kv->n_group;
-  return static_cast<int64_t>(n_tok) * Hq <= 0x3f000000 && units * kv->Hk <= 0x3f000000 ? AT_GRPO_OK : AT_GRPO_EUNSUPPORTED;
+  return static_cast<int64_t>(n_tok) * Hq <= 0x3f000000 && units * kv->Hk <= 0x0f000000 ? AT_GRPO_OK : AT_GRPO_EUNSUPPORTED;
 }
 
-// Chunks are ceil(cost / kTarget) blocks of 64 tokens long or longer (cost: blocks times tiles times key heads), so they cut the rows of
-// all units into at most kTarget * kMaxRows rows of parts more than one for each query, head and kind of unit.
 struct Scratch {
   int4* units;
   float *part_lse, *part_out;
 };
 
 Scratch lay_out(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, WsAlloc& ws) {
-  const size_t rows = static_cast<size_t>(kTarget) * kMaxRows + static_cast<size_t>(n_tok) * Hq * (kv->n_group > 0 ? 2 : 1);
+  const size_t rows = static_cast<size_t>(kMostGroups) * kMaxRows + static_cast<size_t>(n_tok) * Hq * (kv->n_group > 0 ? 2 : 1);
   Scratch s;
-  s.units = ws.take<int4>(static_cast<size_t>(kv->n_seq) + kv->n_group);
+  s.units = ws.take<int4>(static_cast<size_t>(kv->n_seq) + kv->n_group + 1);
   s.part_lse = ws.take<float>(rows);
   s.part_out = ws.take<float>(rows * kv->D);
   return s;
@@ -606,19 +650,19 @@ Scratch lay_out(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, WsAlloc& ws) {
 typedef void (*Kernel)(KvView, Args);
 struct Choice {
   Kernel kernel;
-  int rows_p, rows_o;
+  int rows_p, rows_o, per_unit;
 };
 
 template <typename T, int D, bool EXACT>
 Choice choose_of(int rows_p, int rows_o) {
   constexpr int kMost = sizeof(T) == 4 || D == 256 ? 2 : 4;
   if constexpr (!EXACT) {
-    return {k_attend<T, D, kMost, kMost, false>, 16 * kMost, 16 * kMost};
+    return {k_attend<T, D, kMost, kMost, false>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>};
   } else {
-    if (rows_o > 16) return {k_attend<T, D, kMost, kMost, true>, 16 * kMost, 16 * kMost};
-    if (rows_p > 32 && kMost == 4) return {k_attend<T, D, kMost, 1, true>, 16 * kMost, 16};
-    if (rows_p > 16) return {k_attend<T, D, 2, 1, true>, 32, 16};
-    return {k_attend<T, D, 1, 1, true>, 16, 16};
+    if (rows_o > 16) return {k_attend<T, D, kMost, kMost, true>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>};
+    if (rows_p > 32 && kMost == 4) return {k_attend<T, D, kMost, 1, true>, 16 * kMost, 16, kPerUnit<D, kMost>};
+    if (rows_p > 16) return {k_attend<T, D, 2, 1, true>, 32, 16, kPerUnit<D, 2>};
+    return {k_attend<T, D, 1, 1, true>, 16, 16, kPerUnit<D, 1>};
   }
 }
 
@@ -664,15 +708,12 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
   auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
   const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, small(rows_p), small(rows_o)) : choose<float>(kv->D, small(rows_p), small(rows_o));
-  // as many workgroups as there can be items, to whole rounds over the XCDs; beyond that they loop
-  const int64_t tiles = (kv->n_group ? all_rows / k.rows_p + kv->n_group : 0) + all_rows / k.rows_o + kv->n_seq;
-  const int64_t items = kTarget + tiles * kv->Hk;
-  const unsigned blocks = static_cast<unsigned>(items < 16384 ? round_up(items, 8) : 16384);
+  const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
   ProfScope ps(PROF_ATTENTION, s);
   hipLaunchKernelGGL(k.kernel, dim3(blocks), dim3(256), 0, s, view, args);
   ATG_LAUNCH_CHECK();
   auto join = kv->dtype == AT_GRPO_BF16 ? k_join<bf16_t> : k_join<float>;
-  hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * Hq, 4))), dim3(256), 0, s, view, args);
+  hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * Hq, 4))), dim3(256), 0, s, view, args, k.rows_p, k.rows_o);
   ATG_LAUNCH_CHECK();
   return AT_GRPO_OK;
 }
