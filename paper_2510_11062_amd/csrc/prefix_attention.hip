@@ -15,6 +15,7 @@
 //   P^T             is at once the second product's operand: no lane needs a weight that another one computed
 //   O^T += V^T P^T  a lane loads whole rows of V, eight elements of eight tokens, and transposes that block by itself
 // The four wavefronts of a workgroup take turns in a run's tokens and add up at its end.
+#include "gemm_bf16.hpp"
 #include "kv_common.hpp"
 
 #include <math.h>
@@ -26,6 +27,7 @@ namespace atg {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMostGroups = 1024;     // workgroups of a launch
@@ -34,7 +36,8 @@ constexpr int kCachedUnits = 512;     // units whose sizes are kept in LDS
 // three blocks at least, so that every wavefront has a tile to begin with.
 constexpr int kRunCost = 1, kMinShare = 3;
 constexpr int kPageSlots = 1024;     // page ids of a chunk in LDS at a time
-constexpr int kMaxRows = 64;         // rows of the largest tile
+constexpr int kMaxRows = 128;        // rows of the largest tile
+constexpr int kWideRows = 128;       // of the tiles below that four wavefronts share by rows
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum is raised where a score passes it by more than this (in powers of two): weights of at most 2^8 lose nothing in
 // fp32 sums, nor in bf16, whose error is relative, and most tokens then leave the sums as they are.
@@ -199,7 +202,7 @@ struct Lds {
   Schedule S;
   int scan[4];
   int pages[kPageSlots];
-  float ml[4][kMaxRows][2];
+  float ml[4][64][2];
   float slab[4][16][128 + 4];
 };
 
@@ -334,15 +337,13 @@ __device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit
 #pragma unroll
         for (int y = 0; y < SUB; ++y) {
           const int t4 = t + 16 * y + 4 * g;
-          const bool there = t4 < to && lds.pages[(t4 >> kv.page_shift) - page0] >= 0;
+          const int last = to - t4, seen = last > 0 && lds.pages[(min(t4, to - 1) >> kv.page_shift) - page0] >= 0 ? last : 0;
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
 #pragma unroll
-            for (int n = 0; n < NR; ++n)
-              if (!there || t4 + i >= limit[n]) s[n][y][i] = -INFINITY;
-            if (!there || t4 + i >= to)
+            for (int n = 0; n < NR; ++n) s[n][y][i] = i < min(seen, limit[n] - t4) ? s[n][y][i] : -INFINITY;
 #pragma unroll
-              for (int b = 0; b < NB; ++b) v[b][4 * y + i] = typename Z::VV{};
+            for (int b = 0; b < NB; ++b) v[b][4 * y + i] = i < seen ? v[b][4 * y + i] : typename Z::VV{};
           }
         }
       }
@@ -480,15 +481,199 @@ __device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit
   }
 }
 
-// Workgroups on a compute unit, by the registers of a wavefront.
-template <int D, int NRP>
-constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
+// ---- many queries ----------------------------------------------------------------------------------
+// Where a tile has 128 rows the products bound the call, not the tokens' passage.  Each wavefront then has 32 rows of its own, and the
+// four read the same 64 tokens from LDS, into which they come by direct loads, one tile ahead.  MFMA 32x32: a lane has 16 tokens of one
+// query in S^T, which are P^T's operand as they are, and V^T's operand comes from rows of V by transposing reads.
+//
+// A token's row is 2 D bytes in LDS; its 16-byte pieces are exchanged so that the reads meet no bank twice: piece c of K's row r lies at
+// c ^ (r & 15) (64-wide heads, whose rows take turns in the banks' halves: c ^ ((r >> 1) & 7)), of V's at c ^ 2 (r & 7) (c ^ 2 ((r >> 1) & 3)).
+constexpr int kWideTok = 64;
 
-template <typename T, int D, int NRP, int NRO, bool EXACT>
-__global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
-  __shared__ Lds lds;
-  Schedule& S = lds.S;
-  make_schedule<16 * NRP, 16 * NRO>(kv, a, S, lds.scan);
+struct WideLds {
+  Schedule S;
+  int scan[4];
+  int pages[kPageSlots];
+};
+
+template <int D>
+__device__ __forceinline__ int swizzle_k(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int swizzle_v(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
+
+template <int D>
+__device__ void attend_wide(const KvView& kv, const Args& a, WideLds& lds, char* tiles_lds, const Unit& u, bool own, int run, int cost, int cost0, int cost1,
+                            int group) {
+  constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 31, g = lane >> 5;
+  const int rows = u.ntok * a.share, tiles = tiles_of(u.ntok, a.share, kWideRows), hk = run / tiles, tile = tile_at(run - hk * tiles, tiles);
+  const int r0 = tile * kWideRows;
+  const bool steps = own && a.causal;
+  const int first = u.len - u.ntok + 1;
+  const int last_tok = (min(rows, r0 + kWideRows) - 1) / a.share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
+  const int k0 = cut(cost0, cost, end), k1 = cut(cost1, cost, end);
+  const int r = r0 + 32 * wave + m, tq = min(r, rows - 1) / a.share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
+  const int limit = steps ? min(k1, first + tq) : k1;
+  const int all_see = steps ? first + min(r0 + 32 * wave, rows - 1) / a.share : k1;      // a wavefront's first row sees least
+
+  uint4 q[KC];
+  const bf16_t* from_q = static_cast<const bf16_t*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
+#pragma unroll
+  for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const uint4*>(from_q + 16 * c + 8 * g);
+  const float to_log2 = a.scale * kLog2e;
+  f32x16 acc[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+  float top = -INFINITY, ref = 0.f, sum = 0.f;
+
+  // where this lane reads: K piece 2 c + g of row m (XOR 32 c), V four elements of row 4 g + (lane & 15) / 4 (XOR 64 t)
+  const int read_k = m * (2 * D) + ((g ^ swizzle_k<D>(m)) << 4);
+  const int i16 = lane & 15, row_v = 4 * g + (i16 >> 2);
+  const int read_v = row_v * (2 * D) + (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ swizzle_v<D>(row_v)) << 4) + (i16 & 1) * 8;
+
+  const int32_t* const table = own ? kv.pages + static_cast<int64_t>(u.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(u.row) * kv.max_prefix_pages;
+  const int64_t page_step = (static_cast<int64_t>(kv.Hk) * D) << kv.page_shift;
+  const int in_page = (1 << kv.page_shift) - 1;
+  const bf16_t* const kbase = static_cast<const bf16_t*>(kv.k) + ((static_cast<int64_t>(hk) * D) << kv.page_shift);
+  const bf16_t* const vbase = static_cast<const bf16_t*>(kv.v) + ((static_cast<int64_t>(hk) * D) << kv.page_shift);
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr32(tiles_lds)) + wave * NL * 1024;
+
+  for (int from = k0; from < k1;) {
+    const int page0 = from >> kv.page_shift, to = min(k1, (page0 + kPageSlots) << kv.page_shift);
+    const int n_slots = ((to - 1) >> kv.page_shift) - page0 + 1;
+    bool missing = false;
+    __syncthreads();
+    for (int i = tid; i < n_slots; i += 256) {
+      int id = table[page0 + i];
+      if (static_cast<unsigned>(id) >= static_cast<unsigned>(kv.n_pages)) {
+        id = -1;
+        missing = true;
+      }
+      lds.pages[i] = id;
+    }
+    const bool holes = __syncthreads_or(missing);
+    if (missing) raise_data_error(a.data_error, AT_GRPO_DATA_PAGE);
+
+    auto request = [&](int t, int buffer) {      // rows behind the last are the last
+#pragma unroll
+      for (int i = 0; i < NL; ++i) {
+        const int row = (wave * NL + i) * LROWS + lane / PIECES, piece = lane & (PIECES - 1), token = min(t + row, to - 1);
+        const int id = max(0, lds.pages[(token >> kv.page_shift) - page0]);
+        const int64_t at = id * page_step + static_cast<int64_t>(token & in_page) * D;
+        direct_load_v(reinterpret_cast<const char*>(kbase + at + 8 * (piece ^ swizzle_k<D>(row))), lds0 + buffer * 2 * TB + i * 1024);
+        direct_load_v(reinterpret_cast<const char*>(vbase + at + 8 * (piece ^ swizzle_v<D>(row))), lds0 + buffer * 2 * TB + TB + i * 1024);
+      }
+    };
+
+    int buffer = 0;
+    request(from, 0);
+    for (int t = from; t < to; t += kWideTok, buffer ^= 1) {
+      asm volatile("" ::: "memory");
+      wait_loads_but<0>();
+      __builtin_amdgcn_s_barrier();
+      asm volatile("" ::: "memory");
+      if (t + kWideTok < to) request(t + kWideTok, buffer ^ 1);
+      const char* const kt = tiles_lds + buffer * 2 * TB;
+      char* const vt = tiles_lds + buffer * 2 * TB + TB;
+      if (holes) {      // what stands for a token of no page must not be NaN
+        for (int i = tid; i < kWideTok * PIECES; i += 256) {
+          const int token = t + i / PIECES;
+          if (token < to && lds.pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
+        }
+        __syncthreads();
+      }
+      f32x16 s[2];
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < KC; ++c)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (read_k ^ (c << 5)) + y * 32 * 2 * D);
+          s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, q[c]), s[y], 0, 0, 0);
+        }
+      if (t + kWideTok > min(to, all_see) || holes) {
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+#pragma unroll
+          for (int b = 0; b < 4; ++b) {      // four tokens that start at a multiple of four share a page
+            const int t4 = t + 32 * y + 8 * b + 4 * g;
+            int left = limit - t4;
+            if (holes) left = lds.pages[(min(t4, to - 1) >> kv.page_shift) - page0] < 0 ? 0 : left;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[y][4 * b + i] = i < left ? s[y][4 * b + i] : -INFINITY;
+          }
+      }
+      float high = -INFINITY;
+#pragma unroll
+      for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) high = fmaxf(high, s[y][i]);
+      high *= to_log2;
+      if (__any(high > top + kSlack)) {
+        high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
+        const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top - now);
+        top = high;
+        ref = now;
+        sum *= keep;
+#pragma unroll
+        for (int x = 0; x < DT; ++x) acc[x] *= keep;
+      }
+      uint4 w[4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) {
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[j] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + j], to_log2, -ref));
+          sum += p[j];
+        }
+        w[ks] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+      }
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+        for (int x = 0; x < DT; ++x) {
+          const char* p = vt + (read_v ^ (x << 6)) + ks * 16 * 2 * D;
+          const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 8 * 2 * D);
+          acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y)), __builtin_bit_cast(bf16x8, w[ks]),
+                                                           acc[x], 0, 0, 0);
+        }
+    }
+    from = to;
+  }
+
+  sum += __shfl_xor(sum, 32, 64);
+  if (r >= rows) return;
+  const float f = sum == 0.f ? 0.f : 1.f / sum, x = sum == 0.f ? -INFINITY : fmaf(ref, kLn2, logf(sum));
+  const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h;
+  if (kv.n_group == 0 && cost0 == 0 && cost1 == cost) {
+    if (a.lse && g == 0) a.lse[by_query] = x;
+    bf16_t* to = static_cast<bf16_t*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 4 * g;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *reinterpret_cast<uint2*>(to + 32 * t + 2 * i) = make_uint2(pack_bf16x2(acc[t][i] * f, acc[t][i + 1] * f), pack_bf16x2(acc[t][i + 2] * f, acc[t][i + 3] * f));
+  } else {
+    const int64_t part = cost0 == 0 ? by_query : static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1) + static_cast<int64_t>(group) * kMaxRows + (r - r0);
+    if (g == 0) a.part_lse[part] = x;
+    float* to = a.part_out + part * D + 4 * g;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(to + 32 * t + 2 * i) = f32x4{acc[t][i] * f, acc[t][i + 1] * f, acc[t][i + 2] * f, acc[t][i + 3] * f};
+  }
+}
+
+// A workgroup's share: f(unit, whether it is a sequence's own tokens, run, cost of the run, the part of that cost, number of the workgroup)
+template <int RP, int RO, typename F>
+__device__ __forceinline__ void for_share(const KvView& kv, const Args& a, Schedule& S, int* scan_lds, F f) {
+  make_schedule<RP, RO>(kv, a, S, scan_lds);
   // neighbouring shares go to one XCD
   const int per_xcd = gridDim.x >> 3, w = per_xcd << 3 == gridDim.x ? (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3) : blockIdx.x;
   const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, total = S.first[256];
@@ -501,7 +686,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
     bool falls = false;
     return u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
   };
-  auto runs_of = [&](const Unit& x, bool own) { return tiles_of(x.ntok, a.share, own ? 16 * NRO : 16 * NRP) * kv.Hk; };
+  auto runs_of = [&](const Unit& x, bool own) { return tiles_of(x.ntok, a.share, own ? RO : RP) * kv.Hk; };
   if (S.first[tid] <= at && at < S.first[tid + 1]) {
     int base = S.first[tid], u = tid * per;
     for (;; ++u) {
@@ -522,13 +707,34 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
     const int cost = run_cost(x, own && a.causal, S.coarse), all = runs_of(x, own) * cost;
     while (at < min(stop, base + all)) {
       const int run = (at - base) / cost, run0 = base + run * cost, to = min(stop, run0 + cost);
-      if (own) attend_run<T, D, NRO, EXACT>(kv, a, lds, x, true, run, cost, at - run0, to - run0, w);
-      else attend_run<T, D, NRP, EXACT>(kv, a, lds, x, false, run, cost, at - run0, to - run0, w);
+      f(x, own, run, cost, at - run0, to - run0, w);
       at = to;
     }
     base += all;
     ++u;
   }
+}
+
+// Workgroups on a compute unit, by the registers of a wavefront.
+template <int D, int NRP>
+constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
+
+template <typename T, int D, int NRP, int NRO, bool EXACT>
+__global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
+  __shared__ Lds lds;
+  for_share<16 * NRP, 16 * NRO>(kv, a, lds.S, lds.scan, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
+    if (own) attend_run<T, D, NRO, EXACT>(kv, a, lds, u, true, run, cost, cost0, cost1, group);
+    else attend_run<T, D, NRP, EXACT>(kv, a, lds, u, false, run, cost, cost0, cost1, group);
+  });
+}
+
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
+  extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
+  WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * kWideTok * D * 2);
+  for_share<kWideRows, kWideRows>(kv, a, lds.S, lds.scan, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
+    attend_wide<D>(kv, a, lds, smem, u, own, run, cost, cost0, cost1, group);
+  });
 }
 
 // out = sum_p exp(lse_p - lse) out_p over the parts of a row.  A wavefront per query and head: four parts at a time, sixteen lanes for the
@@ -650,19 +856,21 @@ Scratch lay_out(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, WsAlloc& ws) {
 typedef void (*Kernel)(KvView, Args);
 struct Choice {
   Kernel kernel;
-  int rows_p, rows_o, per_unit;
+  int rows_p, rows_o, per_unit, lds;
 };
 
 template <typename T, int D, bool EXACT>
 Choice choose_of(int rows_p, int rows_o) {
   constexpr int kMost = sizeof(T) == 4 || D == 256 ? 2 : 4;
   if constexpr (!EXACT) {
-    return {k_attend<T, D, kMost, kMost, false>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>};
+    return {k_attend<T, D, kMost, kMost, false>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
   } else {
-    if (rows_o > 16) return {k_attend<T, D, kMost, kMost, true>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>};
-    if (rows_p > 32 && kMost == 4) return {k_attend<T, D, kMost, 1, true>, 16 * kMost, 16, kPerUnit<D, kMost>};
-    if (rows_p > 16) return {k_attend<T, D, 2, 1, true>, 32, 16, kPerUnit<D, 2>};
-    return {k_attend<T, D, 1, 1, true>, 16, 16, kPerUnit<D, 1>};
+    if constexpr (sizeof(T) == 2 && D <= 128)
+      if (rows_o > 16) return {k_attend_wide<D>, kWideRows, kWideRows, 2, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
+    if (rows_o > 16) return {k_attend<T, D, kMost, kMost, true>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
+    if (rows_p > 32 && kMost == 4) return {k_attend<T, D, kMost, 1, true>, 16 * kMost, 16, kPerUnit<D, kMost>, 0};
+    if (rows_p > 16) return {k_attend<T, D, 2, 1, true>, 32, 16, kPerUnit<D, 2>, 0};
+    return {k_attend<T, D, 1, 1, true>, 16, 16, kPerUnit<D, 1>, 0};
   }
 }
 
@@ -710,7 +918,8 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, small(rows_p), small(rows_o)) : choose<float>(kv->D, small(rows_p), small(rows_o));
   const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
   ProfScope ps(PROF_ATTENTION, s);
-  hipLaunchKernelGGL(k.kernel, dim3(blocks), dim3(256), 0, s, view, args);
+  if (k.lds) ATG_TRY(allow_big_lds(k.kernel, k.lds));
+  hipLaunchKernelGGL(k.kernel, dim3(blocks), dim3(256), k.lds, s, view, args);
   ATG_LAUNCH_CHECK();
   auto join = kv->dtype == AT_GRPO_BF16 ? k_join<bf16_t> : k_join<float>;
   hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * Hq, 4))), dim3(256), 0, s, view, args, k.rows_p, k.rows_o);
