@@ -33,8 +33,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 constexpr int kMostGroups = 1024;     // workgroups of a launch
 constexpr int kCachedUnits = 512;     // units whose sizes are kept in LDS
 // A run's beginning and end (page ids, queries, adding up) take about as long as a block of 64 tokens, and count as one.  Shares are
-// three blocks at least, so that every wavefront has a tile to begin with.
-constexpr int kRunCost = 1, kMinShare = 3;
+// no smaller than one block and that.
+constexpr int kRunCost = 1, kMinShare = 2;
 constexpr int kPageSlots = 1024;     // page ids of a chunk in LDS at a time
 constexpr int kMaxRows = 128;        // rows of the largest tile
 constexpr int kWideRows = 128;       // of the tiles below that four wavefronts share by rows
@@ -43,8 +43,23 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // fp32 sums, nor in bf16, whose error is relative, and most tokens then leave the sums as they are.
 constexpr float kSlack = 8.f;
 
+// x / d for 0 <= x < 2^31 by a product: ceil(2^(31 + k) / d) with 2^k >= d is off by less than one part in 2^31.
+struct Divisor {
+  uint32_t d, mul, shift;      // shift: k - 1; d == 1 has no product
+};
+Divisor divisor(int d) {
+  int k = 0;
+  while ((int64_t{1} << k) < d) ++k;
+  return Divisor{static_cast<uint32_t>(d), d == 1 ? 0 : static_cast<uint32_t>(((uint64_t{1} << (31 + k)) + d - 1) / d), static_cast<uint32_t>(k - 1)};
+}
+__device__ __forceinline__ int operator/(int x, const Divisor& by) {
+  return by.d == 1 ? x : static_cast<int>(__umulhi(static_cast<uint32_t>(x), by.mul) >> by.shift);
+}
+
 struct Args {
   int n_tok, Hq, share;      // share: Hq / Hk
+  Divisor by_share;
+  int coarse;                // costs are counted in blocks of 64 << coarse tokens
   int causal;
   float scale;
   Rows q, out;
@@ -104,66 +119,86 @@ __device__ __forceinline__ int run_cost(const Unit& u, bool steps, int coarse) {
 
 // Where a run of `cost` over tokens 0 .. end - 1 is cut: the token that stands at `at` of its cost.
 __device__ __forceinline__ int cut(int at, int cost, int end) {
-  return at <= 0 ? 0 : at >= cost ? end : static_cast<int>(static_cast<int64_t>(end) * at / cost) & ~63;
+  const int blocks = (end + 63) >> 6;
+  if (at >= cost) return end;
+  const int block = blocks == cost - kRunCost ? at : static_cast<int>(static_cast<float>(blocks) * (static_cast<float>(at) / static_cast<float>(cost)));
+  return min(end, block << 6);
 }
 
-// The same in every workgroup.
+// A workgroup's share of the runs.
 struct Schedule {
-  int first[257];      // cost in front of each thread's units, and all
-  int share;           // cost of a workgroup
-  int coarse;
-  int unit, base;      // the unit that a workgroup begins in, and the cost in front of it
-  int64_t cost[4];
+  int wave_cost[4], wave_falls[4];
+  int unit, base;      // the unit that the workgroup begins in, and the cost in front of it
   Unit cache[kCachedUnits];
 };
 
+struct Share {
+  int number, at, stop;
+};
+
+// The costs of all units, a contiguous part of them on each thread, and the workgroup's share of them; the same in every workgroup.
 template <int RP, int RO>
-__device__ void make_schedule(const KvView& kv, const Args& a, Schedule& S, int* scan_lds) {
-  const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, u0 = min(n, tid * per), u1 = min(n, u0 + per);
-  int error = 0;
+__device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
+  const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int u0 = min(n, tid * per), u1 = min(n, u0 + per);
+  int error = 0, mine = 0;
   bool falls = false;
-  int64_t cost = 0;
   for (int u = u0; u < u1; ++u) {
     const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
     if (u < kCachedUnits) S.cache[u] = x;
-    cost += static_cast<int64_t>(tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO)) * run_cost(x, a.causal && u >= kv.n_group, 0);
+    mine += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * run_cost(x, a.causal && u >= kv.n_group, a.coarse) * kv.Hk;
   }
-  const bool none = __syncthreads_or(falls);
-  if (none) error |= AT_GRPO_DATA_SEQLENS;
-  if (blockIdx.x == 0) raise_data_error(a.data_error, error);
+  int sum = mine;      // of the threads up to this one
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) cost += __shfl_xor(cost, o, 64);
-  if ((tid & 63) == 0) S.cost[tid >> 6] = cost;
-  __syncthreads();
-  cost = (S.cost[0] + S.cost[1] + S.cost[2] + S.cost[3]) * kv.Hk;
-  int coarse = 0;      // costs are counted in 32 bits
-  while (cost >> coarse > (1 << 29)) ++coarse;
-  int mine = 0;
-  if (!none)
-    for (int u = u0; u < u1; ++u) {
-      const Unit x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-      mine += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * run_cost(x, a.causal && u >= kv.n_group, coarse) * kv.Hk;
-    }
-  int total;
-  int at = block_exclusive_scan<256>(mine, scan_lds, &total);
-  const int share = max(kMinShare, (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x));
-  S.first[tid] = at;
-  if (tid == 0) {
-    S.first[256] = total;
-    S.share = share;
-    S.coarse = coarse;
+  for (int o = 1; o < 64; o <<= 1) {
+    const int up = __shfl_up(sum, o, 64);
+    if (lane >= o) sum += up;
   }
+  const bool wave_falls = __any(falls);
+  if (lane == 63) {
+    S.wave_cost[wave] = sum;
+    S.wave_falls[wave] = wave_falls;
+  }
+  __syncthreads();
+  const bool none = S.wave_falls[0] | S.wave_falls[1] | S.wave_falls[2] | S.wave_falls[3];
+  int total = 0, first = sum - mine;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    if (w < wave) first += S.wave_cost[w];
+    total += S.wave_cost[w];
+  }
+  if (none) total = 0;
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int share = max(kMinShare, (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x));
+  // neighbouring shares go to one XCD
+  const int per_xcd = gridDim.x >> 3, w = per_xcd << 3 == gridDim.x ? (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3) : blockIdx.x;
+  const int at = static_cast<int>(min<int64_t>(total, static_cast<int64_t>(w) * share));
   if (blockIdx.x == 0) {       // for the kernel that joins the parts
+    if (none) error |= AT_GRPO_DATA_SEQLENS;
+    raise_data_error(a.data_error, error);
+    int base = first;
     for (int u = u0; u < u1; ++u) {
       Unit x{0, 0, 0, 0};
       if (!none) x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-      const int c = run_cost(x, a.causal && u >= kv.n_group, coarse);
-      a.units[u] = make_int4(at, c, x.tok0, x.ntok);
-      at += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * c * kv.Hk;
+      const int c = run_cost(x, a.causal && u >= kv.n_group, a.coarse);
+      a.units[u] = make_int4(base, c, x.tok0, x.ntok);
+      base += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * c * kv.Hk;
     }
     if (tid == 0) a.units[n] = make_int4(share, 0, 0, 0);
   }
+  if (at < total && first <= at && at - first < mine) {
+    int base = first, u = u0;
+    for (;; ++u) {
+      const Unit x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
+      const int c = tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * kv.Hk * run_cost(x, a.causal && u >= kv.n_group, a.coarse);
+      if (at < base + c) break;
+      base += c;
+    }
+    S.unit = u;
+    S.base = base;
+  }
   __syncthreads();
+  return Share{w, at, min(total, at + share)};
 }
 
 // What a lane (m, g) = (lane & 15, lane >> 4) holds of a tile of TOK tokens.
@@ -200,7 +235,6 @@ __device__ __forceinline__ bf16x8 transposed(const VV (&v)[8], int e) {
 
 struct Lds {
   Schedule S;
-  int scan[4];
   int pages[kPageSlots];
   float ml[4][64][2];
   float slab[4][16][128 + 4];
@@ -218,14 +252,14 @@ __device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit
   // A causal query sees the own tokens in front of `first + its number among the new tokens`.
   const bool steps = own && a.causal;
   const int first = u.len - u.ntok + 1;
-  const int last_tok = (min(rows, r0 + R) - 1) / a.share, first_tok = r0 / a.share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
+  const int last_tok = (min(rows, r0 + R) - 1) / a.by_share, first_tok = r0 / a.by_share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
   const int k0 = cut(cost0, cost, end), k1 = cut(cost1, cost, end), all_see = steps ? first + first_tok : k1;
 
   typename Z::KV q[NR][KC];
   int limit[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    const int r = r0 + 16 * n + m, tq = min(r, rows - 1) / a.share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
+    const int r = r0 + 16 * n + m, tq = min(r, rows - 1) / a.by_share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
     const T* from = static_cast<const T*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
     limit[n] = steps ? min(k1, first + tq) : k1;
 #pragma unroll
@@ -408,7 +442,8 @@ __device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit
     from = to;
   }
 
-  // The wavefronts' maxima and sums, then their products, each divided by the sum of all.
+  // The wavefronts' maxima and sums, and their products, which sixteen threads a row weigh and add up.
+  if (k0 >= k1) __syncthreads();      // else the loads of page ids have had one since the last run
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
     sum[n] += __shfl_xor(sum[n], 16, 64);
@@ -418,52 +453,53 @@ __device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit
       lds.ml[wave][16 * n + m][1] = sum[n];
     }
   }
-  __syncthreads();
   const bool direct = kv.n_group == 0 && cost0 == 0 && cost1 == cost;
   // where a row's part lies: by its query and head, or with the workgroup's
   const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq, by_group = static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1);
-  auto part_of = [&](int r, int tq, int h) {
-    return cost0 == 0 ? by_query + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h : by_group + static_cast<int64_t>(group) * kMaxRows + (r - r0);
-  };
-  float high[NR], total[NR];
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
-    high[n] = -INFINITY;
-    total[n] = 0.f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) high[n] = fmaxf(high[n], lds.ml[w][16 * n + m][0]);
-    const float now = high[n] == -INFINITY ? 0.f : high[n];
-#pragma unroll
-    for (int w = 0; w < 4; ++w) total[n] += lds.ml[w][16 * n + m][1] * __builtin_amdgcn_exp2f(lds.ml[w][16 * n + m][0] - now);
-    const float f = total[n] == 0.f ? 0.f : __builtin_amdgcn_exp2f(top[n] - now) / total[n];
-    const int r = r0 + 16 * n + m;
-    if (wave == 0 && g == 0 && r < rows) {
-      const int tq = r / a.share, h = hk * a.share + r - tq * a.share;
-      const float x = total[n] == 0.f ? -INFINITY : fmaf(now, kLn2, logf(total[n]));
-      if (!direct) a.part_lse[part_of(r, tq, h)] = x;
-      else if (a.lse) a.lse[static_cast<int64_t>(u.tok0 + tq) * a.Hq + h] = x;
-    }
+    const int row = tid >> 4, r = r0 + 16 * n + row, tq = r / a.by_share, h = hk * a.share + r - tq * a.share;
+    const int64_t part = cost0 == 0 ? by_query + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h : by_group + static_cast<int64_t>(group) * kMaxRows + (r - r0);
+    float f[4];
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      __syncthreads();
+      if (n || b) __syncthreads();
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int e = 0; e < E; e += 4)
           *reinterpret_cast<f32x4*>(&lds.slab[wave][m][E * (4 * g + i) + e]) =
-              f32x4{acc[n][b][e][i] * f, acc[n][b][e + 1][i] * f, acc[n][b][e + 2][i] * f, acc[n][b][e + 3][i] * f};
+              f32x4{acc[n][b][e][i], acc[n][b][e + 1][i], acc[n][b][e + 2][i], acc[n][b][e + 3][i]};
       __syncthreads();
-      const int row = tid >> 4, rr = r0 + 16 * n + row, d = E * (tid & 15);
-      if (rr < rows && (EXACT || 16 * E * b + d < dim)) {
+      if (b == 0) {
+        float high = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) high = fmaxf(high, lds.ml[w][16 * n + row][0]);
+        const float now = high == -INFINITY ? 0.f : high;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          f[w] = __builtin_amdgcn_exp2f(lds.ml[w][16 * n + row][0] - now);
+          total = fmaf(f[w], lds.ml[w][16 * n + row][1], total);
+        }
+        const float one = total == 0.f ? 0.f : __builtin_amdgcn_rcpf(total);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) f[w] *= one;
+        if ((tid & 15) == 0 && r < rows) {
+          const float x = total == 0.f ? -INFINITY : (now + __builtin_amdgcn_logf(total)) * kLn2;
+          if (!direct) a.part_lse[part] = x;
+          else if (a.lse) a.lse[static_cast<int64_t>(u.tok0 + tq) * a.Hq + h] = x;
+        }
+      }
+      const int d = E * (tid & 15);
+      if (r < rows && (EXACT || 16 * E * b + d < dim)) {
         f32x4 o[E / 4];
 #pragma unroll
         for (int e = 0; e < E / 4; ++e) {
           f32x4 x[4];
 #pragma unroll
-          for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&lds.slab[w][row][d + 4 * e]);
+          for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&lds.slab[w][row][d + 4 * e]) * f[w];
           o[e] = (x[0] + x[1]) + (x[2] + x[3]);
         }
-        const int tq = rr / a.share, h = hk * a.share + rr - tq * a.share;
         if (direct) {
           T* to = static_cast<T*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 16 * E * b + d;
 #pragma unroll
@@ -472,7 +508,7 @@ __device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit
             else *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
           }
         } else {
-          float* to = a.part_out + part_of(rr, tq, h) * dim + 16 * E * b + d;
+          float* to = a.part_out + part * dim + 16 * E * b + d;
 #pragma unroll
           for (int e = 0; e < E / 4; ++e) *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
         }
@@ -492,7 +528,6 @@ constexpr int kWideTok = 64;
 
 struct WideLds {
   Schedule S;
-  int scan[4];
   int pages[kPageSlots];
 };
 
@@ -510,11 +545,11 @@ __device__ void attend_wide(const KvView& kv, const Args& a, WideLds& lds, char*
   const int r0 = tile * kWideRows;
   const bool steps = own && a.causal;
   const int first = u.len - u.ntok + 1;
-  const int last_tok = (min(rows, r0 + kWideRows) - 1) / a.share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
+  const int last_tok = (min(rows, r0 + kWideRows) - 1) / a.by_share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
   const int k0 = cut(cost0, cost, end), k1 = cut(cost1, cost, end);
-  const int r = r0 + 32 * wave + m, tq = min(r, rows - 1) / a.share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
+  const int r = r0 + 32 * wave + m, tq = min(r, rows - 1) / a.by_share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
   const int limit = steps ? min(k1, first + tq) : k1;
-  const int all_see = steps ? first + min(r0 + 32 * wave, rows - 1) / a.share : k1;      // a wavefront's first row sees least
+  const int all_see = steps ? first + min(r0 + 32 * wave, rows - 1) / a.by_share : k1;      // a wavefront's first row sees least
 
   uint4 q[KC];
   const bf16_t* from_q = static_cast<const bf16_t*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
@@ -649,7 +684,7 @@ __device__ void attend_wide(const KvView& kv, const Args& a, WideLds& lds, char*
 
   sum += __shfl_xor(sum, 32, 64);
   if (r >= rows) return;
-  const float f = sum == 0.f ? 0.f : 1.f / sum, x = sum == 0.f ? -INFINITY : fmaf(ref, kLn2, logf(sum));
+  const float f = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), x = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
   const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h;
   if (kv.n_group == 0 && cost0 == 0 && cost1 == cost) {
     if (a.lse && g == 0) a.lse[by_query] = x;
@@ -672,42 +707,23 @@ __device__ void attend_wide(const KvView& kv, const Args& a, WideLds& lds, char*
 
 // A workgroup's share: f(unit, whether it is a sequence's own tokens, run, cost of the run, the part of that cost, number of the workgroup)
 template <int RP, int RO, typename F>
-__device__ __forceinline__ void for_share(const KvView& kv, const Args& a, Schedule& S, int* scan_lds, F f) {
-  make_schedule<RP, RO>(kv, a, S, scan_lds);
-  // neighbouring shares go to one XCD
-  const int per_xcd = gridDim.x >> 3, w = per_xcd << 3 == gridDim.x ? (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3) : blockIdx.x;
-  const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, total = S.first[256];
-  const int64_t begin = static_cast<int64_t>(w) * S.share;
-  if (begin >= total) return;
-  int at = static_cast<int>(begin);
-  const int stop = min(total, at + S.share);
-  auto unit_at = [&](int u) {
+__device__ __forceinline__ void for_share(const KvView& kv, const Args& a, Schedule& S, F f) {
+  const Share mine = make_schedule<RP, RO>(kv, a, S);
+  if (mine.at >= mine.stop) return;
+  int at = mine.at, u = __builtin_amdgcn_readfirstlane(S.unit), base = __builtin_amdgcn_readfirstlane(S.base);
+  while (at < mine.stop) {
     int error = 0;
     bool falls = false;
-    return u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-  };
-  auto runs_of = [&](const Unit& x, bool own) { return tiles_of(x.ntok, a.share, own ? RO : RP) * kv.Hk; };
-  if (S.first[tid] <= at && at < S.first[tid + 1]) {
-    int base = S.first[tid], u = tid * per;
-    for (;; ++u) {
-      const Unit x = unit_at(u);
-      const bool own = u >= kv.n_group;
-      const int c = runs_of(x, own) * run_cost(x, own && a.causal, S.coarse);
-      if (at < base + c) break;
-      base += c;
-    }
-    S.unit = u;
-    S.base = base;
-  }
-  __syncthreads();
-  int u = S.unit, base = S.base;
-  while (at < stop) {
-    const Unit x = unit_at(u);
+    Unit x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
+    x.tok0 = __builtin_amdgcn_readfirstlane(x.tok0);
+    x.ntok = __builtin_amdgcn_readfirstlane(x.ntok);
+    x.len = __builtin_amdgcn_readfirstlane(x.len);
+    x.row = __builtin_amdgcn_readfirstlane(x.row);
     const bool own = u >= kv.n_group;
-    const int cost = run_cost(x, own && a.causal, S.coarse), all = runs_of(x, own) * cost;
-    while (at < min(stop, base + all)) {
-      const int run = (at - base) / cost, run0 = base + run * cost, to = min(stop, run0 + cost);
-      f(x, own, run, cost, at - run0, to - run0, w);
+    const int cost = run_cost(x, own && a.causal, a.coarse), all = tiles_of(x.ntok, a.share, own ? RO : RP) * kv.Hk * cost;
+    while (at < min(mine.stop, base + all)) {
+      const int run = (at - base) / cost, run0 = base + run * cost, to = min(mine.stop, run0 + cost);
+      f(x, own, run, cost, at - run0, to - run0, mine.number);
       at = to;
     }
     base += all;
@@ -722,7 +738,7 @@ constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
 template <typename T, int D, int NRP, int NRO, bool EXACT>
 __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
   __shared__ Lds lds;
-  for_share<16 * NRP, 16 * NRO>(kv, a, lds.S, lds.scan, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
+  for_share<16 * NRP, 16 * NRO>(kv, a, lds.S, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
     if (own) attend_run<T, D, NRO, EXACT>(kv, a, lds, u, true, run, cost, cost0, cost1, group);
     else attend_run<T, D, NRP, EXACT>(kv, a, lds, u, false, run, cost, cost0, cost1, group);
   });
@@ -732,7 +748,7 @@ template <int D>
 __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
   WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * kWideTok * D * 2);
-  for_share<kWideRows, kWideRows>(kv, a, lds.S, lds.scan, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
+  for_share<kWideRows, kWideRows>(kv, a, lds.S, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
     attend_wide<D>(kv, a, lds, smem, u, own, run, cost, cost0, cost1, group);
   });
 }
@@ -911,11 +927,16 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < ws.bytes()) return AT_GRPO_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int share = Hq / kv->Hk;
-  const Args args{n_tok, Hq, share, causal != 0, scale, rows_of(q), rows_of(out), lse, data_error, scratch.units, scratch.part_lse, scratch.part_out};
+  Args args{n_tok, Hq, share, divisor(share), 0, causal != 0, scale, rows_of(q), rows_of(out), lse, data_error, scratch.units, scratch.part_lse, scratch.part_out};
   const int64_t all_rows = static_cast<int64_t>(n_tok) * share;
   const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
   auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
   const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, small(rows_p), small(rows_o)) : choose<float>(kv->D, small(rows_p), small(rows_o));
+  // an upper bound of all costs together, which are counted in 32 bits
+  const int64_t tiles_p = kv->n_group ? all_rows / k.rows_p + kv->n_group : 0, tiles_o = all_rows / k.rows_o + kv->n_seq;
+  const auto blocks_of = [&](int64_t pages) { return pages * kv->page_size / 64 + 2 + kRunCost; };
+  double most = (static_cast<double>(tiles_p) * blocks_of(kv->max_prefix_pages) + static_cast<double>(tiles_o) * blocks_of(kv->max_pages)) * kv->Hk;
+  for (; most > 1 << 30; most /= 2) ++args.coarse;
   const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
   ProfScope ps(PROF_ATTENTION, s);
   if (k.lds) ATG_TRY(allow_big_lds(k.kernel, k.lds));
