@@ -65,7 +65,7 @@ struct Args {
   Rows q, out;
   float* lse;                // [n_tok, Hq] or null
   int32_t* data_error;
-  int4* units;               // workspace: [n_group + n_seq] cost in front of the unit, cost of a run, first token, tokens; then {share, ..}
+  int4* units;               // workspace: [n_group + n_seq] cost in front of the unit, cost of a run, first token, tokens; then {share, all cost, whether an index falls}
   // Parts, each divided by its own sum.  A run's first part lies by its query and head, those of prefixes first: [2 or 1][n_tok][Hq].
   // A workgroup's first part, where it begins inside a run, lies behind them: [workgroup][row of the tile].
   float* part_lse;
@@ -184,7 +184,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
       a.units[u] = make_int4(base, c, x.tok0, x.ntok);
       base += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * c * kv.Hk;
     }
-    if (tid == 0) a.units[n] = make_int4(share, 0, 0, 0);
+    if (tid == 0) a.units[n] = make_int4(share, total, none, 0);
   }
   if (at < total && first <= at && at - first < mine) {
     int base = first, u = u0;
@@ -753,73 +753,81 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
   });
 }
 
-// out = sum_p exp(lse_p - lse) out_p over the parts of a row.  A wavefront per query and head: four parts at a time, sixteen lanes for the
-// elements of one.
+// ---- joining the parts --------------------------------------------------------------------------------
+// out = sum_p exp(lse_p - lse) out_p over the parts of a row.
+
+__device__ __forceinline__ float larger(float a, float b) { return b > a || b != b ? b : a; }      // NaN stays
+
 template <typename T>
+__device__ __forceinline__ void store8(T* to, const float* y) {
+  if constexpr (sizeof(T) == 2) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7]));
+  } else {
+    *reinterpret_cast<f32x4*>(to) = f32x4{y[0], y[1], y[2], y[3]};
+    *reinterpret_cast<f32x4*>(to + 4) = f32x4{y[4], y[5], y[6], y[7]};
+  }
+}
+
+// Rows behind prefixes: WAVES wavefronts of a workgroup for each query and head, sixteen lanes for the elements of a part.
+template <typename T, int WAVES>
 __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int rows_o) {
-  const int lane = threadIdx.x & 63, l = lane & 15, slot = lane >> 4, D = kv.D;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + (threadIdx.x >> 6);
+  __shared__ float lds[WAVES == 1 ? 1 : 4][kMaxHeadDim + 1];
+  const int lane = threadIdx.x & 63, l = lane & 15, slot = lane >> 4, wave = threadIdx.x >> 6, mine = WAVES == 1 ? 0 : wave, D = kv.D;
+  const int64_t unit = WAVES == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
   if (unit >= static_cast<int64_t>(a.n_tok) * a.Hq) return;
-  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * a.Hq), hk = h / a.share;
-  const int s = kv.cu_q ? wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1 : t, share = a.units[kv.n_group + kv.n_seq].x;
-  int group0[2] = {0, 0}, count[2] = {0, 0}, row[2] = {0, 0};      // the run's first workgroup, its workgroups, the row in its tile
-  auto look_up = [&](int which, int u, int rows) {
-    const int4 x = a.units[u];
-    if (x.y == 0 || t < x.z || t - x.z >= x.w) return;
-    const int tiles = tiles_of(x.w, a.share, rows), r = (t - x.z) * a.share + h - hk * a.share, tile = r / rows;
+  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * a.Hq), hk = h / a.by_share;
+  const int s = kv.cu_q ? wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1 : t, g = wave_upper_bound(kv.group_seq, kv.n_group + 1, s) - 1;
+  const int share = a.units[kv.n_group + kv.n_seq].x;
+  const bool in_seq = s >= 0 && s < kv.n_seq, in_group = in_seq && g >= 0 && g < kv.n_group;
+  const int4 of_p = in_group ? a.units[g] : make_int4(0, 0, 0, 0), of_o = in_seq ? a.units[kv.n_group + s] : make_int4(0, 0, 0, 0);
+  int group0[2], count[2], row[2];      // the run's first workgroup, its workgroups, the row in its tile
+  auto look_up = [&](int which, const int4& x, int rows) {
+    const int q = t - x.z, tiles = max(1, tiles_of(x.w, a.share, rows)), r = q * a.share + h - hk * a.share, tile = r / rows;
     const int run0 = x.x + (hk * tiles + turn_of(tile, tiles)) * x.y;
     group0[which] = run0 / share;
-    count[which] = (run0 + x.y - 1) / share - group0[which] + 1;
+    count[which] = x.y == 0 || q < 0 || q >= x.w ? 0 : (run0 + x.y - 1) / share - group0[which] + 1;
     row[which] = r - tile * rows;
   };
-  if (s >= 0 && s < kv.n_seq) {
-    look_up(1, kv.n_group + s, rows_o);
-    if (kv.n_group) {
-      const int g = wave_upper_bound(kv.group_seq, kv.n_group + 1, s) - 1;
-      if (g >= 0 && g < kv.n_group) look_up(0, g, rows_p);
-    }
-  }
-  if (kv.n_group == 0 && count[1] == 1) return;      // in its place already
+  look_up(0, of_p, rows_p);
+  look_up(1, of_o, rows_o);
   const int n0 = count[0], n = n0 + count[1];
-  const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq, by_group = queries * (kv.n_group ? 2 : 1);
+  const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
   auto part_of = [&](int p) {
     const bool own = p >= n0;
     const int i = own ? p - n0 : p;
-    return i == 0 ? (own && kv.n_group ? queries : 0) + unit : by_group + static_cast<int64_t>((own ? group0[1] : group0[0]) + i) * kMaxRows + (own ? row[1] : row[0]);
+    return i == 0 ? (own ? queries : 0) + unit : 2 * queries + static_cast<int64_t>((own ? group0[1] : group0[0]) + i) * kMaxRows + (own ? row[1] : row[0]);
   };
-  float high = -INFINITY;
-  for (int c = lane; c < n; c += 64) {
-    const float x = a.part_lse[part_of(c)];
-    high = x > high || x != x ? x : high;      // NaN stays
-  }
+  float high = -INFINITY, total = 0.f, acc[kMaxHeadDim / 16] = {};
+  for (int p0 = 0; p0 < n; p0 += 64) {
+    const int count_here = min(64, n - p0);
+    const float x = lane < count_here ? a.part_lse[part_of(p0 + lane)] : -INFINITY;
+    float now = larger(high, x);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float x = __shfl_xor(high, o, 64);
-    high = x > high || x != x ? x : high;
-  }
-  const float now = high == -INFINITY ? 0.f : high;
-  float total = 0.f, acc[kMaxHeadDim / 16] = {};
-  for (int c0 = 0; c0 < n; c0 += 4) {
-    const int c = c0 + slot;
-    float w = 0.f;
-    if (c < n) {
-      const int64_t p = part_of(c);
-      w = __builtin_amdgcn_exp2f((a.part_lse[p] - now) * kLog2e);
-      const float* from = a.part_out + p * D;
+    for (int o = 32; o > 0; o >>= 1) now = larger(now, __shfl_xor(now, o, 64));
+    const float ref = now == -INFINITY ? 0.f : now, keep = __builtin_amdgcn_exp2f((high - ref) * kLog2e), weight = __builtin_amdgcn_exp2f((x - ref) * kLog2e);
+    high = now;
+    total *= keep;
 #pragma unroll
-      for (int x = 0; x < kMaxHeadDim / 128; ++x) {
-        const int d = 128 * x + 8 * l;
+    for (int i = 0; i < kMaxHeadDim / 16; ++i) acc[i] *= keep;
+#pragma unroll 4
+    for (int c0 = 4 * mine; c0 < count_here; c0 += 4 * WAVES) {
+      const int c = c0 + slot;
+      const float w = __shfl(weight, c, 64);      // 0 behind the last
+      const float* from = a.part_out + part_of(p0 + min(c, count_here - 1)) * D;
+      total += w;
+#pragma unroll
+      for (int x2 = 0; x2 < kMaxHeadDim / 128; ++x2) {
+        const int d = 128 * x2 + 8 * l;
         if (d < D) {
           const f32x4 y0 = *reinterpret_cast<const f32x4*>(from + d), y1 = *reinterpret_cast<const f32x4*>(from + d + 4);
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            acc[8 * x + i] = fmaf(w, y0[i], acc[8 * x + i]);
-            acc[8 * x + 4 + i] = fmaf(w, y1[i], acc[8 * x + 4 + i]);
+            acc[8 * x2 + i] = fmaf(w, y0[i], acc[8 * x2 + i]);
+            acc[8 * x2 + 4 + i] = fmaf(w, y1[i], acc[8 * x2 + 4 + i]);
           }
         }
       }
     }
-    total += w;
   }
   total += __shfl_xor(total, 16, 64);
   total += __shfl_xor(total, 32, 64);
@@ -828,21 +836,120 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int
     acc[i] += __shfl_xor(acc[i], 16, 64);
     acc[i] += __shfl_xor(acc[i], 32, 64);
   }
+  if constexpr (WAVES > 1) {
+    if (slot == 0) {
+#pragma unroll
+      for (int x = 0; x < kMaxHeadDim / 128; ++x)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) lds[wave][128 * x + 8 * l + i] = acc[8 * x + i];
+      if (l == 0) lds[wave][kMaxHeadDim] = total;
+    }
+    __syncthreads();
+    if (wave) return;
+    total = (lds[0][kMaxHeadDim] + lds[1][kMaxHeadDim]) + (lds[2][kMaxHeadDim] + lds[3][kMaxHeadDim]);
+#pragma unroll
+    for (int x = 0; x < kMaxHeadDim / 128; ++x)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int d = 128 * x + 8 * l + i;
+        acc[8 * x + i] = (lds[0][d] + lds[1][d]) + (lds[2][d] + lds[3][d]);
+      }
+  }
   if (slot == 0) {
     const float f = total == 0.f ? 0.f : 1.f / total;
     T* to = static_cast<T*>(a.out.data) + t * a.out.ts + h * a.out.hs;
 #pragma unroll
-    for (int x = 0; x < kMaxHeadDim / 128; ++x) {
-      const int d = 128 * x + 8 * l;
-      if (d < D)
+    for (int i = 0; i < kMaxHeadDim / 16; ++i) acc[i] *= f;
 #pragma unroll
-        for (int i = 0; i < 8; i += 4) {
-          const float* y = acc + 8 * x + i;
-          if constexpr (sizeof(T) == 2) *reinterpret_cast<uint2*>(to + d + i) = make_uint2(pack_bf16x2(y[0] * f, y[1] * f), pack_bf16x2(y[2] * f, y[3] * f));
-          else *reinterpret_cast<f32x4*>(to + d + i) = f32x4{y[0] * f, y[1] * f, y[2] * f, y[3] * f};
-        }
+    for (int x = 0; x < kMaxHeadDim / 128; ++x)
+      if (128 * x + 8 * l < D) store8(to + 128 * x + 8 * l, acc + 8 * x);
+    if (a.lse && l == 0) a.lse[unit] = total == 0.f ? -INFINITY : high + logf(total);
+  }
+}
+
+// A wavefront clears a token's rows.
+template <typename T>
+__device__ void clear_token(const Args& a, int D, int t) {
+  const int lane = threadIdx.x & 63, pieces = D / 8;
+  const float zeros[8] = {};
+  for (int i = lane; i < a.Hq * pieces; i += 64) {
+    const int h = i / pieces;
+    store8(static_cast<T*>(a.out.data) + t * a.out.ts + h * a.out.hs + 8 * (i - h * pieces), zeros);
+  }
+  if (a.lse)
+    for (int h = lane; h < a.Hq; h += 64) a.lse[static_cast<int64_t>(t) * a.Hq + h] = -INFINITY;
+}
+
+// Without prefixes most runs are one workgroup's, and their rows in place.  Workgroup (w, y), w < joins, joins the rows y, y + gridDim.y, ..
+// (sixteens of them) of the run that workgroup w + 1 of the kernel before began inside, if it was the first to.  The others clear the rows
+// that no run has: those of sequences that have nothing to see, and of no sequence.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o, int joins) {
+  const int l = threadIdx.x & 15, D = kv.D, w = blockIdx.x + 1;
+  const int4 all = a.units[kv.n_seq];
+  if (blockIdx.x >= joins) {
+    const int wave = threadIdx.x >> 6, first = ((blockIdx.x - joins) * gridDim.y + blockIdx.y) * 4 + wave, step = (gridDim.x - joins) * gridDim.y * 4;
+    const int t0 = all.z ? a.n_tok : kv.cu_q ? kv.cu_q[0] : 0, t1 = all.z ? a.n_tok : kv.cu_q ? kv.cu_q[kv.n_seq] : a.n_tok;
+    for (int t = first; t < t0; t += step) clear_token<T>(a, D, t);
+    for (int t = t1 + first; t < a.n_tok; t += step) clear_token<T>(a, D, t);
+    for (int s = first; s < kv.n_seq; s += step) {
+      const int4 of = a.units[s];
+      for (int t = of.z; of.y == 0 && t < of.z + of.w; ++t) clear_token<T>(a, D, t);
     }
-    if (a.lse && l == 0) a.lse[unit] = total == 0.f ? -INFINITY : now + logf(total);
+    return;
+  }
+  const int share = all.x, total_cost = all.y;
+  if (static_cast<int64_t>(w) * share >= total_cost) return;
+  const int x = w * share;
+  int u = 0;
+  for (int n = kv.n_seq; n > 1;) {      // the last unit that begins at x or in front of it
+    const int step = (n + 63) >> 6, lane = threadIdx.x & 63, at = lane * step;
+    const int c = __popcll(__ballot(at < n && a.units[u + (at < n ? at : 0)].x <= x));
+    u += (max(c, 1) - 1) * step;
+    n = min(step, n - (max(c, 1) - 1) * step);
+  }
+  const int4 of = a.units[u];
+  const int run = (x - of.x) / of.y, run0 = of.x + run * of.y;
+  if (run0 == x || run0 / share != w - 1) return;
+  const int rows = of.w * a.share, tiles = tiles_of(of.w, a.share, rows_o), hk = run / tiles, r0 = tile_at(run - hk * tiles, tiles) * rows_o;
+  const int n = (run0 + of.y - 1) / share - w + 2;      // parts
+  const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
+  for (int i = blockIdx.y * 16 + (threadIdx.x >> 4); i < rows_o && r0 + i < rows; i += gridDim.y * 16) {
+    const int tq = (r0 + i) / a.by_share, h = hk * a.share + r0 + i - tq * a.share;
+    const int64_t row = static_cast<int64_t>(of.z + tq) * a.Hq + h;
+    auto part_of = [&](int p) { return p == 0 ? row : queries + static_cast<int64_t>(w - 1 + p) * kMaxRows + i; };
+    float high = -INFINITY;
+    for (int p = l; p < n; p += 16) high = larger(high, a.part_lse[part_of(p)]);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) high = larger(high, __shfl_xor(high, o, 64));
+    const float ref = high == -INFINITY ? 0.f : high;
+    float total = 0.f, acc[kMaxHeadDim / 16] = {};
+#pragma unroll 2
+    for (int p = 0; p < n; ++p) {
+      const int64_t part = part_of(p);
+      const float weight = __builtin_amdgcn_exp2f((a.part_lse[part] - ref) * kLog2e);
+      total += weight;
+#pragma unroll
+      for (int y = 0; y < kMaxHeadDim / 128; ++y) {
+        const int d = 128 * y + 8 * l;
+        if (d < D) {
+          const f32x4 y0 = *reinterpret_cast<const f32x4*>(a.part_out + part * D + d), y1 = *reinterpret_cast<const f32x4*>(a.part_out + part * D + d + 4);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            acc[8 * y + e] = fmaf(weight, y0[e], acc[8 * y + e]);
+            acc[8 * y + 4 + e] = fmaf(weight, y1[e], acc[8 * y + 4 + e]);
+          }
+        }
+      }
+    }
+    const float f = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+    for (int e = 0; e < kMaxHeadDim / 16; ++e) acc[e] *= f;
+    T* to = static_cast<T*>(a.out.data) + (of.z + tq) * a.out.ts + h * a.out.hs;
+#pragma unroll
+    for (int y = 0; y < kMaxHeadDim / 128; ++y)
+      if (128 * y + 8 * l < D) store8(to + 128 * y + 8 * l, acc + 8 * y);
+    if (a.lse && l == 0) a.lse[row] = total == 0.f ? -INFINITY : high + logf(total);
   }
 }
 
@@ -942,8 +1049,19 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   if (k.lds) ATG_TRY(allow_big_lds(k.kernel, k.lds));
   hipLaunchKernelGGL(k.kernel, dim3(blocks), dim3(256), k.lds, s, view, args);
   ATG_LAUNCH_CHECK();
-  auto join = kv->dtype == AT_GRPO_BF16 ? k_join<bf16_t> : k_join<float>;
-  hipLaunchKernelGGL(join, dim3(static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * Hq, 4))), dim3(256), 0, s, view, args, k.rows_p, k.rows_o);
+  const bool bf16 = kv->dtype == AT_GRPO_BF16;
+  const int64_t outputs = static_cast<int64_t>(n_tok) * Hq;
+  if (kv->n_group == 0) {
+    const int y = k.rows_o / 16 < 4 ? k.rows_o / 16 : 4, joins = static_cast<int>(blocks) - 1;
+    const int64_t clears = ceil_div(kv->n_seq + 1, 4 * y);
+    hipLaunchKernelGGL(bf16 ? k_join_runs<bf16_t> : k_join_runs<float>, dim3(static_cast<unsigned>(joins + (clears < 256 ? clears : 256)), y), dim3(256), 0, s,
+                       view, args, k.rows_o, joins);
+  } else if (outputs <= 1024) {      // few rows: a workgroup for each
+    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 4> : k_join<float, 4>), dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows_p, k.rows_o);
+  } else {
+    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 1> : k_join<float, 1>), dim3(static_cast<unsigned>(ceil_div(outputs, 4))), dim3(256), 0, s, view, args, k.rows_p,
+                       k.rows_o);
+  }
   ATG_LAUNCH_CHECK();
   return AT_GRPO_OK;
 }
