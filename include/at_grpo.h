@@ -448,7 +448,7 @@ int at_grpo_qk_norm_rope_bwd(const at_grpo_norm_rope* layer, int32_t n_tok, int3
  */
 typedef struct {
   int32_t dtype, Hk, D;          /* of the cache; D as above                                             */
-  int32_t page_size;             /* a power of two, 8 .. 65536                                           */
+  int32_t page_size;             /* a power of two, 8 .. 65536; Hk * page_size * D <= 2^30               */
   int32_t n_pages;               /* > 0                                                                  */
   int32_t n_seq, max_pages;      /* rows and columns of pages                                            */
   int32_t n_group, max_prefix_pages; /* rows and columns of prefix_pages; n_group == 0: no prefixes      */

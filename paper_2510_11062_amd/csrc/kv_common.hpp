@@ -48,6 +48,7 @@ inline int check_kv_sizes(const at_grpo_kv* kv, int32_t n_tok) {
   if (static_cast<int64_t>(kv->max_pages) * kv->page_size > most / 2 || static_cast<int64_t>(kv->max_prefix_pages) * kv->page_size > most / 2 ||
       static_cast<int64_t>(kv->n_seq) + kv->n_group > most / 2)
     return AT_GRPO_EUNSUPPORTED;
+  if (static_cast<int64_t>(kv->Hk) * kv->page_size > (1 << 30) / kv->D) return AT_GRPO_EUNSUPPORTED;      // bytes of a page too
   return AT_GRPO_OK;
 }
 

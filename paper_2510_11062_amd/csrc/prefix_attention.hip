@@ -65,7 +65,7 @@ struct Args {
   Rows q, out;
   float* lse;                // [n_tok, Hq] or null
   int32_t* data_error;
-  int4* units;               // workspace: [n_group + n_seq] cost in front of the unit, cost of a run, first token, tokens; then {share, all cost, whether an index falls}
+  int4* units;               // workspace: [n_group + n_seq] cost in front of the unit, its length, first token, tokens; then {share, all cost, whether an index falls}
   // Parts, each divided by its own sum.  A run's first part lies by its query and head, those of prefixes first: [2 or 1][n_tok][Hq].
   // A workgroup's first part, where it begins inside a run, lies behind them: [workgroup][row of the tile].
   float* part_lse;
@@ -106,15 +106,21 @@ __device__ __forceinline__ Unit unit_of(const KvView& kv, int u, int n_tok, int*
 
 __device__ __forceinline__ int tiles_of(int ntok, int share, int rows) { return (ntok * share + rows - 1) / rows; }
 
-// Tiles of a causal unit see more tokens the later they come.  They take turns from both ends, so that any two neighbours see as many as
-// others, and the mean stands for each.
-__device__ __forceinline__ int tile_at(int turn, int tiles) { return turn & 1 ? turn >> 1 : tiles - 1 - (turn >> 1); }
-__device__ __forceinline__ int turn_of(int tile, int tiles) { return tile < tiles / 2 ? 2 * tile + 1 : 2 * (tiles - 1 - tile); }
-
-// Cost of each run of a unit, in blocks of 64 << coarse tokens.
-__device__ __forceinline__ int run_cost(const Unit& u, bool steps, int coarse) {
-  const int mean = steps ? max(1, u.len - (u.ntok - 1) / 2) : u.len;
-  return u.len == 0 || u.ntok == 0 ? 0 : static_cast<int>(((static_cast<int64_t>(mean) + 63) >> 6 >> coarse) + kRunCost);
+// A unit's tokens up to the last that a tile sees: those of causal tiles rise.
+__device__ __forceinline__ int end_of(const Unit& u, bool steps, const Args& a, int tile, int rows) {
+  const int last = (min(u.ntok * a.share, (tile + 1) * rows) - 1) / a.by_share;
+  return steps ? max(0, min(u.len, u.len - u.ntok + 1 + last)) : u.len;
+}
+// Costs are blocks of 64 << coarse tokens: of a run that ends at `end`, of all runs of one key head, and of the tiles in front of one.
+__device__ __forceinline__ int run_cost(int end, const Args& a) { return ((end + 63) >> 6 >> a.coarse) + kRunCost; }
+__device__ __forceinline__ int tiles_cost(const Unit& u, bool steps, const Args& a, int tiles, int rows) {
+  if (!steps || tiles <= 1) return tiles * run_cost(end_of(u, steps, a, 0, rows), a);
+  int c = 0;
+  for (int i = 0; i < tiles; ++i) c += run_cost(end_of(u, true, a, i, rows), a);
+  return c;
+}
+__device__ __forceinline__ int head_cost(const Unit& u, bool steps, const Args& a, int rows) {
+  return u.len == 0 || u.ntok == 0 ? 0 : tiles_cost(u, steps, a, tiles_of(u.ntok, a.share, rows), rows);
 }
 
 // Where a run of `cost` over tokens 0 .. end - 1 is cut: the token that stands at `at` of its cost.
@@ -146,7 +152,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
   for (int u = u0; u < u1; ++u) {
     const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
     if (u < kCachedUnits) S.cache[u] = x;
-    mine += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * run_cost(x, a.causal && u >= kv.n_group, a.coarse) * kv.Hk;
+    mine += head_cost(x, a.causal && u >= kv.n_group, a, u < kv.n_group ? RP : RO) * kv.Hk;
   }
   int sum = mine;      // of the threads up to this one
 #pragma unroll
@@ -180,9 +186,9 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
     for (int u = u0; u < u1; ++u) {
       Unit x{0, 0, 0, 0};
       if (!none) x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-      const int c = run_cost(x, a.causal && u >= kv.n_group, a.coarse);
-      a.units[u] = make_int4(base, c, x.tok0, x.ntok);
-      base += tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * c * kv.Hk;
+      const int c = head_cost(x, a.causal && u >= kv.n_group, a, u < kv.n_group ? RP : RO);
+      a.units[u] = make_int4(base, x.len, x.tok0, x.ntok);
+      base += c * kv.Hk;
     }
     if (tid == 0) a.units[n] = make_int4(share, total, none, 0);
   }
@@ -190,7 +196,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
     int base = first, u = u0;
     for (;; ++u) {
       const Unit x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-      const int c = tiles_of(x.ntok, a.share, u < kv.n_group ? RP : RO) * kv.Hk * run_cost(x, a.causal && u >= kv.n_group, a.coarse);
+      const int c = head_cost(x, a.causal && u >= kv.n_group, a, u < kv.n_group ? RP : RO) * kv.Hk;
       if (at < base + c) break;
       base += c;
     }
@@ -200,6 +206,75 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
   __syncthreads();
   return Share{w, at, min(total, at + share)};
 }
+
+// The runs of a workgroup's share, one after the other: everything in it is uniform.
+template <int RP, int RO>
+struct Runs {
+  const KvView& kv;
+  const Args& a;
+  const Schedule& S;
+  int number, at, stop;      // of the workgroup; the cost at hand, the end of its share
+  int u, base, unit_stop;    // the unit, the costs in front of it and of the share in it
+  Unit x;
+  bool own, steps;
+  int rows, tiles, hk, tile, run0, cost;
+
+  __device__ __forceinline__ Runs(const KvView& kv_, const Args& a_, const Schedule& S_, const Share& mine)
+      : kv(kv_), a(a_), S(S_), number(mine.number), at(mine.at), stop(mine.stop) {
+    if (!valid()) return;
+    u = __builtin_amdgcn_readfirstlane(S.unit);
+    base = __builtin_amdgcn_readfirstlane(S.base);
+    const int head = enter();
+    hk = (at - base) / head;
+    run0 = base + hk * head;
+    tile = 0;
+    if (!steps) {
+      tile = (at - run0) / cost;
+      run0 += tile * cost;
+    }
+    for (; at >= run0 + cost; cost = run_cost(end_of(x, steps, a, ++tile, rows), a)) run0 += cost;
+  }
+  __device__ __forceinline__ bool valid() const { return at < stop; }
+  __device__ __forceinline__ int from() const { return at - run0; }                      // the part of the run's cost
+  __device__ __forceinline__ int to() const { return min(unit_stop, run0 + cost) - run0; }
+
+  __device__ __forceinline__ void next() {
+    at = min(unit_stop, run0 + cost);
+    if (!valid()) return;
+    run0 += cost;
+    if (++tile == tiles) {
+      tile = 0;
+      ++hk;
+    }
+    while (at >= unit_stop) {
+      base = unit_stop;
+      ++u;
+      enter();
+      hk = tile = 0;
+      run0 = base;
+    }
+    cost = run_cost(end_of(x, steps, a, tile, rows), a);
+  }
+
+ private:
+  __device__ __forceinline__ int enter() {      // unit u, first run; returns the cost of a key head
+    int error = 0;
+    bool falls = false;
+    x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
+    x.tok0 = __builtin_amdgcn_readfirstlane(x.tok0);
+    x.ntok = __builtin_amdgcn_readfirstlane(x.ntok);
+    x.len = __builtin_amdgcn_readfirstlane(x.len);
+    x.row = __builtin_amdgcn_readfirstlane(x.row);
+    own = u >= kv.n_group;
+    steps = own && a.causal;
+    rows = own ? RO : RP;
+    tiles = tiles_of(x.ntok, a.share, rows);
+    const int head = head_cost(x, steps, a, rows);
+    unit_stop = min(stop, base + head * kv.Hk);
+    cost = run_cost(end_of(x, steps, a, 0, rows), a);
+    return head;
+  }
+};
 
 // What a lane (m, g) = (lane & 15, lane >> 4) holds of a tile of TOK tokens.
 //   bf16: K elements 32 c + 8 g .. + 7 of tokens m and 16 + m; V elements 128 b + 8 m .. + 7 (64-wide heads: 4 m .. + 3) of the tokens
@@ -240,19 +315,19 @@ struct Lds {
   float slab[4][16][128 + 4];
 };
 
-// Costs `from` to `to` of run `run` (key head, tile) of unit u: a part of each of its rows.
+// Costs cost0 to cost1 of the run of a tile of unit u's rows for one key head: a part of each row.
 template <typename T, int D, int NR, bool EXACT>
-__device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
+__device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit& u, bool own, int hk, int tile, int cost, int cost0, int cost1, int group) {
   typedef Shape<T, D> Z;
   constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, R = 16 * NR;
   constexpr bool kBf16 = sizeof(T) == 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
-  const int rows = u.ntok * a.share, tiles = tiles_of(u.ntok, a.share, R), hk = run / tiles, tile = tile_at(run - hk * tiles, tiles), r0 = tile * R;
+  const int rows = u.ntok * a.share, r0 = tile * R;
   const int dim = EXACT ? D : kv.D;
   // A causal query sees the own tokens in front of `first + its number among the new tokens`.
   const bool steps = own && a.causal;
   const int first = u.len - u.ntok + 1;
-  const int last_tok = (min(rows, r0 + R) - 1) / a.by_share, first_tok = r0 / a.by_share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
+  const int first_tok = r0 / a.by_share, end = end_of(u, steps, a, tile, R);
   const int k0 = cut(cost0, cost, end), k1 = cut(cost1, cost, end), all_see = steps ? first + first_tok : k1;
 
   typename Z::KV q[NR][KC];
@@ -536,50 +611,43 @@ __device__ __forceinline__ int swizzle_k(int r) { return D == 128 ? r & 15 : (r 
 template <int D>
 __device__ __forceinline__ int swizzle_v(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
 
-template <int D>
-__device__ void attend_wide(const KvView& kv, const Args& a, WideLds& lds, char* tiles_lds, const Unit& u, bool own, int run, int cost, int cost0, int cost1,
-                            int group) {
-  constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 31, g = lane >> 5;
-  const int rows = u.ntok * a.share, tiles = tiles_of(u.ntok, a.share, kWideRows), hk = run / tiles, tile = tile_at(run - hk * tiles, tiles);
-  const int r0 = tile * kWideRows;
-  const bool steps = own && a.causal;
-  const int first = u.len - u.ntok + 1;
-  const int last_tok = (min(rows, r0 + kWideRows) - 1) / a.by_share, end = steps ? max(0, min(u.len, first + last_tok)) : u.len;
-  const int k0 = cut(cost0, cost, end), k1 = cut(cost1, cost, end);
-  const int r = r0 + 32 * wave + m, tq = min(r, rows - 1) / a.by_share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
-  const int limit = steps ? min(k1, first + tq) : k1;
-  const int all_see = steps ? first + min(r0 + 32 * wave, rows - 1) / a.by_share : k1;      // a wavefront's first row sees least
+// A run of a wide tile.
+struct WideRun {
+  int hk, r0, k0, k1;
+};
+template <typename R>
+__device__ __forceinline__ WideRun wide_run(const R& r, const Args& a) {
+  const int end = end_of(r.x, r.steps, a, r.tile, kWideRows);
+  return WideRun{r.hk, r.tile * kWideRows, cut(r.from(), r.cost, end), cut(r.to(), r.cost, end)};
+}
 
-  uint4 q[KC];
-  const bf16_t* from_q = static_cast<const bf16_t*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
-#pragma unroll
-  for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const uint4*>(from_q + 16 * c + 8 * g);
-  const float to_log2 = a.scale * kLog2e;
-  f32x16 acc[DT];
-#pragma unroll
-  for (int t = 0; t < DT; ++t)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
-  float top = -INFINITY, ref = 0.f, sum = 0.f;
+template <int D>
+__global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
+  constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES;
+  extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
+  WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * TB);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 31, g = lane >> 5;
+  const Share mine = make_schedule<kWideRows, kWideRows>(kv, a, lds.S);
+  Runs<kWideRows, kWideRows> run(kv, a, lds.S, mine);
+  if (!run.valid()) return;
 
   // where this lane reads: K piece 2 c + g of row m (XOR 32 c), V four elements of row 4 g + (lane & 15) / 4 (XOR 64 t)
   const int read_k = m * (2 * D) + ((g ^ swizzle_k<D>(m)) << 4);
   const int i16 = lane & 15, row_v = 4 * g + (i16 >> 2);
   const int read_v = row_v * (2 * D) + (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ swizzle_v<D>(row_v)) << 4) + (i16 & 1) * 8;
-
-  const int32_t* const table = own ? kv.pages + static_cast<int64_t>(u.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(u.row) * kv.max_prefix_pages;
-  const int64_t page_step = (static_cast<int64_t>(kv.Hk) * D) << kv.page_shift;
+  const float to_log2 = a.scale * kLog2e;
+  const uint32_t page_bytes = (static_cast<uint32_t>(kv.Hk) * D * 2) << kv.page_shift;      // of all heads
   const int in_page = (1 << kv.page_shift) - 1;
-  const bf16_t* const kbase = static_cast<const bf16_t*>(kv.k) + ((static_cast<int64_t>(hk) * D) << kv.page_shift);
-  const bf16_t* const vbase = static_cast<const bf16_t*>(kv.v) + ((static_cast<int64_t>(hk) * D) << kv.page_shift);
-  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr32(tiles_lds)) + wave * NL * 1024;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr32(smem)) + wave * NL * 1024;
 
-  for (int from = k0; from < k1;) {
-    const int page0 = from >> kv.page_shift, to = min(k1, (page0 + kPageSlots) << kv.page_shift);
-    const int n_slots = ((to - 1) >> kv.page_shift) - page0 + 1;
+  // Page ids of tokens page0 << page_shift .. in LDS: a unit's all, where they fit, for all its runs.
+  int page0 = 0, staged = -1;
+  bool holes = false;
+  auto stage = [&](const int32_t* table, int first_token, int to) {
+    page0 = first_token >> kv.page_shift;
+    const int n_slots = to > first_token ? ((to - 1) >> kv.page_shift) - page0 + 1 : 0;
     bool missing = false;
-    __syncthreads();
+    lds_barrier();
     for (int i = tid; i < n_slots; i += 256) {
       int id = table[page0 + i];
       if (static_cast<unsigned>(id) >= static_cast<unsigned>(kv.n_pages)) {
@@ -588,146 +656,214 @@ __device__ void attend_wide(const KvView& kv, const Args& a, WideLds& lds, char*
       }
       lds.pages[i] = id;
     }
-    const bool holes = __syncthreads_or(missing);
     if (missing) raise_data_error(a.data_error, AT_GRPO_DATA_PAGE);
+    holes = __syncthreads_or(missing);
+  };
+  // A tile of tokens t .. into a buffer; rows behind the last token are the last.
+  auto request = [&](int hk, int t, int to, int buffer) {
+    const char* const kbase = static_cast<const char*>(kv.k) + ((static_cast<int64_t>(hk) * D * 2) << kv.page_shift);
+    const char* const vbase = static_cast<const char*>(kv.v) + ((static_cast<int64_t>(hk) * D * 2) << kv.page_shift);
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+      const int row = (wave * NL + i) * LROWS + lane / PIECES, piece = lane & (PIECES - 1), token = min(t + row, to - 1);
+      const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(max(0, lds.pages[(token >> kv.page_shift) - page0]))) * page_bytes;
+      const uint32_t in = static_cast<uint32_t>(token & in_page) * (2 * D);
+      direct_load_v(kbase + (at + (in + 16 * (piece ^ swizzle_k<D>(row)))), lds0 + buffer * 2 * TB + i * 1024);
+      direct_load_v(vbase + (at + (in + 16 * (piece ^ swizzle_v<D>(row)))), lds0 + buffer * 2 * TB + TB + i * 1024);
+    }
+  };
+  uint4 q[KC];
+  auto load_q = [&](const Unit& x, const WideRun& w) {
+    const int r = min(w.r0 + 32 * wave + m, x.ntok * a.share - 1), tq = r / a.by_share, h = w.hk * a.share + r - tq * a.share;
+    const bf16_t* from = static_cast<const bf16_t*>(a.q.data) + (x.tok0 + tq) * a.q.ts + h * a.q.hs + 8 * g;
+#pragma unroll
+    for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const uint4*>(from + 16 * c);
+  };
+  auto table_of = [&]() {
+    return run.own ? kv.pages + static_cast<int64_t>(run.x.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(run.x.row) * kv.max_prefix_pages;
+  };
 
-    auto request = [&](int t, int buffer) {      // rows behind the last are the last
+  int buffer = 0;
+  bool requested = false;      // the run's first tile, by the run in front of it
+  WideRun w = wide_run(run, a);
+  load_q(run.x, w);
+  for (;;) {
+    const Unit u = run.x;
+    const bool steps = run.steps, own = run.own, fits = ((u.len - 1) >> kv.page_shift) < kPageSlots;
+    const int rows = u.ntok * a.share, r = w.r0 + 32 * wave + m, tq = min(r, rows - 1) / a.by_share, h = w.hk * a.share + min(r, rows - 1) - tq * a.share;
+    const int first = u.len - u.ntok + 1, k1 = w.k1;      // a causal query sees the own tokens in front of `first + its number among the new tokens`
+    const int limit = steps ? min(k1, first + tq) : k1;
+    const int all_see = steps ? first + min(w.r0 + 32 * wave, rows - 1) / a.by_share : k1;      // a wavefront's first row sees least
+    const bool direct = kv.n_group == 0 && run.from() == 0 && run.to() == run.cost, first_part = run.from() == 0;
+    const int group = run.number;
+    if (fits && staged != run.u) {
+      stage(table_of(), 0, u.len);
+      staged = run.u;
+    }
+    f32x16 acc[DT];
 #pragma unroll
-      for (int i = 0; i < NL; ++i) {
-        const int row = (wave * NL + i) * LROWS + lane / PIECES, piece = lane & (PIECES - 1), token = min(t + row, to - 1);
-        const int id = max(0, lds.pages[(token >> kv.page_shift) - page0]);
-        const int64_t at = id * page_step + static_cast<int64_t>(token & in_page) * D;
-        direct_load_v(reinterpret_cast<const char*>(kbase + at + 8 * (piece ^ swizzle_k<D>(row))), lds0 + buffer * 2 * TB + i * 1024);
-        direct_load_v(reinterpret_cast<const char*>(vbase + at + 8 * (piece ^ swizzle_v<D>(row))), lds0 + buffer * 2 * TB + TB + i * 1024);
-      }
-    };
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
+    float top = -INFINITY, ref = 0.f, sum = 0.f;
 
-    int buffer = 0;
-    request(from, 0);
-    for (int t = from; t < to; t += kWideTok, buffer ^= 1) {
-      asm volatile("" ::: "memory");
-      wait_loads_but<0>();
-      __builtin_amdgcn_s_barrier();
-      asm volatile("" ::: "memory");
-      if (t + kWideTok < to) request(t + kWideTok, buffer ^ 1);
-      const char* const kt = tiles_lds + buffer * 2 * TB;
-      char* const vt = tiles_lds + buffer * 2 * TB + TB;
-      if (holes) {      // what stands for a token of no page must not be NaN
-        for (int i = tid; i < kWideTok * PIECES; i += 256) {
-          const int token = t + i / PIECES;
-          if (token < to && lds.pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
-        }
-        __syncthreads();
+    for (int from = w.k0; from < k1;) {
+      int to = k1;
+      if (!fits) {
+        to = min(k1, ((from >> kv.page_shift) + kPageSlots) << kv.page_shift);
+        stage(table_of(), from, to);
+        staged = -1;
       }
-      f32x16 s[2];
-#pragma unroll
-      for (int y = 0; y < 2; ++y)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
-#pragma unroll
-      for (int c = 0; c < KC; ++c)
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          const bf16x8 kf = *reinterpret_cast<const bf16x8*>(kt + (read_k ^ (c << 5)) + y * 32 * 2 * D);
-          s[y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, __builtin_bit_cast(bf16x8, q[c]), s[y], 0, 0, 0);
+      if (!requested) request(w.hk, from, to, buffer);
+      requested = false;
+      for (int t = from; t < to; t += kWideTok, buffer ^= 1) {
+        asm volatile("" ::: "memory");
+        wait_loads_but<0>();
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        if (t + kWideTok < to) request(w.hk, t + kWideTok, to, buffer ^ 1);
+        const char* const kt = smem + buffer * 2 * TB;
+        char* const vt = smem + buffer * 2 * TB + TB;
+        if (holes) {      // what stands for a token of no page must not be NaN
+          for (int i = tid; i < kWideTok * PIECES; i += 256) {
+            const int token = t + i / PIECES;
+            if (token < to && lds.pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
+          }
+          __syncthreads();
         }
-      if (t + kWideTok > min(to, all_see) || holes) {
+        f32x16 s[2];
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int b = 0; b < 4; ++b) {      // four tokens that start at a multiple of four share a page
-            const int t4 = t + 32 * y + 8 * b + 4 * g;
-            int left = limit - t4;
-            if (holes) left = lds.pages[(min(t4, to - 1) >> kv.page_shift) - page0] < 0 ? 0 : left;
+          for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
+        // Fragments are read a group ahead of the products that take them: left to itself the compiler reads each right in front of its own,
+        // and every product waits for LDS (103 us for eight prompts of up to 2048 tokens, so NOWUS).
+        bf16x8 f[2][4];
+        auto read_k_group = [&](int x) {      // two steps of 16 elements, two blocks of 32 tokens
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[y][4 * b + i] = i < left ? s[y][4 * b + i] : -INFINITY;
+          for (int i = 0; i < 4; ++i) f[x & 1][i] = *reinterpret_cast<const bf16x8*>(kt + (read_k ^ ((2 * x + (i >> 1)) << 5)) + (i & 1) * 32 * 2 * D);
+        };
+        read_k_group(0);
+#pragma unroll
+        for (int x = 0; x < KC / 2; ++x) {
+          if (x + 1 < KC / 2) read_k_group(x + 1);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 1][i], __builtin_bit_cast(bf16x8, q[2 * x + (i >> 1)]), s[i & 1], 0, 0, 0);
+        }
+        auto read_v_group = [&](int ks) {      // 16 tokens, all blocks of 32 elements
+#pragma unroll
+          for (int x = 0; x < DT; ++x) {
+            const char* p = vt + (read_v ^ (x << 6)) + ks * 16 * 2 * D;
+            const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 8 * 2 * D);
+            f[ks & 1][x] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
           }
-      }
-      float high = -INFINITY;
+        };
+        read_v_group(0);
+        if (t + kWideTok > min(to, all_see) || holes) {
 #pragma unroll
-      for (int y = 0; y < 2; ++y)
+          for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) high = fmaxf(high, s[y][i]);
-      high *= to_log2;
-      if (__any(high > top + kSlack)) {
-        high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
-        const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top - now);
-        top = high;
-        ref = now;
-        sum *= keep;
+            for (int b = 0; b < 4; ++b) {      // four tokens that start at a multiple of four share a page
+              const int t4 = t + 32 * y + 8 * b + 4 * g;
+              int left = limit - t4;
+              if (holes) left = lds.pages[(min(t4, to - 1) >> kv.page_shift) - page0] < 0 ? 0 : left;
 #pragma unroll
-        for (int x = 0; x < DT; ++x) acc[x] *= keep;
-      }
-      uint4 w[4];
-#pragma unroll
-      for (int ks = 0; ks < 4; ++ks) {
-        float p[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[j] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + j], to_log2, -ref));
-          sum += p[j];
+              for (int i = 0; i < 4; ++i) s[y][4 * b + i] = i < left ? s[y][4 * b + i] : -INFINITY;
+            }
         }
-        w[ks] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-      }
+        float high = -INFINITY;
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks)
+        for (int y = 0; y < 2; ++y)
 #pragma unroll
-        for (int x = 0; x < DT; ++x) {
-          const char* p = vt + (read_v ^ (x << 6)) + ks * 16 * 2 * D;
-          const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 8 * 2 * D);
-          acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y)), __builtin_bit_cast(bf16x8, w[ks]),
-                                                           acc[x], 0, 0, 0);
+          for (int i = 0; i < 16; ++i) high = fmaxf(high, s[y][i]);
+        high *= to_log2;
+        if (__any(high > top + kSlack)) {
+          high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
+          const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top - now);
+          top = high;
+          ref = now;
+          sum *= keep;
+#pragma unroll
+          for (int x = 0; x < DT; ++x) acc[x] *= keep;
         }
+        uint4 w[2];
+        auto weigh = [&](int ks) {
+          float p[8];
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            p[j] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + j], to_log2, -ref));
+            sum += p[j];
+          }
+          w[ks & 1] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+        };
+        weigh(0);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+          __builtin_amdgcn_sched_barrier(0);
+          if (ks < 3) {      // the next tokens' weights are computed between this step's products
+            read_v_group(ks + 1);
+            weigh(ks + 1);
+          }
+#pragma unroll
+          for (int x = 0; x < DT; ++x) acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[ks & 1][x], __builtin_bit_cast(bf16x8, w[ks & 1]), acc[x], 0, 0, 0);
+          if (ks < 3) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * DT, 0);      // LDS reads, then a product and some of the weights in turn
+#pragma unroll
+            for (int x = 0; x < DT; ++x) {
+              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+              __builtin_amdgcn_sched_group_barrier(0x402, 28 / DT, 0);
+            }
+          }
+        }
+      }
+      from = to;
     }
-    from = to;
-  }
 
-  sum += __shfl_xor(sum, 32, 64);
-  if (r >= rows) return;
-  const float f = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), x = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
-  const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h;
-  if (kv.n_group == 0 && cost0 == 0 && cost1 == cost) {
-    if (a.lse && g == 0) a.lse[by_query] = x;
-    bf16_t* to = static_cast<bf16_t*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 4 * g;
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        *reinterpret_cast<uint2*>(to + 32 * t + 2 * i) = make_uint2(pack_bf16x2(acc[t][i] * f, acc[t][i + 1] * f), pack_bf16x2(acc[t][i + 2] * f, acc[t][i + 3] * f));
-  } else {
-    const int64_t part = cost0 == 0 ? by_query : static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1) + static_cast<int64_t>(group) * kMaxRows + (r - r0);
-    if (g == 0) a.part_lse[part] = x;
-    float* to = a.part_out + part * D + 4 * g;
-#pragma unroll
-    for (int t = 0; t < DT; ++t)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) *reinterpret_cast<f32x4*>(to + 32 * t + 2 * i) = f32x4{acc[t][i] * f, acc[t][i + 1] * f, acc[t][i + 2] * f, acc[t][i + 3] * f};
-  }
-}
-
-// A workgroup's share: f(unit, whether it is a sequence's own tokens, run, cost of the run, the part of that cost, number of the workgroup)
-template <int RP, int RO, typename F>
-__device__ __forceinline__ void for_share(const KvView& kv, const Args& a, Schedule& S, F f) {
-  const Share mine = make_schedule<RP, RO>(kv, a, S);
-  if (mine.at >= mine.stop) return;
-  int at = mine.at, u = __builtin_amdgcn_readfirstlane(S.unit), base = __builtin_amdgcn_readfirstlane(S.base);
-  while (at < mine.stop) {
-    int error = 0;
-    bool falls = false;
-    Unit x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-    x.tok0 = __builtin_amdgcn_readfirstlane(x.tok0);
-    x.ntok = __builtin_amdgcn_readfirstlane(x.ntok);
-    x.len = __builtin_amdgcn_readfirstlane(x.len);
-    x.row = __builtin_amdgcn_readfirstlane(x.row);
-    const bool own = u >= kv.n_group;
-    const int cost = run_cost(x, own && a.causal, a.coarse), all = tiles_of(x.ntok, a.share, own ? RO : RP) * kv.Hk * cost;
-    while (at < min(mine.stop, base + all)) {
-      const int run = (at - base) / cost, run0 = base + run * cost, to = min(mine.stop, run0 + cost);
-      f(x, own, run, cost, at - run0, to - run0, mine.number);
-      at = to;
+    // The next run's queries and first tile come while this one's rows are written.  Its buffer is free: who has passed the last tile's
+    // barrier has read the tile in front of that.
+    run.next();
+    const bool more = run.valid();
+    const WideRun before = w;
+    if (more) {
+      w = wide_run(run, a);
+      if (run.u == staged && w.k0 < w.k1) {
+        request(w.hk, w.k0, w.k1, buffer);
+        requested = true;
+      }
+      load_q(run.x, w);
     }
-    base += all;
-    ++u;
+    sum += __shfl_xor(sum, 32, 64);
+    if (r < rows) {
+      const float f = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), x = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+      const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h;
+      if (direct) {
+        if (a.lse && g == 0) a.lse[by_query] = x;
+        // two lanes have 8 bytes each of a row's 16: they exchange them for those of the next 16
+        bf16_t* to = static_cast<bf16_t*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 8 * g;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; i += 8) {
+            uint32_t p[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) p[j] = pack_bf16x2(acc[t][i + 2 * j] * f, acc[t][i + 2 * j + 1] * f);
+            const auto lo = __builtin_amdgcn_permlane32_swap(p[0], p[2], false, false), hi = __builtin_amdgcn_permlane32_swap(p[1], p[3], false, false);
+            *reinterpret_cast<uint4*>(to + 32 * t + 2 * i) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+          }
+      } else {
+        const int64_t part = first_part ? by_query : static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1) + static_cast<int64_t>(group) * kMaxRows + (r - before.r0);
+        if (g == 0) a.part_lse[part] = x;
+        float* to = a.part_out + part * D + 4 * g;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<f32x4*>(to + 32 * t + 2 * i) = f32x4{acc[t][i] * f, acc[t][i + 1] * f, acc[t][i + 2] * f, acc[t][i + 3] * f};
+      }
+    }
+    if (!more) break;
   }
 }
 
@@ -738,19 +874,11 @@ constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
 template <typename T, int D, int NRP, int NRO, bool EXACT>
 __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
   __shared__ Lds lds;
-  for_share<16 * NRP, 16 * NRO>(kv, a, lds.S, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
-    if (own) attend_run<T, D, NRO, EXACT>(kv, a, lds, u, true, run, cost, cost0, cost1, group);
-    else attend_run<T, D, NRP, EXACT>(kv, a, lds, u, false, run, cost, cost0, cost1, group);
-  });
-}
-
-template <int D>
-__global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
-  extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
-  WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * kWideTok * D * 2);
-  for_share<kWideRows, kWideRows>(kv, a, lds.S, [&](const Unit& u, bool own, int run, int cost, int cost0, int cost1, int group) {
-    attend_wide<D>(kv, a, lds, smem, u, own, run, cost, cost0, cost1, group);
-  });
+  const Share mine = make_schedule<16 * NRP, 16 * NRO>(kv, a, lds.S);
+  for (Runs<16 * NRP, 16 * NRO> r(kv, a, lds.S, mine); r.valid(); r.next()) {
+    if (r.own) attend_run<T, D, NRO, EXACT>(kv, a, lds, r.x, true, r.hk, r.tile, r.cost, r.from(), r.to(), r.number);
+    else attend_run<T, D, NRP, EXACT>(kv, a, lds, r.x, false, r.hk, r.tile, r.cost, r.from(), r.to(), r.number);
+  }
 }
 
 // ---- joining the parts --------------------------------------------------------------------------------
@@ -782,10 +910,15 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int
   const int4 of_p = in_group ? a.units[g] : make_int4(0, 0, 0, 0), of_o = in_seq ? a.units[kv.n_group + s] : make_int4(0, 0, 0, 0);
   int group0[2], count[2], row[2];      // the run's first workgroup, its workgroups, the row in its tile
   auto look_up = [&](int which, const int4& x, int rows) {
-    const int q = t - x.z, tiles = max(1, tiles_of(x.w, a.share, rows)), r = q * a.share + h - hk * a.share, tile = r / rows;
-    const int run0 = x.x + (hk * tiles + turn_of(tile, tiles)) * x.y;
+    group0[which] = count[which] = row[which] = 0;
+    const int q = t - x.z;
+    if (x.y == 0 || q < 0 || q >= x.w) return;
+    const Unit of{x.z, x.w, x.y, 0};
+    const bool steps = which && a.causal;
+    const int r = q * a.share + h - hk * a.share, tile = r / rows;
+    const int run0 = x.x + hk * head_cost(of, steps, a, rows) + tiles_cost(of, steps, a, tile, rows), run1 = run0 + run_cost(end_of(of, steps, a, tile, rows), a);
     group0[which] = run0 / share;
-    count[which] = x.y == 0 || q < 0 || q >= x.w ? 0 : (run0 + x.y - 1) / share - group0[which] + 1;
+    count[which] = (run1 - 1) / share - group0[which] + 1;
     row[which] = r - tile * rows;
   };
   look_up(0, of_p, rows_p);
@@ -894,7 +1027,7 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
     for (int t = t1 + first; t < a.n_tok; t += step) clear_token<T>(a, D, t);
     for (int s = first; s < kv.n_seq; s += step) {
       const int4 of = a.units[s];
-      for (int t = of.z; of.y == 0 && t < of.z + of.w; ++t) clear_token<T>(a, D, t);
+      for (int t = of.z; of.y == 0 && t < of.z + of.w; ++t) clear_token<T>(a, D, t);      // nothing to see
     }
     return;
   }
@@ -909,10 +1042,17 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
     n = min(step, n - (max(c, 1) - 1) * step);
   }
   const int4 of = a.units[u];
-  const int run = (x - of.x) / of.y, run0 = of.x + run * of.y;
+  const Unit unit{of.z, of.w, of.y, 0};
+  const int head = head_cost(unit, a.causal, a, rows_o), hk = (x - of.x) / head;
+  int run0 = of.x + hk * head, tile = 0, cost = run_cost(end_of(unit, a.causal, a, 0, rows_o), a);
+  if (!a.causal) {
+    tile = (x - run0) / cost;
+    run0 += tile * cost;
+  }
+  for (; x >= run0 + cost; cost = run_cost(end_of(unit, a.causal, a, ++tile, rows_o), a)) run0 += cost;
   if (run0 == x || run0 / share != w - 1) return;
-  const int rows = of.w * a.share, tiles = tiles_of(of.w, a.share, rows_o), hk = run / tiles, r0 = tile_at(run - hk * tiles, tiles) * rows_o;
-  const int n = (run0 + of.y - 1) / share - w + 2;      // parts
+  const int rows = of.w * a.share, r0 = tile * rows_o;
+  const int n = (run0 + cost - 1) / share - w + 2;      // parts
   const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
   for (int i = blockIdx.y * 16 + (threadIdx.x >> 4); i < rows_o && r0 + i < rows; i += gridDim.y * 16) {
     const int tq = (r0 + i) / a.by_share, h = hk * a.share + r0 + i - tq * a.share;
