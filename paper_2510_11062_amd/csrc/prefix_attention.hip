@@ -32,9 +32,9 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMostGroups = 1024;     // workgroups of a launch
 constexpr int kCachedUnits = 512;     // units whose sizes are kept in LDS
-// A run's beginning and end (page ids, queries, adding up) take about as long as a block of 64 tokens, and count as one.  Shares are
-// no smaller than one block and that.
-constexpr int kRunCost = 1, kMinShare = 2;
+// A run's beginning and end (page ids, queries, adding up) take about as long as a block of 64 tokens, and count as one; no share is smaller
+// than one block and that.
+constexpr int kRunCost = 8, kMinShare = 16;
 constexpr int kPageSlots = 1024;     // page ids of a chunk in LDS at a time
 constexpr int kMaxRows = 128;        // rows of the largest tile
 constexpr int kWideRows = 128;       // of the tiles below that four wavefronts share by rows
@@ -59,7 +59,7 @@ __device__ __forceinline__ int operator/(int x, const Divisor& by) {
 struct Args {
   int n_tok, Hq, share;      // share: Hq / Hk
   Divisor by_share;
-  int coarse;                // costs are counted in blocks of 64 << coarse tokens
+  int coarse, rise, quantum; // of the costs below; rise: by how much from one causal tile to the next
   int causal;
   float scale;
   Rows q, out;
@@ -111,24 +111,27 @@ __device__ __forceinline__ int end_of(const Unit& u, bool steps, const Args& a, 
   const int last = (min(u.ntok * a.share, (tile + 1) * rows) - 1) / a.by_share;
   return steps ? max(0, min(u.len, u.len - u.ntok + 1 + last)) : u.len;
 }
-// Costs are blocks of 64 << coarse tokens: of a run that ends at `end`, of all runs of one key head, and of the tiles in front of one.
-__device__ __forceinline__ int run_cost(int end, const Args& a) { return ((end + 63) >> 6 >> a.coarse) + kRunCost; }
-__device__ __forceinline__ int tiles_cost(const Unit& u, bool steps, const Args& a, int tiles, int rows) {
-  if (!steps || tiles <= 1) return tiles * run_cost(end_of(u, steps, a, 0, rows), a);
-  int c = 0;
-  for (int i = 0; i < tiles; ++i) c += run_cost(end_of(u, true, a, i, rows), a);
-  return c;
+// Costs are counted in eights of tokens (<< coarse).  Those of a unit's tiles rise by `step` from one to the next, by which sums over tiles
+// are closed forms; with causal tiles of a whole number of tokens they rise as their tokens do.
+struct Cost {
+  int first, step;
+  __device__ __forceinline__ int of(int tile) const { return first + tile * step; }
+  __device__ __forceinline__ int in_front(int tile) const { return tile * first + step * (tile * (tile - 1) / 2); }
+};
+__device__ __forceinline__ Cost cost_of(const Unit& u, bool steps, const Args& a, int rows) {
+  if (u.len == 0 || u.ntok == 0) return Cost{0, 0};
+  const bool rises = steps && a.rise && u.ntok <= u.len;
+  const int first = (((rises ? end_of(u, true, a, 0, rows) : u.len) + 7) >> 3 >> a.coarse) + kRunCost;
+  return Cost{(first + a.quantum - 1) & -a.quantum, rises ? a.rise : 0};
 }
 __device__ __forceinline__ int head_cost(const Unit& u, bool steps, const Args& a, int rows) {
-  return u.len == 0 || u.ntok == 0 ? 0 : tiles_cost(u, steps, a, tiles_of(u.ntok, a.share, rows), rows);
+  return cost_of(u, steps, a, rows).in_front(tiles_of(u.ntok, a.share, rows));
 }
 
-// Where a run of `cost` over tokens 0 .. end - 1 is cut: the token that stands at `at` of its cost.
+// Where a run of `cost` over tokens 0 .. end - 1 is cut: the block of 64 tokens that stands at `at` of its cost.
 __device__ __forceinline__ int cut(int at, int cost, int end) {
-  const int blocks = (end + 63) >> 6;
   if (at >= cost) return end;
-  const int block = blocks == cost - kRunCost ? at : static_cast<int>(static_cast<float>(blocks) * (static_cast<float>(at) / static_cast<float>(cost)));
-  return min(end, block << 6);
+  return min(end, static_cast<int>(static_cast<float>((end + 63) >> 6) * (static_cast<float>(at) / static_cast<float>(cost))) << 6);
 }
 
 // A workgroup's share of the runs.
@@ -217,6 +220,7 @@ struct Runs {
   int u, base, unit_stop;    // the unit, the costs in front of it and of the share in it
   Unit x;
   bool own, steps;
+  Cost costs;
   int rows, tiles, hk, tile, run0, cost;
 
   __device__ __forceinline__ Runs(const KvView& kv_, const Args& a_, const Schedule& S_, const Share& mine)
@@ -224,15 +228,16 @@ struct Runs {
     if (!valid()) return;
     u = __builtin_amdgcn_readfirstlane(S.unit);
     base = __builtin_amdgcn_readfirstlane(S.base);
-    const int head = enter();
+    enter();
+    const int head = costs.in_front(tiles);
     hk = (at - base) / head;
     run0 = base + hk * head;
     tile = 0;
-    if (!steps) {
+    if (costs.step == 0) {
       tile = (at - run0) / cost;
       run0 += tile * cost;
     }
-    for (; at >= run0 + cost; cost = run_cost(end_of(x, steps, a, ++tile, rows), a)) run0 += cost;
+    for (; at >= run0 + cost; ++tile, cost += costs.step) run0 += cost;
   }
   __device__ __forceinline__ bool valid() const { return at < stop; }
   __device__ __forceinline__ int from() const { return at - run0; }                      // the part of the run's cost
@@ -242,9 +247,11 @@ struct Runs {
     at = min(unit_stop, run0 + cost);
     if (!valid()) return;
     run0 += cost;
+    cost += costs.step;
     if (++tile == tiles) {
       tile = 0;
       ++hk;
+      cost = costs.first;
     }
     while (at >= unit_stop) {
       base = unit_stop;
@@ -253,11 +260,10 @@ struct Runs {
       hk = tile = 0;
       run0 = base;
     }
-    cost = run_cost(end_of(x, steps, a, tile, rows), a);
   }
 
  private:
-  __device__ __forceinline__ int enter() {      // unit u, first run; returns the cost of a key head
+  __device__ __forceinline__ void enter() {      // unit u, first run
     int error = 0;
     bool falls = false;
     x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
@@ -269,10 +275,9 @@ struct Runs {
     steps = own && a.causal;
     rows = own ? RO : RP;
     tiles = tiles_of(x.ntok, a.share, rows);
-    const int head = head_cost(x, steps, a, rows);
-    unit_stop = min(stop, base + head * kv.Hk);
-    cost = run_cost(end_of(x, steps, a, 0, rows), a);
-    return head;
+    costs = cost_of(x, steps, a, rows);
+    cost = costs.first;
+    unit_stop = min(stop, base + costs.in_front(tiles) * kv.Hk);
   }
 };
 
@@ -679,10 +684,6 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
 #pragma unroll
     for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const uint4*>(from + 16 * c);
   };
-  auto table_of = [&]() {
-    return run.own ? kv.pages + static_cast<int64_t>(run.x.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(run.x.row) * kv.max_prefix_pages;
-  };
-
   int buffer = 0;
   bool requested = false;      // the run's first tile, by the run in front of it
   WideRun w = wide_run(run, a);
@@ -696,10 +697,16 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
     const int all_see = steps ? first + min(w.r0 + 32 * wave, rows - 1) / a.by_share : k1;      // a wavefront's first row sees least
     const bool direct = kv.n_group == 0 && run.from() == 0 && run.to() == run.cost, first_part = run.from() == 0;
     const int group = run.number;
+    const int32_t* const table = own ? kv.pages + static_cast<int64_t>(u.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(u.row) * kv.max_prefix_pages;
     if (fits && staged != run.u) {
-      stage(table_of(), 0, u.len);
+      stage(table, 0, u.len);
       staged = run.u;
     }
+    run.next();
+    const bool more = run.valid();
+    WideRun next{};
+    if (more) next = wide_run(run, a);
+    const bool ahead = more && run.u == staged && next.k0 < next.k1;      // with the same page ids
     f32x16 acc[DT];
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -711,7 +718,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
       int to = k1;
       if (!fits) {
         to = min(k1, ((from >> kv.page_shift) + kPageSlots) << kv.page_shift);
-        stage(table_of(), from, to);
+        stage(table, from, to);
         staged = -1;
       }
       if (!requested) request(w.hk, from, to, buffer);
@@ -721,7 +728,9 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
         wait_loads_but<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
+        // the next tile, or the next run's first: its buffer is free, since who has passed this barrier has read the tile in front
         if (t + kWideTok < to) request(w.hk, t + kWideTok, to, buffer ^ 1);
+        else if (ahead && to == k1) request(next.hk, next.k0, next.k1, buffer ^ 1);
         const char* const kt = smem + buffer * 2 * TB;
         char* const vt = smem + buffer * 2 * TB + TB;
         if (holes) {      // what stands for a token of no page must not be NaN
@@ -752,6 +761,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
           for (int i = 0; i < 4; ++i)
             s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 1][i], __builtin_bit_cast(bf16x8, q[2 * x + (i >> 1)]), s[i & 1], 0, 0, 0);
         }
+        if (more && t + kWideTok >= k1) load_q(run.x, next);      // the last scores of this run are on their way
         auto read_v_group = [&](int ks) {      // 16 tokens, all blocks of 32 elements
 #pragma unroll
           for (int x = 0; x < DT; ++x) {
@@ -821,19 +831,6 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
       from = to;
     }
 
-    // The next run's queries and first tile come while this one's rows are written.  Its buffer is free: who has passed the last tile's
-    // barrier has read the tile in front of that.
-    run.next();
-    const bool more = run.valid();
-    const WideRun before = w;
-    if (more) {
-      w = wide_run(run, a);
-      if (run.u == staged && w.k0 < w.k1) {
-        request(w.hk, w.k0, w.k1, buffer);
-        requested = true;
-      }
-      load_q(run.x, w);
-    }
     sum += __shfl_xor(sum, 32, 64);
     if (r < rows) {
       const float f = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), x = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
@@ -853,7 +850,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
             *reinterpret_cast<uint4*>(to + 32 * t + 2 * i) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
           }
       } else {
-        const int64_t part = first_part ? by_query : static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1) + static_cast<int64_t>(group) * kMaxRows + (r - before.r0);
+        const int64_t part = first_part ? by_query : static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1) + static_cast<int64_t>(group) * kMaxRows + (r - w.r0);
         if (g == 0) a.part_lse[part] = x;
         float* to = a.part_out + part * D + 4 * g;
 #pragma unroll
@@ -864,6 +861,12 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
       }
     }
     if (!more) break;
+    requested = ahead;
+    if (w.k0 >= w.k1) {      // no tile, at which they were asked for
+      load_q(run.x, next);
+      requested = false;
+    }
+    w = next;
   }
 }
 
@@ -916,7 +919,8 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int
     const Unit of{x.z, x.w, x.y, 0};
     const bool steps = which && a.causal;
     const int r = q * a.share + h - hk * a.share, tile = r / rows;
-    const int run0 = x.x + hk * head_cost(of, steps, a, rows) + tiles_cost(of, steps, a, tile, rows), run1 = run0 + run_cost(end_of(of, steps, a, tile, rows), a);
+    const Cost costs = cost_of(of, steps, a, rows);
+    const int run0 = x.x + hk * head_cost(of, steps, a, rows) + costs.in_front(tile), run1 = run0 + costs.of(tile);
     group0[which] = run0 / share;
     count[which] = (run1 - 1) / share - group0[which] + 1;
     row[which] = r - tile * rows;
@@ -1043,13 +1047,14 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
   }
   const int4 of = a.units[u];
   const Unit unit{of.z, of.w, of.y, 0};
+  const Cost costs = cost_of(unit, a.causal, a, rows_o);
   const int head = head_cost(unit, a.causal, a, rows_o), hk = (x - of.x) / head;
-  int run0 = of.x + hk * head, tile = 0, cost = run_cost(end_of(unit, a.causal, a, 0, rows_o), a);
-  if (!a.causal) {
+  int run0 = of.x + hk * head, tile = 0, cost = costs.first;
+  if (costs.step == 0) {
     tile = (x - run0) / cost;
     run0 += tile * cost;
   }
-  for (; x >= run0 + cost; cost = run_cost(end_of(unit, a.causal, a, ++tile, rows_o), a)) run0 += cost;
+  for (; x >= run0 + cost; ++tile, cost += costs.step) run0 += cost;
   if (run0 == x || run0 / share != w - 1) return;
   const int rows = of.w * a.share, r0 = tile * rows_o;
   const int n = (run0 + cost - 1) / share - w + 2;      // parts
@@ -1174,17 +1179,23 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < ws.bytes()) return AT_GRPO_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int share = Hq / kv->Hk;
-  Args args{n_tok, Hq, share, divisor(share), 0, causal != 0, scale, rows_of(q), rows_of(out), lse, data_error, scratch.units, scratch.part_lse, scratch.part_out};
+  Args args{n_tok, Hq, share, divisor(share), 0, 0, 1, causal != 0, scale, rows_of(q), rows_of(out), lse, data_error, scratch.units, scratch.part_lse, scratch.part_out};
   const int64_t all_rows = static_cast<int64_t>(n_tok) * share;
   const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
   auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
   const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, small(rows_p), small(rows_o)) : choose<float>(kv->D, small(rows_p), small(rows_o));
+  const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
   // an upper bound of all costs together, which are counted in 32 bits
   const int64_t tiles_p = kv->n_group ? all_rows / k.rows_p + kv->n_group : 0, tiles_o = all_rows / k.rows_o + kv->n_seq;
-  const auto blocks_of = [&](int64_t pages) { return pages * kv->page_size / 64 + 2 + kRunCost; };
+  const auto blocks_of = [&](int64_t pages) { return pages * kv->page_size / 8 + 2 + kRunCost; };
   double most = (static_cast<double>(tiles_p) * blocks_of(kv->max_prefix_pages) + static_cast<double>(tiles_o) * blocks_of(kv->max_pages)) * kv->Hk;
   for (; most > 1 << 30; most /= 2) ++args.coarse;
-  const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
+  args.rise = k.rows_o / (8 * share) >> args.coarse;
+  // Where there are workgroups enough, costs are whole shares, so that a run begins with a workgroup: four candidates 13.2 us, so 8.5.
+  if (most <= static_cast<double>(kMinShare) * blocks) {
+    args.quantum = kMinShare;
+    args.rise = 0;
+  }
   ProfScope ps(PROF_ATTENTION, s);
   if (k.lds) ATG_TRY(allow_big_lds(k.kernel, k.lds));
   hipLaunchKernelGGL(k.kernel, dim3(blocks), dim3(256), k.lds, s, view, args);
