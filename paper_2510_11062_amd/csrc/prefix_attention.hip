@@ -32,9 +32,8 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int kMostGroups = 1024;     // workgroups of a launch
 constexpr int kCachedUnits = 512;     // units whose sizes are kept in LDS
-// A run's beginning and end (page ids, queries, adding up) take about as long as a block of 64 tokens, and count as one; no share is smaller
-// than one block and that.
-constexpr int kRunCost = 8, kMinShare = 16;
+// A run's beginning and end (queries, first loads, adding up) take about as long as 128 tokens and count as that.
+constexpr int kRunCost = 16, kMinShare = 16;
 constexpr int kPageSlots = 1024;     // page ids of a chunk in LDS at a time
 constexpr int kMaxRows = 128;        // rows of the largest tile
 constexpr int kWideRows = 128;       // of the tiles below that four wavefronts share by rows
@@ -281,6 +280,16 @@ struct Runs {
   }
 };
 
+// A run of a tile: key head, first row, and the tokens that the workgroup has of it.
+struct TileRun {
+  int hk, r0, k0, k1;
+};
+template <typename R>
+__device__ __forceinline__ TileRun tile_run(const R& r, const Args& a) {
+  const int end = end_of(r.x, r.steps, a, r.tile, r.rows);
+  return TileRun{r.hk, r.tile * r.rows, cut(r.from(), r.cost, end), cut(r.to(), r.cost, end)};
+}
+
 // What a lane (m, g) = (lane & 15, lane >> 4) holds of a tile of TOK tokens.
 //   bf16: K elements 32 c + 8 g .. + 7 of tokens m and 16 + m; V elements 128 b + 8 m .. + 7 (64-wide heads: 4 m .. + 3) of the tokens
 //         4 g .. + 3 and 16 + 4 g .. + 3.
@@ -315,287 +324,11 @@ __device__ __forceinline__ bf16x8 transposed(const VV (&v)[8], int e) {
 
 struct Lds {
   Schedule S;
-  int pages[kPageSlots];
+  int pages[2][kPageSlots];
+  int holes[2][4];
   float ml[4][64][2];
   float slab[4][16][128 + 4];
 };
-
-// Costs cost0 to cost1 of the run of a tile of unit u's rows for one key head: a part of each row.
-template <typename T, int D, int NR, bool EXACT>
-__device__ void attend_run(const KvView& kv, const Args& a, Lds& lds, const Unit& u, bool own, int hk, int tile, int cost, int cost0, int cost1, int group) {
-  typedef Shape<T, D> Z;
-  constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, R = 16 * NR;
-  constexpr bool kBf16 = sizeof(T) == 2;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
-  const int rows = u.ntok * a.share, r0 = tile * R;
-  const int dim = EXACT ? D : kv.D;
-  // A causal query sees the own tokens in front of `first + its number among the new tokens`.
-  const bool steps = own && a.causal;
-  const int first = u.len - u.ntok + 1;
-  const int first_tok = r0 / a.by_share, end = end_of(u, steps, a, tile, R);
-  const int k0 = cut(cost0, cost, end), k1 = cut(cost1, cost, end), all_see = steps ? first + first_tok : k1;
-
-  typename Z::KV q[NR][KC];
-  int limit[NR];
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int r = r0 + 16 * n + m, tq = min(r, rows - 1) / a.by_share, h = hk * a.share + min(r, rows - 1) - tq * a.share;
-    const T* from = static_cast<const T*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
-    limit[n] = steps ? min(k1, first + tq) : k1;
-#pragma unroll
-    for (int x = 0; x < KC; ++x) {
-      const int d = 4 * Z::KE * x + Z::KE * g;
-      typename Z::KV z{};
-      if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(from + d);
-      q[n][x] = z;
-    }
-  }
-  const float to_log2 = a.scale * kLog2e;
-  f32x4 acc[NR][NB][E];
-  float top[NR], ref[NR], sum[NR];
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    top[n] = -INFINITY;
-    ref[n] = 0.f;
-    sum[n] = 0.f;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int e = 0; e < E; ++e) acc[n][b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
-  }
-
-  const int32_t* const table = own ? kv.pages + static_cast<int64_t>(u.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(u.row) * kv.max_prefix_pages;
-  const int64_t page_step = (static_cast<int64_t>(kv.Hk) * dim) << kv.page_shift;
-  const int in_page = (1 << kv.page_shift) - 1;
-  const T* const kbase = static_cast<const T*>(kv.k) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
-  const T* const vbase = static_cast<const T*>(kv.v) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
-
-  for (int from = k0; from < k1;) {
-    const int page0 = from >> kv.page_shift, to = min(k1, (page0 + kPageSlots) << kv.page_shift);
-    const int n_slots = ((to - 1) >> kv.page_shift) - page0 + 1;
-    bool missing = false;
-    __syncthreads();
-    for (int i = tid; i < n_slots; i += 256) {
-      int id = table[page0 + i];
-      if (static_cast<unsigned>(id) >= static_cast<unsigned>(kv.n_pages)) {
-        id = -1;
-        missing = true;
-      }
-      lds.pages[i] = id;
-    }
-    const bool holes = __syncthreads_or(missing);
-    if (missing) raise_data_error(a.data_error, AT_GRPO_DATA_PAGE);
-
-    typename Z::KV k[SUB][KC];
-    typename Z::VV v[NB][VJ];
-    auto row_of = [&](int token) {      // a token behind the last stands for it
-      const int i = min(token, to - 1), id = max(0, lds.pages[(i >> kv.page_shift) - page0]);
-      return id * page_step + static_cast<int64_t>(i & in_page) * dim;
-    };
-    auto load_k = [&](int t) {
-#pragma unroll
-      for (int s = 0; s < SUB; ++s) {
-        const T* p = kbase + row_of(t + 16 * s + m);
-#pragma unroll
-        for (int x = 0; x < KC; ++x) {
-          const int d = 4 * Z::KE * x + Z::KE * g;
-          typename Z::KV z{};
-          if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(p + d);
-          k[s][x] = z;
-        }
-      }
-    };
-    auto load_v = [&](int t) {
-#pragma unroll
-      for (int s = 0; s < SUB; ++s) {
-        const T* p = vbase + row_of(min(t + 16 * s + 4 * g, (to - 1) & ~3));      // four tokens that start at a multiple of four share a page
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          const int d = 16 * E * b + E * m;
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            typename Z::VV z{};
-            if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::VV*>(p + static_cast<int64_t>(j) * dim + d);
-            v[b][4 * s + j] = z;
-          }
-        }
-      }
-    };
-
-    // Loads are never behind a branch: the compiler could not tell then which of them are still on their way, and would wait for all.
-    // What is asked for behind the last tile is the last token's row.
-    load_k(from + TOK * wave);
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-    load_v(from + TOK * wave);
-    for (int t = from + TOK * wave; t < to; t += 4 * TOK) {
-      f32x4 s[NR][SUB];
-#pragma unroll
-      for (int n = 0; n < NR; ++n)
-#pragma unroll
-        for (int y = 0; y < SUB; ++y) {
-          s[n][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int x = 0; x < KC; ++x) {
-            if constexpr (kBf16) {
-              s[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][x]), __builtin_bit_cast(bf16x8, q[n][x]), s[n][y], 0, 0, 0);
-            } else {
-#pragma unroll
-              for (int z = 0; z < 4; ++z) s[n][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[y][x][z], q[n][x][z], s[n][y], 0, 0, 0);
-            }
-          }
-        }
-      load_k(t + 4 * TOK);
-      if (t + TOK > min(to, all_see) || holes) {
-        // tokens that a row does not see, and what lies in the cache behind the last or in no page: no weight, and no value
-#pragma unroll
-        for (int y = 0; y < SUB; ++y) {
-          const int t4 = t + 16 * y + 4 * g;
-          const int last = to - t4, seen = last > 0 && lds.pages[(min(t4, to - 1) >> kv.page_shift) - page0] >= 0 ? last : 0;
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-#pragma unroll
-            for (int n = 0; n < NR; ++n) s[n][y][i] = i < min(seen, limit[n] - t4) ? s[n][y][i] : -INFINITY;
-#pragma unroll
-            for (int b = 0; b < NB; ++b) v[b][4 * y + i] = i < seen ? v[b][4 * y + i] : typename Z::VV{};
-          }
-        }
-      }
-      uint32_t w16[NR][4];
-      float w32[NR][4];
-#pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        float high = -INFINITY;
-#pragma unroll
-        for (int y = 0; y < SUB; ++y)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) high = fmaxf(high, s[n][y][i]);
-        high *= to_log2;
-        if (__any(high > top[n] + kSlack)) {
-          high = fmaxf(high, __shfl_xor(high, 16, 64));
-          high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top[n]);
-          const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top[n] - now);
-          top[n] = high;
-          ref[n] = now;
-          sum[n] *= keep;
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int e = 0; e < E; ++e) acc[n][b][e] *= keep;
-        }
-        float p[4 * SUB];
-#pragma unroll
-        for (int y = 0; y < SUB; ++y)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            p[4 * y + i] = __builtin_amdgcn_exp2f(fmaf(s[n][y][i], to_log2, -ref[n]));
-            sum[n] += p[4 * y + i];
-          }
-        if constexpr (kBf16) {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w16[n][j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
-        } else {
-#pragma unroll
-          for (int j = 0; j < 4; ++j) w32[n][j] = p[j];
-        }
-      }
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          if constexpr (kBf16) {
-            const bf16x8 vt = transposed(v[b], e);
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-              acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])),
-                                                                     acc[n][b][e], 0, 0, 0);
-          } else {
-#pragma unroll
-            for (int n = 0; n < NR; ++n)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], acc[n][b][e], 0, 0, 0);
-          }
-        }
-      load_v(t + 4 * TOK);
-      asm volatile("" ::: "memory");      // the loads stay on this side of the jump back
-    }
-    from = to;
-  }
-
-  // The wavefronts' maxima and sums, and their products, which sixteen threads a row weigh and add up.
-  if (k0 >= k1) __syncthreads();      // else the loads of page ids have had one since the last run
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    sum[n] += __shfl_xor(sum[n], 16, 64);
-    sum[n] += __shfl_xor(sum[n], 32, 64);
-    if (g == 0) {
-      lds.ml[wave][16 * n + m][0] = top[n];
-      lds.ml[wave][16 * n + m][1] = sum[n];
-    }
-  }
-  const bool direct = kv.n_group == 0 && cost0 == 0 && cost1 == cost;
-  // where a row's part lies: by its query and head, or with the workgroup's
-  const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq, by_group = static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1);
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int row = tid >> 4, r = r0 + 16 * n + row, tq = r / a.by_share, h = hk * a.share + r - tq * a.share;
-    const int64_t part = cost0 == 0 ? by_query + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h : by_group + static_cast<int64_t>(group) * kMaxRows + (r - r0);
-    float f[4];
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      if (n || b) __syncthreads();
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int e = 0; e < E; e += 4)
-          *reinterpret_cast<f32x4*>(&lds.slab[wave][m][E * (4 * g + i) + e]) =
-              f32x4{acc[n][b][e][i], acc[n][b][e + 1][i], acc[n][b][e + 2][i], acc[n][b][e + 3][i]};
-      __syncthreads();
-      if (b == 0) {
-        float high = -INFINITY, total = 0.f;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) high = fmaxf(high, lds.ml[w][16 * n + row][0]);
-        const float now = high == -INFINITY ? 0.f : high;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-          f[w] = __builtin_amdgcn_exp2f(lds.ml[w][16 * n + row][0] - now);
-          total = fmaf(f[w], lds.ml[w][16 * n + row][1], total);
-        }
-        const float one = total == 0.f ? 0.f : __builtin_amdgcn_rcpf(total);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) f[w] *= one;
-        if ((tid & 15) == 0 && r < rows) {
-          const float x = total == 0.f ? -INFINITY : (now + __builtin_amdgcn_logf(total)) * kLn2;
-          if (!direct) a.part_lse[part] = x;
-          else if (a.lse) a.lse[static_cast<int64_t>(u.tok0 + tq) * a.Hq + h] = x;
-        }
-      }
-      const int d = E * (tid & 15);
-      if (r < rows && (EXACT || 16 * E * b + d < dim)) {
-        f32x4 o[E / 4];
-#pragma unroll
-        for (int e = 0; e < E / 4; ++e) {
-          f32x4 x[4];
-#pragma unroll
-          for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&lds.slab[w][row][d + 4 * e]) * f[w];
-          o[e] = (x[0] + x[1]) + (x[2] + x[3]);
-        }
-        if (direct) {
-          T* to = static_cast<T*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 16 * E * b + d;
-#pragma unroll
-          for (int e = 0; e < E / 4; ++e) {
-            if constexpr (kBf16) *reinterpret_cast<uint2*>(to + 4 * e) = make_uint2(pack_bf16x2(o[e][0], o[e][1]), pack_bf16x2(o[e][2], o[e][3]));
-            else *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
-          }
-        } else {
-          float* to = a.part_out + part * dim + 16 * E * b + d;
-#pragma unroll
-          for (int e = 0; e < E / 4; ++e) *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
-        }
-      }
-    }
-  }
-}
 
 // ---- many queries ----------------------------------------------------------------------------------
 // Where a tile has 128 rows the products bound the call, not the tokens' passage.  Each wavefront then has 32 rows of its own, and the
@@ -615,16 +348,6 @@ template <int D>
 __device__ __forceinline__ int swizzle_k(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
 template <int D>
 __device__ __forceinline__ int swizzle_v(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
-
-// A run of a wide tile.
-struct WideRun {
-  int hk, r0, k0, k1;
-};
-template <typename R>
-__device__ __forceinline__ WideRun wide_run(const R& r, const Args& a) {
-  const int end = end_of(r.x, r.steps, a, r.tile, kWideRows);
-  return WideRun{r.hk, r.tile * kWideRows, cut(r.from(), r.cost, end), cut(r.to(), r.cost, end)};
-}
 
 template <int D>
 __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
@@ -678,7 +401,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
     }
   };
   uint4 q[KC];
-  auto load_q = [&](const Unit& x, const WideRun& w) {
+  auto load_q = [&](const Unit& x, const TileRun& w) {
     const int r = min(w.r0 + 32 * wave + m, x.ntok * a.share - 1), tq = r / a.by_share, h = w.hk * a.share + r - tq * a.share;
     const bf16_t* from = static_cast<const bf16_t*>(a.q.data) + (x.tok0 + tq) * a.q.ts + h * a.q.hs + 8 * g;
 #pragma unroll
@@ -686,7 +409,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
   };
   int buffer = 0;
   bool requested = false;      // the run's first tile, by the run in front of it
-  WideRun w = wide_run(run, a);
+  TileRun w = tile_run(run, a);
   load_q(run.x, w);
   for (;;) {
     const Unit u = run.x;
@@ -704,8 +427,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
     }
     run.next();
     const bool more = run.valid();
-    WideRun next{};
-    if (more) next = wide_run(run, a);
+    TileRun next{};
+    if (more) next = tile_run(run, a);
     const bool ahead = more && run.u == staged && next.k0 < next.k1;      // with the same page ids
     f32x16 acc[DT];
 #pragma unroll
@@ -876,11 +599,342 @@ constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
 
 template <typename T, int D, int NRP, int NRO, bool EXACT>
 __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
+  typedef Shape<T, D> Z;
+  constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, NRM = NRP > NRO ? NRP : NRO;
+  constexpr bool kBf16 = sizeof(T) == 2;
   __shared__ Lds lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+  const int dim = EXACT ? D : kv.D;
   const Share mine = make_schedule<16 * NRP, 16 * NRO>(kv, a, lds.S);
-  for (Runs<16 * NRP, 16 * NRO> r(kv, a, lds.S, mine); r.valid(); r.next()) {
-    if (r.own) attend_run<T, D, NRO, EXACT>(kv, a, lds, r.x, true, r.hk, r.tile, r.cost, r.from(), r.to(), r.number);
-    else attend_run<T, D, NRP, EXACT>(kv, a, lds, r.x, false, r.hk, r.tile, r.cost, r.from(), r.to(), r.number);
+  Runs<16 * NRP, 16 * NRO> run(kv, a, lds.S, mine);
+  if (!run.valid()) return;
+  const uint32_t page_step = static_cast<uint32_t>(kv.Hk * dim) << kv.page_shift;      // elements of a page of all heads
+  const int in_page = (1 << kv.page_shift) - 1;
+  const float to_log2 = a.scale * kLog2e;
+
+  // Page ids of tokens page0 << page_shift .. : a unit's all, where they fit, for all its runs.  Two lists take turns, so that the next
+  // unit's comes in beside a run of this one.
+  const int* pages = lds.pages[0];
+  int page0 = 0, staged = -1, half = 0;
+  bool holes = false;
+  auto slots = [&](int from, int to) { return to > from ? ((to - 1) >> kv.page_shift) - (from >> kv.page_shift) + 1 : 0; };
+  auto put_ids = [&](const int* ids, int n, int at) {      // ids[i]: of slot tid + 256 i; whether one is none, and all lists have been read
+    bool missing = false;
+#pragma unroll
+    for (int i = 0; i < kPageSlots / 256; ++i)
+      if (tid + 256 * i < n) {
+        const bool none = static_cast<unsigned>(ids[i]) >= static_cast<unsigned>(kv.n_pages);
+        lds.pages[at][tid + 256 * i] = none ? -1 : ids[i];
+        missing |= none;
+      }
+    if (missing) raise_data_error(a.data_error, AT_GRPO_DATA_PAGE);
+    const bool any = __any(missing);
+    if (lane == 0) lds.holes[at][wave] = any;
+    lds_barrier();
+    asm volatile("" ::: "memory");
+    return (lds.holes[at][0] | lds.holes[at][1] | lds.holes[at][2] | lds.holes[at][3]) != 0;
+  };
+  auto get_ids = [&](int* ids, const int32_t* table, int n) {
+#pragma unroll
+    for (int i = 0; i < kPageSlots / 256; ++i) ids[i] = tid + 256 * i < n ? table[tid + 256 * i] : 0;
+  };
+  auto table_of = [&](const Unit& x, bool own) {
+    return own ? kv.pages + static_cast<int64_t>(x.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(x.row) * kv.max_prefix_pages;
+  };
+  auto fits = [&](const Unit& x) { return ((x.len - 1) >> kv.page_shift) < kPageSlots; };
+
+  typename Z::KV q[NRM][KC], k[SUB][KC];
+  typename Z::VV v[NB][VJ];
+  auto row_of = [&](int token, int to) {      // a token behind the last stands for it
+    const int i = min(token, to - 1), id = max(0, pages[(i >> kv.page_shift) - page0]);
+    return static_cast<uint64_t>(static_cast<uint32_t>(id)) * page_step + static_cast<uint32_t>((i & in_page) * dim);
+  };
+  auto load_k = [&](int hk, int t, int to) {
+    const T* const base = static_cast<const T*>(kv.k) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+#pragma unroll
+    for (int s = 0; s < SUB; ++s) {
+      const T* p = base + row_of(t + 16 * s + m, to);
+#pragma unroll
+      for (int x = 0; x < KC; ++x) {
+        const int d = 4 * Z::KE * x + Z::KE * g;
+        typename Z::KV z{};
+        if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(p + d);
+        k[s][x] = z;
+      }
+    }
+  };
+  auto load_v = [&](int hk, int t, int to) {
+    const T* const base = static_cast<const T*>(kv.v) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+#pragma unroll
+    for (int s = 0; s < SUB; ++s) {
+      const T* p = base + row_of(min(t + 16 * s + 4 * g, (to - 1) & ~3), to);      // four tokens that start at a multiple of four share a page
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int d = 16 * E * b + E * m;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          typename Z::VV z{};
+          if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::VV*>(p + static_cast<int64_t>(j) * dim + d);
+          v[b][4 * s + j] = z;
+        }
+      }
+    }
+  };
+  auto load_q = [&](const Unit& u, const TileRun& w, auto nr) {
+#pragma unroll
+    for (int n = 0; n < decltype(nr)::value; ++n) {
+      const int r = min(w.r0 + 16 * n + m, u.ntok * a.share - 1), tq = r / a.by_share, h = w.hk * a.share + r - tq * a.share;
+      const T* from = static_cast<const T*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
+#pragma unroll
+      for (int x = 0; x < KC; ++x) {
+        const int d = 4 * Z::KE * x + Z::KE * g;
+        typename Z::KV z{};
+        if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(from + d);
+        q[n][x] = z;
+      }
+    }
+  };
+
+  TileRun w = tile_run(run, a);
+  for (;;) {
+    const Unit u = run.x;
+    const bool steps = run.steps, own = run.own, whole = fits(u), first_part = run.from() == 0;
+    const bool direct = kv.n_group == 0 && first_part && run.to() == run.cost;
+    const int32_t* const table = table_of(u, own);
+    if (whole && staged != run.u) {
+      int ids[kPageSlots / 256];
+      get_ids(ids, table, slots(0, u.len));
+      lds_barrier();      // nobody reads the list any more
+      holes = put_ids(ids, slots(0, u.len), half);
+      pages = lds.pages[half];
+      page0 = 0;
+      staged = run.u;
+    }
+    run.next();
+    const bool more = run.valid();
+    TileRun next{};
+    if (more) next = tile_run(run, a);
+    const bool turn = more && run.u != staged && fits(run.x);      // another unit: its page ids come meanwhile
+    int ids[kPageSlots / 256];
+    if (turn) get_ids(ids, table_of(run.x, run.own), slots(0, run.x.len));
+
+    auto body = [&](auto nr) {
+      constexpr int NR = decltype(nr)::value, R = 16 * NR;
+      const int rows = u.ntok * a.share, hk = w.hk, r0 = w.r0, k0 = w.k0, k1 = w.k1, first = u.len - u.ntok + 1;
+      const int all_see = steps ? first + r0 / a.by_share : k1;
+      int limit[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) limit[n] = steps ? min(k1, first + min(r0 + 16 * n + m, rows - 1) / a.by_share) : k1;
+      f32x4 acc[NR][NB][E];
+      float top[NR], ref[NR], sum[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        top[n] = -INFINITY;
+        ref[n] = 0.f;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[n][b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      load_q(u, w, nr);
+      for (int from = k0; from < k1;) {
+        int to = k1;
+        if (!whole) {      // a part of the list at a time
+          page0 = from >> kv.page_shift;
+          to = min(k1, (page0 + kPageSlots) << kv.page_shift);
+          int part[kPageSlots / 256];
+          get_ids(part, table + page0, slots(from, to));
+          lds_barrier();
+          holes = put_ids(part, slots(from, to), half);
+          pages = lds.pages[half];
+          staged = -1;
+        }
+        // The order of the loads is that of their use.
+        load_k(hk, from + TOK * wave, to);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(hk, from + TOK * wave, to);
+        // Loads are never behind a branch: the compiler could not tell then which of them are still on their way, and would wait for all.
+        // What is asked for behind the last tile is the last token's row.
+        for (int t = from + TOK * wave; t < to; t += 4 * TOK) {
+          f32x4 s[NR][SUB];
+#pragma unroll
+          for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int y = 0; y < SUB; ++y) {
+              s[n][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int x = 0; x < KC; ++x) {
+                if constexpr (kBf16) {
+                  s[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][x]), __builtin_bit_cast(bf16x8, q[n][x]), s[n][y], 0, 0, 0);
+                } else {
+#pragma unroll
+                  for (int z = 0; z < 4; ++z) s[n][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[y][x][z], q[n][x][z], s[n][y], 0, 0, 0);
+                }
+              }
+            }
+          load_k(hk, t + 4 * TOK, to);
+          if (t + TOK > min(to, all_see) || holes) {
+            // tokens that a row does not see, and what lies in the cache behind the last or in no page: no weight, and no value
+#pragma unroll
+            for (int y = 0; y < SUB; ++y) {
+              const int t4 = t + 16 * y + 4 * g;
+              const int last = to - t4, seen = last > 0 && pages[(min(t4, to - 1) >> kv.page_shift) - page0] >= 0 ? last : 0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int n = 0; n < NR; ++n) s[n][y][i] = i < min(seen, limit[n] - t4) ? s[n][y][i] : -INFINITY;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) v[b][4 * y + i] = i < seen ? v[b][4 * y + i] : typename Z::VV{};
+              }
+            }
+          }
+          uint32_t w16[NR][4];
+          float w32[NR][4];
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            float high = -INFINITY;
+#pragma unroll
+            for (int y = 0; y < SUB; ++y)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) high = fmaxf(high, s[n][y][i]);
+            high *= to_log2;
+            if (__any(high > top[n] + kSlack)) {
+              high = fmaxf(high, __shfl_xor(high, 16, 64));
+              high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top[n]);
+              const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top[n] - now);
+              top[n] = high;
+              ref[n] = now;
+              sum[n] *= keep;
+#pragma unroll
+              for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[n][b][e] *= keep;
+            }
+            float p[4 * SUB];
+#pragma unroll
+            for (int y = 0; y < SUB; ++y)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                p[4 * y + i] = __builtin_amdgcn_exp2f(fmaf(s[n][y][i], to_log2, -ref[n]));
+                sum[n] += p[4 * y + i];
+              }
+            if constexpr (kBf16) {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w16[n][j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
+            } else {
+#pragma unroll
+              for (int j = 0; j < 4; ++j) w32[n][j] = p[j];
+            }
+          }
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+#pragma unroll
+            for (int e = 0; e < E; ++e) {
+              if constexpr (kBf16) {
+                const bf16x8 vt = transposed(v[b], e);
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+                  acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])),
+                                                                         acc[n][b][e], 0, 0, 0);
+              } else {
+#pragma unroll
+                for (int n = 0; n < NR; ++n)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], acc[n][b][e], 0, 0, 0);
+              }
+            }
+          load_v(hk, t + 4 * TOK, to);
+          asm volatile("" ::: "memory");      // the loads stay on this side of the jump back
+        }
+        from = to;
+      }
+
+      if (turn) {
+        half ^= 1;
+        holes = put_ids(ids, slots(0, run.x.len), half);
+        pages = lds.pages[half];
+        page0 = 0;
+        staged = run.u;
+      }
+      // The wavefronts' maxima and sums, and their products, which sixteen threads a row weigh and add up.
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        sum[n] += __shfl_xor(sum[n], 16, 64);
+        sum[n] += __shfl_xor(sum[n], 32, 64);
+        if (g == 0) {
+          lds.ml[wave][16 * n + m][0] = top[n];
+          lds.ml[wave][16 * n + m][1] = sum[n];
+        }
+      }
+      // where a row's part lies: by its query and head, or with the workgroup's
+      const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq, by_group = static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1);
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const int row = tid >> 4, r = r0 + 16 * n + row, tq = r / a.by_share, h = hk * a.share + r - tq * a.share;
+        const int64_t part = first_part ? by_query + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h : by_group + static_cast<int64_t>(run.number) * kMaxRows + (r - r0);
+        float f[4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          if (n || b) lds_barrier();
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int e = 0; e < E; e += 4)
+              *reinterpret_cast<f32x4*>(&lds.slab[wave][m][E * (4 * g + i) + e]) =
+                  f32x4{acc[n][b][e][i], acc[n][b][e + 1][i], acc[n][b][e + 2][i], acc[n][b][e + 3][i]};
+          lds_barrier();
+          if (b == 0) {
+            float high = -INFINITY, total = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) high = fmaxf(high, lds.ml[w][16 * n + row][0]);
+            const float now = high == -INFINITY ? 0.f : high;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+              f[w] = __builtin_amdgcn_exp2f(lds.ml[w][16 * n + row][0] - now);
+              total = fmaf(f[w], lds.ml[w][16 * n + row][1], total);
+            }
+            const float one = total == 0.f ? 0.f : __builtin_amdgcn_rcpf(total);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) f[w] *= one;
+            if ((tid & 15) == 0 && r < rows) {
+              const float x = total == 0.f ? -INFINITY : (now + __builtin_amdgcn_logf(total)) * kLn2;
+              if (!direct) a.part_lse[part] = x;
+              else if (a.lse) a.lse[static_cast<int64_t>(u.tok0 + tq) * a.Hq + h] = x;
+            }
+          }
+          const int d = E * (tid & 15);
+          if (r < rows && (EXACT || 16 * E * b + d < dim)) {
+            f32x4 o[E / 4];
+#pragma unroll
+            for (int e = 0; e < E / 4; ++e) {
+              f32x4 x[4];
+#pragma unroll
+              for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&lds.slab[w][row][d + 4 * e]) * f[w];
+              o[e] = (x[0] + x[1]) + (x[2] + x[3]);
+            }
+            if (direct) {
+              T* to = static_cast<T*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 16 * E * b + d;
+#pragma unroll
+              for (int e = 0; e < E / 4; ++e) {
+                if constexpr (kBf16) *reinterpret_cast<uint2*>(to + 4 * e) = make_uint2(pack_bf16x2(o[e][0], o[e][1]), pack_bf16x2(o[e][2], o[e][3]));
+                else *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
+              }
+            } else {
+              float* to = a.part_out + part * dim + 16 * E * b + d;
+#pragma unroll
+              for (int e = 0; e < E / 4; ++e) *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
+            }
+          }
+        }
+      }
+    };
+    if (own) body(std::integral_constant<int, NRO>{});
+    else body(std::integral_constant<int, NRP>{});
+    if (!more) break;
+    lds_barrier();      // what was added up has been read
+    w = next;
   }
 }
 
@@ -946,7 +1000,6 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int
     total *= keep;
 #pragma unroll
     for (int i = 0; i < kMaxHeadDim / 16; ++i) acc[i] *= keep;
-#pragma unroll 4
     for (int c0 = 4 * mine; c0 < count_here; c0 += 4 * WAVES) {
       const int c = c0 + slot;
       const float w = __shfl(weight, c, 64);      // 0 behind the last
