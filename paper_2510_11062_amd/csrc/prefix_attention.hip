@@ -330,6 +330,579 @@ struct Lds {
   float slab[4][16][128 + 4];
 };
 
+// 16 or 8 bytes that nothing reads again while the caches hold them: keys and values of a decode, 117 us for 32 groups without, so 106.
+template <typename V>
+__device__ __forceinline__ V load_once(const void* p) {
+  typedef float Words __attribute__((ext_vector_type(sizeof(V) / 4)));
+  return __builtin_bit_cast(V, __builtin_nontemporal_load(reinterpret_cast<const Words*>(p)));
+}
+
+// S^T = K Q^T of a tile.
+template <typename T, int D, int NR, int NRM>
+__device__ __forceinline__ void scores(const typename Shape<T, D>::KV (&k)[Shape<T, D>::SUB][Shape<T, D>::KC],
+                                       const typename Shape<T, D>::KV (&q)[NRM][Shape<T, D>::KC], f32x4 (&s)[NR][Shape<T, D>::SUB]) {
+  constexpr int SUB = Shape<T, D>::SUB, KC = Shape<T, D>::KC;
+#pragma unroll
+  for (int n = 0; n < NR; ++n)
+#pragma unroll
+    for (int y = 0; y < SUB; ++y) {
+      s[n][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KC; ++x) {
+        if constexpr (sizeof(T) == 2) {
+          s[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][x]), __builtin_bit_cast(bf16x8, q[n][x]), s[n][y], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int z = 0; z < 4; ++z) s[n][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[y][x][z], q[n][x][z], s[n][y], 0, 0, 0);
+        }
+      }
+    }
+}
+
+// The tile's weights into the sums, and their products with its values into the accumulators.
+template <typename T, int D, int NR>
+__device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::SUB], const typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
+                                              float to_log2, f32x4 (&acc)[NR][Shape<T, D>::NB][Shape<T, D>::E], float (&top)[NR], float (&ref)[NR],
+                                              float (&sum)[NR]) {
+  typedef Shape<T, D> Z;
+  constexpr int E = Z::E, NB = Z::NB, SUB = Z::SUB;
+  constexpr bool kBf16 = sizeof(T) == 2;
+  uint32_t w16[NR][4];
+  float w32[NR][4];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    float high = -INFINITY;
+#pragma unroll
+    for (int y = 0; y < SUB; ++y)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) high = fmaxf(high, s[n][y][i]);
+    high *= to_log2;
+    if (__any(high > top[n] + kSlack)) {
+      high = fmaxf(high, __shfl_xor(high, 16, 64));
+      high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top[n]);
+      const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top[n] - now);
+      top[n] = high;
+      ref[n] = now;
+      sum[n] *= keep;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[n][b][e] *= keep;
+    }
+    float p[4 * SUB];
+#pragma unroll
+    for (int y = 0; y < SUB; ++y)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        p[4 * y + i] = __builtin_amdgcn_exp2f(fmaf(s[n][y][i], to_log2, -ref[n]));
+        sum[n] += p[4 * y + i];
+      }
+    if constexpr (kBf16) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w16[n][j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) w32[n][j] = p[j];
+    }
+  }
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      if constexpr (kBf16) {
+        const bf16x8 vt = transposed(v[b], e);
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+          acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])),
+                                                                 acc[n][b][e], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], acc[n][b][e], 0, 0, 0);
+      }
+    }
+}
+
+// Rows r0 .. rows - 1 (at most a tile) of the queries from tok0 on for key head hk.
+struct RowsOf {
+  int tok0, hk, r0, rows;
+};
+
+// The wavefronts' maxima and sums, and their products, which sixteen threads a row weigh and add up.  Into the output, or into a part: by
+// query and head (group < 0), or with the workgroup.
+template <typename T, bool EXACT, typename L, int NR, int NB, int E>
+__device__ __forceinline__ void finish(const Args& a, L& lds, const f32x4 (&acc)[NR][NB][E], const float (&top)[NR], float (&sum)[NR], const RowsOf& of,
+                                       bool direct, int group, int64_t by_query, int64_t by_group, int dim) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    sum[n] += __shfl_xor(sum[n], 16, 64);
+    sum[n] += __shfl_xor(sum[n], 32, 64);
+    if (g == 0) {
+      lds.ml[wave][16 * n + m][0] = top[n];
+      lds.ml[wave][16 * n + m][1] = sum[n];
+    }
+  }
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int row = tid >> 4, r = of.r0 + 16 * n + row, tq = r / a.by_share, h = of.hk * a.share + r - tq * a.share;
+    const int64_t part = group < 0 ? by_query + static_cast<int64_t>(of.tok0 + tq) * a.Hq + h : by_group + static_cast<int64_t>(group) * kMaxRows + (r - of.r0);
+    float f[4];
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      if (n || b) lds_barrier();
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int e = 0; e < E; e += 4)
+          *reinterpret_cast<f32x4*>(&lds.slab[wave][m][E * (4 * g + i) + e]) =
+              f32x4{acc[n][b][e][i], acc[n][b][e + 1][i], acc[n][b][e + 2][i], acc[n][b][e + 3][i]};
+      lds_barrier();
+      if (b == 0) {
+        float high = -INFINITY, total = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) high = fmaxf(high, lds.ml[w][16 * n + row][0]);
+        const float now = high == -INFINITY ? 0.f : high;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          f[w] = __builtin_amdgcn_exp2f(lds.ml[w][16 * n + row][0] - now);
+          total = fmaf(f[w], lds.ml[w][16 * n + row][1], total);
+        }
+        const float one = total == 0.f ? 0.f : __builtin_amdgcn_rcpf(total);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) f[w] *= one;
+        if ((tid & 15) == 0 && r < of.rows) {
+          const float x = total == 0.f ? -INFINITY : (now + __builtin_amdgcn_logf(total)) * kLn2;
+          if (!direct) a.part_lse[part] = x;
+          else if (a.lse) a.lse[static_cast<int64_t>(of.tok0 + tq) * a.Hq + h] = x;
+        }
+      }
+      const int d = E * (tid & 15);
+      if (r < of.rows && (EXACT || 16 * E * b + d < dim)) {
+        f32x4 o[E / 4];
+#pragma unroll
+        for (int e = 0; e < E / 4; ++e) {
+          f32x4 x[4];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&lds.slab[w][row][d + 4 * e]) * f[w];
+          o[e] = (x[0] + x[1]) + (x[2] + x[3]);
+        }
+        if (direct) {
+          T* to = static_cast<T*>(a.out.data) + (of.tok0 + tq) * a.out.ts + h * a.out.hs + 16 * E * b + d;
+#pragma unroll
+          for (int e = 0; e < E / 4; ++e) {
+            if constexpr (kBf16) *reinterpret_cast<uint2*>(to + 4 * e) = make_uint2(pack_bf16x2(o[e][0], o[e][1]), pack_bf16x2(o[e][2], o[e][3]));
+            else *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
+          }
+        } else {
+          float* to = a.part_out + part * dim + 16 * E * b + d;
+#pragma unroll
+          for (int e = 0; e < E / 4; ++e) *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
+        }
+      }
+    }
+  }
+}
+
+// Workgroups on a compute unit, by the registers of a wavefront.
+template <int D, int NRP>
+constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
+
+// ---- one new token, or few, in each sequence ---------------------------------------------------------
+// Here a sequence has no more rows than a tile, and all rows of a group read one stream of tokens: the prefix, then the own tokens of its
+// sequences one behind the other, each beginning a block of 32; a row's scores for other sequences' tokens have no weight.  A unit is a
+// group, or a sequence in none; with as many tiles of rows as it has, each reads the prefix and its own sequences.  What a row needs is
+// in one run, so rows of runs that one workgroup had whole are done, and a run for each sequence and head, most of whose time would be
+// its beginning and end, is saved: 32 groups of up to 8 DECTREE us, with runs of prefixes and of sequences 120 and 11 for their joining.
+constexpr int kDecodeSeqs = 1024;     // sequences whose places are kept in LDS
+constexpr int kDecodeUnits = 256;     // units
+constexpr int kDecodeSlots = 2048;    // page ids of a share of a run; beyond that they are read where they lie
+
+struct DecodeUnit {
+  int tok0, ntok, seq0, seq1, prefix, blocks;      // blocks of 32: of the whole stream
+};
+
+struct DecodeLds {
+  int wave_sum[4][2], wave_falls[4];
+  int unit, base;
+  int place[kDecodeSeqs + 1];      // blocks in front of each sequence, times 32, and how many tokens its last block has, if not 32
+  int pages_before[kDecodeSeqs + 1];
+  DecodeUnit cache[kDecodeUnits];
+  int pages[kDecodeSlots];
+  int holes[4];
+  float ml[4][64][2];
+  float slab[4][16][128 + 4];
+};
+
+__device__ __forceinline__ int blocks_before(const DecodeLds& lds, int s) { return lds.place[s] >> 5; }
+__device__ __forceinline__ int length_of(const DecodeLds& lds, int s) {
+  const int part = lds.place[s] & 31, blocks = blocks_before(lds, s + 1) - blocks_before(lds, s);
+  return 32 * blocks - (part ? 32 - part : 0);
+}
+
+struct GroupSizes {
+  int seq0, seq1, prefix;
+};
+__device__ __forceinline__ GroupSizes group_sizes(const KvView& kv, int g) {
+  return g < kv.n_group ? GroupSizes{kv.group_seq[g], kv.group_seq[g + 1], kv.prefix_len[g]} : GroupSizes{0, 0, 0};
+}
+
+// group_seq and cu_q are known to rise here.
+__device__ __forceinline__ DecodeUnit decode_unit(const KvView& kv, const DecodeLds& lds, int u, const GroupSizes& of, int* error) {
+  DecodeUnit x{0, 0, u - kv.n_group, u - kv.n_group + 1, 0, 0};
+  if (u < kv.n_group) {
+    x.seq0 = of.seq0;
+    x.seq1 = of.seq1;
+    x.prefix = of.prefix;
+    if (x.prefix < 0 || x.prefix > (kv.max_prefix_pages << kv.page_shift)) {
+      *error |= AT_GRPO_DATA_SEQLENS;
+      x.prefix = 0;
+    }
+  } else if (kv.n_group && x.seq0 >= kv.group_seq[0] && x.seq0 < kv.group_seq[kv.n_group]) {
+    x.seq1 = x.seq0;      // a group's
+  }
+  x.tok0 = kv.cu_q ? kv.cu_q[x.seq0] : x.seq0;
+  x.ntok = (kv.cu_q ? kv.cu_q[x.seq1] : x.seq1) - x.tok0;
+  x.blocks = ((x.prefix + 31) >> 5) + blocks_before(lds, x.seq1) - blocks_before(lds, x.seq0);
+  return x;
+}
+
+// Cost of a run: all alike.
+__device__ __forceinline__ int decode_cost(const DecodeUnit& x, const Args& a, int tiles) {
+  if (x.blocks == 0 || x.ntok == 0) return 0;
+  const int prefix = (x.prefix + 31) >> 5, own = x.blocks - prefix;
+  return (4 * (prefix + (own + tiles - 1) / tiles) + kRunCost + a.quantum - 1) & -a.quantum;
+}
+
+template <int R>
+__device__ Share decode_schedule(const KvView& kv, const Args& a, DecodeLds& lds) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = kv.n_group + kv.n_seq;
+  int error = 0;
+  bool falls = false;
+  // Two sums over all threads, in front of this one's share of them.
+  auto scan = [&](int& x, int& y, int* total) {
+    int sx = x, sy = y;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int ux = __shfl_up(sx, o, 64), uy = __shfl_up(sy, o, 64);
+      if (lane >= o) {
+        sx += ux;
+        sy += uy;
+      }
+    }
+    if (lane == 63) {
+      lds.wave_sum[wave][0] = sx;
+      lds.wave_sum[wave][1] = sy;
+    }
+    __syncthreads();
+    x = sx - x;
+    y = sy - y;
+    *total = 0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      if (w < wave) {
+        x += lds.wave_sum[w][0];
+        y += lds.wave_sum[w][1];
+      }
+      *total += lds.wave_sum[w][0];
+    }
+  };
+  const int per_seq = (kv.n_seq + 255) / 256, s0 = min(kv.n_seq, tid * per_seq), s1 = min(kv.n_seq, s0 + per_seq), most = kv.max_pages << kv.page_shift;
+  auto length = [&](int s) {
+    const int len = kv.length[s];
+    return len < 0 || len > most ? -1 : len;
+  };
+  const int per = (n + 255) / 256, u0 = min(n, tid * per);
+  const GroupSizes ahead = group_sizes(kv, u0);      // on its way while the sequences are counted
+  int blocks = 0, page_count = 0, unused;
+  for (int s = s0; s < s1; ++s) {
+    const int len = length(s);
+    if (len < 0) error |= AT_GRPO_DATA_SEQLENS;
+    blocks += (max(0, len) + 31) >> 5;
+    page_count += (max(0, len) + (1 << kv.page_shift) - 1) >> kv.page_shift;
+    if (kv.cu_q) falls |= kv.cu_q[s] < 0 || kv.cu_q[s + 1] < kv.cu_q[s] || kv.cu_q[s + 1] > a.n_tok;
+  }
+  for (int g = tid; g < kv.n_group; g += 256) falls |= kv.group_seq[g] < 0 || kv.group_seq[g + 1] < kv.group_seq[g] || kv.group_seq[g + 1] > kv.n_seq;
+  const bool wave_falls = __any(falls);
+  if (lane == 0) lds.wave_falls[wave] = wave_falls;
+  scan(blocks, page_count, &unused);
+  const bool none = lds.wave_falls[0] | lds.wave_falls[1] | lds.wave_falls[2] | lds.wave_falls[3];
+  for (int s = s0; s < s1; ++s) {
+    const int len = max(0, length(s));
+    lds.place[s] = blocks << 5 | (len & 31);
+    lds.pages_before[s] = page_count;
+    blocks += (len + 31) >> 5;
+    page_count += (len + (1 << kv.page_shift) - 1) >> kv.page_shift;
+    if (s == kv.n_seq - 1) {
+      lds.place[s + 1] = blocks << 5;
+      lds.pages_before[s + 1] = page_count;
+    }
+  }
+  if (kv.n_seq == 0 && tid == 0) lds.place[0] = lds.pages_before[0] = 0;
+  __syncthreads();
+  const int u1 = none ? u0 : min(n, u0 + per);
+  int mine = 0, zero = 0, total;
+  for (int u = u0; u < u1; ++u) {
+    const DecodeUnit x = decode_unit(kv, lds, u, u == u0 ? ahead : group_sizes(kv, u), &error);
+    if (u < kDecodeUnits) lds.cache[u] = x;
+    const int tiles = tiles_of(x.ntok, a.share, R);
+    mine += tiles * decode_cost(x, a, max(1, tiles)) * kv.Hk;
+  }
+  int first = mine;
+  scan(first, zero, &total);
+  total = __builtin_amdgcn_readfirstlane(total);
+  const int share = max(kMinShare, (total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x));
+  const int per_xcd = gridDim.x >> 3, w = per_xcd << 3 == gridDim.x ? (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3) : blockIdx.x;
+  const int at = static_cast<int>(min<int64_t>(total, static_cast<int64_t>(w) * share));
+  if (blockIdx.x == 0) {
+    raise_data_error(a.data_error, error | (none ? AT_GRPO_DATA_SEQLENS : 0));
+    int base = first;
+    for (int u = u0; u < u1; ++u) {
+      const DecodeUnit x = u < kDecodeUnits ? lds.cache[u] : decode_unit(kv, lds, u, group_sizes(kv, u), &error);
+      const int tiles = tiles_of(x.ntok, a.share, R), c = decode_cost(x, a, max(1, tiles));
+      a.units[u] = make_int4(base, c, x.tok0, x.ntok);
+      base += tiles * c * kv.Hk;
+    }
+    if (none)
+      for (int u = tid; u < n; u += 256) a.units[u] = make_int4(0, 0, 0, 0);
+    if (tid == 0) a.units[n] = make_int4(share, total, none, 0);
+  }
+  if (at < total && first <= at && at - first < mine) {
+    int base = first, u = u0;
+    for (;; ++u) {
+      const DecodeUnit x = u < kDecodeUnits ? lds.cache[u] : decode_unit(kv, lds, u, group_sizes(kv, u), &error);
+      const int tiles = tiles_of(x.ntok, a.share, R), c = tiles * decode_cost(x, a, max(1, tiles)) * kv.Hk;
+      if (at < base + c) break;
+      base += c;
+    }
+    lds.unit = u;
+    lds.base = base;
+  }
+  __syncthreads();
+  return Share{w, at, min(total, at + share)};
+}
+
+template <typename T, int D, int NR, bool EXACT>
+__global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Args a) {
+  typedef Shape<T, D> Z;
+  constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, R = 16 * NR;
+  __shared__ DecodeLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+  const int dim = EXACT ? D : kv.D;
+  const Share mine = decode_schedule<R>(kv, a, lds);
+  if (mine.at >= mine.stop) return;
+  const uint32_t page_step = static_cast<uint32_t>(kv.Hk * dim) << kv.page_shift;
+  const int in_page = (1 << kv.page_shift) - 1;
+  const float to_log2 = a.scale * kLog2e;
+  const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
+  int at = mine.at, un = __builtin_amdgcn_readfirstlane(lds.unit), base = __builtin_amdgcn_readfirstlane(lds.base);
+
+  for (; at < mine.stop; ++un) {
+    int error = 0;
+    DecodeUnit u = un < kDecodeUnits ? lds.cache[un] : decode_unit(kv, lds, un, group_sizes(kv, un), &error);
+    u.tok0 = __builtin_amdgcn_readfirstlane(u.tok0);
+    u.ntok = __builtin_amdgcn_readfirstlane(u.ntok);
+    u.seq0 = __builtin_amdgcn_readfirstlane(u.seq0);
+    u.seq1 = __builtin_amdgcn_readfirstlane(u.seq1);
+    u.prefix = __builtin_amdgcn_readfirstlane(u.prefix);
+    u.blocks = __builtin_amdgcn_readfirstlane(u.blocks);
+    const int rows = u.ntok * a.share, tiles = tiles_of(u.ntok, a.share, R), cost = decode_cost(u, a, max(1, tiles)), unit_stop = min(mine.stop, base + tiles * cost * kv.Hk);
+    const int32_t* const prefix_table = kv.prefix_pages + static_cast<int64_t>(un) * kv.max_prefix_pages;      // of a group
+    while (at < unit_stop) {
+      const int run = (at - base) / cost, run0 = base + run * cost, stop = min(unit_stop, run0 + cost), hk = run / tiles, r0 = (run - hk * tiles) * R;
+      const bool first_part = at == run0, whole = first_part && stop == run0 + cost;
+      // the sequences of the tile's rows
+      int seq0 = u.seq0, seq1 = u.seq1;
+      if (tiles > 1) {
+        const int t0 = u.tok0 + r0 / a.by_share, t1 = u.tok0 + (min(rows, r0 + R) - 1) / a.by_share;
+        seq0 = kv.cu_q ? __builtin_amdgcn_readfirstlane(wave_upper_bound(kv.cu_q, kv.n_seq + 1, t0)) - 1 : t0;
+        seq1 = (kv.cu_q ? __builtin_amdgcn_readfirstlane(wave_upper_bound(kv.cu_q, kv.n_seq + 1, t1)) - 1 : t1) + 1;
+      }
+      const int own0 = (u.prefix + 31) & ~31, block0 = __builtin_amdgcn_readfirstlane(blocks_before(lds, seq0));
+      const int end = own0 + 32 * (__builtin_amdgcn_readfirstlane(blocks_before(lds, seq1)) - block0), k0 = cut(at - run0, cost, end), k1 = cut(stop - run0, cost, end);
+      at = stop;
+      // the sequence whose block stands at place t of the stream: the last that begins there or in front of it
+      auto seq_at = [&](int t) {
+        const int y = ((t - own0) >> 5) + block0;
+        int s = seq0 - 1;
+        for (int i = seq0; i < seq1; i += 64) s += __popcll(__ballot(i + lane < seq1 && blocks_before(lds, min(i + lane, seq1)) <= y));
+        return __builtin_amdgcn_readfirstlane(s);
+      };
+      auto begin_of = [&](int s) { return own0 + 32 * (__builtin_amdgcn_readfirstlane(blocks_before(lds, s)) - block0); };
+
+      // Page ids of this part of the stream: those of the prefix, then those of its sequences, the first from `skip` on.
+      const int page0 = k0 >> kv.page_shift, prefix_slots = k0 < u.prefix && k0 < k1 ? ((min(k1, u.prefix) - 1) >> kv.page_shift) - page0 + 1 : 0;
+      int s0 = seq0, s1 = seq0, skip = 0, slots = prefix_slots;
+      if (k1 > own0 && k0 < k1) {
+        s0 = seq_at(max(k0, own0));
+        s1 = seq_at(k1 - 32) + 1;
+        skip = max(0, k0 - begin_of(s0)) >> kv.page_shift;
+        slots += __builtin_amdgcn_readfirstlane(lds.pages_before[s1] - lds.pages_before[s0]) - skip;
+      }
+      const bool listed = slots <= kDecodeSlots;
+      auto slot0_of = [&](int s) { return prefix_slots + __builtin_amdgcn_readfirstlane(lds.pages_before[s] - lds.pages_before[s0]) - skip; };
+      lds_barrier();      // the last run has read its list and what was added up
+      bool missing = false;
+      if (listed) {
+        auto put = [&](int slot, int id) {
+          const bool none = static_cast<unsigned>(id) >= static_cast<unsigned>(kv.n_pages);
+          lds.pages[slot] = none ? -1 : id;
+          missing |= none;
+        };
+        for (int i = tid; i < prefix_slots; i += 256) put(i, prefix_table[page0 + i]);
+        for (int s = s0 + wave; s < s1; s += 4) {
+          const int from = s == s0 ? skip : 0, count = __builtin_amdgcn_readfirstlane(lds.pages_before[s + 1] - lds.pages_before[s]), slot0 = slot0_of(s);
+          for (int i = from + lane; i < count; i += 64) put(slot0 + i, kv.pages[static_cast<int64_t>(s) * kv.max_pages + i]);
+        }
+      } else {      // every tile's are looked at as if one were missing
+        missing = true;
+      }
+      if (missing && listed) raise_data_error(a.data_error, AT_GRPO_DATA_PAGE);
+      const bool any = __any(missing);
+      if (lane == 0) lds.holes[wave] = any;
+
+      typename Z::KV q[NR][KC], k[SUB][KC];
+      typename Z::VV v[NB][VJ];
+      int row_tok[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const int r = min(r0 + 16 * n + m, rows - 1), tq = r / a.by_share, h = hk * a.share + r - tq * a.share;
+        const T* from = static_cast<const T*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
+        row_tok[n] = u.tok0 + tq;
+#pragma unroll
+        for (int x = 0; x < KC; ++x) {
+          const int d = 4 * Z::KE * x + Z::KE * g;
+          typename Z::KV z{};
+          if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(from + d);
+          q[n][x] = z;
+        }
+      }
+      lds_barrier();
+      asm volatile("" ::: "memory");
+      const bool holes = (lds.holes[0] | lds.holes[1] | lds.holes[2] | lds.holes[3]) != 0;
+
+      // A tile of the stream: tokens token .. of a sequence (or of the prefix: -1), of which there are `last`; where its page ids are listed.
+      struct Tile {
+        int seq, token, last, slot0;
+      };
+      auto tile_at = [&](int t) {
+        Tile x{-1, t, u.prefix, -page0};
+        if (t >= own0) {
+          x.seq = seq_at(t);
+          x.token = t - begin_of(x.seq);
+          x.last = __builtin_amdgcn_readfirstlane(length_of(lds, x.seq));
+          x.slot0 = slot0_of(x.seq);
+        }
+        return x;
+      };
+      auto id_of = [&](const Tile& x, int token) {      // negative: none
+        const int page = token >> kv.page_shift;
+        if (listed) return lds.pages[x.slot0 + page];
+        const int id = x.seq < 0 ? prefix_table[page] : kv.pages[static_cast<int64_t>(x.seq) * kv.max_pages + page];
+        const bool none = static_cast<unsigned>(id) >= static_cast<unsigned>(kv.n_pages);
+        if (none) raise_data_error(a.data_error, AT_GRPO_DATA_PAGE);
+        return none ? -1 : id;
+      };
+      auto row_of = [&](const Tile& x, int token) {
+        return static_cast<uint64_t>(static_cast<uint32_t>(max(0, id_of(x, token)))) * page_step + static_cast<uint32_t>((token & in_page) * dim);
+      };
+      const T* const kbase = static_cast<const T*>(kv.k) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+      const T* const vbase = static_cast<const T*>(kv.v) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+      auto load_k = [&](const Tile& tile) {      // a token behind the last stands for it
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+          const T* p = kbase + row_of(tile, min(tile.token + 16 * s + m, tile.last - 1));
+#pragma unroll
+          for (int x = 0; x < KC; ++x) {
+            const int d = 4 * Z::KE * x + Z::KE * g;
+            typename Z::KV z{};
+            if (EXACT || d < dim) z = load_once<typename Z::KV>(p + d);
+            k[s][x] = z;
+          }
+        }
+      };
+      auto load_v = [&](const Tile& tile) {
+#pragma unroll
+        for (int s = 0; s < SUB; ++s) {
+          const T* p = vbase + row_of(tile, min(tile.token + 16 * s + 4 * g, (tile.last - 1) & ~3));
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            const int d = 16 * E * b + E * m;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              typename Z::VV z{};
+              if (EXACT || d < dim) z = load_once<typename Z::VV>(p + static_cast<int64_t>(j) * dim + d);
+              v[b][4 * s + j] = z;
+            }
+          }
+        }
+      };
+
+      f32x4 acc[NR][NB][E];
+      float top[NR], ref[NR], sum[NR];
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        top[n] = -INFINITY;
+        ref[n] = 0.f;
+        sum[n] = 0.f;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[n][b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      int t = k0 + TOK * wave;
+      if (t < k1) {
+        Tile tile = tile_at(t);
+        load_k(tile);
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        load_v(tile);
+        for (;;) {      // loads are not behind a branch (see k_attend): behind the last tile it is the one that is asked for again
+          const bool more = t + 4 * TOK < k1;
+          const Tile next = more ? tile_at(t + 4 * TOK) : tile;
+          f32x4 s[NR][SUB];
+          scores<T, D>(k, q, s);
+          load_k(next);
+          if (tile.seq >= 0 || tile.token + TOK > tile.last || holes) {
+            int q0 = 0, q1 = 0;      // the sequence's queries
+            if (tile.seq >= 0) {
+              q0 = kv.cu_q ? kv.cu_q[tile.seq] : tile.seq;
+              q1 = kv.cu_q ? kv.cu_q[tile.seq + 1] : tile.seq + 1;
+            }
+            int limit[NR];
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+              limit[n] = tile.seq < 0 ? tile.last : row_tok[n] < q0 || row_tok[n] >= q1 ? 0 : a.causal ? tile.last - (q1 - 1 - row_tok[n]) : tile.last;
+            }
+#pragma unroll
+            for (int y = 0; y < SUB; ++y) {
+              const int t4 = tile.token + 16 * y + 4 * g, left = tile.last - t4;
+              const int seen = left > 0 && id_of(tile, min(t4, tile.last - 1)) >= 0 ? left : 0;
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+#pragma unroll
+                for (int n = 0; n < NR; ++n) s[n][y][i] = i < min(seen, limit[n] - t4) ? s[n][y][i] : -INFINITY;
+#pragma unroll
+                for (int b = 0; b < NB; ++b) v[b][4 * y + i] = i < seen ? v[b][4 * y + i] : typename Z::VV{};
+              }
+            }
+          }
+          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum);
+          load_v(next);
+          asm volatile("" ::: "memory");
+          if (!more) break;
+          tile = next;
+          t += 4 * TOK;
+        }
+      }
+      finish<T, EXACT>(a, lds, acc, top, sum, RowsOf{u.tok0, hk, r0, rows}, whole, first_part ? -1 : mine.number, 0, queries, dim);
+    }
+    base += tiles * cost * kv.Hk;
+  }
+}
+
 // ---- many queries ----------------------------------------------------------------------------------
 // Where a tile has 128 rows the products bound the call, not the tokens' passage.  Each wavefront then has 32 rows of its own, and the
 // four read the same 64 tokens from LDS, into which they come by direct loads, one tile ahead.  MFMA 32x32: a lane has 16 tokens of one
@@ -593,10 +1166,6 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
   }
 }
 
-// Workgroups on a compute unit, by the registers of a wavefront.
-template <int D, int NRP>
-constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
-
 template <typename T, int D, int NRP, int NRO, bool EXACT>
 __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
   typedef Shape<T, D> Z;
@@ -759,21 +1328,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
         // What is asked for behind the last tile is the last token's row.
         for (int t = from + TOK * wave; t < to; t += 4 * TOK) {
           f32x4 s[NR][SUB];
-#pragma unroll
-          for (int n = 0; n < NR; ++n)
-#pragma unroll
-            for (int y = 0; y < SUB; ++y) {
-              s[n][y] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-              for (int x = 0; x < KC; ++x) {
-                if constexpr (kBf16) {
-                  s[n][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, k[y][x]), __builtin_bit_cast(bf16x8, q[n][x]), s[n][y], 0, 0, 0);
-                } else {
-#pragma unroll
-                  for (int z = 0; z < 4; ++z) s[n][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(k[y][x][z], q[n][x][z], s[n][y], 0, 0, 0);
-                }
-              }
-            }
+          scores<T, D>(k, q, s);
           load_k(hk, t + 4 * TOK, to);
           if (t + TOK > min(to, all_see) || holes) {
             // tokens that a row does not see, and what lies in the cache behind the last or in no page: no weight, and no value
@@ -790,61 +1345,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
               }
             }
           }
-          uint32_t w16[NR][4];
-          float w32[NR][4];
-#pragma unroll
-          for (int n = 0; n < NR; ++n) {
-            float high = -INFINITY;
-#pragma unroll
-            for (int y = 0; y < SUB; ++y)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) high = fmaxf(high, s[n][y][i]);
-            high *= to_log2;
-            if (__any(high > top[n] + kSlack)) {
-              high = fmaxf(high, __shfl_xor(high, 16, 64));
-              high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top[n]);
-              const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top[n] - now);
-              top[n] = high;
-              ref[n] = now;
-              sum[n] *= keep;
-#pragma unroll
-              for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int e = 0; e < E; ++e) acc[n][b][e] *= keep;
-            }
-            float p[4 * SUB];
-#pragma unroll
-            for (int y = 0; y < SUB; ++y)
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                p[4 * y + i] = __builtin_amdgcn_exp2f(fmaf(s[n][y][i], to_log2, -ref[n]));
-                sum[n] += p[4 * y + i];
-              }
-            if constexpr (kBf16) {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) w16[n][j] = pack_bf16x2(p[2 * j], p[2 * j + 1]);
-            } else {
-#pragma unroll
-              for (int j = 0; j < 4; ++j) w32[n][j] = p[j];
-            }
-          }
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int e = 0; e < E; ++e) {
-              if constexpr (kBf16) {
-                const bf16x8 vt = transposed(v[b], e);
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
-                  acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])),
-                                                                         acc[n][b][e], 0, 0, 0);
-              } else {
-#pragma unroll
-                for (int n = 0; n < NR; ++n)
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], acc[n][b][e], 0, 0, 0);
-              }
-            }
+          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum);
           load_v(hk, t + 4 * TOK, to);
           asm volatile("" ::: "memory");      // the loads stay on this side of the jump back
         }
@@ -858,77 +1359,9 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
         page0 = 0;
         staged = run.u;
       }
-      // The wavefronts' maxima and sums, and their products, which sixteen threads a row weigh and add up.
-#pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        sum[n] += __shfl_xor(sum[n], 16, 64);
-        sum[n] += __shfl_xor(sum[n], 32, 64);
-        if (g == 0) {
-          lds.ml[wave][16 * n + m][0] = top[n];
-          lds.ml[wave][16 * n + m][1] = sum[n];
-        }
-      }
-      // where a row's part lies: by its query and head, or with the workgroup's
-      const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq, by_group = static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1);
-#pragma unroll
-      for (int n = 0; n < NR; ++n) {
-        const int row = tid >> 4, r = r0 + 16 * n + row, tq = r / a.by_share, h = hk * a.share + r - tq * a.share;
-        const int64_t part = first_part ? by_query + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h : by_group + static_cast<int64_t>(run.number) * kMaxRows + (r - r0);
-        float f[4];
-#pragma unroll
-        for (int b = 0; b < NB; ++b) {
-          if (n || b) lds_barrier();
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int e = 0; e < E; e += 4)
-              *reinterpret_cast<f32x4*>(&lds.slab[wave][m][E * (4 * g + i) + e]) =
-                  f32x4{acc[n][b][e][i], acc[n][b][e + 1][i], acc[n][b][e + 2][i], acc[n][b][e + 3][i]};
-          lds_barrier();
-          if (b == 0) {
-            float high = -INFINITY, total = 0.f;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) high = fmaxf(high, lds.ml[w][16 * n + row][0]);
-            const float now = high == -INFINITY ? 0.f : high;
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-              f[w] = __builtin_amdgcn_exp2f(lds.ml[w][16 * n + row][0] - now);
-              total = fmaf(f[w], lds.ml[w][16 * n + row][1], total);
-            }
-            const float one = total == 0.f ? 0.f : __builtin_amdgcn_rcpf(total);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) f[w] *= one;
-            if ((tid & 15) == 0 && r < rows) {
-              const float x = total == 0.f ? -INFINITY : (now + __builtin_amdgcn_logf(total)) * kLn2;
-              if (!direct) a.part_lse[part] = x;
-              else if (a.lse) a.lse[static_cast<int64_t>(u.tok0 + tq) * a.Hq + h] = x;
-            }
-          }
-          const int d = E * (tid & 15);
-          if (r < rows && (EXACT || 16 * E * b + d < dim)) {
-            f32x4 o[E / 4];
-#pragma unroll
-            for (int e = 0; e < E / 4; ++e) {
-              f32x4 x[4];
-#pragma unroll
-              for (int w = 0; w < 4; ++w) x[w] = *reinterpret_cast<const f32x4*>(&lds.slab[w][row][d + 4 * e]) * f[w];
-              o[e] = (x[0] + x[1]) + (x[2] + x[3]);
-            }
-            if (direct) {
-              T* to = static_cast<T*>(a.out.data) + (u.tok0 + tq) * a.out.ts + h * a.out.hs + 16 * E * b + d;
-#pragma unroll
-              for (int e = 0; e < E / 4; ++e) {
-                if constexpr (kBf16) *reinterpret_cast<uint2*>(to + 4 * e) = make_uint2(pack_bf16x2(o[e][0], o[e][1]), pack_bf16x2(o[e][2], o[e][3]));
-                else *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
-              }
-            } else {
-              float* to = a.part_out + part * dim + 16 * E * b + d;
-#pragma unroll
-              for (int e = 0; e < E / 4; ++e) *reinterpret_cast<f32x4*>(to + 4 * e) = o[e];
-            }
-          }
-        }
-      }
+      const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
+      finish<T, EXACT>(a, lds, acc, top, sum, RowsOf{u.tok0, hk, r0, rows}, direct, first_part ? -1 : run.number, own && kv.n_group ? queries : 0,
+                       queries * (kv.n_group ? 2 : 1), dim);
     };
     if (own) body(std::integral_constant<int, NRO>{});
     else body(std::integral_constant<int, NRP>{});
@@ -1070,19 +1503,19 @@ __device__ void clear_token(const Args& a, int D, int t) {
     for (int h = lane; h < a.Hq; h += 64) a.lse[static_cast<int64_t>(t) * a.Hq + h] = -INFINITY;
 }
 
-// Without prefixes most runs are one workgroup's, and their rows in place.  Workgroup (w, y), w < joins, joins the rows y, y + gridDim.y, ..
-// (sixteens of them) of the run that workgroup w + 1 of the kernel before began inside, if it was the first to.  The others clear the rows
+// Where rows have no prefix, or it is in their own run, most runs are one workgroup's, and their rows in place.  The workgroups (w, y), w < joins, share the rows of the
+// run that workgroup w + 1 of the kernel before began inside, if it was the first to.  The others clear the rows
 // that no run has: those of sequences that have nothing to see, and of no sequence.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o, int joins) {
+__global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o, int joins, int n_units, int decode) {
   const int l = threadIdx.x & 15, D = kv.D, w = blockIdx.x + 1;
-  const int4 all = a.units[kv.n_seq];
+  const int4 all = a.units[n_units];
   if (blockIdx.x >= joins) {
     const int wave = threadIdx.x >> 6, first = ((blockIdx.x - joins) * gridDim.y + blockIdx.y) * 4 + wave, step = (gridDim.x - joins) * gridDim.y * 4;
     const int t0 = all.z ? a.n_tok : kv.cu_q ? kv.cu_q[0] : 0, t1 = all.z ? a.n_tok : kv.cu_q ? kv.cu_q[kv.n_seq] : a.n_tok;
     for (int t = first; t < t0; t += step) clear_token<T>(a, D, t);
     for (int t = t1 + first; t < a.n_tok; t += step) clear_token<T>(a, D, t);
-    for (int s = first; s < kv.n_seq; s += step) {
+    for (int s = first; s < n_units; s += step) {
       const int4 of = a.units[s];
       for (int t = of.z; of.y == 0 && t < of.z + of.w; ++t) clear_token<T>(a, D, t);      // nothing to see
     }
@@ -1092,7 +1525,7 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
   if (static_cast<int64_t>(w) * share >= total_cost) return;
   const int x = w * share;
   int u = 0;
-  for (int n = kv.n_seq; n > 1;) {      // the last unit that begins at x or in front of it
+  for (int n = n_units; n > 1;) {      // the last unit that begins at x or in front of it
     const int step = (n + 63) >> 6, lane = threadIdx.x & 63, at = lane * step;
     const int c = __popcll(__ballot(at < n && a.units[u + (at < n ? at : 0)].x <= x));
     u += (max(c, 1) - 1) * step;
@@ -1100,8 +1533,8 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
   }
   const int4 of = a.units[u];
   const Unit unit{of.z, of.w, of.y, 0};
-  const Cost costs = cost_of(unit, a.causal, a, rows_o);
-  const int head = head_cost(unit, a.causal, a, rows_o), hk = (x - of.x) / head;
+  const Cost costs = decode ? Cost{of.y, 0} : cost_of(unit, a.causal, a, rows_o);      // a decode's unit has its runs' cost for its length
+  const int head = costs.in_front(tiles_of(of.w, a.share, rows_o)), hk = (x - of.x) / head;
   int run0 = of.x + hk * head, tile = 0, cost = costs.first;
   if (costs.step == 0) {
     tile = (x - run0) / cost;
@@ -1112,41 +1545,62 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
   const int rows = of.w * a.share, r0 = tile * rows_o;
   const int n = (run0 + cost - 1) / share - w + 2;      // parts
   const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
-  for (int i = blockIdx.y * 16 + (threadIdx.x >> 4); i < rows_o && r0 + i < rows; i += gridDim.y * 16) {
+  // Few parts: sixteen lanes a row; many: a wavefront, four parts at a time.
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, slots = n <= 8 ? 1 : 4, slot = slots == 1 ? 0 : lane >> 4, rows_wave = 4 / slots;
+  for (int i0 = (blockIdx.y * 4 + wave) * rows_wave; i0 < rows_o && r0 + i0 < rows; i0 += gridDim.y * 4 * rows_wave) {
+    const int i = min(i0 + (slots == 1 ? lane >> 4 : 0), min(rows_o, rows - r0) - 1);      // behind the last: the last, once more
     const int tq = (r0 + i) / a.by_share, h = hk * a.share + r0 + i - tq * a.share;
     const int64_t row = static_cast<int64_t>(of.z + tq) * a.Hq + h;
     auto part_of = [&](int p) { return p == 0 ? row : queries + static_cast<int64_t>(w - 1 + p) * kMaxRows + i; };
     float high = -INFINITY;
-    for (int p = l; p < n; p += 16) high = larger(high, a.part_lse[part_of(p)]);
+    for (int p = slot * 16 + l; p < n; p += 16 * slots) high = larger(high, a.part_lse[part_of(p)]);
 #pragma unroll
-    for (int o = 8; o > 0; o >>= 1) high = larger(high, __shfl_xor(high, o, 64));
+    for (int o = 1; o < 64; o <<= 1)
+      if (o < 16 * slots) high = larger(high, __shfl_xor(high, o, 64));
     const float ref = high == -INFINITY ? 0.f : high;
     float total = 0.f, acc[kMaxHeadDim / 16] = {};
-#pragma unroll 2
-    for (int p = 0; p < n; ++p) {
-      const int64_t part = part_of(p);
-      const float weight = __builtin_amdgcn_exp2f((a.part_lse[part] - ref) * kLog2e);
-      total += weight;
+    for (int p0 = 0; p0 < n; p0 += 2 * slots) {      // two in flight
+      float weight[2];
+      f32x4 y[2][kMaxHeadDim / 64];
 #pragma unroll
-      for (int y = 0; y < kMaxHeadDim / 128; ++y) {
-        const int d = 128 * y + 8 * l;
-        if (d < D) {
-          const f32x4 y0 = *reinterpret_cast<const f32x4*>(a.part_out + part * D + d), y1 = *reinterpret_cast<const f32x4*>(a.part_out + part * D + d + 4);
+      for (int c = 0; c < 2; ++c) {
+        const int p = p0 + c * slots + slot;
+        const int64_t part = part_of(min(p, n - 1));
+        weight[c] = p < n ? a.part_lse[part] : -INFINITY;
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            acc[8 * y + e] = fmaf(weight, y0[e], acc[8 * y + e]);
-            acc[8 * y + 4 + e] = fmaf(weight, y1[e], acc[8 * y + 4 + e]);
+        for (int x = 0; x < kMaxHeadDim / 128; ++x)
+          if (128 * x + 8 * l < D) {
+            y[c][2 * x] = *reinterpret_cast<const f32x4*>(a.part_out + part * D + 128 * x + 8 * l);
+            y[c][2 * x + 1] = *reinterpret_cast<const f32x4*>(a.part_out + part * D + 128 * x + 8 * l + 4);
           }
-        }
+      }
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const float f = __builtin_amdgcn_exp2f((weight[c] - ref) * kLog2e);
+        total += f;
+#pragma unroll
+        for (int x = 0; x < kMaxHeadDim / 128; ++x)
+          if (128 * x + 8 * l < D)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[8 * x + e] = fmaf(f, y[c][2 * x + (e >> 2)][e & 3], acc[8 * x + e]);
       }
     }
+    if (slots == 4) {
+#pragma unroll
+      for (int o = 16; o < 64; o <<= 1) {
+        total += __shfl_xor(total, o, 64);
+#pragma unroll
+        for (int e = 0; e < kMaxHeadDim / 16; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+      }
+    }
+    if (slot) continue;
     const float f = total == 0.f ? 0.f : 1.f / total;
 #pragma unroll
     for (int e = 0; e < kMaxHeadDim / 16; ++e) acc[e] *= f;
     T* to = static_cast<T*>(a.out.data) + (of.z + tq) * a.out.ts + h * a.out.hs;
 #pragma unroll
-    for (int y = 0; y < kMaxHeadDim / 128; ++y)
-      if (128 * y + 8 * l < D) store8(to + 128 * y + 8 * l, acc + 8 * y);
+    for (int x = 0; x < kMaxHeadDim / 128; ++x)
+      if (128 * x + 8 * l < D) store8(to + 128 * x + 8 * l, acc + 8 * x);
     if (a.lse && l == 0) a.lse[row] = total == 0.f ? -INFINITY : high + logf(total);
   }
 }
@@ -1180,29 +1634,30 @@ struct Choice {
   int rows_p, rows_o, per_unit, lds;
 };
 
+// Rows of a prefix (or, without prefixes, of a sequence) on average, and of a sequence at most.
 template <typename T, int D, bool EXACT>
-Choice choose_of(int rows_p, int rows_o) {
+Choice choose_of(int rows_p, int rows_o, bool decode) {
   constexpr int kMost = sizeof(T) == 4 || D == 256 ? 2 : 4;
-  if constexpr (!EXACT) {
-    return {k_attend<T, D, kMost, kMost, false>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
-  } else {
-    if constexpr (sizeof(T) == 2 && D <= 128)
-      if (rows_o > 16) return {k_attend_wide<D>, kWideRows, kWideRows, 2, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
-    if (rows_o > 16) return {k_attend<T, D, kMost, kMost, true>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
-    if (rows_p > 32 && kMost == 4) return {k_attend<T, D, kMost, 1, true>, 16 * kMost, 16, kPerUnit<D, kMost>, 0};
-    if (rows_p > 16) return {k_attend<T, D, 2, 1, true>, 32, 16, kPerUnit<D, 2>, 0};
-    return {k_attend<T, D, 1, 1, true>, 16, 16, kPerUnit<D, 1>, 0};
+  if (decode) {
+    if constexpr (EXACT) {
+      if (rows_p <= 16) return {k_decode<T, D, 1, true>, 16, 16, kPerUnit<D, 1>, 0};
+      if (rows_p <= 32 || kMost == 2) return {k_decode<T, D, 2, true>, 32, 32, kPerUnit<D, 2>, 0};
+    }
+    return {k_decode<T, D, kMost, EXACT>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
   }
+  if constexpr (EXACT && sizeof(T) == 2 && D <= 128)
+    if (rows_o > 16) return {k_attend_wide<D>, kWideRows, kWideRows, 2, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
+  return {k_attend<T, D, kMost, kMost, EXACT>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
 }
 
 template <typename T>
-Choice choose(int D, int rows_p, int rows_o) {
-  if (D == 64) return choose_of<T, 64, true>(rows_p, rows_o);
-  if (D == 128) return choose_of<T, 128, true>(rows_p, rows_o);
-  if (D == 256) return choose_of<T, 256, true>(rows_p, rows_o);
-  if (D < 64) return choose_of<T, 64, false>(rows_p, rows_o);
-  if (D < 128) return choose_of<T, 128, false>(rows_p, rows_o);
-  return choose_of<T, 256, false>(rows_p, rows_o);
+Choice choose(int D, int rows_p, int rows_o, bool decode) {
+  if (D == 64) return choose_of<T, 64, true>(rows_p, rows_o, decode);
+  if (D == 128) return choose_of<T, 128, true>(rows_p, rows_o, decode);
+  if (D == 256) return choose_of<T, 256, true>(rows_p, rows_o, decode);
+  if (D < 64) return choose_of<T, 64, false>(rows_p, rows_o, decode);
+  if (D < 128) return choose_of<T, 128, false>(rows_p, rows_o, decode);
+  return choose_of<T, 256, false>(rows_p, rows_o, decode);
 }
 
 }  // namespace
@@ -1236,12 +1691,18 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   const int64_t all_rows = static_cast<int64_t>(n_tok) * share;
   const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
   auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
-  const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, small(rows_p), small(rows_o)) : choose<float>(kv->D, small(rows_p), small(rows_o));
+  const auto cost_of_pages = [&](int64_t pages) { return static_cast<double>(pages) * kv->page_size / 8 + 8 + kRunCost + kMinShare; };
+  // Few rows a sequence, as many sequences as LDS has places for, their blocks counted in 26 bits and all costs in 30.
+  const double decode_most = kv->Hk * ((all_rows / 16 + kv->n_group + kv->n_seq) * cost_of_pages(kv->max_prefix_pages) + kv->n_seq * cost_of_pages(kv->max_pages));
+  const bool decode = rows_o <= 16 && kv->n_seq <= kDecodeSeqs && static_cast<int64_t>(kv->n_seq + 1) * kv->max_pages * kv->page_size < 1 << 30 &&
+                      decode_most < 1 << 30;
+  const int rows_u = small(kv->n_group ? rows_p : rows_o);
+  const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, rows_u, small(rows_o), decode) : choose<float>(kv->D, rows_u, small(rows_o), decode);
   const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
   // an upper bound of all costs together, which are counted in 32 bits
   const int64_t tiles_p = kv->n_group ? all_rows / k.rows_p + kv->n_group : 0, tiles_o = all_rows / k.rows_o + kv->n_seq;
-  const auto blocks_of = [&](int64_t pages) { return pages * kv->page_size / 8 + 2 + kRunCost; };
-  double most = (static_cast<double>(tiles_p) * blocks_of(kv->max_prefix_pages) + static_cast<double>(tiles_o) * blocks_of(kv->max_pages)) * kv->Hk;
+  double most = decode ? kv->Hk * ((tiles_o + tiles_p) * (kRunCost + 8.0) + tiles_p * cost_of_pages(kv->max_prefix_pages) + kv->n_seq * cost_of_pages(kv->max_pages))
+                       : kv->Hk * (tiles_p * cost_of_pages(kv->max_prefix_pages) + tiles_o * cost_of_pages(kv->max_pages));
   for (; most > 1 << 30; most /= 2) ++args.coarse;
   args.rise = k.rows_o / (8 * share) >> args.coarse;
   // Where there are workgroups enough, costs are whole shares, so that a run begins with a workgroup: four candidates 13.2 us, so 8.5.
@@ -1255,11 +1716,12 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   ATG_LAUNCH_CHECK();
   const bool bf16 = kv->dtype == AT_GRPO_BF16;
   const int64_t outputs = static_cast<int64_t>(n_tok) * Hq;
-  if (kv->n_group == 0) {
-    const int y = k.rows_o / 16 < 4 ? k.rows_o / 16 : 4, joins = static_cast<int>(blocks) - 1;
-    const int64_t clears = ceil_div(kv->n_seq + 1, 4 * y);
+  if (kv->n_group == 0 || decode) {
+    const int n_units = kv->n_seq + kv->n_group;
+    const int y = 4, joins = static_cast<int>(blocks) - 1;
+    const int64_t clears = ceil_div(n_units + 1, 4 * y);
     hipLaunchKernelGGL(bf16 ? k_join_runs<bf16_t> : k_join_runs<float>, dim3(static_cast<unsigned>(joins + (clears < 256 ? clears : 256)), y), dim3(256), 0, s,
-                       view, args, k.rows_o, joins);
+                       view, args, k.rows_o, joins, n_units, decode);
   } else if (outputs <= 1024) {      // few rows: a workgroup for each
     hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 4> : k_join<float, 4>), dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows_p, k.rows_o);
   } else {
