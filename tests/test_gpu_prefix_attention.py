@@ -303,3 +303,84 @@ def test_workspace_sizes_and_refusals_on_the_host():
         got = [size(**{key: v, "cu_q": 4096}) for v in values]
         assert got == sorted(got) and got[0] > 0, key
     assert size(n_group=0) <= size(n_group=1)
+
+
+def repeated(dev, dtype, Hk, D, page, distinct, columns, used, seed=0):
+    """A cache of `distinct` pages and a table of `columns` of them in turn (`used` tokens): what a softmax over it gives is that over the
+    distinct tokens, if each comes as often."""
+    rs = np.random.default_rng(seed)
+    dt = DTYPES[dtype]
+    k, v = (rounded(rs.normal(size=(distinct, Hk, page, D)), dt) for _ in range(2))
+    table = torch.arange(columns, device=dev, dtype=torch.int32) % distinct
+    flat = lambda c: c.transpose(0, 2, 1, 3).reshape(distinct * page, Hk, D)
+    return k, v, flat(k), flat(v), table, dt
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new,max_q", [(1, 1), (1, 64), (3, 64)], ids=["decode", "many", "message"])
+@pytest.mark.parametrize("own", [False, True], ids=["prefix", "own"])
+def test_more_pages_than_a_list_holds(gpu_device, dtype, new, max_q, own):
+    """Nine million tokens in pages of 8: whatever a workgroup has of them is more pages than it keeps ids of.  One id in a thousand is
+    none of the cache's in the second pass, that of a whole distinct page, which is then not seen."""
+    Hk, Hq, D, page, distinct = 1, 2, 64, 8, 40
+    columns = 40 * 28000
+    n = columns * page
+    k, v, fk, fv, table, dt = repeated(gpu_device, dtype, Hk, D, page, distinct, columns, n)
+    rs = np.random.default_rng(1)
+    q64 = rounded(rs.normal(size=(new, Hq, D)), dt)
+    q = to_dev(q64, dt, gpu_device)
+    for hole in (False, True):
+        t = torch.where(table == 7, distinct + 5, table) if hole else table
+        keep = np.array([i // page != 7 for i in range(distinct * page)]) if hole else np.ones(distinct * page, dtype=bool)
+        kw = dict(cu_q=i32([0, new], gpu_device))
+        if own:
+            kv = api.KVBatch(to_dev(k, dt, gpu_device), to_dev(v, dt, gpu_device), t[None].contiguous(), i32([n], gpu_device), **kw)
+        else:
+            kv = api.KVBatch(to_dev(k, dt, gpu_device), to_dev(v, dt, gpu_device), i32([[0]], gpu_device), i32([0], gpu_device),
+                             group_seq=i32([0, 1], gpu_device), prefix_len=i32([n], gpu_device), prefix_pages=t[None].contiguous(), **kw)
+        word = torch.zeros(1, dtype=torch.int32, device=gpu_device)
+        out = attend(kv, q, causal=False, max_q=max_q, want_lse=True, data_error=word)
+        assert int(word) == (32 if hole else 0)
+        o, lse, mag, big = oracle.attention(q64, fk[keep], fv[keep], D ** -0.5, [int(keep.sum())] * new)
+        bo, bl = attention_bounds(dt, D, o, mag, big, np.full(new, n))
+        assert_within(host64(out["out"]), o, bo, "out")
+        assert_within(host64(out["lse"]), lse + np.log(columns / distinct), bl + 1e-5, "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("new", [None, [2, 9, 40]])
+def test_tables_far_wider_than_what_is_in_them(gpu_device, dtype, new):
+    """Costs are counted in larger blocks where their bound passes 32 bits: it goes by the tables' columns."""
+    p = Paged(dtype, 2, 64, 16, [50, 90, 70], new, [2], [3000], seed=8)
+    q64 = p.queries(4)
+    wide = torch.full((1, 1 << 25), -1, dtype=torch.int32, device=gpu_device)
+    wide[:, :p.prefix_pages.shape[1]] = i32(p.prefix_pages, gpu_device)
+    out = attend(p.device(gpu_device, prefix_pages=wide), to_dev(q64, p.dtype, gpu_device), max_q=int(p.new.max()), want_lse=True)
+    check(p, q64, out, p.attention(q64, 0.125))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_seq,size", [(1024, [300, 0, 1, 723]), (1025, [65] * 15 + [50]), (1300, [1] * 600), (700, [])])
+def test_many_sequences(gpu_device, n_seq, size):
+    """On both sides of the number of sequences and units that are kept in LDS, in groups of more sequences than lanes and rows."""
+    rs = np.random.default_rng(n_seq)
+    length = rs.integers(0, 40, n_seq)
+    length[::97] = 0
+    p = Paged("bf16", 1, 64, 16, length, None, size, rs.integers(0, 90, len(size)), seed=2)
+    q64 = p.queries(2)
+    out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), causal=False, want_lse=True)
+    check(p, q64, out, p.attention(q64, 0.125, causal=False))
+    out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), want_lse=True)
+    check(p, q64, out, p.attention(q64, 0.125))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_new_tokens_than_the_bound(gpu_device, dtype):
+    """max_q only picks the kernel."""
+    p = Paged(dtype, 2, 64, 16, [150, 90, 70, 200], [100, 3, 20, 1], [2, 2], [130, 40], seed=8)
+    q64 = p.queries(4)
+    out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), max_q=1, want_lse=True)
+    check(p, q64, out, p.attention(q64, 0.125))
