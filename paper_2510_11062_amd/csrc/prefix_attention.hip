@@ -3,14 +3,17 @@
 //   out = sum_i p_i v_i / sum_i p_i,  p_i = exp(scale <q, k_i> - m)  over the visible tokens i
 //
 // in one pass with a running maximum m.  What there is to read is the keys and values, and where few queries read them their passage
-// from memory bounds the call.  Hence units of work that read a token once for all queries that see it: the prefix of a group with the
-// queries of all its sequences, and a sequence's own tokens with its queries.  A unit's rows are its queries times the Hq / Hk heads
-// that share a key head, cut into tiles of 16 to 64; a tile's passage over a unit's tokens for one key head is a run.  The runs of the
-// whole batch, one behind the other, are dealt to the workgroups in equal shares of 64-token blocks, wherever that cuts a run: long
-// prompts and ragged responses fill the chip alike, whatever their lengths, which only the device knows.  A second kernel joins the
-// parts of a row: that of its prefix, that of its own tokens, and those of the workgroups that began in the middle of its run.
+// from memory bounds the call; with many queries the products do.  Hence units of work that read a token once for all queries that see
+// it.  A unit's rows are its queries times the Hq / Hk heads that share a key head, cut into tiles of 16 to 128; a tile's passage over a
+// unit's tokens for one key head is a run.  The runs of the whole batch, one behind the other, are dealt to the workgroups in shares of
+// equal cost, wherever that cuts a run: long prompts and ragged responses fill the chip alike, whatever their lengths, which only the
+// device knows.  A second kernel joins the parts of a row.  Three kernels, by the rows of a sequence:
+//   k_decode        at most 16: a unit is a group, whose rows read its prefix and then its sequences' own tokens as one stream
+//   k_attend        more, and where k_decode's tables end: units are the prefix of a group with the queries of all its sequences, and a
+//                   sequence's own tokens with its queries
+//   k_attend_wide   k_attend for bf16 and heads of 64 and 128, tiles of 128 rows
 //
-// A wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
+// In the first two a wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
 //   S^T = K Q^T     MFMA 16x16: tokens down, queries across, so that a lane has four consecutive tokens of one query
 //   P^T             is at once the second product's operand: no lane needs a weight that another one computed
 //   O^T += V^T P^T  a lane loads whole rows of V, eight elements of eight tokens, and transposes that block by itself
@@ -145,7 +148,7 @@ struct Share {
 };
 
 // The costs of all units, a contiguous part of them on each thread, and the workgroup's share of them; the same in every workgroup.
-template <int RP, int RO>
+template <int R>
 __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
   const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int u0 = min(n, tid * per), u1 = min(n, u0 + per);
@@ -154,7 +157,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
   for (int u = u0; u < u1; ++u) {
     const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
     if (u < kCachedUnits) S.cache[u] = x;
-    mine += head_cost(x, a.causal && u >= kv.n_group, a, u < kv.n_group ? RP : RO) * kv.Hk;
+    mine += head_cost(x, a.causal && u >= kv.n_group, a, R) * kv.Hk;
   }
   int sum = mine;      // of the threads up to this one
 #pragma unroll
@@ -188,7 +191,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
     for (int u = u0; u < u1; ++u) {
       Unit x{0, 0, 0, 0};
       if (!none) x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-      const int c = head_cost(x, a.causal && u >= kv.n_group, a, u < kv.n_group ? RP : RO);
+      const int c = head_cost(x, a.causal && u >= kv.n_group, a, R);
       a.units[u] = make_int4(base, x.len, x.tok0, x.ntok);
       base += c * kv.Hk;
     }
@@ -198,7 +201,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
     int base = first, u = u0;
     for (;; ++u) {
       const Unit x = u < kCachedUnits ? S.cache[u] : unit_of(kv, u, a.n_tok, &error, &falls);
-      const int c = head_cost(x, a.causal && u >= kv.n_group, a, u < kv.n_group ? RP : RO) * kv.Hk;
+      const int c = head_cost(x, a.causal && u >= kv.n_group, a, R) * kv.Hk;
       if (at < base + c) break;
       base += c;
     }
@@ -210,7 +213,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
 }
 
 // The runs of a workgroup's share, one after the other: everything in it is uniform.
-template <int RP, int RO>
+template <int R>
 struct Runs {
   const KvView& kv;
   const Args& a;
@@ -220,7 +223,7 @@ struct Runs {
   Unit x;
   bool own, steps;
   Cost costs;
-  int rows, tiles, hk, tile, run0, cost;
+  int tiles, hk, tile, run0, cost;
 
   __device__ __forceinline__ Runs(const KvView& kv_, const Args& a_, const Schedule& S_, const Share& mine)
       : kv(kv_), a(a_), S(S_), number(mine.number), at(mine.at), stop(mine.stop) {
@@ -272,9 +275,8 @@ struct Runs {
     x.row = __builtin_amdgcn_readfirstlane(x.row);
     own = u >= kv.n_group;
     steps = own && a.causal;
-    rows = own ? RO : RP;
-    tiles = tiles_of(x.ntok, a.share, rows);
-    costs = cost_of(x, steps, a, rows);
+    tiles = tiles_of(x.ntok, a.share, R);
+    costs = cost_of(x, steps, a, R);
     cost = costs.first;
     unit_stop = min(stop, base + costs.in_front(tiles) * kv.Hk);
   }
@@ -284,10 +286,10 @@ struct Runs {
 struct TileRun {
   int hk, r0, k0, k1;
 };
-template <typename R>
-__device__ __forceinline__ TileRun tile_run(const R& r, const Args& a) {
-  const int end = end_of(r.x, r.steps, a, r.tile, r.rows);
-  return TileRun{r.hk, r.tile * r.rows, cut(r.from(), r.cost, end), cut(r.to(), r.cost, end)};
+template <int R>
+__device__ __forceinline__ TileRun tile_run(const Runs<R>& r, const Args& a) {
+  const int end = end_of(r.x, r.steps, a, r.tile, R);
+  return TileRun{r.hk, r.tile * R, cut(r.from(), r.cost, end), cut(r.to(), r.cost, end)};
 }
 
 // What a lane (m, g) = (lane & 15, lane >> 4) holds of a tile of TOK tokens.
@@ -322,6 +324,25 @@ __device__ __forceinline__ bf16x8 transposed(const VV (&v)[8], int e) {
   return __builtin_bit_cast(bf16x8, make_uint4(o[0], o[1], o[2], o[3]));
 }
 
+// The largest magnitude as an integer, of two bfloat16 a word or of float32: infinities and NaN are above every number.
+typedef unsigned short Halves __attribute__((ext_vector_type(2)));
+template <typename V>
+__device__ __forceinline__ uint32_t largest_bits(uint32_t high, const V& v) {
+  if constexpr (std::is_same<V, f32x4>::value) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) high = max(high, __float_as_uint(v[i]) & 0x7fffffffu);
+  } else {
+#pragma unroll
+    for (int i = 0; i < static_cast<int>(sizeof(V) / 4); ++i)
+      high = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(Halves, high), __builtin_bit_cast(Halves, dword(v, i) & 0x7fff7fffu)));
+  }
+  return high;
+}
+template <typename T>
+__device__ __forceinline__ bool not_finite(uint32_t high) {
+  return sizeof(T) == 4 ? high >= 0x7f800000u : (high & 0xffffu) >= 0x7f80u || high >= 0x7f800000u;
+}
+
 struct Lds {
   Schedule S;
   int pages[2][kPageSlots];
@@ -330,7 +351,7 @@ struct Lds {
   float slab[4][16][128 + 4];
 };
 
-// 16 or 8 bytes that nothing reads again while the caches hold them: keys and values of a decode, 117 us for 32 groups without, so 106.
+// 16 or 8 bytes that nothing reads again while the caches hold them: keys and values of a decode, 117 us for 32 groups, then 106.
 template <typename V>
 __device__ __forceinline__ V load_once(const void* p) {
   typedef float Words __attribute__((ext_vector_type(sizeof(V) / 4)));
@@ -338,9 +359,9 @@ __device__ __forceinline__ V load_once(const void* p) {
 }
 
 // S^T = K Q^T of a tile.
-template <typename T, int D, int NR, int NRM>
+template <typename T, int D, int NR>
 __device__ __forceinline__ void scores(const typename Shape<T, D>::KV (&k)[Shape<T, D>::SUB][Shape<T, D>::KC],
-                                       const typename Shape<T, D>::KV (&q)[NRM][Shape<T, D>::KC], f32x4 (&s)[NR][Shape<T, D>::SUB]) {
+                                       const typename Shape<T, D>::KV (&q)[NR][Shape<T, D>::KC], f32x4 (&s)[NR][Shape<T, D>::SUB]) {
   constexpr int SUB = Shape<T, D>::SUB, KC = Shape<T, D>::KC;
 #pragma unroll
   for (int n = 0; n < NR; ++n)
@@ -359,11 +380,12 @@ __device__ __forceinline__ void scores(const typename Shape<T, D>::KV (&k)[Shape
     }
 }
 
-// The tile's weights into the sums, and their products with its values into the accumulators.
+// The tile's weights into the sums, and their products with its values into the accumulators.  A weight of 0 does not keep an infinite or NaN
+// value out of a product: a tile that holds one and is not of all rows is `apart`, and only the rows of which `of_row` says so take its products.
 template <typename T, int D, int NR>
-__device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::SUB], const typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
+__device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::SUB], typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
                                               float to_log2, f32x4 (&acc)[NR][Shape<T, D>::NB][Shape<T, D>::E], float (&top)[NR], float (&ref)[NR],
-                                              float (&sum)[NR]) {
+                                              float (&sum)[NR], bool apart, const bool (&of_row)[NR]) {
   typedef Shape<T, D> Z;
   constexpr int E = Z::E, NB = Z::NB, SUB = Z::SUB;
   constexpr bool kBf16 = sizeof(T) == 2;
@@ -405,22 +427,42 @@ __device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::
       for (int j = 0; j < 4; ++j) w32[n][j] = p[j];
     }
   }
+  auto product = [&](int n, int b, int e, bf16x8 vt, f32x4 x) {
+    if constexpr (kBf16) {
+      return __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])), x, 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], x, 0, 0, 0);
+      return x;
+    }
+  };
+  if (apart) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        bf16x8 vt;
+        if constexpr (kBf16) vt = transposed(v[b], e);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          const f32x4 x = product(n, b, e, vt, f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[n][b][e][i] += of_row[n] ? x[i] : 0.f;
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < 4 * SUB; ++j) v[b][j] = typename Z::VV{};
+    }
+  }
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      if constexpr (kBf16) {
-        const bf16x8 vt = transposed(v[b], e);
+      bf16x8 vt;
+      if constexpr (kBf16) vt = transposed(v[b], e);
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
-          acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])),
-                                                                 acc[n][b][e], 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int n = 0; n < NR; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[n][b][e] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[b][i][e], w32[n][i], acc[n][b][e], 0, 0, 0);
-      }
+      for (int n = 0; n < NR; ++n) acc[n][b][e] = product(n, b, e, vt, acc[n][b][e]);
     }
 }
 
@@ -507,16 +549,20 @@ __device__ __forceinline__ void finish(const Args& a, L& lds, const f32x4 (&acc)
 }
 
 // Workgroups on a compute unit, by the registers of a wavefront.
-template <int D, int NRP>
-constexpr int kPerUnit = D == 256 || D * NRP >= 512 ? 1 : 2;
+template <int D, int NR>
+constexpr int kPerUnit = D == 256 || D * NR >= 512 ? 1 : 2;
 
 // ---- one new token, or few, in each sequence ---------------------------------------------------------
 // Here a sequence has no more rows than a tile, and all rows of a group read one stream of tokens: the prefix, then the own tokens of its
 // sequences one behind the other, each beginning a block of 32; a row's scores for other sequences' tokens have no weight.  A unit is a
 // group, or a sequence in none; with as many tiles of rows as it has, each reads the prefix and its own sequences.  What a row needs is
 // in one run, so rows of runs that one workgroup had whole are done, and a run for each sequence and head, most of whose time would be
-// its beginning and end, is saved: 32 groups of up to 8 DECTREE us, with runs of prefixes and of sequences 120 and 11 for their joining.
-constexpr int kDecodeSeqs = 1024;     // sequences whose places are kept in LDS
+// its beginning and end, is saved: 32 groups of up to 8 take 108 us
+// (540 MB, 5.0 TB/s) and 7 for their joining, with runs of prefixes and of sequences 120 and 11; two groups behind 40000 tokens 62 and 9 (5.3 TB/s),
+// one group of four 10 and 4.
+// Sequences whose places are kept in LDS, which is at most 64 KB so.  1280 behind prefixes of 600 tokens with 64 of their own, 32 heads on 8 of
+// 128: 175 us, by k_attend 268.
+constexpr int kDecodeSeqs = 1792;
 constexpr int kDecodeUnits = 256;     // units
 constexpr int kDecodeSlots = 2048;    // page ids of a share of a run; beyond that they are read where they lie
 
@@ -865,31 +911,41 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
           f32x4 s[NR][SUB];
           scores<T, D>(k, q, s);
           load_k(next);
+          bool of_row[NR], apart = false;      // whether the tile is the row's sequence's
           if (tile.seq >= 0 || tile.token + TOK > tile.last || holes) {
-            int q0 = 0, q1 = 0;      // the sequence's queries
-            if (tile.seq >= 0) {
-              q0 = kv.cu_q ? kv.cu_q[tile.seq] : tile.seq;
-              q1 = kv.cu_q ? kv.cu_q[tile.seq + 1] : tile.seq + 1;
-            }
-            int limit[NR];
+            int left[NR];
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-              limit[n] = tile.seq < 0 ? tile.last : row_tok[n] < q0 || row_tok[n] >= q1 ? 0 : a.causal ? tile.last - (q1 - 1 - row_tok[n]) : tile.last;
+            for (int n = 0; n < NR; ++n) left[n] = tile.last - tile.token;
+            if (tile.seq >= 0) {
+              const int q0 = kv.cu_q ? kv.cu_q[tile.seq] : tile.seq, q1 = kv.cu_q ? kv.cu_q[tile.seq + 1] : tile.seq + 1;      // the sequence's queries
+#pragma unroll
+              for (int n = 0; n < NR; ++n) {
+                of_row[n] = row_tok[n] >= q0 && row_tok[n] < q1;
+                left[n] = of_row[n] ? left[n] - (a.causal ? q1 - 1 - row_tok[n] : 0) : 0;
+              }
             }
 #pragma unroll
             for (int y = 0; y < SUB; ++y) {
-              const int t4 = tile.token + 16 * y + 4 * g, left = tile.last - t4;
-              const int seen = left > 0 && id_of(tile, min(t4, tile.last - 1)) >= 0 ? left : 0;
+              const int at = 16 * y + 4 * g, t4 = tile.token + at, last = tile.last - t4;
+              const int seen = last > 0 && id_of(tile, min(t4, tile.last - 1)) >= 0 ? last : 0;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
 #pragma unroll
-                for (int n = 0; n < NR; ++n) s[n][y][i] = i < min(seen, limit[n] - t4) ? s[n][y][i] : -INFINITY;
+                for (int n = 0; n < NR; ++n) s[n][y][i] = i < min(seen, left[n] - at) ? s[n][y][i] : -INFINITY;
 #pragma unroll
                 for (int b = 0; b < NB; ++b) v[b][4 * y + i] = i < seen ? v[b][4 * y + i] : typename Z::VV{};
               }
             }
+            if (tile.seq >= 0 && seq1 - seq0 > 1) {
+              uint32_t high = 0;
+#pragma unroll
+              for (int b = 0; b < NB; ++b)
+#pragma unroll
+                for (int j = 0; j < VJ; ++j) high = largest_bits(high, v[b][j]);
+              apart = __any(not_finite<T>(high));
+            }
           }
-          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum);
+          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, apart, of_row);
           load_v(next);
           asm volatile("" ::: "memory");
           if (!more) break;
@@ -906,7 +962,8 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
 // ---- many queries ----------------------------------------------------------------------------------
 // Where a tile has 128 rows the products bound the call, not the tokens' passage.  Each wavefront then has 32 rows of its own, and the
 // four read the same 64 tokens from LDS, into which they come by direct loads, one tile ahead.  MFMA 32x32: a lane has 16 tokens of one
-// query in S^T, which are P^T's operand as they are, and V^T's operand comes from rows of V by transposing reads.
+// query in S^T, which are P^T's operand as they are, and V^T's operand comes from rows of V by transposing reads.  Eight prompts of 763 to
+// 2048 tokens, 16 heads on 8 of 128: 84 us and 15 for joining what was cut, 620 TFLOP/s in the kernel; a large product makes 1216.
 //
 // A token's row is 2 D bytes in LDS; its 16-byte pieces are exchanged so that the reads meet no bank twice: piece c of K's row r lies at
 // c ^ (r & 15) (64-wide heads, whose rows take turns in the banks' halves: c ^ ((r >> 1) & 7)), of V's at c ^ 2 (r & 7) (c ^ 2 ((r >> 1) & 3)).
@@ -928,8 +985,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
   extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
   WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * TB);
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 31, g = lane >> 5;
-  const Share mine = make_schedule<kWideRows, kWideRows>(kv, a, lds.S);
-  Runs<kWideRows, kWideRows> run(kv, a, lds.S, mine);
+  const Share mine = make_schedule<kWideRows>(kv, a, lds.S);
+  Runs<kWideRows> run(kv, a, lds.S, mine);
   if (!run.valid()) return;
 
   // where this lane reads: K piece 2 c + g of row m (XOR 32 c), V four elements of row 4 g + (lane & 15) / 4 (XOR 64 t)
@@ -1042,7 +1099,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
         // Fragments are read a group ahead of the products that take them: left to itself the compiler reads each right in front of its own,
-        // and every product waits for LDS (103 us for eight prompts of up to 2048 tokens, so NOWUS).
+        // and every product waits for LDS (103 us for eight prompts of up to 2048 tokens, then 90).
         bf16x8 f[2][4];
         auto read_k_group = [&](int x) {      // two steps of 16 elements, two blocks of 32 tokens
 #pragma unroll
@@ -1166,16 +1223,16 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
   }
 }
 
-template <typename T, int D, int NRP, int NRO, bool EXACT>
-__global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, Args a) {
+template <typename T, int D, int NR, bool EXACT>
+__global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_attend(KvView kv, Args a) {
   typedef Shape<T, D> Z;
-  constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, NRM = NRP > NRO ? NRP : NRO;
+  constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, R = 16 * NR;
   constexpr bool kBf16 = sizeof(T) == 2;
   __shared__ Lds lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
   const int dim = EXACT ? D : kv.D;
-  const Share mine = make_schedule<16 * NRP, 16 * NRO>(kv, a, lds.S);
-  Runs<16 * NRP, 16 * NRO> run(kv, a, lds.S, mine);
+  const Share mine = make_schedule<R>(kv, a, lds.S);
+  Runs<R> run(kv, a, lds.S, mine);
   if (!run.valid()) return;
   const uint32_t page_step = static_cast<uint32_t>(kv.Hk * dim) << kv.page_shift;      // elements of a page of all heads
   const int in_page = (1 << kv.page_shift) - 1;
@@ -1212,7 +1269,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
   };
   auto fits = [&](const Unit& x) { return ((x.len - 1) >> kv.page_shift) < kPageSlots; };
 
-  typename Z::KV q[NRM][KC], k[SUB][KC];
+  typename Z::KV q[NR][KC], k[SUB][KC];
   typename Z::VV v[NB][VJ];
   auto row_of = [&](int token, int to) {      // a token behind the last stands for it
     const int i = min(token, to - 1), id = max(0, pages[(i >> kv.page_shift) - page0]);
@@ -1249,9 +1306,9 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
       }
     }
   };
-  auto load_q = [&](const Unit& u, const TileRun& w, auto nr) {
+  auto load_q = [&](const Unit& u, const TileRun& w) {
 #pragma unroll
-    for (int n = 0; n < decltype(nr)::value; ++n) {
+    for (int n = 0; n < NR; ++n) {
       const int r = min(w.r0 + 16 * n + m, u.ntok * a.share - 1), tq = r / a.by_share, h = w.hk * a.share + r - tq * a.share;
       const T* from = static_cast<const T*>(a.q.data) + (u.tok0 + tq) * a.q.ts + h * a.q.hs;
 #pragma unroll
@@ -1287,8 +1344,9 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
     int ids[kPageSlots / 256];
     if (turn) get_ids(ids, table_of(run.x, run.own), slots(0, run.x.len));
 
-    auto body = [&](auto nr) {
-      constexpr int NR = decltype(nr)::value, R = 16 * NR;
+    // Twice: where all rows see all tokens nothing is kept for each.  Prompts, heads of 96: 646 us in one, 579 so.
+    auto body = [&](auto causal) {
+      constexpr bool steps = decltype(causal)::value;
       const int rows = u.ntok * a.share, hk = w.hk, r0 = w.r0, k0 = w.k0, k1 = w.k1, first = u.len - u.ntok + 1;
       const int all_see = steps ? first + r0 / a.by_share : k1;
       int limit[NR];
@@ -1306,7 +1364,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
 #pragma unroll
           for (int e = 0; e < E; ++e) acc[n][b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      load_q(u, w, nr);
+      load_q(u, w);
       for (int from = k0; from < k1;) {
         int to = k1;
         if (!whole) {      // a part of the list at a time
@@ -1345,7 +1403,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
               }
             }
           }
-          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum);
+          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, false, {});
           load_v(hk, t + 4 * TOK, to);
           asm volatile("" ::: "memory");      // the loads stay on this side of the jump back
         }
@@ -1363,8 +1421,8 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NRP>)) void k_attend(KvView kv, A
       finish<T, EXACT>(a, lds, acc, top, sum, RowsOf{u.tok0, hk, r0, rows}, direct, first_part ? -1 : run.number, own && kv.n_group ? queries : 0,
                        queries * (kv.n_group ? 2 : 1), dim);
     };
-    if (own) body(std::integral_constant<int, NRO>{});
-    else body(std::integral_constant<int, NRP>{});
+    if (steps) body(std::true_type{});
+    else body(std::false_type{});
     if (!more) break;
     lds_barrier();      // what was added up has been read
     w = next;
@@ -1388,7 +1446,7 @@ __device__ __forceinline__ void store8(T* to, const float* y) {
 
 // Rows behind prefixes: WAVES wavefronts of a workgroup for each query and head, sixteen lanes for the elements of a part.
 template <typename T, int WAVES>
-__global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int rows_o) {
+__global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int tile_rows) {
   __shared__ float lds[WAVES == 1 ? 1 : 4][kMaxHeadDim + 1];
   const int lane = threadIdx.x & 63, l = lane & 15, slot = lane >> 4, wave = threadIdx.x >> 6, mine = WAVES == 1 ? 0 : wave, D = kv.D;
   const int64_t unit = WAVES == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
@@ -1412,8 +1470,8 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int rows_p, int
     count[which] = (run1 - 1) / share - group0[which] + 1;
     row[which] = r - tile * rows;
   };
-  look_up(0, of_p, rows_p);
-  look_up(1, of_o, rows_o);
+  look_up(0, of_p, tile_rows);
+  look_up(1, of_o, tile_rows);
   const int n0 = count[0], n = n0 + count[1];
   const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
   auto part_of = [&](int p) {
@@ -1507,7 +1565,7 @@ __device__ void clear_token(const Args& a, int D, int t) {
 // run that workgroup w + 1 of the kernel before began inside, if it was the first to.  The others clear the rows
 // that no run has: those of sequences that have nothing to see, and of no sequence.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o, int joins, int n_units, int decode) {
+__global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int tile_rows, int joins, int n_units, int decode) {
   const int l = threadIdx.x & 15, D = kv.D, w = blockIdx.x + 1;
   const int4 all = a.units[n_units];
   if (blockIdx.x >= joins) {
@@ -1533,8 +1591,8 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
   }
   const int4 of = a.units[u];
   const Unit unit{of.z, of.w, of.y, 0};
-  const Cost costs = decode ? Cost{of.y, 0} : cost_of(unit, a.causal, a, rows_o);      // a decode's unit has its runs' cost for its length
-  const int head = costs.in_front(tiles_of(of.w, a.share, rows_o)), hk = (x - of.x) / head;
+  const Cost costs = decode ? Cost{of.y, 0} : cost_of(unit, a.causal, a, tile_rows);      // a decode's unit has its runs' cost for its length
+  const int head = costs.in_front(tiles_of(of.w, a.share, tile_rows)), hk = (x - of.x) / head;
   int run0 = of.x + hk * head, tile = 0, cost = costs.first;
   if (costs.step == 0) {
     tile = (x - run0) / cost;
@@ -1542,13 +1600,13 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int rows_o
   }
   for (; x >= run0 + cost; ++tile, cost += costs.step) run0 += cost;
   if (run0 == x || run0 / share != w - 1) return;
-  const int rows = of.w * a.share, r0 = tile * rows_o;
+  const int rows = of.w * a.share, r0 = tile * tile_rows;
   const int n = (run0 + cost - 1) / share - w + 2;      // parts
   const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
   // Few parts: sixteen lanes a row; many: a wavefront, four parts at a time.
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, slots = n <= 8 ? 1 : 4, slot = slots == 1 ? 0 : lane >> 4, rows_wave = 4 / slots;
-  for (int i0 = (blockIdx.y * 4 + wave) * rows_wave; i0 < rows_o && r0 + i0 < rows; i0 += gridDim.y * 4 * rows_wave) {
-    const int i = min(i0 + (slots == 1 ? lane >> 4 : 0), min(rows_o, rows - r0) - 1);      // behind the last: the last, once more
+  for (int i0 = (blockIdx.y * 4 + wave) * rows_wave; i0 < tile_rows && r0 + i0 < rows; i0 += gridDim.y * 4 * rows_wave) {
+    const int i = min(i0 + (slots == 1 ? lane >> 4 : 0), min(tile_rows, rows - r0) - 1);      // behind the last: the last, once more
     const int tq = (r0 + i) / a.by_share, h = hk * a.share + r0 + i - tq * a.share;
     const int64_t row = static_cast<int64_t>(of.z + tq) * a.Hq + h;
     auto part_of = [&](int p) { return p == 0 ? row : queries + static_cast<int64_t>(w - 1 + p) * kMaxRows + i; };
@@ -1631,23 +1689,29 @@ Scratch lay_out(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, WsAlloc& ws) {
 typedef void (*Kernel)(KvView, Args);
 struct Choice {
   Kernel kernel;
-  int rows_p, rows_o, per_unit, lds;
+  int rows, per_unit, lds;
 };
 
 // Rows of a prefix (or, without prefixes, of a sequence) on average, and of a sequence at most.
 template <typename T, int D, bool EXACT>
 Choice choose_of(int rows_p, int rows_o, bool decode) {
-  constexpr int kMost = sizeof(T) == 4 || D == 256 ? 2 : 4;
   if (decode) {
-    if constexpr (EXACT) {
-      if (rows_p <= 16) return {k_decode<T, D, 1, true>, 16, 16, kPerUnit<D, 1>, 0};
-      if (rows_p <= 32 || kMost == 2) return {k_decode<T, D, 2, true>, 32, 32, kPerUnit<D, 2>, 0};
+    // Rows in as many registers as leave two workgroups (heads of 256: one) and none in memory.  32 groups of 8, 64 rows, behind 2400 tokens with
+    // 800 of their own, heads of 128: 64 rows a tile 355 us, 32 229 (5.0 TB/s), though each reads the prefix; with 64 of their own 105 and 109.
+    // 32 rows of heads of 256: 32 a tile 343 us, 16 216 (own 64: 121 and 102), fp32 501 and 222.
+    constexpr int kMost = sizeof(T) == 4 && D == 64 ? 2 : 256 / D;
+    if constexpr (EXACT && kMost > 1) {
+      if (rows_p <= 16) return {k_decode<T, D, 1, true>, 16, kPerUnit<D, 1>, 0};
+      if (rows_p <= 32) return {k_decode<T, D, 2, true>, 32, kPerUnit<D, 2>, 0};
     }
-    return {k_decode<T, D, kMost, EXACT>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
+    return {k_decode<T, D, kMost, EXACT>, 16 * kMost, kPerUnit<D, kMost>, 0};
   }
+  // Likewise: bf16 heads of 128, tiles of 64 rows: 558 us for 1280 sequences behind prefixes, of 32 268; heads of 96: messages of 40 tokens 162
+  // and 124, prompts 655 and 579.  fp32 heads of 256, 32 rows: messages 394 us, 16 284; bf16 heads of 256, prompts: 32 rows 1664, 16 2647.
+  constexpr int kMost = sizeof(T) == 4 ? (D == 256 ? 1 : 2) : (D == 64 ? 4 : 2);
   if constexpr (EXACT && sizeof(T) == 2 && D <= 128)
-    if (rows_o > 16) return {k_attend_wide<D>, kWideRows, kWideRows, 2, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
-  return {k_attend<T, D, kMost, kMost, EXACT>, 16 * kMost, 16 * kMost, kPerUnit<D, kMost>, 0};
+    if (rows_o > 16) return {k_attend_wide<D>, kWideRows, 2, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
+  return {k_attend<T, D, kMost, EXACT>, 16 * kMost, kPerUnit<D, kMost>, 0};
 }
 
 template <typename T>
@@ -1700,12 +1764,13 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, rows_u, small(rows_o), decode) : choose<float>(kv->D, rows_u, small(rows_o), decode);
   const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
   // an upper bound of all costs together, which are counted in 32 bits
-  const int64_t tiles_p = kv->n_group ? all_rows / k.rows_p + kv->n_group : 0, tiles_o = all_rows / k.rows_o + kv->n_seq;
+  const int64_t tiles_p = kv->n_group ? all_rows / k.rows + kv->n_group : 0, tiles_o = all_rows / k.rows + kv->n_seq;
   double most = decode ? kv->Hk * ((tiles_o + tiles_p) * (kRunCost + 8.0) + tiles_p * cost_of_pages(kv->max_prefix_pages) + kv->n_seq * cost_of_pages(kv->max_pages))
                        : kv->Hk * (tiles_p * cost_of_pages(kv->max_prefix_pages) + tiles_o * cost_of_pages(kv->max_pages));
   for (; most > 1 << 30; most /= 2) ++args.coarse;
-  args.rise = k.rows_o / (8 * share) >> args.coarse;
-  // Where there are workgroups enough, costs are whole shares, so that a run begins with a workgroup: four candidates 13.2 us, so 8.5.
+  args.rise = k.rows / (8 * share) >> args.coarse;
+  // Where there are workgroups enough, costs are whole shares, so that a run begins with a workgroup: one group of four by
+  // k_attend 13.2 us, then 8.0.
   if (most <= static_cast<double>(kMinShare) * blocks) {
     args.quantum = kMinShare;
     args.rise = 0;
@@ -1721,12 +1786,11 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
     const int y = 4, joins = static_cast<int>(blocks) - 1;
     const int64_t clears = ceil_div(n_units + 1, 4 * y);
     hipLaunchKernelGGL(bf16 ? k_join_runs<bf16_t> : k_join_runs<float>, dim3(static_cast<unsigned>(joins + (clears < 256 ? clears : 256)), y), dim3(256), 0, s,
-                       view, args, k.rows_o, joins, n_units, decode);
+                       view, args, k.rows, joins, n_units, decode);
   } else if (outputs <= 1024) {      // few rows: a workgroup for each
-    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 4> : k_join<float, 4>), dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows_p, k.rows_o);
+    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 4> : k_join<float, 4>), dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows);
   } else {
-    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 1> : k_join<float, 1>), dim3(static_cast<unsigned>(ceil_div(outputs, 4))), dim3(256), 0, s, view, args, k.rows_p,
-                       k.rows_o);
+    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 1> : k_join<float, 1>), dim3(static_cast<unsigned>(ceil_div(outputs, 4))), dim3(256), 0, s, view, args, k.rows);
   }
   ATG_LAUNCH_CHECK();
   return AT_GRPO_OK;

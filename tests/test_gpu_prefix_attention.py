@@ -384,3 +384,59 @@ def test_more_new_tokens_than_the_bound(gpu_device, dtype):
     q64 = p.queries(4)
     out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), max_q=1, want_lse=True)
     check(p, q64, out, p.attention(q64, 0.125))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 72, 128, 256])
+@pytest.mark.parametrize("new,max_q", [(None, 1), ([1, 2, 1, 1, 2], 2), ([1, 2, 1, 1, 2], 64)], ids=["decode", "message", "many"])
+def test_infinities_and_nan_stay_in_their_sequence(gpu_device, dtype, D, new, max_q):
+    # the sequences of a group are read for each other's queries too; what one holds must not reach the others, and reaches its own by the formula
+    p = Paged(dtype, 2, D, 16, [3, 100, 41, 2, 70], new, [5], [70], seed=30 + D)
+    q64 = p.queries(8)
+    scale = 1.0 / np.sqrt(D)
+    out, lse, mag, big, n = p.attention(q64, scale)
+    at = p.pages[1][37 // 16], 0, 37 % 16      # token 37 of sequence 1, key head 0: its rows are heads 0 .. 3
+    for d, x in [(1, np.inf), (5, -np.inf), (9, np.nan)]:
+        p.v[at + (d,)] = x
+    later = p.pages[1][95 // 16], 0, 95 % 16
+    p.v[later + (11,)] = np.inf
+    p.v[at + (11,)] = -np.inf
+    far = p.pages[4][50 // 16], 1, 50 % 16      # a key of sequence 4, key head 1: its rows' scores, and so their results, are NaN there
+    p.k[far + (3,)] = np.nan
+    got = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), scale=scale, max_q=max_q, want_lse=True)
+    o, l = host64(got["out"]), host64(got["lse"])
+    mine, theirs = slice(p.cu_q[1], p.cu_q[2]), slice(p.cu_q[4], p.cu_q[5])
+    bad = np.zeros(o.shape, dtype=bool)
+    for d in (1, 5, 9, 11):
+        bad[mine, :4, d] = True
+    assert (o[mine, :4, 1] == np.inf).all() and (o[mine, :4, 5] == -np.inf).all() and np.isnan(o[mine, :4][..., [9, 11]]).all()
+    assert np.isnan(o[theirs, 4:]).all() and np.isnan(l[theirs, 4:]).all()
+    bad[theirs, 4:] = True
+    bo, bl = attention_bounds(p.dtype, D, out, mag, big, n)
+    assert_within(np.where(bad, 0, o), np.where(bad, 0, out), bo, "out")
+    lost = bad.all(axis=2)
+    assert_within(np.where(lost, 0, l), np.where(lost, 0, lse), bl + 1e-6, "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n_seq,size", [(1792, [500, 0, 7, 1200]), (1793, [64] * 28), (1792, [])])
+def test_as_many_sequences_as_are_kept(gpu_device, n_seq, size):
+    rs = np.random.default_rng(n_seq)
+    length = rs.integers(0, 40, n_seq)
+    length[::89] = 0
+    p = Paged("bf16", 1, 64, 16, length, None, size, rs.integers(0, 90, len(size)), seed=3)
+    q64 = p.queries(2)
+    out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), want_lse=True)
+    check(p, q64, out, p.attention(q64, 0.125))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("bf16", 72), ("bf16", 128), ("bf16", 256), ("f32", 128), ("f32", 256)])
+@pytest.mark.parametrize("size", [5, 12])
+def test_groups_of_more_rows_than_a_tile(gpu_device, dtype, D, size):
+    # 8 heads on one, one or two new tokens: 56 and 144 rows of a group, each sequence's own tokens in one tile or at a tile's border
+    p = Paged(dtype, 1, D, 16, [5 * i % 71 for i in range(size + 2)], [1 + i % 2 for i in range(size + 2)], [size], [150], seed=D + size)
+    q64 = p.queries(8)
+    out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), max_q=2, want_lse=True)
+    check(p, q64, out, p.attention(q64, 1.0 / np.sqrt(D)))
