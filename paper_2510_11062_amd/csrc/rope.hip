@@ -154,35 +154,35 @@ struct Spot {
   int64_t at;
 };
 
-__device__ __forceinline__ Spot find_spot(const KvView& kv, int n_pos, int t, int32_t* data_error) {
+// Sequence and group of new token t: one that there is not, or one out of range, is found out by find_spot.
+struct Owner {
+  int s, g;
+};
+__device__ __forceinline__ Owner find_owner(const KvView& kv, int t) {
+  const int s = kv.cu_q ? __builtin_amdgcn_readfirstlane(wave_upper_bound(kv.cu_q, kv.n_seq + 1, t)) - 1 : t;
+  return Owner{s, kv.n_group > 0 ? __builtin_amdgcn_readfirstlane(wave_upper_bound(kv.group_seq, kv.n_group + 1, s)) - 1 : -1};
+}
+
+// What depends on nothing is asked for together, without branches in between.
+__device__ __forceinline__ Spot find_spot(const KvView& kv, int n_pos, int t, const Owner& of, int32_t* data_error) {
   Spot spot{-1, 0};
-  int error = 0, s = t, q0 = t, q1 = t + 1;
-  if (kv.cu_q) {
-    s = wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1;
-    if (s >= 0 && s < kv.n_seq) {
+  const bool there = of.s >= 0 && of.s < kv.n_seq, grouped = of.g >= 0 && of.g < kv.n_group;
+  const int s = there ? of.s : 0;
+  int length = 0, q0 = t, q1 = t + 1, prefix = 0;
+  if (kv.n_seq > 0) {
+    length = kv.length[s];
+    if (kv.cu_q) {
       q0 = kv.cu_q[s];
       q1 = kv.cu_q[s + 1];
     }
   }
-  int place = -1;
-  if (s < 0 || s >= kv.n_seq || q0 < 0 || q0 > t || q1 <= t) {
+  if (grouped) prefix = kv.prefix_len[of.g];
+  int error = 0, place = -1;
+  if (!there || q0 < 0 || q0 > t || q1 <= t || length < 0 || length > (kv.max_pages << kv.page_shift) || q1 - q0 > length || prefix < 0 ||
+      prefix > (kv.max_prefix_pages << kv.page_shift))
     error = AT_GRPO_DATA_SEQLENS;
-  } else {
-    const int length = kv.length[s], most = kv.max_pages << kv.page_shift;
-    if (length < 0 || length > most || q1 - q0 > length) error = AT_GRPO_DATA_SEQLENS;
-    else place = length - (q1 - t);
-  }
-  int prefix = 0;
-  if (place >= 0 && kv.n_group > 0) {
-    const int g = wave_upper_bound(kv.group_seq, kv.n_group + 1, s) - 1;
-    if (g >= 0 && g < kv.n_group) {
-      prefix = kv.prefix_len[g];
-      if (prefix < 0 || prefix > (kv.max_prefix_pages << kv.page_shift)) {
-        error = AT_GRPO_DATA_SEQLENS;
-        place = -1;
-      }
-    }
-  }
+  else
+    place = length - (q1 - t);
   if (place >= 0) {
     const int page = kv.pages[static_cast<int64_t>(s) * kv.max_pages + (place >> kv.page_shift)];
     if (static_cast<unsigned>(page) >= static_cast<unsigned>(kv.n_pages)) error |= AT_GRPO_DATA_PAGE;
@@ -224,13 +224,18 @@ struct Rotator {
   const Places p;
   const int l, grp;
   const bool mine;
-  Pairs wq{{1.f, 1.f, 1.f, 1.f}, {1.f, 1.f, 1.f, 1.f}}, wk = wq;
-  Raw<T> x[kBatch];
+  Raw<T> raw_wq{}, raw_wk{}, x[kBatch];
+  Pairs wq, wk;
 
   __device__ __forceinline__ explicit Rotator(const Layer& layer)
       : L(layer), p(places_of<VEC>(layer, threadIdx.x & (LANES - 1))), l(threadIdx.x & (LANES - 1)), grp((threadIdx.x & 63) / LANES), mine(8 * l < layer.D) {
-    if (mine && L.qw) wq = pairs_of(load_raw<VEC>(static_cast<const T*>(L.qw), p), p);
-    if (mine && L.kw) wk = pairs_of(load_raw<VEC>(static_cast<const T*>(L.kw), p), p);
+    if (mine && L.qw) raw_wq = load_raw<VEC>(static_cast<const T*>(L.qw), p);
+    if (mine && L.kw) raw_wk = load_raw<VEC>(static_cast<const T*>(L.kw), p);
+  }
+  // Once the first rows are on their way; store looks at no weight that there is not.
+  __device__ __forceinline__ void take_weights() {
+    wq = pairs_of(raw_wq, p);
+    wk = pairs_of(raw_wk, p);
   }
 
   __device__ __forceinline__ void load(const Token<T>& t, int j0, int step) {
@@ -275,7 +280,7 @@ struct Rotator {
 template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts, int Hq, int Hk, Rows q, Rows k, const int32_t* __restrict__ position,
                                                    Rows q_out, Rows k_out, int32_t* data_error) {
-  const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = unit / parts, part = unit - t * parts;
   if (t >= n_tok) return;
   const Token<T> token{{static_cast<const T*>(q.data) + t * q.ts, static_cast<const T*>(k.data) + t * k.ts, nullptr},
@@ -290,6 +295,7 @@ __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts
   if (bad && part == 0 && (threadIdx.x & 63) == 0) raise_data_error(data_error, AT_GRPO_DATA_POSITION);
   Pairs turn{{1.f, 1.f, 1.f, 1.f}, {}};
   if (!bad && L.half) turn = load_turn<VEC>(L, R.l, pos);
+  R.take_weights();
   for (;;) {
     R.store(token, j0, step, turn, bad);
     j0 += kBatch * step;
@@ -303,9 +309,10 @@ __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts
 template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_kv_append(KvView kv, Layer L, int n_tok, int parts, int Hq, Rows q, Rows k, Rows v, Rows q_out,
                                                    int32_t* data_error) {
-  const int unit = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int t = unit / parts, part = unit - t * parts;
   if (t >= n_tok) return;
+  const Owner owner = find_owner(kv, t);
   const int64_t hs = static_cast<int64_t>(kv.D) << kv.page_shift;
   Token<T> token{{static_cast<const T*>(q.data) + t * q.ts, static_cast<const T*>(k.data) + t * k.ts, static_cast<const T*>(v.data) + t * v.ts},
                  {static_cast<T*>(q_out.data) + t * q_out.ts, static_cast<T*>(kv.k), static_cast<T*>(kv.v)},
@@ -314,10 +321,11 @@ __global__ __launch_bounds__(256) void k_kv_append(KvView kv, Layer L, int n_tok
   const int step = parts * R.G;
   int j0 = part * R.G;
   R.load(token, j0, step);      // rows do not wait for where they go
-  const Spot spot = find_spot(kv, L.half ? L.n_pos : -1, t, part == 0 ? data_error : nullptr);
+  const Spot spot = find_spot(kv, L.half ? L.n_pos : -1, t, owner, part == 0 ? data_error : nullptr);
   const bool bad = spot.position < 0;
   Pairs turn{{1.f, 1.f, 1.f, 1.f}, {}};
   if (!bad && L.half) turn = load_turn<VEC>(L, R.l, spot.position);
+  R.take_weights();
   token.dst[1] += spot.at;
   token.dst[2] += spot.at;
   if (bad) token.end[1] = token.end[2] = Hq;
