@@ -354,7 +354,7 @@ __device__ __forceinline__ void rotate_rows_back(const Layer& L, const T* dy, in
     for (int i = 0; i < kGradBatch; ++i) {
       const int h = h0 + i * parts * G + grp;
       rx[i] = rg[i] = Raw<T>{};
-      if (mine && h < H && !zero) {
+      if (mine && h < H) {
         rg[i] = load_raw<VEC>(dy + h * dy_hs, p);
         if (norm) rx[i] = load_raw<VEC>(src + h * src_hs, p);
       }
@@ -439,7 +439,7 @@ __global__ __launch_bounds__(256) void k_norm_rope_bwd(Layer L, int n_tok, int p
   if (8 * l < L.D && L.qw) wq = pairs_of(load_raw<VEC>(static_cast<const T*>(L.qw), p), p);
   if (8 * l < L.D && L.kw) wk = pairs_of(load_raw<VEC>(static_cast<const T*>(L.kw), p), p);
   const int64_t units = static_cast<int64_t>(n_tok) * parts;
-  for (int64_t unit = blockIdx.x * 4 + (threadIdx.x >> 6); unit < units; unit += gridDim.x * 4) {
+  for (int64_t unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); unit < units; unit += gridDim.x * 4) {
     const int64_t t = unit / parts;
     const int part = static_cast<int>(unit - t * parts);
     const int pos = L.half ? position[t] : 0;
