@@ -343,6 +343,25 @@ __device__ __forceinline__ bool not_finite(uint32_t high) {
   return sizeof(T) == 4 ? high >= 0x7f800000u : (high & 0xffffu) >= 0x7f80u || high >= 0x7f800000u;
 }
 
+__device__ __forceinline__ float element(const f32x4& v, int e) { return v[e]; }
+template <typename V>
+__device__ __forceinline__ float element(const V& v, int e) {
+  return __uint_as_float(e & 1 ? dword(v, e >> 1) & 0xffff0000u : dword(v, e >> 1) << 16);
+}
+__device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
+// 0 in place of infinities and NaN
+__device__ __forceinline__ uint32_t finite_halves(uint32_t x) {
+  return ((x & 0x7f80u) == 0x7f80u ? 0 : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0 : x & 0xffff0000u);
+}
+__device__ __forceinline__ uint4 finite_of(const uint4& v) { return make_uint4(finite_halves(v.x), finite_halves(v.y), finite_halves(v.z), finite_halves(v.w)); }
+__device__ __forceinline__ uint2 finite_of(const uint2& v) { return make_uint2(finite_halves(v.x), finite_halves(v.y)); }
+__device__ __forceinline__ f32x4 finite_of(const f32x4& v) {
+  f32x4 x;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) x[i] = not_finite(v[i]) ? 0.f : v[i];
+  return x;
+}
+
 struct Lds {
   Schedule S;
   int pages[2][kPageSlots];
@@ -380,12 +399,54 @@ __device__ __forceinline__ void scores(const typename Shape<T, D>::KV (&k)[Shape
     }
 }
 
-// The tile's weights into the sums, and their products with its values into the accumulators.  A weight of 0 does not keep an infinite or NaN
-// value out of a product: a tile that holds one and is not of all rows is `apart`, and only the rows of which `of_row` says so take its products.
-template <typename T, int D, int NR>
-__device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::SUB], typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
+// A weight of 0 does not keep an infinite or NaN value out of a product.  In a tile that some rows do not see in full such values are added to
+// the rows that see them, one by one, and the products get 0 in their place.  `slab`: a wavefront's part of LDS for 32 tokens of 128 elements.
+template <typename T, int D, int NR, typename Sees>
+__device__ __forceinline__ void set_apart(float* slab, typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
+                                          f32x4 (&acc)[NR][Shape<T, D>::NB][Shape<T, D>::E], Sees sees) {
+  typedef Shape<T, D> Z;
+  typedef typename Z::VV VV;
+  uint32_t high = 0;
+#pragma unroll
+  for (int b = 0; b < Z::NB; ++b)
+#pragma unroll
+    for (int j = 0; j < 4 * Z::SUB; ++j) high = largest_bits(high, v[b][j]);
+  if (!__any(not_finite<T>(high))) return;
+  const int lane = threadIdx.x & 63, m = lane & 15, g = lane >> 4;
+  VV* const at = reinterpret_cast<VV*>(slab);
+#pragma unroll
+  for (int b = 0; b < Z::NB; ++b) {
+#pragma unroll
+    for (int j = 0; j < 4 * Z::SUB; ++j) {
+      at[(16 * (j >> 2) + 4 * g + (j & 3)) * 16 + m] = v[b][j];
+      v[b][j] = finite_of(v[b][j]);
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+#pragma unroll 1
+    for (int i = 0; i < 16 * Z::TOK; ++i) {
+      const VV x = at[i];
+      if (!__any(not_finite<T>(largest_bits(0u, x)))) continue;
+      const int token = i >> 4, of = i & 15;      // whose elements E of .. are those of the fourth of the lanes of / 4
+#pragma unroll
+      for (int n = 0; n < NR; ++n) {
+        const bool on = g == of >> 2 && sees(n, token);
+#pragma unroll
+        for (int e = 0; e < Z::E; ++e) {
+          const float y = element(x, e), add = on && not_finite(y) ? y : 0.f;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) acc[n][b][e][c] += c == (of & 3) ? add : 0.f;
+        }
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+}
+
+// The tile's weights into the sums, and their products with its values into the accumulators; `before` the products, once these are scaled.
+template <typename T, int D, int NR, typename Before>
+__device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::SUB], const typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
                                               float to_log2, f32x4 (&acc)[NR][Shape<T, D>::NB][Shape<T, D>::E], float (&top)[NR], float (&ref)[NR],
-                                              float (&sum)[NR], bool apart, const bool (&of_row)[NR]) {
+                                              float (&sum)[NR], Before before) {
   typedef Shape<T, D> Z;
   constexpr int E = Z::E, NB = Z::NB, SUB = Z::SUB;
   constexpr bool kBf16 = sizeof(T) == 2;
@@ -427,6 +488,7 @@ __device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::
       for (int j = 0; j < 4; ++j) w32[n][j] = p[j];
     }
   }
+  before();
   auto product = [&](int n, int b, int e, bf16x8 vt, f32x4 x) {
     if constexpr (kBf16) {
       return __builtin_amdgcn_mfma_f32_16x16x32_bf16(vt, __builtin_bit_cast(bf16x8, make_uint4(w16[n][0], w16[n][1], w16[n][2], w16[n][3])), x, 0, 0, 0);
@@ -436,25 +498,6 @@ __device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::
       return x;
     }
   };
-  if (apart) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        bf16x8 vt;
-        if constexpr (kBf16) vt = transposed(v[b], e);
-#pragma unroll
-        for (int n = 0; n < NR; ++n) {
-          const f32x4 x = product(n, b, e, vt, f32x4{0.f, 0.f, 0.f, 0.f});
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[n][b][e][i] += of_row[n] ? x[i] : 0.f;
-        }
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int j = 0; j < 4 * SUB; ++j) v[b][j] = typename Z::VV{};
-    }
-  }
 #pragma unroll
   for (int b = 0; b < NB; ++b)
 #pragma unroll
@@ -911,17 +954,15 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
           f32x4 s[NR][SUB];
           scores<T, D>(k, q, s);
           load_k(next);
-          bool of_row[NR], apart = false;      // whether the tile is the row's sequence's
+          int left[NR];
           if (tile.seq >= 0 || tile.token + TOK > tile.last || holes) {
-            int left[NR];
 #pragma unroll
             for (int n = 0; n < NR; ++n) left[n] = tile.last - tile.token;
             if (tile.seq >= 0) {
               const int q0 = kv.cu_q ? kv.cu_q[tile.seq] : tile.seq, q1 = kv.cu_q ? kv.cu_q[tile.seq + 1] : tile.seq + 1;      // the sequence's queries
 #pragma unroll
               for (int n = 0; n < NR; ++n) {
-                of_row[n] = row_tok[n] >= q0 && row_tok[n] < q1;
-                left[n] = of_row[n] ? left[n] - (a.causal ? q1 - 1 - row_tok[n] : 0) : 0;
+                left[n] = row_tok[n] >= q0 && row_tok[n] < q1 ? left[n] - (a.causal ? q1 - 1 - row_tok[n] : 0) : 0;
               }
             }
 #pragma unroll
@@ -936,16 +977,10 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
                 for (int b = 0; b < NB; ++b) v[b][4 * y + i] = i < seen ? v[b][4 * y + i] : typename Z::VV{};
               }
             }
-            if (tile.seq >= 0 && seq1 - seq0 > 1) {
-              uint32_t high = 0;
-#pragma unroll
-              for (int b = 0; b < NB; ++b)
-#pragma unroll
-                for (int j = 0; j < VJ; ++j) high = largest_bits(high, v[b][j]);
-              apart = __any(not_finite<T>(high));
-            }
           }
-          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, apart, of_row);
+          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, [&] {
+            if (tile.seq >= 0 && u.ntok > 1) set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) { return token < left[n]; });
+          });
           load_v(next);
           asm volatile("" ::: "memory");
           if (!more) break;
@@ -963,7 +998,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
 // Where a tile has 128 rows the products bound the call, not the tokens' passage.  Each wavefront then has 32 rows of its own, and the
 // four read the same 64 tokens from LDS, into which they come by direct loads, one tile ahead.  MFMA 32x32: a lane has 16 tokens of one
 // query in S^T, which are P^T's operand as they are, and V^T's operand comes from rows of V by transposing reads.  Eight prompts of 763 to
-// 2048 tokens, 16 heads on 8 of 128: 84 us and 15 for joining what was cut, 620 TFLOP/s in the kernel; a large product makes 1216.
+// 2048 tokens, 16 heads on 8 of 128: 87 us and 16 for joining what was cut, 600 TFLOP/s in the kernel; a large product makes 1216.
 //
 // A token's row is 2 D bytes in LDS; its 16-byte pieces are exchanged so that the reads meet no bank twice: piece c of K's row r lies at
 // c ^ (r & 15) (64-wide heads, whose rows take turns in the banks' halves: c ^ ((r >> 1) & 7)), of V's at c ^ 2 (r & 7) (c ^ 2 ((r >> 1) & 3)).
@@ -971,6 +1006,7 @@ constexpr int kWideTok = 64;
 
 struct WideLds {
   Schedule S;
+  int not_finite[4];
   int pages[kPageSlots];
 };
 
@@ -1047,7 +1083,8 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
     const int rows = u.ntok * a.share, r = w.r0 + 32 * wave + m, tq = min(r, rows - 1) / a.by_share, h = w.hk * a.share + min(r, rows - 1) - tq * a.share;
     const int first = u.len - u.ntok + 1, k1 = w.k1;      // a causal query sees the own tokens in front of `first + its number among the new tokens`
     const int limit = steps ? min(k1, first + tq) : k1;
-    const int all_see = steps ? first + min(w.r0 + 32 * wave, rows - 1) / a.by_share : k1;      // a wavefront's first row sees least
+    // a first row sees least: the tile's, and the wavefront's
+    const int all_see = steps ? first + w.r0 / a.by_share : k1, wave_sees = steps ? first + min(w.r0 + 32 * wave, rows - 1) / a.by_share : k1;
     const bool direct = kv.n_group == 0 && run.from() == 0 && run.to() == run.cost, first_part = run.from() == 0;
     const int group = run.number;
     const int32_t* const table = own ? kv.pages + static_cast<int64_t>(u.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(u.row) * kv.max_prefix_pages;
@@ -1086,12 +1123,21 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
         else if (ahead && to == k1) request(next.hk, next.k0, next.k1, buffer ^ 1);
         const char* const kt = smem + buffer * 2 * TB;
         char* const vt = smem + buffer * 2 * TB + TB;
-        if (holes) {      // what stands for a token of no page must not be NaN
+        if (holes || t + kWideTok > to) {      // what stands for a token behind the last or of no page counts as 0
           for (int i = tid; i < kWideTok * PIECES; i += 256) {
             const int token = t + i / PIECES;
-            if (token < to && lds.pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
+            if (token >= to || lds.pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
           }
-          __syncthreads();
+          lds_barrier();
+          asm volatile("" ::: "memory");
+        }
+        const bool partly = t + kWideTok > all_see;      // as in set_apart; each wavefront looks at a fourth of the values
+        if (partly) {
+          uint32_t high = 0;
+#pragma unroll
+          for (int i = 0; i < kWideTok * PIECES / 256; ++i) high = largest_bits(high, *reinterpret_cast<const uint4*>(vt + (tid + 256 * i) * 16));
+          const bool any = __any(not_finite<bf16_t>(high));
+          if (lane == 0) lds.not_finite[wave] = any;
         }
         f32x16 s[2];
 #pragma unroll
@@ -1124,7 +1170,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
           }
         };
         read_v_group(0);
-        if (t + kWideTok > min(to, all_see) || holes) {
+        if (t + kWideTok > min(to, wave_sees) || holes) {
 #pragma unroll
           for (int y = 0; y < 2; ++y)
 #pragma unroll
@@ -1150,6 +1196,34 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
           sum *= keep;
 #pragma unroll
           for (int x = 0; x < DT; ++x) acc[x] *= keep;
+        }
+        bool apart = false;
+        if (partly) {
+          lds_barrier();
+          asm volatile("" ::: "memory");
+          apart = (lds.not_finite[0] | lds.not_finite[1] | lds.not_finite[2] | lds.not_finite[3]) != 0;
+        }
+        if (apart) {
+#pragma unroll 1
+          for (int i = 0; i < kWideTok * PIECES; ++i) {
+            const int token = i / PIECES, c = i & (PIECES - 1);      // elements 8 c ..
+            const uint4 x = *reinterpret_cast<const uint4*>(vt + (token * PIECES + (c ^ swizzle_v<D>(token))) * 16);
+            if (!__any(not_finite<bf16_t>(largest_bits(0u, x)))) continue;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {      // of this lane's four
+              const float y = g ? element(x, 4 + j) : element(x, j), add = not_finite(y) && t + token < limit ? y : 0.f;
+#pragma unroll
+              for (int d = 0; d < 4 * DT; ++d) acc[d >> 2][4 * (d & 3) + j] += d == c ? add : 0.f;
+            }
+          }
+          lds_barrier();
+          for (int i = tid; i < kWideTok * PIECES; i += 256) {
+            uint4* const piece = reinterpret_cast<uint4*>(vt + i * 16);
+            *piece = finite_of(*piece);
+          }
+          lds_barrier();
+          asm volatile("" ::: "memory");
+          read_v_group(0);
         }
         uint4 w[2];
         auto weigh = [&](int ks) {
@@ -1403,7 +1477,9 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_attend(KvView kv, Ar
               }
             }
           }
-          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, false, {});
+          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, [&] {
+            if (steps && t + TOK > all_see) set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) { return t + token < limit[n]; });
+          });
           load_v(hk, t + 4 * TOK, to);
           asm volatile("" ::: "memory");      // the loads stay on this side of the jump back
         }
@@ -1501,10 +1577,11 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int tile_rows) 
         const int d = 128 * x2 + 8 * l;
         if (d < D) {
           const f32x4 y0 = *reinterpret_cast<const f32x4*>(from + d), y1 = *reinterpret_cast<const f32x4*>(from + d + 4);
+          const bool there = c < count_here;      // behind the last not 0 times an infinity of that
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
-            acc[8 * x2 + i] = fmaf(w, y0[i], acc[8 * x2 + i]);
-            acc[8 * x2 + 4 + i] = fmaf(w, y1[i], acc[8 * x2 + 4 + i]);
+            acc[8 * x2 + i] = fmaf(w, there ? y0[i] : 0.f, acc[8 * x2 + i]);
+            acc[8 * x2 + 4 + i] = fmaf(w, there ? y1[i] : 0.f, acc[8 * x2 + 4 + i]);
           }
         }
       }
@@ -1635,12 +1712,13 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int tile_r
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const float f = __builtin_amdgcn_exp2f((weight[c] - ref) * kLog2e);
+        const bool there = p0 + c * slots + slot < n;      // behind the last not 0 times an infinity of that
         total += f;
 #pragma unroll
         for (int x = 0; x < kMaxHeadDim / 128; ++x)
           if (128 * x + 8 * l < D)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) acc[8 * x + e] = fmaf(f, y[c][2 * x + (e >> 2)][e & 3], acc[8 * x + e]);
+            for (int e = 0; e < 8; ++e) acc[8 * x + e] = fmaf(f, there ? y[c][2 * x + (e >> 2)][e & 3] : 0.f, acc[8 * x + e]);
       }
     }
     if (slots == 4) {

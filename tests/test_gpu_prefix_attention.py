@@ -440,3 +440,38 @@ def test_groups_of_more_rows_than_a_tile(gpu_device, dtype, D, size):
     q64 = p.queries(8)
     out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), max_q=2, want_lse=True)
     check(p, q64, out, p.attention(q64, 1.0 / np.sqrt(D)))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 72, 128, 256])
+@pytest.mark.parametrize("new,max_q,group", [([3, 1, 2], 3, True), ([3, 1, 2], 3, False), ([3, 1, 2], 64, True), ([40, 9, 70], 70, True), ([200, 9, 70], 200, False)],
+                         ids=["few", "few-alone", "few-many", "message", "prompt"])
+def test_infinities_and_nan_stay_with_the_queries_that_see_them(gpu_device, dtype, D, new, max_q, group):
+    p = Paged(dtype, 2, D, 16, [200, 30, 90], new, *(([2, 1], [70, 45]) if group else ()), seed=50 + D)
+    q64 = p.queries(4)
+    scale = 1.0 / np.sqrt(D)
+    out, lse, mag, big, n = p.attention(q64, scale)
+    # values of new tokens: the last of sequence 0, one in its middle, and the first of sequence 2; a key in the middle of sequence 2
+    plant = [(0, 199, 3, np.inf), (0, 199, D - 1, np.nan), (0, 200 - (new[0] + 1) // 2, 5, -np.inf), (0, 199, 5, np.inf), (2, 90 - new[2], 0, np.nan)]
+    bad, sign = np.zeros(out.shape, dtype=bool), np.zeros(out.shape)
+    for s, at, d, x in plant:
+        p.v[p.pages[s][at // 16], 1, at % 16, d] = x
+        place = p.length[s] - p.new[s] + np.arange(p.new[s])      # of the new tokens
+        rows = p.cu_q[s] + np.flatnonzero(place >= at)
+        for r in rows:
+            bad[r, 2:, d] = True
+            with np.errstate(invalid="ignore"):
+                sign[r, 2:, d] += x      # inf - inf and NaN: NaN
+    key = 90 - (new[2] + 1) // 2
+    p.k[p.pages[2][key // 16], 0, key % 16, 1] = np.nan
+    lost = np.zeros(lse.shape, dtype=bool)
+    lost[p.cu_q[2] + np.flatnonzero(90 - new[2] + np.arange(new[2]) >= key), :2] = True
+    got = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), scale=scale, max_q=max_q, want_lse=True)
+    o, l = host64(got["out"]), host64(got["lse"])
+    assert np.isnan(o[lost]).all() and np.isnan(l[lost]).all()
+    assert np.array_equal(o[bad], sign[bad], equal_nan=True)
+    bad |= lost[..., None]
+    bo, bl = attention_bounds(p.dtype, D, out, mag, big, n)
+    assert_within(np.where(bad, 0, o), np.where(bad, 0, out), bo, "out")
+    assert_within(np.where(lost, 0, l), np.where(lost, 0, lse), bl + 2.0 ** -22 * np.abs(lse), "lse")
