@@ -5,7 +5,9 @@
  * (arXiv 2510.11062): agent- and turn-wise grouped advantages (Alg. 1, Phase 1; Eq. 1),
  * log pi_theta(token) from the LM head (the ratio below Eq. 2), the clipped surrogate with
  * masked averaging per policy (Eq. 2; per-model batches B_m of Sec. 3) and its gradients
- * with respect to the final hidden states and the head weights.
+ * with respect to the final hidden states and the head weights.  Beside that, of the layers in front of
+ * the head: norms and rotation of queries and keys with their gradient, a paged cache of the rollout's keys
+ * and values, and attention over it.
  *
  * Conventions common to every call
  *   - Pointers are DEVICE pointers unless the comment says "host".  The caller owns every
@@ -517,7 +519,7 @@ int32_t at_grpo_version(void);
  *   duration in milliseconds since recording started; the name is a static string.  Small fp32
  *   batches compute both gradients of the head in one launch, which counts as "head_dh", and in the
  *   one-call step their loss beside the backward's preparation, which counts as "token_prep" ("surrogate"
- *   has no launch there).
+ *   has no launch there).  Calls on queries, keys and the cache count as "rope", attention as "attention".
  */
 int at_grpo_profile_enable(int32_t on);
 int32_t at_grpo_profile_classes(void);

@@ -276,7 +276,7 @@ struct Rotator {
   }
 };
 
-// 16384 tokens of 40 heads of 128, bf16: 72 us, 4.7 TB/s.  197 tokens of 24 heads: 4.0 us, one wait for memory behind another.
+// 16384 tokens of 40 heads of 128, bf16: 65 to 67 us, 5.0 to 5.2 TB/s.  197 tokens of 24 heads: 3.8 us, one wait for memory behind another.
 template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts, int Hq, int Hk, Rows q, Rows k, const int32_t* __restrict__ position,
                                                    Rows q_out, Rows k_out, int32_t* data_error) {
@@ -305,7 +305,7 @@ __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts
 }
 
 // A token finds its sequence by bisection, its position and its page, while its rows are on their way.  46659 tokens of 64 prompts, 32 heads
-// of 128 in and out, bf16: 157 us, 4.9 TB/s.  1339 single tokens of 48 heads: 13.4 us, 2.5 TB/s; four: 5.0 us, a chain of waits.
+// of 128 in and out, bf16: 150 us, 5.1 TB/s.  1339 single tokens of 48 heads: 11 us, 3.0 TB/s; four: 4.0 us, a chain of waits.
 template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_kv_append(KvView kv, Layer L, int n_tok, int parts, int Hq, Rows q, Rows k, Rows v, Rows q_out,
                                                    int32_t* data_error) {
@@ -426,7 +426,7 @@ __device__ void store_partial(const Layer& L, Pairs dw, float* lds, float* __res
   if (d < L.D) partial[d] = (lds[d] + lds[kMaxHeadDim + d]) + (lds[2 * kMaxHeadDim + d] + lds[3 * kMaxHeadDim + d]);
 }
 
-// 16383 tokens of 24 heads of 128, bf16: 58 us, 5.2 TB/s; 3001 of 16 of 64, fp32: 12 us, 3.0 TB/s.  A workgroup keeps the weights'
+// 16383 tokens of 24 heads of 128, bf16: 55 us, 5.5 TB/s; 3001 of 16 of 64, fp32: 12 us, 3.0 TB/s.  A workgroup keeps the weights'
 // gradients of its rows in registers and writes them once; k_weight_grad adds up the workgroups' (5 us).
 template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_norm_rope_bwd(Layer L, int n_tok, int parts, int Hq, int Hk, Rows dq_out, Rows dk_out, Rows q, Rows k,
