@@ -1010,27 +1010,37 @@ struct WideLds {
   int pages[kPageSlots];
 };
 
+// Workgroups on a compute unit: heads of 256 take 128 KB of LDS.
 template <int D>
-__device__ __forceinline__ int swizzle_k(int r) { return D == 128 ? r & 15 : (r >> 1) & 7; }
-template <int D>
-__device__ __forceinline__ int swizzle_v(int r) { return D == 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
+constexpr int kWidePerUnit = D == 256 ? 1 : 2;
 
 template <int D>
-__global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
+__device__ __forceinline__ int swizzle_k(int r) { return D >= 128 ? r & 15 : (r >> 1) & 7; }
+template <int D>
+__device__ __forceinline__ int swizzle_v(int r) { return D >= 128 ? 2 * (r & 7) : 2 * ((r >> 1) & 3); }
+
+template <int D, bool EXACT>
+__global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv, Args a) {
   constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES;
   extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
   WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * TB);
+  const int dim = EXACT ? D : kv.D;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 31, g = lane >> 5;
   const Share mine = make_schedule<kWideRows>(kv, a, lds.S);
   Runs<kWideRows> run(kv, a, lds.S, mine);
   if (!run.valid()) return;
+  if (!EXACT) {      // what no load writes: the elements behind a head's last count as 0
+    for (int i = tid; i < 4 * TB / 16; i += 256) *reinterpret_cast<uint4*>(smem + i * 16) = make_uint4(0, 0, 0, 0);
+    lds_barrier();
+    asm volatile("" ::: "memory");
+  }
 
   // where this lane reads: K piece 2 c + g of row m (XOR 32 c), V four elements of row 4 g + (lane & 15) / 4 (XOR 64 t)
   const int read_k = m * (2 * D) + ((g ^ swizzle_k<D>(m)) << 4);
   const int i16 = lane & 15, row_v = 4 * g + (i16 >> 2);
   const int read_v = row_v * (2 * D) + (((2 * ((lane >> 4) & 1) + ((i16 >> 1) & 1)) ^ swizzle_v<D>(row_v)) << 4) + (i16 & 1) * 8;
   const float to_log2 = a.scale * kLog2e;
-  const uint32_t page_bytes = (static_cast<uint32_t>(kv.Hk) * D * 2) << kv.page_shift;      // of all heads
+  const uint32_t page_bytes = (static_cast<uint32_t>(kv.Hk) * dim * 2) << kv.page_shift;      // of all heads
   const int in_page = (1 << kv.page_shift) - 1;
   const uint32_t lds0 = __builtin_amdgcn_readfirstlane(lds_addr32(smem)) + wave * NL * 1024;
 
@@ -1055,15 +1065,16 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
   };
   // A tile of tokens t .. into a buffer; rows behind the last token are the last.
   auto request = [&](int hk, int t, int to, int buffer) {
-    const char* const kbase = static_cast<const char*>(kv.k) + ((static_cast<int64_t>(hk) * D * 2) << kv.page_shift);
-    const char* const vbase = static_cast<const char*>(kv.v) + ((static_cast<int64_t>(hk) * D * 2) << kv.page_shift);
+    const char* const kbase = static_cast<const char*>(kv.k) + ((static_cast<int64_t>(hk) * dim * 2) << kv.page_shift);
+    const char* const vbase = static_cast<const char*>(kv.v) + ((static_cast<int64_t>(hk) * dim * 2) << kv.page_shift);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int row = (wave * NL + i) * LROWS + lane / PIECES, piece = lane & (PIECES - 1), token = min(t + row, to - 1);
       const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(max(0, lds.pages[(token >> kv.page_shift) - page0]))) * page_bytes;
-      const uint32_t in = static_cast<uint32_t>(token & in_page) * (2 * D);
-      direct_load_v(kbase + (at + (in + 16 * (piece ^ swizzle_k<D>(row)))), lds0 + buffer * 2 * TB + i * 1024);
-      direct_load_v(vbase + (at + (in + 16 * (piece ^ swizzle_v<D>(row)))), lds0 + buffer * 2 * TB + TB + i * 1024);
+      const uint32_t in = static_cast<uint32_t>(token & in_page) * (2 * dim);
+      const int of_k = piece ^ swizzle_k<D>(row), of_v = piece ^ swizzle_v<D>(row);
+      if (EXACT || 8 * of_k < dim) direct_load_v(kbase + (at + (in + 16 * of_k)), lds0 + buffer * 2 * TB + i * 1024);
+      if (EXACT || 8 * of_v < dim) direct_load_v(vbase + (at + (in + 16 * of_v)), lds0 + buffer * 2 * TB + TB + i * 1024);
     }
   };
   uint4 q[KC];
@@ -1071,7 +1082,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
     const int r = min(w.r0 + 32 * wave + m, x.ntok * a.share - 1), tq = r / a.by_share, h = w.hk * a.share + r - tq * a.share;
     const bf16_t* from = static_cast<const bf16_t*>(a.q.data) + (x.tok0 + tq) * a.q.ts + h * a.q.hs + 8 * g;
 #pragma unroll
-    for (int c = 0; c < KC; ++c) q[c] = *reinterpret_cast<const uint4*>(from + 16 * c);
+    for (int c = 0; c < KC; ++c) q[c] = EXACT || 16 * c + 8 * g < dim ? *reinterpret_cast<const uint4*>(from + 16 * c) : make_uint4(0, 0, 0, 0);
   };
   int buffer = 0;
   bool requested = false;      // the run's first tile, by the run in front of it
@@ -1146,7 +1157,7 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
           for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
         // Fragments are read a group ahead of the products that take them: left to itself the compiler reads each right in front of its own,
         // and every product waits for LDS (103 us for eight prompts of up to 2048 tokens, then 90).
-        bf16x8 f[2][4];
+        bf16x8 f[2][DT > 4 ? DT : 4];
         auto read_k_group = [&](int x) {      // two steps of 16 elements, two blocks of 32 tokens
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[x & 1][i] = *reinterpret_cast<const bf16x8*>(kt + (read_k ^ ((2 * x + (i >> 1)) << 5)) + (i & 1) * 32 * 2 * D);
@@ -1274,17 +1285,17 @@ __global__ __launch_bounds__(256, 2) void k_attend_wide(KvView kv, Args a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) p[j] = pack_bf16x2(acc[t][i + 2 * j] * f, acc[t][i + 2 * j + 1] * f);
             const auto lo = __builtin_amdgcn_permlane32_swap(p[0], p[2], false, false), hi = __builtin_amdgcn_permlane32_swap(p[1], p[3], false, false);
-            *reinterpret_cast<uint4*>(to + 32 * t + 2 * i) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
+            if (EXACT || 32 * t + 2 * i + 8 * g < dim) *reinterpret_cast<uint4*>(to + 32 * t + 2 * i) = make_uint4(lo[0], hi[0], lo[1], hi[1]);
           }
       } else {
         const int64_t part = first_part ? by_query : static_cast<int64_t>(a.n_tok) * a.Hq * (kv.n_group ? 2 : 1) + static_cast<int64_t>(group) * kMaxRows + (r - w.r0);
         if (g == 0) a.part_lse[part] = x;
-        float* to = a.part_out + part * D + 4 * g;
+        float* to = a.part_out + part * dim + 4 * g;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
           for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<f32x4*>(to + 32 * t + 2 * i) = f32x4{acc[t][i] * f, acc[t][i + 1] * f, acc[t][i + 2] * f, acc[t][i + 3] * f};
+            if (EXACT || 32 * t + 2 * i + 4 * g < dim) *reinterpret_cast<f32x4*>(to + 32 * t + 2 * i) = f32x4{acc[t][i] * f, acc[t][i + 1] * f, acc[t][i + 2] * f, acc[t][i + 3] * f};
       }
     }
     if (!more) break;
@@ -1787,8 +1798,8 @@ Choice choose_of(int rows_p, int rows_o, bool decode) {
   // Likewise: bf16 heads of 128, tiles of 64 rows: 558 us for 1280 sequences behind prefixes, of 32 268; heads of 96: messages of 40 tokens 162
   // and 124, prompts 655 and 579.  fp32 heads of 256, 32 rows: messages 394 us, 16 284; bf16 heads of 256, prompts: 32 rows 1664, 16 2647.
   constexpr int kMost = sizeof(T) == 4 ? (D == 256 ? 1 : 2) : (D == 64 ? 4 : 2);
-  if constexpr (EXACT && sizeof(T) == 2 && D <= 128)
-    if (rows_o > 16) return {k_attend_wide<D>, kWideRows, 2, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
+  if constexpr (sizeof(T) == 2)
+    if (rows_o > 16) return {k_attend_wide<D, EXACT>, kWideRows, kWidePerUnit<D>, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
   return {k_attend<T, D, kMost, EXACT>, 16 * kMost, kPerUnit<D, kMost>, 0};
 }
 
