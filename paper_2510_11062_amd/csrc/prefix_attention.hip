@@ -9,11 +9,11 @@
 // equal cost, wherever that cuts a run: long prompts and ragged responses fill the chip alike, whatever their lengths, which only the
 // device knows.  A second kernel joins the parts of a row.  Three kernels, by the rows of a sequence:
 //   k_decode        at most 16: a unit is a group, whose rows read its prefix and then its sequences' own tokens as one stream
-//   k_attend        more, and where k_decode's tables end: units are the prefix of a group with the queries of all its sequences, and a
-//                   sequence's own tokens with its queries
-//   k_attend_wide   k_attend for bf16 and heads of 64 and 128, tiles of 128 rows
+//   k_attend_wide   more, in bf16: units are the prefix of a group with the queries of all its sequences, and a sequence's own tokens with its
+//                   queries; tiles of 128 rows
+//   k_attend        the same in fp32, and where k_decode's tables end, tiles of 16 to 64
 //
-// In the first two a wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
+// In the first and the last a wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
 //   S^T = K Q^T     MFMA 16x16: tokens down, queries across, so that a lane has four consecutive tokens of one query
 //   P^T             is at once the second product's operand: no lane needs a weight that another one computed
 //   O^T += V^T P^T  a lane loads whole rows of V, eight elements of eight tokens, and transposes that block by itself
@@ -998,7 +998,8 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
 // Where a tile has 128 rows the products bound the call, not the tokens' passage.  Each wavefront then has 32 rows of its own, and the
 // four read the same 64 tokens from LDS, into which they come by direct loads, one tile ahead.  MFMA 32x32: a lane has 16 tokens of one
 // query in S^T, which are P^T's operand as they are, and V^T's operand comes from rows of V by transposing reads.  Eight prompts of 763 to
-// 2048 tokens, 16 heads on 8 of 128: 87 us and 16 for joining what was cut, 600 TFLOP/s in the kernel; a large product makes 1216.
+// 2048 tokens, 16 heads on 8 of 128: 88 us and 16 for joining what was cut, 600 TFLOP/s in the kernel; a large product makes 1216.  Eight of
+// 2000 tokens, 16 heads on 4 of 256: 704 us whole, 370 TFLOP/s (by k_attend 1640); on 8 of 96: 331 (576).
 //
 // A token's row is 2 D bytes in LDS; its 16-byte pieces are exchanged so that the reads meet no bank twice: piece c of K's row r lies at
 // c ^ (r & 15) (64-wide heads, whose rows take turns in the banks' halves: c ^ ((r >> 1) & 7)), of V's at c ^ 2 (r & 7) (c ^ 2 ((r >> 1) & 3)).
@@ -1021,7 +1022,7 @@ __device__ __forceinline__ int swizzle_v(int r) { return D >= 128 ? 2 * (r & 7) 
 
 template <int D, bool EXACT>
 __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv, Args a) {
-  constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES;
+  constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES, VG = DT > 4 ? 2 : 1, DB = DT / VG;
   extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
   WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * TB);
   const int dim = EXACT ? D : kv.D;
@@ -1157,7 +1158,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
           for (int i = 0; i < 16; ++i) s[y][i] = 0.f;
         // Fragments are read a group ahead of the products that take them: left to itself the compiler reads each right in front of its own,
         // and every product waits for LDS (103 us for eight prompts of up to 2048 tokens, then 90).
-        bf16x8 f[2][DT > 4 ? DT : 4];
+        bf16x8 f[2][4];
         auto read_k_group = [&](int x) {      // two steps of 16 elements, two blocks of 32 tokens
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[x & 1][i] = *reinterpret_cast<const bf16x8*>(kt + (read_k ^ ((2 * x + (i >> 1)) << 5)) + (i & 1) * 32 * 2 * D);
@@ -1172,12 +1173,12 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
             s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 1][i], __builtin_bit_cast(bf16x8, q[2 * x + (i >> 1)]), s[i & 1], 0, 0, 0);
         }
         if (more && t + kWideTok >= k1) load_q(run.x, next);      // the last scores of this run are on their way
-        auto read_v_group = [&](int ks) {      // 16 tokens, all blocks of 32 elements
+        auto read_v_group = [&](int k) {      // 16 tokens, all blocks of 32 elements or half of them
 #pragma unroll
-          for (int x = 0; x < DT; ++x) {
-            const char* p = vt + (read_v ^ (x << 6)) + ks * 16 * 2 * D;
+          for (int x = 0; x < DB; ++x) {
+            const char* p = vt + (read_v ^ ((DB * (k % VG) + x) << 6)) + k / VG * 16 * 2 * D;
             const uint2 lo = lds_read_tr(p), hi = lds_read_tr(p + 8 * 2 * D);
-            f[ks & 1][x] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
+            f[k & 1][x] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
           }
         };
         read_v_group(0);
@@ -1248,20 +1249,21 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
         };
         weigh(0);
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
+        for (int k = 0; k < 4 * VG; ++k) {
+          const int ks = k / VG;
           __builtin_amdgcn_sched_barrier(0);
-          if (ks < 3) {      // the next tokens' weights are computed between this step's products
-            read_v_group(ks + 1);
-            weigh(ks + 1);
-          }
+          const bool weighing = k % VG == 0 && ks < 3;
+          if (k + 1 < 4 * VG) read_v_group(k + 1);
+          if (weighing) weigh(ks + 1);      // the next tokens' weights are computed between this step's products
 #pragma unroll
-          for (int x = 0; x < DT; ++x) acc[x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[ks & 1][x], __builtin_bit_cast(bf16x8, w[ks & 1]), acc[x], 0, 0, 0);
-          if (ks < 3) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 2 * DT, 0);      // LDS reads, then a product and some of the weights in turn
+          for (int x = 0; x < DB; ++x)
+            acc[DB * (k % VG) + x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[k & 1][x], __builtin_bit_cast(bf16x8, w[ks & 1]), acc[DB * (k % VG) + x], 0, 0, 0);
+          if (weighing) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);      // LDS reads, then a product and some of the weights in turn
 #pragma unroll
-            for (int x = 0; x < DT; ++x) {
+            for (int x = 0; x < DB; ++x) {
               __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-              __builtin_amdgcn_sched_group_barrier(0x402, 28 / DT, 0);
+              __builtin_amdgcn_sched_group_barrier(0x402, 28 / DB, 0);
             }
           }
         }
@@ -1429,7 +1431,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_attend(KvView kv, Ar
     int ids[kPageSlots / 256];
     if (turn) get_ids(ids, table_of(run.x, run.own), slots(0, run.x.len));
 
-    // Twice: where all rows see all tokens nothing is kept for each.  Prompts, heads of 96: 646 us in one, 579 so.
+    // Twice: where all rows see all tokens nothing is kept for each.  Messages in fp32, heads of 128: 257 us in one, 242 so.
     auto body = [&](auto causal) {
       constexpr bool steps = decltype(causal)::value;
       const int rows = u.ntok * a.share, hk = w.hk, r0 = w.r0, k0 = w.k0, k1 = w.k1, first = u.len - u.ntok + 1;
@@ -1795,8 +1797,8 @@ Choice choose_of(int rows_p, int rows_o, bool decode) {
     }
     return {k_decode<T, D, kMost, EXACT>, 16 * kMost, kPerUnit<D, kMost>, 0};
   }
-  // Likewise: bf16 heads of 128, tiles of 64 rows: 558 us for 1280 sequences behind prefixes, of 32 268; heads of 96: messages of 40 tokens 162
-  // and 124, prompts 655 and 579.  fp32 heads of 256, 32 rows: messages 394 us, 16 284; bf16 heads of 256, prompts: 32 rows 1664, 16 2647.
+  // Likewise: bf16 heads of 128, tiles of 64 rows: 558 us for 1280 sequences behind prefixes, of 32 268.  fp32 heads of 256, 32 rows: messages of
+  // 40 tokens 394 us, 16 284.
   constexpr int kMost = sizeof(T) == 4 ? (D == 256 ? 1 : 2) : (D == 64 ? 4 : 2);
   if constexpr (sizeof(T) == 2)
     if (rows_o > 16) return {k_attend_wide<D, EXACT>, kWideRows, kWidePerUnit<D>, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};

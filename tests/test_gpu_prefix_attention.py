@@ -475,3 +475,15 @@ def test_infinities_and_nan_stay_with_the_queries_that_see_them(gpu_device, dtyp
     bo, bl = attention_bounds(p.dtype, D, out, mag, big, n)
     assert_within(np.where(bad, 0, o), np.where(bad, 0, out), bo, "out")
     assert_within(np.where(lost, 0, l), np.where(lost, 0, lse), bl + 2.0 ** -22 * np.abs(lse), "lse")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [8, 24, 56, 104, 136, 248])
+@pytest.mark.parametrize("group", [False, True])
+def test_many_queries_of_heads_of_any_size(gpu_device, dtype, D, group):
+    p = Paged(dtype, 2, D, 16, [150, 33, 200], [150, 33, 70], *(([2, 1], [70, 45]) if group else ()), seed=D)
+    q64 = p.queries(6)
+    for causal in (True, False):
+        out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), max_q=150, want_lse=True, causal=causal)
+        check(p, q64, out, p.attention(q64, 1.0 / np.sqrt(D), causal=causal), f"causal {causal}")
