@@ -11,7 +11,7 @@
 //   k_decode        at most 16: a unit is a group, whose rows read its prefix and then its sequences' own tokens as one stream
 //   k_attend_wide   more, in bf16: units are the prefix of a group with the queries of all its sequences, and a sequence's own tokens with its
 //                   queries; tiles of 128 rows
-//   k_attend        the same in fp32, and where k_decode's tables end, tiles of 16 to 64
+//   k_attend        the same in fp32, and where k_decode's tables end; tiles of 16 or 32 rows
 //
 // In the first and the last a wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
 //   S^T = K Q^T     MFMA 16x16: tokens down, queries across, so that a lane has four consecutive tokens of one query
@@ -1797,9 +1797,10 @@ Choice choose_of(int rows_p, int rows_o, bool decode) {
     }
     return {k_decode<T, D, kMost, EXACT>, 16 * kMost, kPerUnit<D, kMost>, 0};
   }
-  // Likewise: bf16 heads of 128, tiles of 64 rows: 558 us for 1280 sequences behind prefixes, of 32 268.  fp32 heads of 256, 32 rows: messages of
-  // 40 tokens 394 us, 16 284.
-  constexpr int kMost = sizeof(T) == 4 ? (D == 256 ? 1 : 2) : (D == 64 ? 4 : 2);
+  // Here bf16 has few rows a sequence, fp32 all that are not few.  1840 sequences behind 600 tokens with 64 of their own, bf16: tiles of 64 rows (heads of
+  // 64) 379 us, of 32 298, of 16 286; heads of 128, 2000 in groups of their own, of 32 720, of 16 626; heads of 256, of 32 577, of 16 391.  fp32 heads
+  // of 256, messages of 40 tokens: tiles of 32 rows 394 us, of 16 284.
+  constexpr int kMost = sizeof(T) == 2 || D == 256 ? 1 : 2;
   if constexpr (sizeof(T) == 2)
     if (rows_o > 16) return {k_attend_wide<D, EXACT>, kWideRows, kWidePerUnit<D>, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
   return {k_attend<T, D, kMost, EXACT>, 16 * kMost, kPerUnit<D, kMost>, 0};
