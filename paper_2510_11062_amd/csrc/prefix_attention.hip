@@ -1533,41 +1533,136 @@ __device__ __forceinline__ void store8(T* to, const float* y) {
   }
 }
 
-// Rows behind prefixes: WAVES wavefronts of a workgroup for each query and head, sixteen lanes for the elements of a part.
-template <typename T, int WAVES>
-__global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int tile_rows) {
-  __shared__ float lds[WAVES == 1 ? 1 : 4][kMaxHeadDim + 1];
-  const int lane = threadIdx.x & 63, l = lane & 15, slot = lane >> 4, wave = threadIdx.x >> 6, mine = WAVES == 1 ? 0 : wave, D = kv.D;
-  const int64_t unit = WAVES == 1 ? static_cast<int64_t>(blockIdx.x) * 4 + wave : blockIdx.x;
-  if (unit >= static_cast<int64_t>(a.n_tok) * a.Hq) return;
-  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * a.Hq), hk = h / a.by_share;
+// One row of n parts, by sixteen lanes, eight elements a lane, or where `spread` by a whole wavefront, every fourth part each; by all wavefront's lanes.
+template <typename T, typename PartOf>
+__device__ __forceinline__ void join_row(const Args& a, int D, int n, bool spread, bool write, PartOf part_of, T* to, float* lse) {
+  const int lane = threadIdx.x & 63, l = lane & 15, slot = spread ? lane >> 4 : 0, slots = spread ? 4 : 1;
+  float high = -INFINITY;
+  for (int p = slot * 16 + l; p < n; p += 16 * slots) high = larger(high, a.part_lse[part_of(p)]);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1)
+    if (o < 16 * slots) high = larger(high, __shfl_xor(high, o, 64));
+  const float ref = high == -INFINITY ? 0.f : high;
+  float total = 0.f, acc[kMaxHeadDim / 16] = {};
+  for (int p0 = 0; p0 < n; p0 += 2 * slots) {      // two in flight
+    float weight[2];
+    f32x4 y[2][kMaxHeadDim / 64];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const int p = p0 + c * slots + slot;
+      const int64_t part = part_of(min(p, n - 1));
+      weight[c] = p < n ? a.part_lse[part] : -INFINITY;
+#pragma unroll
+      for (int x = 0; x < kMaxHeadDim / 128; ++x)
+        if (128 * x + 8 * l < D) {
+          y[c][2 * x] = *reinterpret_cast<const f32x4*>(a.part_out + part * D + 128 * x + 8 * l);
+          y[c][2 * x + 1] = *reinterpret_cast<const f32x4*>(a.part_out + part * D + 128 * x + 8 * l + 4);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      const float f = __builtin_amdgcn_exp2f((weight[c] - ref) * kLog2e);
+      const bool there = p0 + c * slots + slot < n;      // behind the last not 0 times an infinity of that
+      total += f;
+#pragma unroll
+      for (int x = 0; x < kMaxHeadDim / 128; ++x)
+        if (128 * x + 8 * l < D)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) acc[8 * x + e] = fmaf(f, there ? y[c][2 * x + (e >> 2)][e & 3] : 0.f, acc[8 * x + e]);
+    }
+  }
+  if (spread) {
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+      total += __shfl_xor(total, o, 64);
+#pragma unroll
+      for (int e = 0; e < kMaxHeadDim / 16; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
+    }
+  }
+  if (slot || !write) return;
+  const float f = total == 0.f ? 0.f : 1.f / total;
+#pragma unroll
+  for (int e = 0; e < kMaxHeadDim / 16; ++e) acc[e] *= f;
+#pragma unroll
+  for (int x = 0; x < kMaxHeadDim / 128; ++x)
+    if (128 * x + 8 * l < D) store8(to + 128 * x + 8 * l, acc + 8 * x);
+  if (lse && l == 0) *lse = total == 0.f ? -INFINITY : high + logf(total);
+}
+
+// The units of a token: its group's prefix, and its sequence.
+struct UnitsOf {
+  int4 prefix, own;
+  int share;
+};
+__device__ __forceinline__ UnitsOf units_of(const KvView& kv, const Args& a, int t) {
   const int s = kv.cu_q ? wave_upper_bound(kv.cu_q, kv.n_seq + 1, t) - 1 : t, g = wave_upper_bound(kv.group_seq, kv.n_group + 1, s) - 1;
-  const int share = a.units[kv.n_group + kv.n_seq].x;
   const bool in_seq = s >= 0 && s < kv.n_seq, in_group = in_seq && g >= 0 && g < kv.n_group;
-  const int4 of_p = in_group ? a.units[g] : make_int4(0, 0, 0, 0), of_o = in_seq ? a.units[kv.n_group + s] : make_int4(0, 0, 0, 0);
+  return UnitsOf{in_group ? a.units[g] : make_int4(0, 0, 0, 0), in_seq ? a.units[kv.n_group + s] : make_int4(0, 0, 0, 0), a.units[kv.n_group + kv.n_seq].x};
+}
+
+// The parts of row (t, h): of the prefix, then of its sequence.
+struct RowParts {
   int group0[2], count[2], row[2];      // the run's first workgroup, its workgroups, the row in its tile
-  auto look_up = [&](int which, const int4& x, int rows) {
+  int64_t queries, unit;
+
+  __device__ __forceinline__ RowParts(const Args& a, const UnitsOf& units, int t, int h, int tile_rows)
+      : queries(static_cast<int64_t>(a.n_tok) * a.Hq), unit(static_cast<int64_t>(t) * a.Hq + h) {
+    look_up(0, a, units, units.prefix, false, t, h, tile_rows);
+    look_up(1, a, units, units.own, a.causal, t, h, tile_rows);
+  }
+  __device__ __forceinline__ int parts() const { return count[0] + count[1]; }
+  __device__ __forceinline__ int64_t operator()(int p) const {
+    const bool own = p >= count[0];
+    const int i = own ? p - count[0] : p;
+    return i == 0 ? (own ? queries : 0) + unit : 2 * queries + static_cast<int64_t>((own ? group0[1] : group0[0]) + i) * kMaxRows + (own ? row[1] : row[0]);
+  }
+
+ private:
+  __device__ __forceinline__ void look_up(int which, const Args& a, const UnitsOf& units, const int4& x, bool steps, int t, int h, int rows) {
     group0[which] = count[which] = row[which] = 0;
-    const int q = t - x.z;
+    const int q = t - x.z, hk = h / a.by_share;
     if (x.y == 0 || q < 0 || q >= x.w) return;
     const Unit of{x.z, x.w, x.y, 0};
-    const bool steps = which && a.causal;
     const int r = q * a.share + h - hk * a.share, tile = r / rows;
     const Cost costs = cost_of(of, steps, a, rows);
     const int run0 = x.x + hk * head_cost(of, steps, a, rows) + costs.in_front(tile), run1 = run0 + costs.of(tile);
-    group0[which] = run0 / share;
-    count[which] = (run1 - 1) / share - group0[which] + 1;
+    group0[which] = run0 / units.share;
+    count[which] = (run1 - 1) / units.share - group0[which] + 1;
     row[which] = r - tile * rows;
-  };
-  look_up(0, of_p, tile_rows);
-  look_up(1, of_o, tile_rows);
-  const int n0 = count[0], n = n0 + count[1];
-  const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
-  auto part_of = [&](int p) {
-    const bool own = p >= n0;
-    const int i = own ? p - n0 : p;
-    return i == 0 ? (own ? queries : 0) + unit : 2 * queries + static_cast<int64_t>((own ? group0[1] : group0[0]) + i) * kMaxRows + (own ? row[1] : row[0]);
-  };
+  }
+};
+
+// Rows behind prefixes: a wavefront for four heads of a token, so that what belongs to the token is looked up once.  3840 tokens of 32 heads of 128
+// 50 us; a wavefront for each row 111.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join_heads(KvView kv, Args a, int tile_rows) {
+  const int lane = threadIdx.x & 63, per_token = (a.Hq + 3) / 4;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= static_cast<int64_t>(a.n_tok) * per_token) return;
+  const int t = static_cast<int>(unit / per_token), h0 = 4 * static_cast<int>(unit - static_cast<int64_t>(t) * per_token);
+  const UnitsOf units = units_of(kv, a, t);
+  const RowParts of_slot(a, units, t, min(h0 + (lane >> 4), a.Hq - 1), tile_rows);
+  T* const to = static_cast<T*>(a.out.data) + t * a.out.ts;
+  if (!__any(of_slot.parts() > 8)) {
+    const int h = h0 + (lane >> 4);
+    join_row(a, kv.D, of_slot.parts(), false, h < a.Hq, of_slot, to + h * a.out.hs, a.lse ? a.lse + of_slot.unit : nullptr);
+    return;
+  }
+  for (int h = h0; h < min(h0 + 4, a.Hq); ++h) {
+    const RowParts of(a, units, t, h, tile_rows);
+    join_row(a, kv.D, of.parts(), true, true, of, to + h * a.out.hs, a.lse ? a.lse + of.unit : nullptr);
+  }
+}
+
+// The same for few rows: a workgroup for each, four parts at a time by each of its wavefronts.
+template <typename T>
+__global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int tile_rows) {
+  __shared__ float lds[4][kMaxHeadDim + 1];
+  const int lane = threadIdx.x & 63, l = lane & 15, slot = lane >> 4, wave = threadIdx.x >> 6, D = kv.D;
+  const int64_t unit = blockIdx.x;
+  const int t = static_cast<int>(unit / a.Hq), h = static_cast<int>(unit - static_cast<int64_t>(t) * a.Hq);
+  const RowParts part_of(a, units_of(kv, a, t), t, h, tile_rows);
+  const int n = part_of.parts();
   float high = -INFINITY, total = 0.f, acc[kMaxHeadDim / 16] = {};
   for (int p0 = 0; p0 < n; p0 += 64) {
     const int count_here = min(64, n - p0);
@@ -1580,7 +1675,7 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int tile_rows) 
     total *= keep;
 #pragma unroll
     for (int i = 0; i < kMaxHeadDim / 16; ++i) acc[i] *= keep;
-    for (int c0 = 4 * mine; c0 < count_here; c0 += 4 * WAVES) {
+    for (int c0 = 4 * wave; c0 < count_here; c0 += 16) {
       const int c = c0 + slot;
       const float w = __shfl(weight, c, 64);      // 0 behind the last
       const float* from = a.part_out + part_of(p0 + min(c, count_here - 1)) * D;
@@ -1607,25 +1702,23 @@ __global__ __launch_bounds__(256) void k_join(KvView kv, Args a, int tile_rows) 
     acc[i] += __shfl_xor(acc[i], 16, 64);
     acc[i] += __shfl_xor(acc[i], 32, 64);
   }
-  if constexpr (WAVES > 1) {
-    if (slot == 0) {
-#pragma unroll
-      for (int x = 0; x < kMaxHeadDim / 128; ++x)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) lds[wave][128 * x + 8 * l + i] = acc[8 * x + i];
-      if (l == 0) lds[wave][kMaxHeadDim] = total;
-    }
-    __syncthreads();
-    if (wave) return;
-    total = (lds[0][kMaxHeadDim] + lds[1][kMaxHeadDim]) + (lds[2][kMaxHeadDim] + lds[3][kMaxHeadDim]);
+  if (slot == 0) {
 #pragma unroll
     for (int x = 0; x < kMaxHeadDim / 128; ++x)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int d = 128 * x + 8 * l + i;
-        acc[8 * x + i] = (lds[0][d] + lds[1][d]) + (lds[2][d] + lds[3][d]);
-      }
+      for (int i = 0; i < 8; ++i) lds[wave][128 * x + 8 * l + i] = acc[8 * x + i];
+    if (l == 0) lds[wave][kMaxHeadDim] = total;
   }
+  __syncthreads();
+  if (wave) return;
+  total = (lds[0][kMaxHeadDim] + lds[1][kMaxHeadDim]) + (lds[2][kMaxHeadDim] + lds[3][kMaxHeadDim]);
+#pragma unroll
+  for (int x = 0; x < kMaxHeadDim / 128; ++x)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int d = 128 * x + 8 * l + i;
+      acc[8 * x + i] = (lds[0][d] + lds[1][d]) + (lds[2][d] + lds[3][d]);
+    }
   if (slot == 0) {
     const float f = total == 0.f ? 0.f : 1.f / total;
     T* to = static_cast<T*>(a.out.data) + t * a.out.ts + h * a.out.hs;
@@ -1694,63 +1787,13 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int tile_r
   const int n = (run0 + cost - 1) / share - w + 2;      // parts
   const int64_t queries = static_cast<int64_t>(a.n_tok) * a.Hq;
   // Few parts: sixteen lanes a row; many: a wavefront, four parts at a time.
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, slots = n <= 8 ? 1 : 4, slot = slots == 1 ? 0 : lane >> 4, rows_wave = 4 / slots;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, slots = n <= 8 ? 1 : 4, rows_wave = 4 / slots;
   for (int i0 = (blockIdx.y * 4 + wave) * rows_wave; i0 < tile_rows && r0 + i0 < rows; i0 += gridDim.y * 4 * rows_wave) {
     const int i = min(i0 + (slots == 1 ? lane >> 4 : 0), min(tile_rows, rows - r0) - 1);      // behind the last: the last, once more
     const int tq = (r0 + i) / a.by_share, h = hk * a.share + r0 + i - tq * a.share;
     const int64_t row = static_cast<int64_t>(of.z + tq) * a.Hq + h;
     auto part_of = [&](int p) { return p == 0 ? row : queries + static_cast<int64_t>(w - 1 + p) * kMaxRows + i; };
-    float high = -INFINITY;
-    for (int p = slot * 16 + l; p < n; p += 16 * slots) high = larger(high, a.part_lse[part_of(p)]);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1)
-      if (o < 16 * slots) high = larger(high, __shfl_xor(high, o, 64));
-    const float ref = high == -INFINITY ? 0.f : high;
-    float total = 0.f, acc[kMaxHeadDim / 16] = {};
-    for (int p0 = 0; p0 < n; p0 += 2 * slots) {      // two in flight
-      float weight[2];
-      f32x4 y[2][kMaxHeadDim / 64];
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const int p = p0 + c * slots + slot;
-        const int64_t part = part_of(min(p, n - 1));
-        weight[c] = p < n ? a.part_lse[part] : -INFINITY;
-#pragma unroll
-        for (int x = 0; x < kMaxHeadDim / 128; ++x)
-          if (128 * x + 8 * l < D) {
-            y[c][2 * x] = *reinterpret_cast<const f32x4*>(a.part_out + part * D + 128 * x + 8 * l);
-            y[c][2 * x + 1] = *reinterpret_cast<const f32x4*>(a.part_out + part * D + 128 * x + 8 * l + 4);
-          }
-      }
-#pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const float f = __builtin_amdgcn_exp2f((weight[c] - ref) * kLog2e);
-        const bool there = p0 + c * slots + slot < n;      // behind the last not 0 times an infinity of that
-        total += f;
-#pragma unroll
-        for (int x = 0; x < kMaxHeadDim / 128; ++x)
-          if (128 * x + 8 * l < D)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) acc[8 * x + e] = fmaf(f, there ? y[c][2 * x + (e >> 2)][e & 3] : 0.f, acc[8 * x + e]);
-      }
-    }
-    if (slots == 4) {
-#pragma unroll
-      for (int o = 16; o < 64; o <<= 1) {
-        total += __shfl_xor(total, o, 64);
-#pragma unroll
-        for (int e = 0; e < kMaxHeadDim / 16; ++e) acc[e] += __shfl_xor(acc[e], o, 64);
-      }
-    }
-    if (slot) continue;
-    const float f = total == 0.f ? 0.f : 1.f / total;
-#pragma unroll
-    for (int e = 0; e < kMaxHeadDim / 16; ++e) acc[e] *= f;
-    T* to = static_cast<T*>(a.out.data) + (of.z + tq) * a.out.ts + h * a.out.hs;
-#pragma unroll
-    for (int x = 0; x < kMaxHeadDim / 128; ++x)
-      if (128 * x + 8 * l < D) store8(to + 128 * x + 8 * l, acc + 8 * x);
-    if (a.lse && l == 0) a.lse[row] = total == 0.f ? -INFINITY : high + logf(total);
+    join_row(a, D, n, slots == 4, true, part_of, static_cast<T*>(a.out.data) + (of.z + tq) * a.out.ts + h * a.out.hs, a.lse ? a.lse + row : nullptr);
   }
 }
 
@@ -1880,9 +1923,10 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
     hipLaunchKernelGGL(bf16 ? k_join_runs<bf16_t> : k_join_runs<float>, dim3(static_cast<unsigned>(joins + (clears < 256 ? clears : 256)), y), dim3(256), 0, s,
                        view, args, k.rows, joins, n_units, decode);
   } else if (outputs <= 1024) {      // few rows: a workgroup for each
-    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 4> : k_join<float, 4>), dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows);
+    hipLaunchKernelGGL(bf16 ? k_join<bf16_t> : k_join<float>, dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows);
   } else {
-    hipLaunchKernelGGL((bf16 ? k_join<bf16_t, 1> : k_join<float, 1>), dim3(static_cast<unsigned>(ceil_div(outputs, 4))), dim3(256), 0, s, view, args, k.rows);
+    const int64_t waves = static_cast<int64_t>(n_tok) * ceil_div(Hq, 4);
+    hipLaunchKernelGGL(bf16 ? k_join_heads<bf16_t> : k_join_heads<float>, dim3(static_cast<unsigned>(ceil_div(waves, 4))), dim3(256), 0, s, view, args, k.rows);
   }
   ATG_LAUNCH_CHECK();
   return AT_GRPO_OK;
