@@ -1749,7 +1749,7 @@ __device__ void clear_token(const Args& a, int D, int t) {
 // that no run has: those of sequences that have nothing to see, and of no sequence.
 template <typename T>
 __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int tile_rows, int joins, int n_units, int decode) {
-  const int l = threadIdx.x & 15, D = kv.D, w = blockIdx.x + 1;
+  const int D = kv.D, w = blockIdx.x + 1;
   const int4 all = a.units[n_units];
   if (blockIdx.x >= joins) {
     const int wave = threadIdx.x >> 6, first = ((blockIdx.x - joins) * gridDim.y + blockIdx.y) * 4 + wave, step = (gridDim.x - joins) * gridDim.y * 4;
