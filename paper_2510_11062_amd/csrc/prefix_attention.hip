@@ -597,7 +597,7 @@ constexpr int kPerUnit = D == 256 || D * NR >= 512 ? 1 : 2;
 
 // ---- one new token, or few, in each sequence ---------------------------------------------------------
 // Here a sequence has no more rows than a tile, and all rows of a group read one stream of tokens: the prefix, then the own tokens of its
-// sequences one behind the other, each beginning a block of 32; a row's scores for other sequences' tokens have no weight.  A unit is a
+// sequences that have new ones, one behind the other, each beginning a block of 32; a row's scores for other sequences' tokens have no weight.  A unit is a
 // group, or a sequence in none; with as many tiles of rows as it has, each reads the prefix and its own sequences.  What a row needs is
 // in one run, so rows of runs that one workgroup had whole are done, and a run for each sequence and head, most of whose time would be
 // its beginning and end, is saved: 32 groups of up to 8 take 108 us
@@ -616,7 +616,7 @@ struct DecodeUnit {
 struct DecodeLds {
   int wave_sum[4][2], wave_falls[4];
   int unit, base;
-  int place[kDecodeSeqs + 1];      // blocks in front of each sequence, times 32, and how many tokens its last block has, if not 32
+  int place[kDecodeSeqs + 1];      // blocks in front of each sequence, times 32, and how many tokens its last block has, if not 32; of the stream's tokens
   int pages_before[kDecodeSeqs + 1];
   DecodeUnit cache[kDecodeUnits];
   int pages[kDecodeSlots];
@@ -699,18 +699,21 @@ __device__ Share decode_schedule(const KvView& kv, const Args& a, DecodeLds& lds
     }
   };
   const int per_seq = (kv.n_seq + 255) / 256, s0 = min(kv.n_seq, tid * per_seq), s1 = min(kv.n_seq, s0 + per_seq), most = kv.max_pages << kv.page_shift;
-  auto length = [&](int s) {
+  // Of a sequence without new tokens nothing is read: no query sees it, and its pages may be somebody else's by now.
+  auto length = [&](int s, bool* error) {
     const int len = kv.length[s];
-    return len < 0 || len > most ? -1 : len;
+    *error = len < 0 || len > most;
+    return *error || (kv.cu_q && kv.cu_q[s + 1] <= kv.cu_q[s]) ? 0 : len;
   };
   const int per = (n + 255) / 256, u0 = min(n, tid * per);
   const GroupSizes ahead = group_sizes(kv, u0);      // on its way while the sequences are counted
   int blocks = 0, page_count = 0, unused;
   for (int s = s0; s < s1; ++s) {
-    const int len = length(s);
-    if (len < 0) error |= AT_GRPO_DATA_SEQLENS;
-    blocks += (max(0, len) + 31) >> 5;
-    page_count += (max(0, len) + (1 << kv.page_shift) - 1) >> kv.page_shift;
+    bool wrong;
+    const int len = length(s, &wrong);
+    if (wrong) error |= AT_GRPO_DATA_SEQLENS;
+    blocks += (len + 31) >> 5;
+    page_count += (len + (1 << kv.page_shift) - 1) >> kv.page_shift;
     if (kv.cu_q) falls |= kv.cu_q[s] < 0 || kv.cu_q[s + 1] < kv.cu_q[s] || kv.cu_q[s + 1] > a.n_tok;
   }
   for (int g = tid; g < kv.n_group; g += 256) falls |= kv.group_seq[g] < 0 || kv.group_seq[g + 1] < kv.group_seq[g] || kv.group_seq[g + 1] > kv.n_seq;
@@ -719,7 +722,8 @@ __device__ Share decode_schedule(const KvView& kv, const Args& a, DecodeLds& lds
   scan(blocks, page_count, &unused);
   const bool none = lds.wave_falls[0] | lds.wave_falls[1] | lds.wave_falls[2] | lds.wave_falls[3];
   for (int s = s0; s < s1; ++s) {
-    const int len = max(0, length(s));
+    bool wrong;
+    const int len = length(s, &wrong);
     lds.place[s] = blocks << 5 | (len & 31);
     lds.pages_before[s] = page_count;
     blocks += (len + 31) >> 5;
@@ -979,6 +983,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
             }
           }
           weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, [&] {
+            // the one new token of a unit sees its stream whole: that of its sequence alone
             if (tile.seq >= 0 && u.ntok > 1) set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) { return token < left[n]; });
           });
           load_v(next);

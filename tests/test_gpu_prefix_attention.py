@@ -487,3 +487,32 @@ def test_many_queries_of_heads_of_any_size(gpu_device, dtype, D, group):
     for causal in (True, False):
         out = attend(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), max_q=150, want_lse=True, causal=causal)
         check(p, q64, out, p.attention(q64, 1.0 / np.sqrt(D), causal=causal), f"causal {causal}")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D", [64, 72, 128, 256])
+@pytest.mark.parametrize("max_q", [1, 2, 64])
+@pytest.mark.parametrize("new", [[0, 1, 0, 0, 0, 1, 0], [0, 0, 0, 0, 2, 0, 1], [1, 0, 1, 0, 0, 0, 0]], ids=["one", "two", "half"])
+def test_candidates_that_have_ended(gpu_device, dtype, D, max_q, new):
+    # siblings without new tokens: nobody sees what they hold, and their pages may be somebody else's or nobody's by now
+    p = Paged(dtype, 2, D, 16, [3, 100, 41, 0, 70, 33, 64], new, [4, 2], [70, 45], seed=70 + D)
+    q64 = p.queries(8)
+    scale = 1.0 / np.sqrt(D)
+    for causal in (True, False):
+        ref = p.attention(q64, scale, causal)
+        for s in range(7):
+            if not p.new[s]:
+                for i, x in enumerate((np.inf, np.nan, -np.inf)):
+                    if i < p.length[s]:
+                        p.v[p.pages[s][i // 16], :, i % 16] = x
+                        p.k[p.pages[s][i // 16], :, i % 16] = x
+        q = to_dev(q64, p.dtype, gpu_device)
+        out = attend(p.device(gpu_device), q, scale=scale, max_q=max_q, want_lse=True, causal=causal)
+        check(p, q64, out, ref, f"causal {causal}")
+        released = p.pages.copy()
+        released[p.new == 0] = -1
+        word = torch.zeros(1, dtype=torch.int32, device=gpu_device)
+        again = attend(p.device(gpu_device, pages=i32(released, gpu_device)), q, scale=scale, max_q=max_q, want_lse=True, causal=causal, data_error=word)
+        assert int(word) == 0
+        assert torch.equal(again["out"], out["out"]) and torch.equal(again["lse"], out["lse"])
