@@ -79,6 +79,11 @@ struct Unit {
   int tok0, ntok, len, row;      // row: of the page table
 };
 
+// Without sequences nothing else looks at the one entry of cu_q, up to which and from which on rows belong to nobody.
+__device__ __forceinline__ bool no_sequence_falls(const KvView& kv, int n_tok) {
+  return kv.n_seq == 0 && kv.cu_q && (kv.cu_q[0] < 0 || kv.cu_q[0] > n_tok);
+}
+
 __device__ __forceinline__ Unit unit_of(const KvView& kv, int u, int n_tok, int* error, bool* falls) {
   int s0 = u - kv.n_group, s1 = s0 + 1, len, most;
   if (u < kv.n_group) {
@@ -153,7 +158,7 @@ __device__ Share make_schedule(const KvView& kv, const Args& a, Schedule& S) {
   const int n = kv.n_group + kv.n_seq, per = (n + 255) / 256, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int u0 = min(n, tid * per), u1 = min(n, u0 + per);
   int error = 0, mine = 0;
-  bool falls = false;
+  bool falls = no_sequence_falls(kv, a.n_tok);
   for (int u = u0; u < u1; ++u) {
     const Unit x = unit_of(kv, u, a.n_tok, &error, &falls);
     if (u < kCachedUnits) S.cache[u] = x;
@@ -669,7 +674,7 @@ template <int R>
 __device__ Share decode_schedule(const KvView& kv, const Args& a, DecodeLds& lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = kv.n_group + kv.n_seq;
   int error = 0;
-  bool falls = false;
+  bool falls = no_sequence_falls(kv, a.n_tok);
   // Two sums over all threads, in front of this one's share of them.
   auto scan = [&](int& x, int& y, int* total) {
     int sx = x, sy = y;

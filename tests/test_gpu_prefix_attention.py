@@ -516,3 +516,23 @@ def test_candidates_that_have_ended(gpu_device, dtype, D, max_q, new):
         again = attend(p.device(gpu_device, pages=i32(released, gpu_device)), q, scale=scale, max_q=max_q, want_lse=True, causal=causal, data_error=word)
         assert int(word) == 0
         assert torch.equal(again["out"], out["out"]) and torch.equal(again["lse"], out["lse"])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("max_q", [1, 64])
+@pytest.mark.parametrize("group", [False, True])
+@pytest.mark.parametrize("first", [-(1 << 31), -2, 0, 2, 3, 4, 9, (1 << 31) - 1])
+def test_no_sequences(gpu_device, dtype, max_q, group, first):
+    """Every row belongs to nobody, wherever the one entry of cu_q stands; nothing beside the rows is written."""
+    dt, n = DTYPES[dtype], 3
+    cache = torch.full((2, 2, 16, 64), float("nan"), dtype=dt, device=gpu_device)
+    none = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=gpu_device)
+    kw = dict(group_seq=none(2), prefix_len=i32([16], gpu_device), prefix_pages=none(1, 1)) if group else {}
+    kv = api.KVBatch(cache, cache, none(0, 2), none(0), cu_q=i32([first], gpu_device), **kw)
+    around = torch.full((n + 40, 4, 64), 7.0, dtype=dt, device=gpu_device)
+    word = none(1)
+    out = attend(kv, torch.ones(n, 4, 64, dtype=dt, device=gpu_device), max_q=max_q, want_lse=True, out=around[20:20 + n], data_error=word)
+    assert int(word) == (0 if 0 <= first <= n else 8)
+    assert not around[20:20 + n].any() and torch.isneginf(out["lse"]).all()
+    assert (around[:20] == 7).all() and (around[20 + n:] == 7).all()
