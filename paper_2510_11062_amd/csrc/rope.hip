@@ -112,7 +112,8 @@ __device__ __forceinline__ Raw<T> raw_of(const Pairs& x, const Places& p) {
     return Raw<T>{make_uint2(pack_bf16x2(lo[0], lo[1]), pack_bf16x2(lo[2], lo[3])), make_uint2(pack_bf16x2(hi[0], hi[1]), pack_bf16x2(hi[2], hi[3]))};
 }
 
-// Cosines and sines of a lane's pairs; 1 and 0 behind the last that turns.
+// Cosines and sines of a lane's pairs; 1 and 0 behind the last that turns (such a pair is passed by, not multiplied: 0 times an infinite
+// partner would be NaN).
 template <bool VEC>
 __device__ __forceinline__ Pairs load_turn(const Layer& L, int l, int position) {
   Pairs t{{1.f, 1.f, 1.f, 1.f}, {}};
@@ -222,13 +223,14 @@ struct Rotator {
   static constexpr int G = 64 / LANES;
   const Layer& L;
   const Places p;
-  const int l, grp;
+  const int l, grp, turning;      // of the lane's pairs the first `turning` turn
   const bool mine;
   Raw<T> raw_wq{}, raw_wk{}, x[kBatch];
   Pairs wq, wk;
 
   __device__ __forceinline__ explicit Rotator(const Layer& layer)
-      : L(layer), p(places_of<VEC>(layer, threadIdx.x & (LANES - 1))), l(threadIdx.x & (LANES - 1)), grp((threadIdx.x & 63) / LANES), mine(8 * l < layer.D) {
+      : L(layer), p(places_of<VEC>(layer, threadIdx.x & (LANES - 1))), l(threadIdx.x & (LANES - 1)), grp((threadIdx.x & 63) / LANES), turning(layer.half - 4 * l),
+        mine(8 * l < layer.D) {
     if (mine && L.qw) raw_wq = load_raw<VEC>(static_cast<const T*>(L.qw), p);
     if (mine && L.kw) raw_wk = load_raw<VEC>(static_cast<const T*>(L.kw), p);
   }
@@ -265,8 +267,8 @@ struct Rotator {
             u.a[e] *= r * (is_q ? wq.a[e] : wk.a[e]);
             u.b[e] *= r * (is_q ? wq.b[e] : wk.b[e]);
           }
-          v.a[e] = fmaf(u.a[e], turn.a[e], -u.b[e] * turn.b[e]);
-          v.b[e] = fmaf(u.b[e], turn.a[e], u.a[e] * turn.b[e]);
+          v.a[e] = e < turning ? fmaf(u.a[e], turn.a[e], -u.b[e] * turn.b[e]) : u.a[e];
+          v.b[e] = e < turning ? fmaf(u.b[e], turn.a[e], u.a[e] * turn.b[e]) : u.b[e];
         }
         y = raw_of<T>(v, p);
       }
@@ -347,6 +349,7 @@ __device__ __forceinline__ void rotate_rows_back(const Layer& L, const T* dy, in
                                                  const Pairs& w, bool norm, const Pairs& turn, const Places& p, bool zero, int part, int parts, Pairs& dw) {
   constexpr int G = 64 / LANES;
   const int l = threadIdx.x & (LANES - 1), grp = (threadIdx.x & 63) / LANES;
+  const int turning = L.half - 4 * l;
   const bool mine = 8 * l < L.D;
   for (int h0 = part * G; h0 < H; h0 += kGradBatch * parts * G) {
     Raw<T> rx[kGradBatch], rg[kGradBatch];
@@ -368,8 +371,8 @@ __device__ __forceinline__ void rotate_rows_back(const Layer& L, const T* dy, in
       Pairs x = pairs_of(rx[i], p), g;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        g.a[e] = fmaf(d.a[e], turn.a[e], d.b[e] * turn.b[e]);
-        g.b[e] = fmaf(d.b[e], turn.a[e], -d.a[e] * turn.b[e]);
+        g.a[e] = e < turning ? fmaf(d.a[e], turn.a[e], d.b[e] * turn.b[e]) : d.a[e];
+        g.b[e] = e < turning ? fmaf(d.b[e], turn.a[e], -d.a[e] * turn.b[e]) : d.b[e];
       }
       if (norm) {
         const float r = inverse_size<LANES>(x, L);

@@ -274,3 +274,38 @@ def test_refusals_of_the_library_on_the_host():
         a.update(kw)
         assert lib.at_grpo_rope_table(C.byref(api._Rope(*a.values())), 4, 4096, None) == status, kw
     assert lib.at_grpo_rope_table(None, 4, 4096, None) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("D,rot,inter", [(64, 0, False), (64, 32, False), (64, 32, True), (80, 20, False), (80, 50, True), (256, 192, False), (128, 2, False)])
+@pytest.mark.parametrize("normed", [False, True])
+def test_elements_that_do_not_turn(gpu_device, dtype, D, rot, inter, normed):
+    """Behind rot_dim an element is its own: infinities, NaN and signs of zeros of one do not reach another, forward and in the gradient
+    (with a norm, what goes into the row's size and mean reaches all of the row by the formula)."""
+    c, dv = case(gpu_device, dtype, 7, 3, 2, D, rot, inter, (normed, normed), seed=3)
+    dt = DTYPES[dtype]
+    for name in ("q", "dq", "k", "dk"):
+        x = c[name]
+        if name.startswith("d") or not normed:
+            x[0, 0, rot + 1], x[1, 1, D - 2], x[2, 0, rot], x[2, 0, D - 1] = np.inf, np.nan, -np.inf, np.inf
+        x[3, 1, rot], x[3, 1, rot + 1] = -0.0, -1.5
+        x[4, 0, rot], x[4, 0, rot + 1] = -0.0, 1.5
+        dv[name] = to_dev(x, dt, gpu_device)
+    out, grad = forward(dv, inter), backward(dv, inter)
+    for name in ("q", "k"):
+        args = c[name + "_weight"], c["table"], c["position"]
+        with np.errstate(invalid="ignore"):
+            ref = oracle.norm_rope(c[name], *args, 1e-5, inter)
+            dx, dw = oracle.norm_rope_grad(c["d" + name], c[name], *args, 1e-5, inter)
+        got, gx = host64(out[name]), host64(grad["d" + name])
+        for mine, want in ((got, ref), (gx, dx)):
+            assert np.array_equal(np.isnan(mine), np.isnan(want)) and np.array_equal(np.isinf(mine), np.isinf(want))
+            assert np.array_equal(mine[np.isinf(mine)], want[np.isinf(want)])
+            zero = want == 0
+            assert np.array_equal(np.signbit(mine[zero]), np.signbit(want[zero]))
+        if normed:
+            assert np.array_equal(np.isnan(host64(grad[f"d{name}_weight"])), np.isnan(dw)) and np.array_equal(np.isinf(host64(grad[f"d{name}_weight"])), np.isinf(dw))
+        else:
+            keep = slice(rot, None)
+            assert np.array_equal(got[..., keep], c[name][..., keep], equal_nan=True) and np.array_equal(gx[..., keep], c["d" + name][..., keep], equal_nan=True)
