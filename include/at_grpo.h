@@ -466,9 +466,10 @@ typedef struct {
 /*
  * The new tokens' keys, normed and rotated by their positions as at_grpo_qk_norm_rope does, and their values as
  * they are go into the cache; their queries, normed and rotated, to q_out (Hq == 0: none).  `length` already
- * counts the new tokens.  Rows q [n_tok, Hq, D], k and v [n_tok, kv->Hk, D].  A token that belongs to no sequence
- * (AT_GRPO_DATA_SEQLENS), whose position lies outside the table (AT_GRPO_DATA_POSITION) or whose page is none of
- * the cache's (AT_GRPO_DATA_PAGE) is left out of the cache, and its q_out rows are zeros.
+ * counts the new tokens.  Rows q [n_tok, Hq, D], k and v [n_tok, kv->Hk, D].  A token that belongs to no sequence,
+ * or that the entries of group_seq in front of it and behind it do not enclose, since they fall or leave their
+ * range (AT_GRPO_DATA_SEQLENS), whose position lies outside the table (AT_GRPO_DATA_POSITION) or whose page is
+ * none of the cache's (AT_GRPO_DATA_PAGE) is left out of the cache, and its q_out rows are zeros.
  */
 int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* layer, int32_t n_tok, int32_t Hq,
                       const at_grpo_rows* q, const at_grpo_rows* k, const at_grpo_rows* v,

@@ -169,7 +169,7 @@ __device__ __forceinline__ Spot find_spot(const KvView& kv, int n_pos, int t, co
   Spot spot{-1, 0};
   const bool there = of.s >= 0 && of.s < kv.n_seq, grouped = of.g >= 0 && of.g < kv.n_group;
   const int s = there ? of.s : 0;
-  int length = 0, q0 = t, q1 = t + 1, prefix = 0;
+  int length = 0, q0 = t, q1 = t + 1, prefix = 0, g0 = s, g1 = s + 1;
   if (kv.n_seq > 0) {
     length = kv.length[s];
     if (kv.cu_q) {
@@ -177,10 +177,14 @@ __device__ __forceinline__ Spot find_spot(const KvView& kv, int n_pos, int t, co
       q1 = kv.cu_q[s + 1];
     }
   }
-  if (grouped) prefix = kv.prefix_len[of.g];
+  if (grouped) {
+    prefix = kv.prefix_len[of.g];
+    g0 = kv.group_seq[of.g];
+    g1 = kv.group_seq[of.g + 1];
+  }
   int error = 0, place = -1;
   if (!there || q0 < 0 || q0 > t || q1 <= t || length < 0 || length > (kv.max_pages << kv.page_shift) || q1 - q0 > length || prefix < 0 ||
-      prefix > (kv.max_prefix_pages << kv.page_shift))
+      prefix > (kv.max_prefix_pages << kv.page_shift) || g0 < 0 || g0 > s || g1 <= s || g1 > kv.n_seq)
     error = AT_GRPO_DATA_SEQLENS;
   else
     place = length - (q1 - t);

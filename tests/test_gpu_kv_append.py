@@ -203,3 +203,23 @@ def test_refusals_of_the_library_on_the_host():
                        (dict(pages=None), 1), (dict(length=None), 1), (dict(group_seq=None), 1), (dict(prefix_len=None), 1),
                        (dict(prefix_pages=None), 1), (dict(n=3), 1), (dict(n=-1), 1), (dict(hq=-1), 1), (dict(max_pages=1 << 28), 2), (dict(k=4100), 1)]:
         assert call(**kw) == status, kw
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group_seq,lost", [([0, 3, 2], [2]), ([0, 2, 5], [2, 3]), ([-1, 2, 4], [0, 1]), ([3, 2, 4], [2]), ([0, 1 << 30, 4], [0, 1, 2, 3])])
+def test_groups_that_fall_or_leave_their_range(gpu_device, group_seq, lost):
+    """A sequence that the entries around it do not enclose has no prefix to go by: its tokens are left out, as those of no sequence are."""
+    spec = ("bf16", 4, 2, 64, 64, False, 16, [5, 40, 16, 9], [2, 3, 1, 4], [2, 2], [9, 20])
+    p, c, dv = case(gpu_device, spec)
+    word = torch.zeros(1, dtype=torch.int32, device=gpu_device)
+    kv = p.device(gpu_device, group_seq=i32(group_seq, gpu_device))
+    q = append(kv, dv, False, data_error=word)["q"]
+    assert int(word) == 8
+    empty = p.device(gpu_device)
+    for s in range(4):
+        mine = slice(int(p.cu_q[s]), int(p.cu_q[s + 1]))
+        assert bool(q[mine].any()) == (s not in lost)
+        for i in range(int(p.length[s] - p.new[s]), int(p.length[s])):
+            at = p.pages[s][i // 16], slice(None), i % 16
+            for got, before in ((kv.cache_k, empty.cache_k), (kv.cache_v, empty.cache_v)):
+                assert torch.equal(got[at].view(torch.int16), before[at].view(torch.int16)) == (s in lost)
