@@ -17,7 +17,8 @@
  *   - `workspace` is caller-provided device scratch of at least at_grpo_workspace_bytes()
  *     bytes, 256-byte aligned.  Its first int32 is an error word: 0, or the bit-or of
  *     AT_GRPO_DATA_* flags raised by data that is only visible on the device.  Offending
- *     elements are treated as masked out.  Read it after synchronising the stream.
+ *     elements are treated as masked out.  Read it after synchronising the stream.  (The calls on queries,
+ *     keys and the cache use the first word as scratch: they raise their flags in `data_error`.)
  *   - Return value: an at_grpo_status.  Argument errors are detected on the host before
  *     anything is launched; nothing is thrown and nothing aborts.
  *   - Matrices are row-major and dense.  `hidden` is [n_tok, H]; each head W is [V, H].

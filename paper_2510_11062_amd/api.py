@@ -202,6 +202,7 @@ def _dev_check(*tensors):
 
 _workspace_cache = {}
 _workspace_retired = []
+_scratch_cache = {}      # (device, stream): (workspace, its part behind the error word)
 
 
 def _workspace(nbytes: int, device) -> torch.Tensor:
@@ -220,9 +221,26 @@ def _workspace(nbytes: int, device) -> torch.Tensor:
     return ws
 
 
+def _scratch(nbytes: int, device) -> torch.Tensor:
+    """The workspace behind its first 256 bytes, for calls that keep no error word: the last word of those that do stays there."""
+    ws = _workspace(int(nbytes) + 256, device)
+    scratch = ws[256:]
+    scratch.keeps_no_error_word = True
+    _scratch_cache[device.index, _raw_stream(device.index)] = ws, scratch
+    return scratch
+
+
+def _scratch_at_hand(device) -> Optional[torch.Tensor]:
+    """What _scratch gave last for this device and stream, if it is still part of the workspace."""
+    key = (device.index, _raw_stream(device.index))
+    ws, scratch = _scratch_cache.get(key, (None, None))
+    return scratch if ws is _workspace_cache.get(key) else None
+
+
 def release_workspace():
     """Drops every cached workspace (only when no captured graph that used the binding will be replayed)."""
     _workspace_cache.clear()
+    _scratch_cache.clear()
     _workspace_retired.clear()
 
 
@@ -609,7 +627,9 @@ def at_grpo_policy_loss_fwd_bwd(batch: Batch, old_logp, adv, eps_low: float, eps
 
 
 def error_word(workspace: torch.Tensor) -> int:
-    """Device error word of the last call that used this workspace (synchronises)."""
+    """Device error word of the last call that used this workspace (synchronises).  The calls on queries, keys and the cache keep none there."""
+    if getattr(workspace, "keeps_no_error_word", False):
+        raise AtGrpoError("this call keeps no error word in its workspace: it raises its bits in the data_error that it is given")
     return int(workspace[:4].view(torch.int32).item())
 
 
@@ -710,7 +730,9 @@ def at_grpo_qk_norm_rope_bwd(dq_out, dk_out, q, k, rope, position, q_weight=None
     x = q if q is not None else k
     out = None
     if x is not None and x.is_cuda:
-        ws = _workspace(_rope_bwd_bytes(), x.device)
+        ws = _scratch_at_hand(x.device)
+        if ws is None or ws.numel() < _rope_bwd_bytes():
+            ws = _scratch(_rope_bwd_bytes(), x.device)
         out = _binding.qk_norm_rope_bwd(_fn["at_grpo_qk_norm_rope_bwd"], dq_out, dk_out, q, k, rope, position, q_weight, k_weight, eps, interleaved,
                                         dq, dk, data_error, ws.data_ptr(), ws.numel(), _stream())
     if type(out) is dict:
@@ -827,12 +849,12 @@ def at_grpo_prefix_attention(kv: KVBatch, q, scale: Optional[float] = None, caus
     res = None
     if q.is_cuda:
         stream = _stream()
-        ws = _workspace_cache.get((q.device.index, stream))
+        ws = _scratch_at_hand(q.device)
         call = lambda: _binding.prefix_attention(_fn["at_grpo_prefix_attention"], _fn["at_grpo_prefix_attention_workspace_bytes"], kv, q, scale,
                                                  causal, max_q, out, want_lse, data_error, ws, stream)
         res = call()
         if type(res) is tuple:
-            ws = _workspace(res[0], q.device)
+            ws = _scratch(res[0], q.device)
             res = call()
     if type(res) is dict:
         res["workspace"] = ws
