@@ -1869,13 +1869,52 @@ Choice choose(int D, int rows_p, int rows_o, bool decode) {
   return choose_of<T, 256, false>(rows_p, rows_o, decode);
 }
 
+// Everything that goes by sizes alone.
+struct Plan {
+  Choice choice;
+  bool decode;
+  int coarse;
+  double most;      // an upper bound of all costs together
+};
+
+int make_plan(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q, Plan* out) {
+  ATG_TRY(check_sizes(kv, n_tok, Hq, max_q));
+  const int share = Hq / kv->Hk;
+  const int64_t all_rows = static_cast<int64_t>(n_tok) * share;
+  const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
+  auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
+  const auto eights_of = [&](int64_t pages) { return static_cast<double>(pages) * kv->page_size / 8; };
+  const double fixed = 8 + kRunCost + kMinShare;
+  // Few rows a sequence, as many sequences as LDS has places for, their blocks counted in 26 bits and all costs in 30.
+  const double decode_most = kv->Hk * ((all_rows / 16 + kv->n_group + kv->n_seq) * (eights_of(kv->max_prefix_pages) + fixed) + kv->n_seq * (eights_of(kv->max_pages) + fixed));
+  out->decode = rows_o <= 16 && kv->n_seq <= kDecodeSeqs && static_cast<int64_t>(kv->n_seq + 1) * kv->max_pages * kv->page_size < 1 << 30 &&
+                decode_most < 1 << 30;
+  const int rows_u = small(kv->n_group ? rows_p : rows_o);
+  out->choice = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, rows_u, small(rows_o), out->decode) : choose<float>(kv->D, rows_u, small(rows_o), out->decode);
+  const int64_t tiles_p = kv->n_group ? all_rows / out->choice.rows + kv->n_group : 0, tiles_o = all_rows / out->choice.rows + kv->n_seq;
+  out->coarse = 0;
+  if (out->decode) {
+    out->most = kv->Hk * ((tiles_o + tiles_p) * (kRunCost + 8.0) + tiles_p * (eights_of(kv->max_prefix_pages) + fixed) + kv->n_seq * (eights_of(kv->max_pages) + fixed));
+    return AT_GRPO_OK;
+  }
+  // Costs are added up in 32 bits.  Those of tokens are counted in larger blocks where need be; what each run costs beside them (kRunCost, and
+  // up to 1 by rounding up) does not shrink.
+  const double runs = kv->Hk * static_cast<double>(tiles_p + tiles_o), beside = runs * (kRunCost + 1);
+  double tokens = kv->Hk * (tiles_p * eights_of(kv->max_prefix_pages) + tiles_o * eights_of(kv->max_pages));
+  if (beside > 1 << 30) return AT_GRPO_EUNSUPPORTED;
+  out->most = tokens + runs * fixed;
+  for (; tokens + beside > 3 << 29; tokens /= 2) ++out->coarse;
+  return AT_GRPO_OK;
+}
+
 }  // namespace
 }  // namespace atg
 
 using namespace atg;
 
 extern "C" size_t at_grpo_prefix_attention_workspace_bytes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q) {
-  if (check_sizes(kv, n_tok, Hq, max_q) != AT_GRPO_OK) return 0;
+  Plan plan;
+  if (make_plan(kv, n_tok, Hq, max_q, &plan) != AT_GRPO_OK) return 0;
   WsAlloc ws(nullptr);
   lay_out(kv, n_tok, Hq, ws);
   return ws.bytes();
@@ -1884,7 +1923,8 @@ extern "C" size_t at_grpo_prefix_attention_workspace_bytes(const at_grpo_kv* kv,
 extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* q, float scale, int32_t causal,
                                         int32_t max_q, const at_grpo_rows* out, float* lse, int32_t* data_error, void* workspace,
                                         size_t workspace_bytes, void* hip_stream) {
-  ATG_TRY(check_sizes(kv, n_tok, Hq, max_q));
+  Plan plan;
+  ATG_TRY(make_plan(kv, n_tok, Hq, max_q, &plan));
   if (!(scale > 0.f) || !isfinite(scale)) return AT_GRPO_EINVAL;
   KvView view;
   ATG_TRY(check_kv(kv, n_tok, &view));
@@ -1896,27 +1936,14 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < ws.bytes()) return AT_GRPO_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int share = Hq / kv->Hk;
-  Args args{n_tok, Hq, share, divisor(share), 0, 0, 1, causal != 0, scale, rows_of(q), rows_of(out), lse, data_error, scratch.units, scratch.part_lse, scratch.part_out};
-  const int64_t all_rows = static_cast<int64_t>(n_tok) * share;
-  const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
-  auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
-  const auto cost_of_pages = [&](int64_t pages) { return static_cast<double>(pages) * kv->page_size / 8 + 8 + kRunCost + kMinShare; };
-  // Few rows a sequence, as many sequences as LDS has places for, their blocks counted in 26 bits and all costs in 30.
-  const double decode_most = kv->Hk * ((all_rows / 16 + kv->n_group + kv->n_seq) * cost_of_pages(kv->max_prefix_pages) + kv->n_seq * cost_of_pages(kv->max_pages));
-  const bool decode = rows_o <= 16 && kv->n_seq <= kDecodeSeqs && static_cast<int64_t>(kv->n_seq + 1) * kv->max_pages * kv->page_size < 1 << 30 &&
-                      decode_most < 1 << 30;
-  const int rows_u = small(kv->n_group ? rows_p : rows_o);
-  const Choice k = kv->dtype == AT_GRPO_BF16 ? choose<bf16_t>(kv->D, rows_u, small(rows_o), decode) : choose<float>(kv->D, rows_u, small(rows_o), decode);
+  const Choice& k = plan.choice;
+  const bool decode = plan.decode;
   const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
-  // an upper bound of all costs together, which are counted in 32 bits
-  const int64_t tiles_p = kv->n_group ? all_rows / k.rows + kv->n_group : 0, tiles_o = all_rows / k.rows + kv->n_seq;
-  double most = decode ? kv->Hk * ((tiles_o + tiles_p) * (kRunCost + 8.0) + tiles_p * cost_of_pages(kv->max_prefix_pages) + kv->n_seq * cost_of_pages(kv->max_pages))
-                       : kv->Hk * (tiles_p * cost_of_pages(kv->max_prefix_pages) + tiles_o * cost_of_pages(kv->max_pages));
-  for (; most > 1 << 30; most /= 2) ++args.coarse;
+  Args args{n_tok, Hq, share, divisor(share), plan.coarse, 0, 1, causal != 0, scale, rows_of(q), rows_of(out), lse, data_error, scratch.units, scratch.part_lse, scratch.part_out};
   args.rise = k.rows / (8 * share) >> args.coarse;
   // Where there are workgroups enough, costs are whole shares, so that a run begins with a workgroup: one group of four by
   // k_attend 13.2 us, then 8.0.
-  if (most <= static_cast<double>(kMinShare) * blocks) {
+  if (plan.most <= static_cast<double>(kMinShare) * blocks) {
     args.quantum = kMinShare;
     args.rise = 0;
   }

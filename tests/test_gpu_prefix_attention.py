@@ -536,3 +536,22 @@ def test_no_sequences(gpu_device, dtype, max_q, group, first):
     assert int(word) == (0 if 0 <= first <= n else 8)
     assert not around[20:20 + n].any() and torch.isneginf(out["lse"]).all()
     assert (around[:20] == 7).all() and (around[20 + n:] == 7).all()
+
+
+def test_batches_whose_costs_pass_32_bits_are_refused_on_the_host():
+    """Each run of a sequence, key head and tile costs 16 eights of tokens beside its own, and all are added up in 32 bits."""
+    lib, C = api.load_library(), api.C
+    r = C.byref(api._Rows(4096, 8, 8))
+
+    def kv(n_seq, n_group=0, max_pages=1, Hk=100):
+        return C.byref(api._KV(dtype=1, Hk=Hk, D=8, page_size=8, n_pages=9, n_seq=n_seq, max_pages=max_pages, n_group=n_group, max_prefix_pages=1, k=4096, v=4096,
+                               pages=4096, length=4096, cu_q=4096, group_seq=4096, prefix_len=4096, prefix_pages=4096))
+
+    for n_tok, n_seq, n_group, ok in [(2000000, 2000000, 0, False), (1, 2000000, 0, False), (600000, 600000, 0, False), (590000, 590000, 0, True),
+                                      (100, 100, 2000000, False), (300000, 300000, 300000, False), (270000, 270000, 270000, True), (1, 1000, 0, True)]:
+        size = lib.at_grpo_prefix_attention_workspace_bytes(kv(n_seq, n_group), n_tok, 100, 1)
+        assert (size > 0) == ok, (n_tok, n_seq, n_group)
+        if not ok:
+            assert lib.at_grpo_prefix_attention(kv(n_seq, n_group), n_tok, 100, r, 1.0, 1, 1, r, None, None, 4096, 1 << 40, None) == 2
+    # whatever the tables' width, their tokens are counted in blocks large enough
+    assert lib.at_grpo_prefix_attention_workspace_bytes(kv(590000, 0, 1 << 26), 590000, 100, 1) > 0
