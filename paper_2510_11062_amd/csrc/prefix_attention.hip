@@ -704,22 +704,19 @@ __device__ Share decode_schedule(const KvView& kv, const Args& a, DecodeLds& lds
     }
   };
   const int per_seq = (kv.n_seq + 255) / 256, s0 = min(kv.n_seq, tid * per_seq), s1 = min(kv.n_seq, s0 + per_seq), most = kv.max_pages << kv.page_shift;
-  // Of a sequence without new tokens nothing is read: no query sees it, and its pages may be somebody else's by now.
-  auto length = [&](int s, bool* error) {
-    const int len = kv.length[s];
-    *error = len < 0 || len > most;
-    return *error || (kv.cu_q && kv.cu_q[s + 1] <= kv.cu_q[s]) ? 0 : len;
-  };
   const int per = (n + 255) / 256, u0 = min(n, tid * per);
   const GroupSizes ahead = group_sizes(kv, u0);      // on its way while the sequences are counted
   int blocks = 0, page_count = 0, unused;
   for (int s = s0; s < s1; ++s) {
-    bool wrong;
-    const int len = length(s, &wrong);
+    const int length = kv.length[s], q0 = kv.cu_q ? kv.cu_q[s] : s, q1 = kv.cu_q ? kv.cu_q[s + 1] : s + 1;
+    falls |= q0 < 0 || q1 < q0 || q1 > a.n_tok;
+    const bool wrong = length < 0 || length > most;
     if (wrong) error |= AT_GRPO_DATA_SEQLENS;
+    // Of a sequence without new tokens nothing is read: no query sees it, and its pages may be somebody else's by now.
+    const int len = wrong || q1 <= q0 ? 0 : length;
+    lds.place[s] = len;
     blocks += (len + 31) >> 5;
     page_count += (len + (1 << kv.page_shift) - 1) >> kv.page_shift;
-    if (kv.cu_q) falls |= kv.cu_q[s] < 0 || kv.cu_q[s + 1] < kv.cu_q[s] || kv.cu_q[s + 1] > a.n_tok;
   }
   for (int g = tid; g < kv.n_group; g += 256) falls |= kv.group_seq[g] < 0 || kv.group_seq[g + 1] < kv.group_seq[g] || kv.group_seq[g + 1] > kv.n_seq;
   const bool wave_falls = __any(falls);
@@ -727,8 +724,7 @@ __device__ Share decode_schedule(const KvView& kv, const Args& a, DecodeLds& lds
   scan(blocks, page_count, &unused);
   const bool none = lds.wave_falls[0] | lds.wave_falls[1] | lds.wave_falls[2] | lds.wave_falls[3];
   for (int s = s0; s < s1; ++s) {
-    bool wrong;
-    const int len = length(s, &wrong);
+    const int len = lds.place[s];      // this thread's own
     lds.place[s] = blocks << 5 | (len & 31);
     lds.pages_before[s] = page_count;
     blocks += (len + 31) >> 5;
