@@ -230,11 +230,10 @@ def _scratch(nbytes: int, device) -> torch.Tensor:
     return scratch
 
 
-def _scratch_at_hand(device) -> Optional[torch.Tensor]:
-    """What _scratch gave last for this device and stream, if it is still part of the workspace."""
-    key = (device.index, _raw_stream(device.index))
-    ws, scratch = _scratch_cache.get(key, (None, None))
-    return scratch if ws is _workspace_cache.get(key) else None
+def _scratch_at_hand(key) -> Optional[torch.Tensor]:
+    """What _scratch gave last for this (device, stream), if it is still part of the workspace."""
+    held = _scratch_cache.get(key)
+    return held[1] if held is not None and held[0] is _workspace_cache.get(key) else None
 
 
 def release_workspace():
@@ -730,11 +729,12 @@ def at_grpo_qk_norm_rope_bwd(dq_out, dk_out, q, k, rope, position, q_weight=None
     x = q if q is not None else k
     out = None
     if x is not None and x.is_cuda:
-        ws = _scratch_at_hand(x.device)
+        stream = _stream()
+        ws = _scratch_at_hand((x.device.index, stream))
         if ws is None or ws.numel() < _rope_bwd_bytes():
             ws = _scratch(_rope_bwd_bytes(), x.device)
         out = _binding.qk_norm_rope_bwd(_fn["at_grpo_qk_norm_rope_bwd"], dq_out, dk_out, q, k, rope, position, q_weight, k_weight, eps, interleaved,
-                                        dq, dk, data_error, ws.data_ptr(), ws.numel(), _stream())
+                                        dq, dk, data_error, ws.data_ptr(), ws.numel(), stream)
     if type(out) is dict:
         out["workspace"] = ws
         return out
@@ -849,7 +849,7 @@ def at_grpo_prefix_attention(kv: KVBatch, q, scale: Optional[float] = None, caus
     res = None
     if q.is_cuda:
         stream = _stream()
-        ws = _scratch_at_hand(q.device)
+        ws = _scratch_at_hand((q.device.index, stream))
         call = lambda: _binding.prefix_attention(_fn["at_grpo_prefix_attention"], _fn["at_grpo_prefix_attention_workspace_bytes"], kv, q, scale,
                                                  causal, max_q, out, want_lse, data_error, ws, stream)
         res = call()
