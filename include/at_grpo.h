@@ -488,6 +488,7 @@ int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* layer, int3
  * 0, and where cu_q or group_seq fall or leave their range no sequence sees anything (AT_GRPO_DATA_SEQLENS).
  * What a query does not see does not reach its results, infinities and NaN included: what lies in the cache behind
  * a sequence's length, tokens of other sequences, and with causal != 0 those behind the query.
+ * out may not share memory with q (AT_GRPO_EINVAL); both may be views of one buffer, of the same strides.
  * max_q (host): an upper bound of the new tokens of one sequence; it picks the kernel, results do not depend on
  * it but for rounding.  scale > 0.  Scores and sums are fp32; bf16 weights are rounded to bf16 for the product
  * with v.  Workspace: at_grpo_prefix_attention_workspace_bytes (0 on invalid arguments; no pointer in kv is read).

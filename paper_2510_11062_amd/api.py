@@ -843,7 +843,8 @@ def at_grpo_kv_append(kv: KVBatch, q, k, v, rope, q_weight=None, k_weight=None, 
 def at_grpo_prefix_attention(kv: KVBatch, q, scale: Optional[float] = None, causal: bool = True, max_q: int = 1, out=None,
                              want_lse: bool = False, data_error=None):
     """Attention of the new tokens' queries q [n, Hq, D] over their sequences' tokens and their groups' prefixes (1 / sqrt(D) where no
-    scale is given).  max_q: an upper bound of the new tokens of one sequence.  out may not be q.  Returns dict(out, lse, workspace)."""
+    scale is given).  max_q: an upper bound of the new tokens of one sequence.  out may not share memory with q.
+    Returns dict(out, lse, workspace)."""
     if _binding is None:
         load_binding()
     res = None

@@ -38,6 +38,35 @@ inline int check_rows(const at_grpo_rows* r, int32_t dtype) {
   return r->token_stride % step == 0 && r->head_stride % step == 0 ? AT_GRPO_OK : AT_GRPO_EINVAL;
 }
 
+// Whether rows [n, H, D] of `a` and `b` share memory: exact where their strides are the same (views of one buffer that lie between each
+// other's rows do not); with other strides they do where their ranges meet.
+inline bool rows_meet(const at_grpo_rows& a, const at_grpo_rows& b, int64_t n, int64_t H, int64_t D, int elem) {
+  const int64_t width = D * elem, apart = static_cast<int64_t>(reinterpret_cast<intptr_t>(b.data) - reinterpret_cast<intptr_t>(a.data));
+  const auto range = [&](const at_grpo_rows& r, int64_t* lo, int64_t* hi) {      // of the rows' first bytes
+    const int64_t t = (n - 1) * r.token_stride * elem, h = (H - 1) * r.head_stride * elem;
+    *lo = (t < 0 ? t : 0) + (h < 0 ? h : 0);
+    *hi = (t > 0 ? t : 0) + (h > 0 ? h : 0);
+  };
+  int64_t lo_a, hi_a, lo_b, hi_b;
+  range(a, &lo_a, &hi_a);
+  range(b, &lo_b, &hi_b);
+  if (apart + lo_b >= hi_a + width || lo_a >= apart + hi_b + width) return false;
+  if ((n > 1 && a.token_stride != b.token_stride) || (H > 1 && a.head_stride != b.head_stride)) return true;
+  // Rows (t, h) of b and (t', h') of a are apart + i * outer + j * inner bytes from each other, i and j the differences of their numbers: for
+  // each of the fewer i's the j's that bring that next to 0.
+  const bool by_token = n < H;
+  const int64_t outer = (by_token ? a.token_stride : a.head_stride) * elem, inner = (by_token ? a.head_stride : a.token_stride) * elem;
+  const int64_t most = by_token ? n : H, other = by_token ? H : n;
+  for (int64_t i = 1 - most; i < most; ++i) {
+    const int64_t x = apart + i * outer, j = inner ? -x / inner : 0;
+    for (int64_t y = j - 1; y <= j + 1; ++y) {
+      const int64_t k = y <= -other ? 1 - other : y >= other ? other - 1 : y;
+      if (x + k * inner < width && x + k * inner > -width) return true;
+    }
+  }
+  return false;
+}
+
 inline int check_kv_sizes(const at_grpo_kv* kv, int32_t n_tok) {
   if (!kv) return AT_GRPO_EINVAL;
   ATG_TRY(check_head_dim(kv->dtype, kv->D));

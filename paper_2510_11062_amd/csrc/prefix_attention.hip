@@ -1930,6 +1930,8 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
   WsAlloc ws(workspace);
   const Scratch scratch = lay_out(kv, n_tok, Hq, ws);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < ws.bytes()) return AT_GRPO_EWORKSPACE;
+  // a run's rows are stored while other runs still read the same queries
+  if (rows_meet(*q, *out, n_tok, Hq, kv->D, elem_size(kv->dtype))) return AT_GRPO_EINVAL;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int share = Hq / kv->Hk;
   const Choice& k = plan.choice;

@@ -555,3 +555,43 @@ def test_batches_whose_costs_pass_32_bits_are_refused_on_the_host():
             assert lib.at_grpo_prefix_attention(kv(n_seq, n_group), n_tok, 100, r, 1.0, 1, 1, r, None, None, 4096, 1 << 40, None) == 2
     # whatever the tables' width, their tokens are counted in blocks large enough
     assert lib.at_grpo_prefix_attention_workspace_bytes(kv(590000, 0, 1 << 26), 590000, 100, 1) > 0
+
+
+def test_results_in_place_of_queries_are_refused_on_the_host():
+    """Nothing is launched: shared memory is found from addresses, strides and sizes."""
+    lib, C = api.load_library(), api.C
+    at = 1 << 20
+
+    def call(q, out, n=4, hq=4, dtype=1):
+        kv = api._KV(dtype=dtype, Hk=2, D=64, page_size=16, n_pages=9, n_seq=4, max_pages=3, n_group=0, max_prefix_pages=0, k=4096, v=4096, pages=4096, length=4096,
+                     cu_q=4096)
+        return lib.at_grpo_prefix_attention(C.byref(kv), n, hq, C.byref(api._Rows(*q)), 1.0, 1, 1, C.byref(api._Rows(*out)), None, None, 4096, 1 << 40, None)
+
+    dense, heads_first, fused = (256, 64), (64, 256), (1152, 64)
+    for q, out in [((at, *dense), (at, *dense)), ((at, *dense), (at + 64 * 2, *dense)), ((at, *dense), (at + (3 * 256 + 3 * 64 + 56) * 2, *dense)),
+                   ((at, *dense), (at - (3 * 256 + 3 * 64 + 56) * 2, *dense)), ((at, *heads_first), (at + 16, *heads_first)), ((at, *dense), (at, *heads_first)),
+                   ((at, *fused), (at + 3 * 64 * 2, *fused)), ((at, *fused), (at - 3 * 64 * 2, *fused)), ((at, *fused), (at + (3 * 1152 - 192) * 2, *fused)),
+                   ((at, -256, 64), (at - 3 * 256 * 2, 256, 64)), ((at, 0, 64), (at + 64 * 2, 0, 64)), ((at, 64, 0), (at + 3 * 64 * 2, 64, 0))]:
+        assert call(q, out) == 1, (q, out)
+    assert call((at, *dense), (at + (3 * 256 + 3 * 64 + 60) * 4, *dense), dtype=0) == 1
+    assert call((at, 8, 64), (at + 64 * 2, 16, 64), n=1) == 1      # one token: its stride does not matter
+
+
+@pytest.mark.gpu
+def test_results_beside_and_in_place_of_queries(gpu_device):
+    p = Paged("bf16", 2, 64, 16, [61, 37, 40], [37, 5, 40], [3], [90], seed=6)
+    q64 = p.queries(4)
+    q, kv, n = to_dev(q64, p.dtype, gpu_device), p.device(gpu_device), p.n_tok
+    want = attend(kv, q, max_q=40)["out"].clone()
+    for heads_first in (False, True):
+        buffer = torch.full((12, n + 3, 64) if heads_first else (n + 3, 12, 64), 7.0, dtype=p.dtype, device=gpu_device)
+        rows = buffer.transpose(0, 1) if heads_first else buffer
+        rows[:n, 1:5] = q
+        for out in (rows[:n, 1:5], rows[:n, 4:8], rows[:n, :4], rows[3:, 1:5], rows[3:, 3:7]):
+            with pytest.raises(api.AtGrpoError):
+                attend(kv, rows[:n, 1:5], max_q=40, out=out)
+        assert torch.equal(rows[:n, 1:5], q) and (rows[:, 5:] == 7).all()
+        for first in (5, 8):
+            attend(kv, rows[:n, 1:5], max_q=40, out=rows[:n, first:first + 4])
+            assert torch.equal(rows[:n, first:first + 4], want) and torch.equal(rows[:n, 1:5], q)
+        assert (rows[:, 0] == 7).all() and (rows[n:] == 7).all()
