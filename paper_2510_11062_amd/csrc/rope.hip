@@ -520,6 +520,12 @@ int check_layer(const at_grpo_norm_rope* a, Layer* out) {
   return AT_GRPO_OK;
 }
 
+// Rows of a token are counted in 32 bits, up to some 10^5 behind their last.
+int check_heads(int64_t q, int64_t k) {
+  if (q < 0 || k < 0) return AT_GRPO_EINVAL;
+  return q + k <= 1 << 30 ? AT_GRPO_OK : AT_GRPO_EUNSUPPORTED;
+}
+
 int lanes_of(int D) { return D <= 64 ? 8 : D <= 128 ? 16 : 32; }
 
 // Few tokens are shared by several wavefronts each, so that the chip has work: about 4096 wavefronts, or all groups of heads.
@@ -588,7 +594,8 @@ extern "C" int at_grpo_qk_norm_rope(const at_grpo_norm_rope* layer, int32_t n_to
                                     void* hip_stream) {
   Layer L;
   ATG_TRY(check_layer(layer, &L));
-  if (n_tok < 0 || Hq < 0 || Hk < 0 || (Hq == 0 && Hk == 0)) return AT_GRPO_EINVAL;
+  if (n_tok < 0 || (Hq == 0 && Hk == 0)) return AT_GRPO_EINVAL;
+  ATG_TRY(check_heads(Hq, Hk));
   if (n_tok == 0) return AT_GRPO_OK;
   if (L.half && !position) return AT_GRPO_EINVAL;
   if (Hq) ATG_TRY(check_rows(q, layer->dtype));
@@ -614,7 +621,8 @@ extern "C" int at_grpo_qk_norm_rope_bwd(const at_grpo_norm_rope* layer, int32_t 
                                         void* workspace, size_t workspace_bytes, void* hip_stream) {
   Layer L;
   ATG_TRY(check_layer(layer, &L));
-  if (n_tok < 0 || Hq < 0 || Hk < 0 || (Hq == 0 && Hk == 0)) return AT_GRPO_EINVAL;
+  if (n_tok < 0 || (Hq == 0 && Hk == 0)) return AT_GRPO_EINVAL;
+  ATG_TRY(check_heads(Hq, Hk));
   if (!Hq) L.qw = nullptr;
   if (!Hk) L.kw = nullptr;
   if ((L.qw && !dq_weight) || (L.kw && !dk_weight)) return AT_GRPO_EINVAL;
@@ -661,7 +669,8 @@ extern "C" int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* 
   KvView view;
   ATG_TRY(check_layer(layer, &L));
   ATG_TRY(check_kv(kv, n_tok, &view));
-  if (kv->dtype != layer->dtype || kv->D != layer->D || Hq < 0) return AT_GRPO_EINVAL;
+  if (kv->dtype != layer->dtype || kv->D != layer->D) return AT_GRPO_EINVAL;
+  ATG_TRY(check_heads(Hq, 2 * static_cast<int64_t>(kv->Hk)));
   if (n_tok == 0) return AT_GRPO_OK;
   ATG_TRY(check_rows(k, layer->dtype));
   ATG_TRY(check_rows(v, layer->dtype));

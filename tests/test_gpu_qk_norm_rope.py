@@ -309,3 +309,19 @@ def test_elements_that_do_not_turn(gpu_device, dtype, D, rot, inter, normed):
         else:
             keep = slice(rot, None)
             assert np.array_equal(got[..., keep], c[name][..., keep], equal_nan=True) and np.array_equal(gx[..., keep], c["d" + name][..., keep], equal_nan=True)
+
+
+def test_more_heads_than_are_counted_are_refused_on_the_host():
+    lib, C = api.load_library(), api.C
+    r = C.byref(api._Rows(4096, 64, 64))
+    L = C.byref(api._NormRope(1, 64, 0, 0, 0, 1e-6, None, 4096, 4096))
+    ws = lib.at_grpo_workspace_bytes(api.CALL_QK_NORM_ROPE_BWD, None, 0, 0, 0, 0)
+    kv = C.byref(api._KV(dtype=1, Hk=2, D=64, page_size=16, n_pages=9, n_seq=4, max_pages=3, n_group=0, max_prefix_pages=0, k=4096, v=4096, pages=4096, length=4096))
+    most = (1 << 31) - 1
+    for hq, hk in [(most, 0), (0, most), (most, most), (1 << 30, 1), (most - 100, 100)]:
+        assert lib.at_grpo_qk_norm_rope(L, 4, hq, hk, r, r, None, r, r, None, None) == 2
+        assert lib.at_grpo_qk_norm_rope_bwd(L, 4, hq, hk, r, r, r, r, None, r, r, 4096, 4096, None, 4096, ws, None) == 2
+    for hq in (most, most - 4, 1 << 30):
+        assert lib.at_grpo_kv_append(kv, L, 4, hq, r, r, r, r, None, None) == 2
+    assert lib.at_grpo_qk_norm_rope(L, 4, -1, 2, r, r, None, r, r, None, None) == 1
+    assert lib.at_grpo_qk_norm_rope_bwd(L, 4, 2, -1, r, r, r, r, None, r, r, 4096, 4096, None, 4096, ws, None) == 1
