@@ -96,6 +96,14 @@ inline int check_kv(const at_grpo_kv* kv, int32_t n_tok, KvView* out) {
 }
 
 #ifdef __HIPCC__
+// A launch's threads along one dimension are counted in 32 bits: workgroups of 256 of which there may be more than 2^24 stand in rows of 2^23, and
+// those behind the last of them find that they have nothing to do.
+inline dim3 grid_of(int64_t blocks) {
+  const int64_t x = blocks < 1 << 23 ? blocks : 1 << 23;
+  return dim3(static_cast<unsigned>(x), static_cast<unsigned>(ceil_div(blocks, x)));
+}
+__device__ __forceinline__ uint32_t flat_block() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 __device__ __forceinline__ float to_f32(float x) { return x; }
 __device__ __forceinline__ float to_f32(bf16_t x) { return bf16_to_f32(x); }
 

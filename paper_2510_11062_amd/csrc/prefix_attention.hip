@@ -1643,7 +1643,7 @@ struct RowParts {
 template <typename T>
 __global__ __launch_bounds__(256) void k_join_heads(KvView kv, Args a, int tile_rows) {
   const int lane = threadIdx.x & 63, per_token = (a.Hq + 3) / 4;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit = static_cast<int64_t>(flat_block()) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= static_cast<int64_t>(a.n_tok) * per_token) return;
   const int t = static_cast<int>(unit / per_token), h0 = 4 * static_cast<int>(unit - static_cast<int64_t>(t) * per_token);
   const UnitsOf units = units_of(kv, a, t);
@@ -1961,7 +1961,7 @@ extern "C" int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int
     hipLaunchKernelGGL(bf16 ? k_join<bf16_t> : k_join<float>, dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows);
   } else {
     const int64_t waves = static_cast<int64_t>(n_tok) * ceil_div(Hq, 4);
-    hipLaunchKernelGGL(bf16 ? k_join_heads<bf16_t> : k_join_heads<float>, dim3(static_cast<unsigned>(ceil_div(waves, 4))), dim3(256), 0, s, view, args, k.rows);
+    hipLaunchKernelGGL(bf16 ? k_join_heads<bf16_t> : k_join_heads<float>, grid_of(ceil_div(waves, 4)), dim3(256), 0, s, view, args, k.rows);
   }
   ATG_LAUNCH_CHECK();
   return AT_GRPO_OK;

@@ -286,9 +286,10 @@ struct Rotator {
 template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts, int Hq, int Hk, Rows q, Rows k, const int32_t* __restrict__ position,
                                                    Rows q_out, Rows k_out, int32_t* data_error) {
-  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = unit / parts, part = unit - t * parts;
-  if (t >= n_tok) return;
+  const uint32_t unit = flat_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t token_of = unit / static_cast<uint32_t>(parts);
+  if (token_of >= static_cast<uint32_t>(n_tok)) return;
+  const int t = static_cast<int>(token_of), part = static_cast<int>(unit - token_of * parts);
   const Token<T> token{{static_cast<const T*>(q.data) + t * q.ts, static_cast<const T*>(k.data) + t * k.ts, nullptr},
                        {static_cast<T*>(q_out.data) + t * q_out.ts, static_cast<T*>(k_out.data) + t * k_out.ts, nullptr},
                        {q.hs, k.hs, 0}, {q_out.hs, k_out.hs, 0}, {Hq, Hq + Hk, Hq + Hk}};
@@ -315,9 +316,10 @@ __global__ __launch_bounds__(256) void k_norm_rope(Layer L, int n_tok, int parts
 template <typename T, int LANES, bool VEC>
 __global__ __launch_bounds__(256) void k_kv_append(KvView kv, Layer L, int n_tok, int parts, int Hq, Rows q, Rows k, Rows v, Rows q_out,
                                                    int32_t* data_error) {
-  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int t = unit / parts, part = unit - t * parts;
-  if (t >= n_tok) return;
+  const uint32_t unit = flat_block() * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint32_t token_of = unit / static_cast<uint32_t>(parts);
+  if (token_of >= static_cast<uint32_t>(n_tok)) return;
+  const int t = static_cast<int>(token_of), part = static_cast<int>(unit - token_of * parts);
   const Owner owner = find_owner(kv, t);
   const int64_t hs = static_cast<int64_t>(kv.D) << kv.page_shift;
   Token<T> token{{static_cast<const T*>(q.data) + t * q.ts, static_cast<const T*>(k.data) + t * k.ts, static_cast<const T*>(v.data) + t * v.ts},
@@ -604,11 +606,11 @@ extern "C" int at_grpo_qk_norm_rope(const at_grpo_norm_rope* layer, int32_t n_to
   if (Hk) ATG_TRY(check_rows(k_out, layer->dtype));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int parts = parts_of(n_tok, Hq + Hk, lanes_of(L.D));
-  const int64_t blocks = ceil_div(static_cast<int64_t>(n_tok) * parts, 4);
-  if (blocks > 0x7fffffff || static_cast<int64_t>(n_tok) * parts > 0x7fffffff) return AT_GRPO_EUNSUPPORTED;
+  if (static_cast<int64_t>(n_tok) * parts > 0x7fffffff) return AT_GRPO_EUNSUPPORTED;
+  const dim3 blocks = grid_of(ceil_div(static_cast<int64_t>(n_tok) * parts, 4));
   ProfScope ps(PROF_ROPE, s);
   return by_shape(layer->dtype, L, [&](auto t, auto n, auto vec) -> int {
-    hipLaunchKernelGGL((k_norm_rope<decltype(t), decltype(n)::value, decltype(vec)::value>), dim3(static_cast<unsigned>(blocks)), dim3(256), 0, s, L, n_tok, parts, Hq, Hk,
+    hipLaunchKernelGGL((k_norm_rope<decltype(t), decltype(n)::value, decltype(vec)::value>), blocks, dim3(256), 0, s, L, n_tok, parts, Hq, Hk,
                        Hq ? rows_of(q) : Rows{}, Hk ? rows_of(k) : Rows{}, position, Hq ? rows_of(q_out) : Rows{}, Hk ? rows_of(k_out) : Rows{}, data_error);
     ATG_LAUNCH_CHECK();
     return AT_GRPO_OK;
@@ -679,10 +681,10 @@ extern "C" int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* 
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int parts = parts_of(n_tok, Hq + 2 * kv->Hk, lanes_of(L.D));
   if (static_cast<int64_t>(n_tok) * parts > 0x7fffffff) return AT_GRPO_EUNSUPPORTED;
-  const unsigned blocks = static_cast<unsigned>(ceil_div(static_cast<int64_t>(n_tok) * parts, 4));
+  const dim3 blocks = grid_of(ceil_div(static_cast<int64_t>(n_tok) * parts, 4));
   ProfScope ps(PROF_ROPE, s);
   return by_shape(layer->dtype, L, [&](auto t, auto n, auto vec) -> int {
-    hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(n)::value, decltype(vec)::value>), dim3(blocks), dim3(256), 0, s, view, L, n_tok, parts, Hq,
+    hipLaunchKernelGGL((k_kv_append<decltype(t), decltype(n)::value, decltype(vec)::value>), blocks, dim3(256), 0, s, view, L, n_tok, parts, Hq,
                        Hq ? rows_of(q) : Rows{}, rows_of(k), rows_of(v), Hq ? rows_of(q_out) : Rows{}, data_error);
     ATG_LAUNCH_CHECK();
     return AT_GRPO_OK;

@@ -223,3 +223,16 @@ def test_groups_that_fall_or_leave_their_range(gpu_device, group_seq, lost):
             at = p.pages[s][i // 16], slice(None), i % 16
             for got, before in ((kv.cache_k, empty.cache_k), (kv.cache_v, empty.cache_v)):
                 assert torch.equal(got[at].view(torch.int16), before[at].view(torch.int16)) == (s in lost)
+
+
+@pytest.mark.gpu
+def test_more_tokens_than_a_launch_counts_threads(gpu_device):
+    """A wavefront a token: 7 * 10^7 new tokens are more than 2^32 threads."""
+    n, page = 70_000_000, 1024
+    n_pages = -(-n // page)
+    cache = [torch.zeros(n_pages, 1, page, 8, dtype=torch.bfloat16, device=gpu_device) for _ in range(2)]
+    kv = api.KVBatch(*cache, pages=torch.arange(n_pages, dtype=torch.int32, device=gpu_device)[None], length=i32([n], gpu_device), cu_q=i32([0, n], gpu_device))
+    k = (torch.arange(n, device=gpu_device) % 251 + 1).bfloat16()[:, None, None].expand(n, 1, 8).contiguous()
+    api.at_grpo_kv_append(kv, None, k, -k, None)
+    assert torch.equal(cache[0].view(-1, 8)[:n], k[:, 0]) and torch.equal(cache[1].view(-1, 8)[:n], -k[:, 0])
+    assert not cache[0].view(-1, 8)[n:].any()

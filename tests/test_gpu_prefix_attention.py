@@ -595,3 +595,25 @@ def test_results_beside_and_in_place_of_queries(gpu_device):
             attend(kv, rows[:n, 1:5], max_q=40, out=rows[:n, first:first + 4])
             assert torch.equal(rows[:n, first:first + 4], want) and torch.equal(rows[:n, 1:5], q)
         assert (rows[:, 0] == 7).all() and (rows[n:] == 7).all()
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_launch_counts_threads(gpu_device):
+    """Joining takes a wavefront for four heads of a token: 1.75 * 10^6 tokens of 160 heads are more than 2^32 threads.  The queries repeat."""
+    period, times, Hq, D = 875, 2000, 160, 8
+    gen = torch.Generator().manual_seed(0)
+    k, v, q = (torch.randn(*s, generator=gen).bfloat16().to(gpu_device) for s in ((1, 1, 8, D), (1, 1, 8, D), (period, Hq, D)))
+    none = lambda *shape: torch.zeros(shape, dtype=torch.int32, device=gpu_device)
+
+    def call(q):
+        kv = api.KVBatch(k, v, none(1, 1), none(1), cu_q=i32([0, len(q)], gpu_device), group_seq=i32([0, 1], gpu_device), prefix_len=i32([8], gpu_device),
+                         prefix_pages=none(1, 1))
+        return attend(kv, q, max_q=len(q), causal=False, want_lse=True)
+
+    want = call(q)
+    got = call(q.repeat(times, 1, 1))
+    assert torch.equal(got["out"].view(times, -1), want["out"].view(1, -1).expand(times, -1))
+    assert torch.equal(got["lse"].view(times, -1), want["lse"].view(1, -1).expand(times, -1))
+    p64 = torch.softmax(torch.matmul(q[:5].double(), k[0, 0].double().T) * D ** -0.5, -1)
+    assert (want["out"][:5].double() - torch.matmul(p64, v[0, 0].double())).abs().max() < 4 * 2.0 ** -8 * v.abs().max()
+    api.release_workspace()

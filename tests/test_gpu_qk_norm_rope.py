@@ -325,3 +325,15 @@ def test_more_heads_than_are_counted_are_refused_on_the_host():
         assert lib.at_grpo_kv_append(kv, L, 4, hq, r, r, r, r, None, None) == 2
     assert lib.at_grpo_qk_norm_rope(L, 4, -1, 2, r, r, None, r, r, None, None) == 1
     assert lib.at_grpo_qk_norm_rope_bwd(L, 4, 2, -1, r, r, r, r, None, r, r, 4096, 4096, None, 4096, ws, None) == 1
+
+
+@pytest.mark.gpu
+def test_more_rows_than_a_launch_counts_threads(gpu_device):
+    """A wavefront a row: 7 * 10^7 rows are more than 2^32 threads."""
+    n = 70_000_001
+    x, w = torch.ones(n, 1, 8, dtype=torch.bfloat16, device=gpu_device), torch.full((8,), 2.0, dtype=torch.bfloat16, device=gpu_device)
+    x[-1] = -1
+    y = api.at_grpo_qk_norm_rope(x, None, None, None, w)["q"]      # 1 / sqrt(1 + 1e-6) rounds to 1
+    assert (y[:-1] == 2).all() and (y[-1] == -2).all()
+    out = api.at_grpo_qk_norm_rope_bwd(x, None, x, None, None, None, None)
+    assert torch.equal(out["dq"], x)
