@@ -360,6 +360,9 @@ int at_grpo_head_update(int32_t dtype, int32_t H, int32_t V, int32_t n_heads, vo
  * and rotation of queries and keys (with the gradient that training needs), the same on the way into a
  * paged cache, and attention that reads a prompt's keys and values once for the candidates that share it.
  *
+ * Norms and rotation have a gradient here; the attention has none: these calls serve the rollout and the training pass's
+ * norms, whose attention is the caller's.
+ *
  * They have no error word of their own in a workspace: where `data_error` is not NULL the AT_GRPO_DATA_*
  * bits of offending elements are or'ed into that int32 in device memory, which the caller clears when it
  * likes (once per rollout, say).
@@ -489,6 +492,8 @@ int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* layer, int3
  * What a query does not see does not reach its results, infinities and NaN included: what lies in the cache behind
  * a sequence's length, tokens of other sequences, and with causal != 0 those behind the query.
  * out may not share memory with q (AT_GRPO_EINVAL); both may be views of one buffer, of the same strides.
+ * Weights are divided by their sum at the end: the values of V times 2^8 times the visible tokens have to stay in fp32's
+ * range.
  * max_q (host): an upper bound of the new tokens of one sequence; it picks the kernel, results do not depend on
  * it but for rounding.  scale > 0.  Scores and sums are fp32; bf16 weights are rounded to bf16 for the product
  * with v.  Workspace: at_grpo_prefix_attention_workspace_bytes (0 on invalid arguments; no pointer in kv is read).
