@@ -662,6 +662,8 @@ def at_grpo_rope_table(n_pos: int, rot_dim: int, base: float = 10000.0, scaling:
     "parts" (pairs that turn more than `fast` times over the trained positions keep their frequency, those that turn less than `slow`
     times get frequency / factor, a ramp between)."""
     lib = load_library()
+    if not 0 <= n_pos < 1 << 31 or not 0 < rot_dim <= 256 or rot_dim % 2:
+        raise AtGrpoError("a rotation table has 0 to 2^31 - 1 positions and an even rot_dim of 2 to 256")
     table = torch.empty((n_pos, rot_dim // 2, 2), dtype=torch.float32, device="cuda" if device is None else device)
     _dev_check(table)
     c = _Rope(rot_dim, ROPE_SCALING[scaling], base, factor, trained, slow, fast, magnitude)

@@ -337,3 +337,10 @@ def test_more_rows_than_a_launch_counts_threads(gpu_device):
     assert (y[:-1] == 2).all() and (y[-1] == -2).all()
     out = api.at_grpo_qk_norm_rope_bwd(x, None, x, None, None, None, None)
     assert torch.equal(out["dq"], x)
+
+
+@pytest.mark.parametrize("n_pos,rot_dim", [(1 << 31, 2), ((1 << 32) + 5, 2), (-1, 64), (4, 0), (4, -2), (4, 63), (0, (1 << 32) + 64), (4, 258)])
+def test_tables_of_sizes_that_there_are_not(n_pos, rot_dim):
+    """Before anything is allocated, and not modulo 2^32."""
+    with pytest.raises(api.AtGrpoError):
+        api.at_grpo_rope_table(n_pos, rot_dim)
