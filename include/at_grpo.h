@@ -420,8 +420,9 @@ typedef struct {
  *   y_a = c u_a - s u_b,  y_b = c u_b + s u_a  for the pairs (a, b) of the layout, (c, s) = table[position[t]]
  *   y_d = u_d for d >= rot_dim
  * in fp32, rounded once.  q [n_tok, Hq, D], k [n_tok, Hk, D]; Hk == 0 (or Hq == 0) leaves one of them out.
- * An output may be its input itself (same data and strides).  A token whose position lies outside the table
- * raises AT_GRPO_DATA_POSITION and gets rows of zeros.  n_tok == 0 is no error and does nothing.
+ * An output may be its input itself (same data and strides) or lie apart from it: one that meets it otherwise is
+ * AT_GRPO_EINVAL (views of one buffer that do not meet have the same strides).  A token whose position lies
+ * outside the table raises AT_GRPO_DATA_POSITION and gets rows of zeros.  n_tok == 0 is no error and does nothing.
  */
 int at_grpo_qk_norm_rope(const at_grpo_norm_rope* layer, int32_t n_tok, int32_t Hq, int32_t Hk,
                          const at_grpo_rows* q, const at_grpo_rows* k, const int32_t* position,
@@ -432,7 +433,7 @@ int at_grpo_qk_norm_rope(const at_grpo_norm_rope* layer, int32_t n_tok, int32_t 
  * Its gradient.  With g the rotated-back gradient of a row (g_a = c dy_a + s dy_b, g_b = c dy_b - s dy_a),
  * r = 1 / sqrt(mean(x^2) + eps) and n = x r:
  *   dx = r (g weight - n mean(g weight n)),   d_weight = sum over all rows of g n     (dx = g without a weight)
- *   dq, dk as q, k (dq may be dq_out itself, dk dk_out);  dq_weight[D], dk_weight[D] fp32, overwritten, required
+ *   dq, dk as q, k (dq may be dq_out or q itself, dk dk_out or k);  dq_weight[D], dk_weight[D] fp32, overwritten, required
  *   where the layer has the weight.
  * Tokens whose position lies outside the table get zeros and add nothing.  Sums are taken in a fixed order.
  * Workspace: AT_GRPO_CALL_QK_NORM_ROPE_BWD.

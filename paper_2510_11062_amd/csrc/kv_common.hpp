@@ -67,6 +67,12 @@ inline bool rows_meet(const at_grpo_rows& a, const at_grpo_rows& b, int64_t n, i
   return false;
 }
 
+// An output of rows that are read once may be its input itself, or lie apart from it.
+inline int check_in_place(const at_grpo_rows* in, const at_grpo_rows* out, int64_t n, int64_t H, int64_t D, int32_t dtype) {
+  if (in->data == out->data && (n == 1 || in->token_stride == out->token_stride) && (H == 1 || in->head_stride == out->head_stride)) return AT_GRPO_OK;
+  return rows_meet(*in, *out, n, H, D, elem_size(dtype)) ? AT_GRPO_EINVAL : AT_GRPO_OK;
+}
+
 inline int check_kv_sizes(const at_grpo_kv* kv, int32_t n_tok) {
   if (!kv) return AT_GRPO_EINVAL;
   ATG_TRY(check_head_dim(kv->dtype, kv->D));

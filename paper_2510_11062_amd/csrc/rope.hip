@@ -604,6 +604,8 @@ extern "C" int at_grpo_qk_norm_rope(const at_grpo_norm_rope* layer, int32_t n_to
   if (Hq) ATG_TRY(check_rows(q_out, layer->dtype));
   if (Hk) ATG_TRY(check_rows(k, layer->dtype));
   if (Hk) ATG_TRY(check_rows(k_out, layer->dtype));
+  if (Hq) ATG_TRY(check_in_place(q, q_out, n_tok, Hq, L.D, layer->dtype));
+  if (Hk) ATG_TRY(check_in_place(k, k_out, n_tok, Hk, L.D, layer->dtype));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int parts = parts_of(n_tok, Hq + Hk, lanes_of(L.D));
   if (static_cast<int64_t>(n_tok) * parts > 0x7fffffff) return AT_GRPO_EUNSUPPORTED;
@@ -634,11 +636,15 @@ extern "C" int at_grpo_qk_norm_rope_bwd(const at_grpo_norm_rope* layer, int32_t 
       ATG_TRY(check_rows(dq_out, layer->dtype));
       ATG_TRY(check_rows(dq, layer->dtype));
       if (L.qw) ATG_TRY(check_rows(q, layer->dtype));
+      ATG_TRY(check_in_place(dq_out, dq, n_tok, Hq, L.D, layer->dtype));
+      if (L.qw) ATG_TRY(check_in_place(q, dq, n_tok, Hq, L.D, layer->dtype));
     }
     if (Hk) {
       ATG_TRY(check_rows(dk_out, layer->dtype));
       ATG_TRY(check_rows(dk, layer->dtype));
       if (L.kw) ATG_TRY(check_rows(k, layer->dtype));
+      ATG_TRY(check_in_place(dk_out, dk, n_tok, Hk, L.D, layer->dtype));
+      if (L.kw) ATG_TRY(check_in_place(k, dk, n_tok, Hk, L.D, layer->dtype));
     }
   }
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < qk_norm_rope_bwd_workspace()) return AT_GRPO_EWORKSPACE;
@@ -678,6 +684,7 @@ extern "C" int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* 
   ATG_TRY(check_rows(v, layer->dtype));
   if (Hq) ATG_TRY(check_rows(q, layer->dtype));
   if (Hq) ATG_TRY(check_rows(q_out, layer->dtype));
+  if (Hq) ATG_TRY(check_in_place(q, q_out, n_tok, Hq, L.D, layer->dtype));
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   const int parts = parts_of(n_tok, Hq + 2 * kv->Hk, lanes_of(L.D));
   if (static_cast<int64_t>(n_tok) * parts > 0x7fffffff) return AT_GRPO_EUNSUPPORTED;

@@ -344,3 +344,41 @@ def test_tables_of_sizes_that_there_are_not(n_pos, rot_dim):
     """Before anything is allocated, and not modulo 2^32."""
     with pytest.raises(api.AtGrpoError):
         api.at_grpo_rope_table(n_pos, rot_dim)
+
+
+def test_outputs_that_meet_their_inputs_otherwise_are_refused_on_the_host():
+    lib, C = api.load_library(), api.C
+    at, r = 1 << 24, lambda *a: C.byref(api._Rows(*a))
+    L = C.byref(api._NormRope(1, 64, 0, 0, 0, 1e-6, None, 4096, 4096))
+    ws = lib.at_grpo_workspace_bytes(api.CALL_QK_NORM_ROPE_BWD, None, 0, 0, 0, 0)
+    kv = C.byref(api._KV(dtype=1, Hk=2, D=64, page_size=16, n_pages=9, n_seq=4, max_pages=3, n_group=0, max_prefix_pages=0, k=4096, v=4096, pages=4096, length=4096))
+    there, far = r(at, 512, 64), r(at + (1 << 20), 512, 64)
+    for other in (r(at + 64 * 2, 512, 64), r(at - 16, 512, 64), r(at + 512 * 2, 512, 64), r(at, 64, 512), r(at, 256, 64)):
+        for a, b in ((there, other), (other, there)):
+            assert lib.at_grpo_qk_norm_rope(L, 4, 4, 0, a, None, None, b, None, None, None) == 1
+            assert lib.at_grpo_qk_norm_rope(L, 4, 0, 4, None, a, None, None, b, None, None) == 1
+            assert lib.at_grpo_kv_append(kv, L, 4, 4, a, far, far, b, None, None) == 1
+            assert lib.at_grpo_qk_norm_rope_bwd(L, 4, 4, 0, a, None, far, None, None, b, None, 4096, 4096, None, 4096, ws, None) == 1
+            assert lib.at_grpo_qk_norm_rope_bwd(L, 4, 4, 0, far, None, a, None, None, b, None, 4096, 4096, None, 4096, ws, None) == 1
+            assert lib.at_grpo_qk_norm_rope_bwd(L, 4, 0, 4, None, far, None, a, None, None, b, 4096, 4096, None, 4096, ws, None) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_outputs_beside_and_over_their_inputs(gpu_device, dtype):
+    c, dv = case(gpu_device, dtype, 21, 4, 2, 64, 64, False, (True, True))
+    ref, gref = forward(dv, False), backward(dv, False)
+    buffer = torch.zeros(24, 12, 64, dtype=DTYPES[dtype], device=gpu_device)
+    rows = buffer[:21, 1:5]
+    rows.copy_(dv["q"])
+    for out in (buffer[:21, 4:8], buffer[:21, :4], buffer[3:, 1:5]):
+        with pytest.raises(api.AtGrpoError):
+            forward({**dv, "q": rows}, False, q_out=out)
+        with pytest.raises(api.AtGrpoError):
+            backward({**dv, "dq": rows}, False, dq=out)
+    assert torch.equal(rows, dv["q"])
+    forward({**dv, "q": rows}, False, q_out=buffer[:21, 5:9])      # between each other's rows
+    assert torch.equal(buffer[:21, 5:9], ref["q"]) and torch.equal(rows, dv["q"])
+    g = backward({**dv, "q": rows}, False, dq=rows)      # in place of the queries
+    assert torch.equal(rows, gref["dq"]) and torch.equal(g["dq_weight"], gref["dq_weight"])
+    assert not buffer[21:].any() and not buffer[:, 9:].any() and not buffer[:, 0].any()
