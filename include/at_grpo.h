@@ -77,7 +77,10 @@ enum {
   AT_GRPO_DATA_SEQLENS = 8,      /* cu_seqlens not monotone within [0, n_tok]         */
   AT_GRPO_DATA_AGENT_RANGE = 16, /* resp_agent / head_of_agent entry out of range     */
   AT_GRPO_DATA_PAGE = 32,        /* page id outside the cache, or a token behind its page table */
-  AT_GRPO_DATA_POSITION = 64     /* position outside the rotation table               */
+  AT_GRPO_DATA_POSITION = 64,    /* position outside the rotation table               */
+  AT_GRPO_DATA_TREE = 128,       /* a drafted token whose parent does not stand in front of it */
+  AT_GRPO_DATA_POOL = 256,       /* a pool that has too few pages, or whose state no pool can have */
+  AT_GRPO_DATA_RULE = 512        /* a penalty, temperature, bias list or mask that is none */
 };
 
 /* Bits of clip_mask[t] (Eq. 2's clip, decided in log space on d = logp - old_logp, one fp32
@@ -505,6 +508,55 @@ int at_grpo_prefix_attention(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, co
                              int32_t causal, int32_t max_q, const at_grpo_rows* out, float* lse,
                              int32_t* data_error, void* workspace, size_t workspace_bytes, void* hip_stream);
 size_t at_grpo_prefix_attention_workspace_bytes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q);
+
+/*
+ * ---- Drafted tokens ---------------------------------------------------------------------------------
+ * A rollout that drafts its next tokens gives every sequence a tree of them: token j of a sequence's new ones hangs
+ * on its token parent[j] < j, or (parent -1) on the sequence itself.  A step plans the tokens' pages, appends their keys and
+ * values, attends (each token to the sequence and its own path), applies the rules of sampling to the logits
+ * behind each token, and keeps the path that the choices agree with; the next plan gives the others' pages back.
+ * These calls serve the rollout and have no gradient.  They too raise their flags in `data_error`.
+ */
+
+/* The free pages of a cache and the tables of its sequences.  Free pages stand in a ring: with state {first, count} they are
+ * ring[(first + i) % n_pages], i < count. */
+typedef struct {
+  int32_t page_size;             /* a power of two, 8 .. 65536                                           */
+  int32_t n_pages;               /* of the cache: what the ring has room for                             */
+  int32_t n_seq, max_pages;      /* rows and columns of pages; n_seq * max_pages < 2^31, max_pages * page_size <= 2^30 */
+  int32_t n_group;               /* 0: no prefixes                                                       */
+  int32_t* pages;                /* [n_seq, max_pages]                                                   */
+  int32_t* ring;                 /* [n_pages]                                                            */
+  const int32_t* group_seq;      /* [n_group + 1], not falling, as in at_grpo_kv                         */
+  const int32_t* prefix_len;     /* [n_group]                                                            */
+} at_grpo_page_pool;
+
+/*
+ * The step from one length of every sequence to the next.  Sequence s has length[s] tokens, keeps the first keep[s] of them
+ * (NULL: all) and gets add[s] new ones behind those:
+ *   length_out[s] = keep[s] + add[s]
+ *   pages[s]      grows by pages from the front of the ring, in the order of the sequences; or the pages behind its last one go
+ *                 to the ring's end, in that order (their entries stay)
+ *   cu_q[s]       = sum of add in front of s, [n_seq + 1]
+ * and for each new token t = cu_q[s] + j, all of which may be NULL:
+ *   seq[t] = s,  slot[t] = page of place keep[s] + j * page_size + its place there (64 bits)
+ *   position[t]   = prefix of the sequence's group + keep[s] + j;  with `parent` the token's depth in place of j
+ *   ancestors[t]  with `parent` [n_tok]: bit i for each token i of the sequence's new ones on t's path, its own among them
+ * Entries of the outputs behind the last new token are left as they were.  Pages that a call gives back are taken from the next call on.
+ * All or nothing: where the ring has too few pages or its state is none (AT_GRPO_DATA_POOL), a length, keep or add is out of range, the
+ * new tokens are more than n_tok, or with `parent` more than 64 of a sequence (AT_GRPO_DATA_SEQLENS), nothing is taken, given or
+ * added: length_out and state_out become what length and state are, cu_q zeros.  A parent that does not stand in front of its token
+ * counts as -1 (AT_GRPO_DATA_TREE); where group_seq falls or leaves its range there are no prefixes, a negative prefix_len or one past
+ * 2^30 counts as 0 (AT_GRPO_DATA_SEQLENS).  Page ids are passed on as they stand in the ring.
+ * length_out may be length itself and state_out state itself; apart from that outputs, pages and ring share memory with nothing
+ * (AT_GRPO_EINVAL).  n_tok: rows of the tokens' outputs.  Workspace: at_grpo_kv_plan_workspace_bytes.
+ */
+int at_grpo_kv_plan(const at_grpo_page_pool* pool, int32_t n_tok, const int32_t* length, const int32_t* keep,
+                    const int32_t* add, const int32_t* parent, const int32_t* state, int32_t* length_out,
+                    int32_t* state_out, int32_t* cu_q, int32_t* seq, int32_t* position, int64_t* slot,
+                    uint64_t* ancestors, int32_t* data_error, void* workspace, size_t workspace_bytes,
+                    void* hip_stream);
+size_t at_grpo_kv_plan_workspace_bytes(int32_t n_seq);
 
 /*
  * Bytes of workspace a call needs.  `batch` may be NULL for AT_GRPO_CALL_GROUP_ADVANTAGE; the

@@ -7,6 +7,7 @@ no fallback: if the HIP library is missing or a call fails, an exception is rais
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import functools
 import os
@@ -41,7 +42,7 @@ EXPORTS = [
     "at_grpo_policy_loss_fwd", "at_grpo_policy_loss_bwd", "at_grpo_policy_loss_fwd_bwd", "at_grpo_head_update", "at_grpo_workspace_bytes",
     "at_grpo_status_string", "at_grpo_version", "at_grpo_profile_enable", "at_grpo_profile_classes",
     "at_grpo_profile_read", "at_grpo_rope_table", "at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append",
-    "at_grpo_prefix_attention", "at_grpo_prefix_attention_workspace_bytes",
+    "at_grpo_prefix_attention", "at_grpo_prefix_attention_workspace_bytes", "at_grpo_kv_plan", "at_grpo_kv_plan_workspace_bytes",
 ]
 
 
@@ -74,6 +75,11 @@ class _KV(C.Structure):
                 ("n_seq", C.c_int32), ("max_pages", C.c_int32), ("n_group", C.c_int32), ("max_prefix_pages", C.c_int32),
                 ("k", C.c_void_p), ("v", C.c_void_p), ("pages", C.c_void_p), ("length", C.c_void_p), ("cu_q", C.c_void_p),
                 ("group_seq", C.c_void_p), ("prefix_len", C.c_void_p), ("prefix_pages", C.c_void_p)]
+
+
+class _PagePool(C.Structure):
+    _fields_ = [("page_size", C.c_int32), ("n_pages", C.c_int32), ("n_seq", C.c_int32), ("max_pages", C.c_int32), ("n_group", C.c_int32),
+                ("pages", C.c_void_p), ("ring", C.c_void_p), ("group_seq", C.c_void_p), ("prefix_len", C.c_void_p)]
 
 
 class _Batch(C.Structure):
@@ -157,6 +163,10 @@ def load_library():
         getattr(lib, name).restype = C.c_int
     lib.at_grpo_prefix_attention_workspace_bytes.argtypes = [kv, i32, i32, i32]
     lib.at_grpo_prefix_attention_workspace_bytes.restype = sz
+    lib.at_grpo_kv_plan.argtypes = [C.POINTER(_PagePool), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.at_grpo_kv_plan.restype = C.c_int
+    lib.at_grpo_kv_plan_workspace_bytes.argtypes = [i32]
+    lib.at_grpo_kv_plan_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -174,7 +184,7 @@ def load_binding():
         _group_fn = C.cast(lib.at_grpo_group_advantage, C.c_void_p).value
         _mixed_fn = C.cast(lib.at_grpo_group_advantage_mixed, C.c_void_p).value
         for name in ("at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append", "at_grpo_prefix_attention",
-                     "at_grpo_prefix_attention_workspace_bytes"):
+                     "at_grpo_prefix_attention_workspace_bytes", "at_grpo_kv_plan", "at_grpo_kv_plan_workspace_bytes"):
             _fn[name] = C.cast(getattr(lib, name), C.c_void_p).value
         _binding = binding
     return _binding
@@ -870,3 +880,83 @@ def at_grpo_prefix_attention(kv: KVBatch, q, scale: Optional[float] = None, caus
     if res is None:
         raise AtGrpoError("at_grpo_prefix_attention: heads, head size, page size, tokens or max_q that it does not cover")
     _refused(res, "at_grpo_prefix_attention")
+
+
+# ---- drafted tokens -----------------------------------------------------------------------------------
+def _on(device):
+    """The device as the current one, and its current stream: where a call's kernels go."""
+    if device.index == torch.cuda.current_device():
+        return contextlib.nullcontext(), _raw_stream(device.index)
+    return torch.cuda.device(device), _raw_stream(device.index)
+
+
+def _with_scratch(call, device, stream):
+    """call(workspace), once more with a larger one where it says (bytes,).  Returns the workspace and what the call said."""
+    ws = _scratch_at_hand((device.index, stream))
+    res = call(ws)
+    if type(res) is tuple:
+        ws = _scratch(res[0], device)
+        res = call(ws)
+    return ws, res
+
+
+def _tensor_on_gpu(name: str, t):
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+        raise AtGrpoError(f"{name} must be a CUDA/HIP tensor")
+    return t.device
+
+
+@dataclass
+class PagePool:
+    """Python-side mirror of at_grpo_page_pool.  pages and ring are written by the calls."""
+    pages: torch.Tensor                         # int32 [n_seq, max_pages]
+    ring: torch.Tensor                          # int32 [pages of the cache]
+    page_size: int
+    group_seq: Optional[torch.Tensor] = None    # int32 [n_group + 1]; None: no prefixes
+    prefix_len: Optional[torch.Tensor] = None   # int32 [n_group]
+
+
+def _explain_groups(group_seq, beside, name: str, device):
+    if group_seq is None:
+        return
+    if not isinstance(group_seq, torch.Tensor) or group_seq.dim() != 1 or group_seq.numel() < 1:
+        raise AtGrpoError("group_seq must have n_group + 1 elements")
+    _vector("group_seq", group_seq, group_seq.numel(), torch.int32, device)
+    if beside is None:
+        raise AtGrpoError(f"groups need {name} [n_group]")
+    _vector(name, beside, group_seq.numel() - 1, torch.int32, device)
+
+
+def at_grpo_kv_plan(pool: PagePool, length, add, state, n_tok: int, keep=None, parent=None, length_out=None, state_out=None, data_error=None):
+    """The step from `length` [n_seq] to keep + add: sequences keep their first `keep` tokens (None: all) and get `add` new ones, pages come from
+    the pool's ring or go back to it; state [2] is the ring's front and its number of free pages.  parent [n_tok]: trees of drafted tokens.
+    n_tok: rows of the new tokens' outputs, at least as many as there are new tokens; rows behind the last are not written.  length_out may
+    be length itself, state_out state itself.  Where the pool does not suffice nothing is done (see data_error).  All int32.
+    Returns dict(length, state, cu_q [n_seq + 1], seq, position, slot (int64) [n_tok], ancestors (int64 bits, or None), workspace)."""
+    if _binding is None:
+        load_binding()
+    device = _tensor_on_gpu("length", length)
+    on, stream = _on(device)
+    with on:
+        ws, res = _with_scratch(lambda ws: _binding.kv_plan(_fn["at_grpo_kv_plan"], _fn["at_grpo_kv_plan_workspace_bytes"], pool, length, add, state, n_tok,
+                                                            keep, parent, length_out, state_out, data_error, ws, stream), device, stream)
+    if type(res) is dict:
+        res["workspace"] = ws
+        return res
+    n_seq = length.numel()
+    _vector("length", length, n_seq, torch.int32, device)
+    for name, t, n in (("add", add, n_seq), ("state", state, 2)):
+        if t is None:
+            raise AtGrpoError(f"{name} is needed")
+        _vector(name, t, n, torch.int32, device)
+    for name, t, n in (("keep", keep, n_seq), ("length_out", length_out, n_seq), ("state_out", state_out, 2), ("parent", parent, n_tok)):
+        _vector(name, t, n, torch.int32, device)
+    if not isinstance(pool.pages, torch.Tensor) or pool.pages.dim() != 2 or pool.pages.shape[0] != n_seq or pool.pages.dtype != torch.int32 or \
+            pool.pages.device != device or not pool.pages.is_contiguous():
+        raise AtGrpoError(f"pages must be a contiguous int32 [n_seq, max_pages] tensor on {device}")
+    if not isinstance(pool.ring, torch.Tensor):
+        raise AtGrpoError("ring must be a tensor")
+    _vector("ring", pool.ring, pool.ring.numel(), torch.int32, device)
+    _explain_groups(pool.group_seq, pool.prefix_len, "prefix_len", device)
+    _word(data_error, device)
+    _refused(res, "at_grpo_kv_plan")

@@ -22,7 +22,7 @@ struct ProfState {
 ProfState g_prof;
 const char* const kProfNames[PROF_N] = {"group_advantage", "token_prep", "head_fwd", "lse_combine",
                                         "surrogate", "coef", "transpose", "head_dz", "head_dh",
-                                        "head_dw", "fill", "grad_norm", "adam", "head_fe", "rope", "attention"};
+                                        "head_dw", "fill", "grad_norm", "adam", "head_fe", "rope", "attention", "kv_plan", "logit_rules"};
 }  // namespace
 
 void prof_begin(int cls, hipStream_t s) {

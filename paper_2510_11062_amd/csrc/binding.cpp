@@ -382,6 +382,122 @@ PyObject* prefix_attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+// ---- drafted tokens -----------------------------------------------------------------------------------
+
+enum Planned { LENGTH, STATE, CU_Q, SEQ, POSITION, SLOT, ANCESTORS, PLANNED };
+const char* const kPlanned[PLANNED] = {"length", "state", "cu_q", "seq", "position", "slot", "ancestors"};
+enum PoolField { POOL_PAGES, RING, PAGE_SIZE, GROUP_SEQ, PREFIX_LEN, POOL_FIELDS };
+const char* const kPoolFields[POOL_FIELDS] = {"pages", "ring", "page_size", "group_seq", "prefix_len"};
+PyObject *g_planned[PLANNED], *g_pool[POOL_FIELDS];
+
+template <typename X>
+X* data(const at::Tensor& t) { return t.defined() ? static_cast<X*>(t.data_ptr()) : nullptr; }
+
+// The vector that the caller gave for an output, or a new one.
+bool vector_out(PyObject* given, int64_t n, at::ScalarType dtype, const at::Tensor& like, at::Tensor* out) {
+  const void* at;
+  if (given != Py_None) {
+    if (!vector(given, n, dtype, like.device(), &at)) return false;
+    *out = *as_tensor(given);
+    return true;
+  }
+  const WithoutPythonLock others_run;
+  *out = at::empty({n}, like.options().dtype(dtype));
+  return true;
+}
+
+// The attributes `names` of an object, kept alive; false where one is missing.
+template <int N>
+bool fields_of(PyObject* o, PyObject* const (&names)[N], THPObjectPtr (&held)[N]) {
+  for (int i = 0; i < N; ++i) {
+    held[i] = THPObjectPtr(PyObject_GetAttr(o, names[i]));
+    if (!held[i]) {
+      PyErr_Clear();
+      return false;
+    }
+  }
+  return true;
+}
+
+// A contiguous int32 matrix of so many rows on the device.
+const at::Tensor* matrix(PyObject* o, int64_t n_rows, at::ScalarType dtype, at::Device device) {
+  const at::Tensor* t = as_tensor(o);
+  return t && t->dim() == 2 && (n_rows < 0 || t->size(0) == n_rows) && t->size(0) <= 0x7fffffff && t->size(1) <= 0x7fffffff &&
+                 t->scalar_type() == dtype && t->device() == device && t->is_contiguous()
+             ? t
+             : nullptr;
+}
+
+// group_seq and what stands beside it, [n_group]: both or none
+bool groups_of(PyObject* group_seq, PyObject* beside, at::Device device, const void** seq, const void** len, int32_t* n_group) {
+  *seq = *len = nullptr;
+  *n_group = 0;
+  if (group_seq == Py_None) return true;
+  const at::Tensor* t = as_tensor(group_seq);
+  if (!t || t->dim() != 1 || t->size(0) < 1 || t->size(0) > 0x7fffffff || beside == Py_None) return false;
+  *n_group = static_cast<int32_t>(t->size(0) - 1);
+  return vector(group_seq, t->size(0), at::kInt, device, seq) && vector(beside, *n_group, at::kInt, device, len);
+}
+
+// kv_plan(function's address, its workspace query's, PagePool, length, add, state, n_tok, keep, parent, length_out, state_out, data_error,
+//         workspace or None, stream)
+// Where the workspace is none or too small: (bytes,).
+PyObject* kv_plan(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (n_args != 14) {
+    PyErr_SetString(PyExc_TypeError, "kv_plan takes 14 arguments");
+    return nullptr;
+  }
+  THPObjectPtr held[POOL_FIELDS];
+  if (!fields_of(v[2], g_pool, held)) Py_RETURN_NONE;
+  const at::Tensor *length = as_tensor(v[3]), *ring = as_tensor(held[RING].get());
+  if (!length || length->dim() != 1 || !length->is_cuda() || length->size(0) > 0x7fffffff || !ring || ring->dim() != 1 || ring->size(0) > 0x7fffffff)
+    Py_RETURN_NONE;
+  const int64_t n_seq = length->size(0), page_size = PyLong_AsLongLong(held[PAGE_SIZE].get()), n_tok = PyLong_AsLongLong(v[6]);
+  void* stream = PyLong_AsVoidPtr(v[13]);
+  if (PyErr_Occurred()) return nullptr;
+  const at::Device device = length->device();
+  const at::Tensor* pages = matrix(held[POOL_PAGES].get(), n_seq, at::kInt, device);
+  const void *lengths, *free_pages, *adds, *states, *keeps, *parents, *group_seq, *prefix_len, *word;
+  int32_t n_group;
+  if (!pages || page_size < 0 || page_size > 0x7fffffff || n_tok < 0 || n_tok > 0x7fffffff || v[5] == Py_None || v[4] == Py_None ||
+      !vector(v[3], n_seq, at::kInt, device, &lengths) || !vector(held[RING].get(), ring->size(0), at::kInt, device, &free_pages) ||
+      !vector(v[4], n_seq, at::kInt, device, &adds) || !vector(v[5], 2, at::kInt, device, &states) || !vector(v[7], n_seq, at::kInt, device, &keeps) ||
+      !vector(v[8], n_tok, at::kInt, device, &parents) || !vector(v[11], 1, at::kInt, device, &word) ||
+      !groups_of(held[GROUP_SEQ].get(), held[PREFIX_LEN].get(), device, &group_seq, &prefix_len, &n_group))
+    Py_RETURN_NONE;
+  const at_grpo_page_pool pool{static_cast<int32_t>(page_size), static_cast<int32_t>(ring->size(0)), static_cast<int32_t>(n_seq),
+                               static_cast<int32_t>(pages->size(1)), n_group, data<int32_t>(*pages),
+                               static_cast<int32_t*>(const_cast<void*>(free_pages)), static_cast<const int32_t*>(group_seq),
+                               static_cast<const int32_t*>(prefix_len)};
+  const size_t bytes = reinterpret_cast<decltype(&at_grpo_kv_plan_workspace_bytes)>(PyLong_AsVoidPtr(v[1]))(pool.n_seq);
+  const at::Tensor* ws = as_tensor(v[12]);
+  if (!ws || static_cast<size_t>(ws->numel()) < bytes) return Py_BuildValue("(n)", static_cast<Py_ssize_t>(bytes));
+  at::Tensor out[PLANNED];
+  if (!vector_out(v[9], n_seq, at::kInt, *length, &out[LENGTH]) || !vector_out(v[10], 2, at::kInt, *length, &out[STATE])) Py_RETURN_NONE;
+  {
+    const WithoutPythonLock others_run;
+    const auto i32 = length->options(), i64 = i32.dtype(at::kLong);
+    out[CU_Q] = at::empty({n_seq + 1}, i32);
+    out[SEQ] = at::empty({n_tok}, i32);
+    out[POSITION] = at::empty({n_tok}, i32);
+    out[SLOT] = at::empty({n_tok}, i64);
+    if (v[8] != Py_None) out[ANCESTORS] = at::empty({n_tok}, i64);
+  }
+  const int status = reinterpret_cast<decltype(&at_grpo_kv_plan)>(PyLong_AsVoidPtr(v[0]))(
+      &pool, static_cast<int32_t>(n_tok), static_cast<const int32_t*>(lengths), static_cast<const int32_t*>(keeps), static_cast<const int32_t*>(adds),
+      static_cast<const int32_t*>(parents), static_cast<const int32_t*>(states), data<int32_t>(out[LENGTH]), data<int32_t>(out[STATE]),
+      data<int32_t>(out[CU_Q]), data<int32_t>(out[SEQ]), data<int32_t>(out[POSITION]), data<int64_t>(out[SLOT]), data<uint64_t>(out[ANCESTORS]),
+      static_cast<int32_t*>(const_cast<void*>(word)), ws->data_ptr(), static_cast<size_t>(ws->numel()), stream);
+  if (status != AT_GRPO_OK) return PyLong_FromLong(status);
+  THPObjectPtr dict(PyDict_New());
+  if (!dict) return nullptr;
+  for (int i = 0; i < PLANNED; ++i)
+    if (!put(dict.get(), g_planned[i], std::move(out[i]))) return nullptr;
+  return dict.release();
+  END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 PyCFunction fast(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f));
@@ -393,6 +509,7 @@ PyMethodDef g_methods[] = {{"group_advantage", fast(group_advantage), METH_FASTC
                            {"check_kv", check_kv, METH_O, nullptr},
                            {"kv_append", fast(kv_append), METH_FASTCALL, nullptr},
                            {"prefix_attention", fast(prefix_attention), METH_FASTCALL, nullptr},
+                           {"kv_plan", fast(kv_plan), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -403,6 +520,10 @@ PyMODINIT_FUNC PyInit__binding() {
     if (!(g_keys[k] = PyUnicode_InternFromString(kKeyNames[k]))) return nullptr;
   for (int k = 0; k < 8; ++k)
     if (!(g_names[k] = PyUnicode_InternFromString(kFields[k]))) return nullptr;
+  for (int k = 0; k < PLANNED; ++k)
+    if (!(g_planned[k] = PyUnicode_InternFromString(kPlanned[k]))) return nullptr;
+  for (int k = 0; k < POOL_FIELDS; ++k)
+    if (!(g_pool[k] = PyUnicode_InternFromString(kPoolFields[k]))) return nullptr;
   const std::pair<PyObject**, const char*> more[] = {{&g_q, "q"}, {&g_k, "k"}, {&g_dq, "dq"}, {&g_dk, "dk"}, {&g_dqw, "dq_weight"},
                                                      {&g_dkw, "dk_weight"}, {&g_out, "out"}, {&g_lse, "lse"}};
   for (const auto& [name, text] : more)

@@ -67,6 +67,8 @@ enum ProfClass {
   PROF_HEAD_FE,        // head contraction that writes the exponentials (one-pass forward + backward)
   PROF_ROPE,           // norms and rotation of queries and keys, their gradient, appending to a cache
   PROF_ATTENTION,      // attention over a paged cache
+  PROF_PLAN,           // pages and slots of a step's tokens
+  PROF_RULES,          // rules of sampling on logits
   PROF_N
 };
 

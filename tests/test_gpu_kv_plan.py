@@ -1,0 +1,252 @@
+"""Pages, slots and positions of a step's tokens against the oracle, entry by entry."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import draft_oracle as oracle
+from paper_2510_11062_amd import api
+from tests.rollout_case import i32
+
+
+class Pool:
+    """Sequences that hold pages, and a ring of the free ones."""
+
+    def __init__(self, page, length, most, free, first=0, size=(), prefix=(), seed=0):
+        self.page, self.length = page, np.array(length, np.int64)
+        rs = self.rs = np.random.default_rng(seed)
+        used = [-(-int(x) // page) for x in length]
+        self.n_pages = max(1, sum(used) + free)
+        ids = rs.permutation(self.n_pages)
+        self.pages = np.full((len(length), -(-most // page)), -7, np.int64)
+        at = 0
+        for s, u in enumerate(used):
+            self.pages[s, :u] = ids[at:at + u]
+            at += u
+        self.ring = np.full(self.n_pages, -9, np.int64)
+        first %= self.n_pages
+        self.ring[(first + np.arange(free)) % self.n_pages] = ids[at:at + free]
+        self.state = np.array([first, free])
+        self.group_seq, self.prefix = np.concatenate([[0], np.cumsum(size)]).astype(np.int64), np.array(prefix, np.int64)
+
+    def device(self, dev):
+        grouped = len(self.prefix) > 0
+        return api.PagePool(i32(self.pages, dev), i32(self.ring, dev), self.page, i32(self.group_seq, dev) if grouped else None,
+                            i32(self.prefix, dev) if grouped else None)
+
+    def want(self, add, n_tok, keep=None, parent=None):
+        return oracle.plan(self.page, self.pages, self.ring, self.length, self.length if keep is None else keep, add, self.state, n_tok,
+                           self.group_seq, self.prefix, parent)
+
+
+MARK = -77
+
+
+def check(p, dev, add, n_tok=None, keep=None, parent=None, in_place=False):
+    """The call against the oracle; rows behind the last token keep what they held."""
+    add = np.array(add, np.int64)
+    keep = None if keep is None else np.array(keep, np.int64)
+    total = int(add.sum())
+    n_tok = total if n_tok is None else n_tok
+    if parent is not None:
+        parent = np.concatenate([parent, np.full(max(0, n_tok - len(parent)), 5)]).astype(np.int64)[:n_tok]
+    want = p.want(add, n_tok, keep, parent)
+    pool, word = p.device(dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    length, state = i32(p.length, dev), i32(p.state, dev)
+    if torch.cuda.is_available():      # what the allocator hands out next holds the mark
+        for dt in (torch.int32, torch.int64):
+            marks = [torch.full((max(1, n_tok),), MARK, dtype=dt, device=dev) for _ in range(4)]
+            del marks
+    o = api.at_grpo_kv_plan(pool, length, i32(add, dev), state, n_tok, keep=None if keep is None else i32(keep, dev),
+                            parent=None if parent is None else i32(parent, dev), length_out=length if in_place else None,
+                            state_out=state if in_place else None, data_error=word)
+    host = lambda t: t.cpu().numpy().tolist()
+    assert host(word) == [want["error"]]
+    assert host(o["length"]) == want["length"] and host(o["state"]) == want["state"] and host(o["cu_q"]) == want["cu_q"]
+    assert np.array_equal(pool.pages.cpu().numpy(), want["pages"]) and np.array_equal(pool.ring.cpu().numpy(), want["ring"])
+    n = len(want["seq"])
+    for name in ("seq", "position", "slot"):
+        assert host(o[name][:n]) == want[name], name
+    if parent is None:
+        assert o["ancestors"] is None
+    else:
+        assert np.array_equal(o["ancestors"][:n].cpu().numpy(), oracle.as_bits(want["ancestors"]))
+    if in_place:
+        assert o["length"].data_ptr() == length.data_ptr() and o["state"].data_ptr() == state.data_ptr()
+    return o, pool, want
+
+
+def trees(rs, add, back=8):
+    return np.concatenate([[j - rs.integers(1, min(j, back) + 1) if j and rs.random() < 0.9 else -1 for j in range(n)] for n in add] + [[]]).astype(np.int64)
+
+
+# page, lengths held, most a sequence, free pages, ring's front, keep (None: all), added, group sizes, prefixes
+CASES = {
+    "one token": (16, [0], 16, 1, 0, None, [1], [], []),
+    "turn": (16, [31, 32, 1, 16], 64, 3, 5, None, [1, 1, 1, 1], [4], [197]),
+    "edges of pages": (8, [0, 7, 8, 9, 15, 16, 17, 0], 64, 60, 3, None, [8, 1, 1, 1, 17, 16, 15, 0], [3, 0, 5], [5, 9, 0]),
+    "given back": (16, [100, 64, 65, 10, 48], 160, 2, 7, [0, 33, 64, 10, 16], [0, 0, 0, 0, 0], [2, 2], [40, 7]),
+    "taken and given": (16, [100, 64, 65, 10, 48, 0], 160, 14, 7, [3, 33, 64, 10, 48, 0], [0, 60, 2, 100, 3, 40], [], []),
+    "all that is free": (8, [8, 8, 8], 32, 6, 4, None, [8, 24, 16], [], []),
+    "nothing": (16, [20, 0, 3], 32, 0, 0, None, [0, 0, 0], [3], [9]),
+    "prompts": (64, [0] * 20, 1200, 400, 11, None, list(range(1, 1200, 60)), [], []),
+    "wide pages, too few": (1024, [1000, 1024, 5000], 9000, 9, 1, [1000, 0, 4097], [30, 9000, 4096], [1], [40000]),      # 13 are needed
+    "wide pages": (1024, [1000, 1024, 5000], 9000, 13, 1, [1000, 0, 4097], [30, 9000, 4096], [1], [40000]),
+    "many": (16, [s % 70 for s in range(3000)], 128, 12000, 900, None, [s % 5 for s in range(3000)], [3] * 900, [s % 50 for s in range(900)]),
+    "many, kept in part": (8, [s % 70 for s in range(5000)], 128, 25000, 4000, [s % 70 * (s % 3) // 2 for s in range(5000)], [(s * 7) % 30 for s in range(5000)],
+                           [0, 2500, 1], [8, 9, 10]),
+    "no pages": (16, [0, 0], 0, 3, 1, None, [0, 0], [], []),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("name", CASES)
+def test_against_the_oracle(gpu_device, name, in_place):
+    page, length, most, free, first, keep, add, size, prefix = CASES[name]
+    p = Pool(page, length, most, free, first, size, prefix)
+    want = check(p, gpu_device, add, keep=keep, in_place=in_place)[2]
+    assert want["error"] == (oracle.POOL if "too few" in name else 0)
+    check(p, gpu_device, add, keep=keep, n_tok=sum(add) + 300, in_place=in_place)
+    if max(add, default=0) <= 64:
+        check(p, gpu_device, add, keep=keep, parent=trees(p.rs, add), in_place=in_place)
+        check(p, gpu_device, add, keep=keep, parent=trees(p.rs, add, 1), n_tok=sum(add) + 1, in_place=in_place)
+
+
+@pytest.mark.gpu
+def test_rows_behind_the_last_token_stay(gpu_device):
+    p = Pool(16, [5, 20], 64, 4)
+    lib = api.load_library()
+    dev = gpu_device
+    length, add, state, word = i32(p.length, dev), i32([3, 2], dev), i32(p.state, dev), torch.zeros(1, dtype=torch.int32, device=dev)
+    pages, ring = i32(p.pages, dev), i32(p.ring, dev)
+    seq, position = (torch.full((9,), MARK, dtype=torch.int32, device=dev) for _ in range(2))
+    slot, bits = (torch.full((9,), MARK, dtype=torch.int64, device=dev) for _ in range(2))
+    parent = i32([-1, 0, 0, -1, 0, 99, 99, 99, 99], dev)
+    cu, out, state_out = torch.zeros(3, dtype=torch.int32, device=dev), torch.zeros(2, dtype=torch.int32, device=dev), torch.zeros(2, dtype=torch.int32, device=dev)
+    ws = torch.empty(lib.at_grpo_kv_plan_workspace_bytes(2), dtype=torch.uint8, device=dev)
+    pool = api._PagePool(16, p.n_pages, 2, pages.shape[1], 0, pages.data_ptr(), ring.data_ptr(), None, None)
+    stream = torch.cuda.current_stream().cuda_stream
+    args = [api.C.byref(pool), 9, length.data_ptr(), None, add.data_ptr(), parent.data_ptr(), state.data_ptr(), out.data_ptr(), state_out.data_ptr(), cu.data_ptr(),
+            seq.data_ptr(), position.data_ptr(), slot.data_ptr(), bits.data_ptr(), word.data_ptr(), ws.data_ptr(), ws.numel(), stream]
+    assert lib.at_grpo_kv_plan(*args) == 0
+    want = p.want(np.array([3, 2]), 9, None, np.array([-1, 0, 0, -1, 0]))
+    assert seq.tolist() == want["seq"] + [MARK] * 4 and position.tolist() == want["position"] + [MARK] * 4
+    assert slot.tolist() == want["slot"] + [MARK] * 4 and bits.tolist() == want["ancestors"] + [MARK] * 4 and int(word) == 0
+    for t in (seq, position, slot, bits):
+        t.fill_(MARK)
+    args[10:14] = [None] * 4      # none of them
+    assert lib.at_grpo_kv_plan(*args) == 0
+    assert cu.tolist() == [0, 3, 5] and out.tolist() == [8, 22] and (slot == MARK).all() and (seq == MARK).all()
+
+
+REFUSED = {
+    "too few pages": dict(add=[40, 40, 40]),
+    "length below 0": dict(length=[-1, 10, 20]),
+    "length past the table": dict(length=[65, 10, 20]),
+    "more kept than held": dict(keep=[11, 10, 20]),
+    "less than nothing kept": dict(keep=[5, -1, 20]),
+    "less than nothing added": dict(add=[1, -1, 1]),
+    "added past the table": dict(add=[1, 55, 1]),
+    "added past 32 bits": dict(add=[2 ** 31 - 1] * 3),
+    "more than there are rows": dict(n_tok=2),
+    "a front outside the ring": dict(state=[8, 3]),
+    "a front below 0": dict(state=[-1, 3]),
+    "more free than there are": dict(state=[0, 9]),
+    "free below 0": dict(state=[0, -1], add=[0, 0, 0]),
+    "given back twice": dict(state=[0, 8], keep=[0, 0, 0], add=[0, 0, 0]),
+}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("name", REFUSED)
+def test_all_or_nothing(gpu_device, name, in_place):
+    p = Pool(16, [10, 10, 20], 64, 4, 2, [2], [30])
+    what = dict(dict(add=[1, 1, 1], n_tok=200), **REFUSED[name])
+    p.length = np.array(what.get("length", p.length))
+    p.state = np.array(what.get("state", p.state))
+    want = check(p, gpu_device, what["add"], n_tok=what["n_tok"], keep=what.get("keep"), in_place=in_place)[2]
+    assert want["error"] in (oracle.SEQLENS, oracle.POOL) and want["cu_q"] == [0] * 4
+    assert np.array_equal(want["pages"], p.pages) and np.array_equal(want["ring"], p.ring)
+
+
+@pytest.mark.gpu
+def test_trees_that_are_none(gpu_device):
+    p = Pool(16, [10, 10, 20], 256, 40)
+    for parent in ([-1, 0, 5, -1, 0, 1, -1], [-1, -2, 1, 0, -1, -(1 << 30), 1 << 30], [0, 1, 2, 0, 0, 0, 0]):
+        want = check(p, gpu_device, [3, 3, 1], parent=np.array(parent))[2]
+        assert want["error"] == oracle.TREE
+    deep = np.concatenate([np.arange(-1, 63), np.arange(-1, 63), [-1]])
+    assert check(p, gpu_device, [64, 64, 1], parent=deep)[2]["error"] == 0
+    assert check(p, gpu_device, [65, 1, 1], parent=np.full(67, -1))[2]["error"] == oracle.SEQLENS
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("group_seq,prefix", [([0, 2, 1], [5, 6]), ([-1, 2, 3], [5, 6]), ([0, 2, 4], [5, 6]), ([0, 1, 3], [-5, 6]), ([0, 1, 3], [2 ** 31 - 1, 6]),
+                                              ([1, 2, 2], [5, 6])])
+def test_groups_that_fall_or_leave_their_range(gpu_device, group_seq, prefix):
+    p = Pool(16, [10, 10, 20], 64, 4)
+    p.group_seq, p.prefix = np.array(group_seq), np.array(prefix)
+    want = check(p, gpu_device, [1, 2, 3])[2]
+    assert want["error"] == (0 if group_seq == [1, 2, 2] else oracle.SEQLENS)
+
+
+@pytest.mark.gpu
+def test_a_rollout_of_steps(gpu_device):
+    """Sequences that draft, keep what was accepted, end and begin again: no page belongs to two of them, none is lost, and the oracle agrees
+    with every step."""
+    rs = np.random.default_rng(5)
+    n = 37
+    p = Pool(8, [0] * n, 200, 600, 590, [5] * 7, list(range(3, 10)))
+    pool, length, state = p.device(gpu_device), i32(p.length, gpu_device), i32(p.state, gpu_device)
+    for step in range(40):
+        new = rs.integers(0, 30, n)
+        keep = np.maximum(0, p.length - rs.integers(0, 20, n))
+        keep[rs.random(n) < 0.1] = 0
+        new = np.minimum(new, 200 - keep)
+        parent = trees(rs, new)
+        want = p.want(new, len(parent), keep, parent)
+        o = api.at_grpo_kv_plan(pool, length, i32(new, gpu_device), state, len(parent), keep=i32(keep, gpu_device), parent=i32(parent, gpu_device),
+                                length_out=length, state_out=state)
+        assert o["slot"].tolist() == want["slot"] and np.array_equal(o["ancestors"].cpu().numpy(), oracle.as_bits(want["ancestors"]))
+        p.pages, p.ring, p.length, p.state = want["pages"], want["ring"], np.array(want["length"]), np.array(want["state"])
+        assert np.array_equal(pool.pages.cpu().numpy(), p.pages) and length.tolist() == want["length"] and state.tolist() == want["state"]
+        held = [x for s in range(n) for x in p.pages[s, :-(-int(p.length[s]) // 8)]]
+        free = p.ring[(p.state[0] + np.arange(p.state[1])) % p.n_pages].tolist()
+        assert want["error"] & oracle.POOL or sorted(held + free) == list(range(p.n_pages))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n", [4, 3000])
+def test_streams_and_graphs(gpu_device, n):
+    """A step in place as a captured graph: each replay is the next step, as the calls one after the other make it."""
+    p = Pool(8, [3] * n, 128, 16 * n, 5, [2] * (n // 2), list(range(n // 2)), seed=3)
+    new = np.tile([5, 1, 0, 9], n)[:n]
+    parent = trees(p.rs, new)
+    ours, theirs = p.device(gpu_device), p.device(gpu_device)
+    add, up = i32(new, gpu_device), i32(parent, gpu_device)
+
+    def step(pool, length, state, keep):
+        return api.at_grpo_kv_plan(pool, length, add, state, len(parent), keep=keep, parent=up, length_out=length, state_out=state)
+
+    side, g = torch.cuda.Stream(device=gpu_device), torch.cuda.CUDAGraph()
+    a = i32(p.length, gpu_device), i32(p.state, gpu_device), i32(p.length, gpu_device)
+    b = tuple(t.clone() for t in a)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(p.device(gpu_device), *(t.clone() for t in a))
+    side.synchronize()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(g, stream=side):
+            out = step(ours, *a)
+    for k in range(4):
+        keep = i32(np.maximum(0, b[0].cpu().numpy() - k), gpu_device)
+        a[2].copy_(keep), b[2].copy_(keep)
+        want = step(theirs, *b)
+        for name in ("seq", "position", "slot", "ancestors", "cu_q"):
+            out[name].fill_(MARK)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[name], want[name]) for name in ("length", "state", "cu_q", "seq", "position", "slot", "ancestors")), k
+        assert torch.equal(ours.pages, theirs.pages) and torch.equal(ours.ring, theirs.ring)
