@@ -559,6 +559,55 @@ int at_grpo_kv_plan(const at_grpo_page_pool* pool, int32_t n_tok, const int32_t*
 size_t at_grpo_kv_plan_workspace_bytes(int32_t n_seq);
 
 /*
+ * The rules of sampling.  Row t of the logits belongs to sequence s, cu_q[s] <= t < cu_q[s + 1] (cu_q NULL: row s).  What stands in
+ * front of the token that the row is for: the prompt of the sequence's group, its own tokens, and with `ancestors` those of its new
+ * tokens that its bits name (as at_grpo_kv_plan writes them; `drafted` holds the new tokens).
+ *   x <- logit
+ *   x <- x > 0 ? x / repetition : x * repetition         where the token occurs in the prompt or behind it
+ *   x <- x - frequency * count - presence                 where it occurs count > 0 times behind the prompt
+ *   x <- x + bias                                         where the sequence has a bias for it
+ *   x <- -inf                                             where the row has a mask and its bit is 0
+ *   best = arg max x;  out = x / temperature;  lse = ln sum exp(out)
+ * Every pointer of a rule may be NULL: no penalty of that kind (1 for repetition, 0 for the others), temperature 1, ...
+ */
+typedef struct {
+  int32_t dtype, out_dtype;      /* of the logits; of out: the same, or AT_GRPO_F32                      */
+  int32_t V, n_seq, n_group;
+  int32_t max_tokens, max_prompt; /* columns of tokens and prompt                                        */
+  int32_t n_bias, n_mask;        /* entries of all bias lists; rows of allowed                           */
+  const int32_t* cu_q;           /* [n_seq + 1], not falling; NULL: n_rows == n_seq                      */
+  const int32_t* tokens;         /* [n_seq, max_tokens]: each sequence's own tokens; NULL: none          */
+  const int32_t* length;         /* [n_seq], 0 .. max_tokens                                             */
+  const int32_t* group_seq;      /* [n_group + 1], not falling                                           */
+  const int32_t* prompt;         /* [n_group, max_prompt]; NULL: none                                    */
+  const int32_t* prompt_len;     /* [n_group], 0 .. max_prompt                                           */
+  const int32_t* drafted;        /* [n_rows]                                                             */
+  const uint64_t* ancestors;     /* [n_rows]; NULL: no drafted tokens                                    */
+  const float *repetition, *presence, *frequency, *temperature; /* [n_seq] each; repetition and temperature > 0, all finite */
+  const int32_t* bias_cu;        /* [n_seq + 1], not falling; NULL: no biases                            */
+  const int32_t* bias_token;     /* [n_bias]; of two entries for one token the last counts               */
+  const float* bias;             /* [n_bias]                                                             */
+  const int32_t* mask_row;       /* [n_rows]: row of allowed, or -1 for none                             */
+  const uint32_t* allowed;       /* [n_mask, (V + 31) / 32]: bit v % 32 of word v / 32; NULL: no masks   */
+} at_grpo_sampling_rules;
+
+/*
+ * Rows of logits by the rules, in one pass.  out[t] at out + t * out_stride (elements), or NULL; out may be the logits themselves
+ * (same dtype and stride) and shares no memory with them otherwise.  lse [n_rows] fp32 and best [n_rows] int32, or NULL.
+ * All arithmetic is fp32, each operation rounded by itself (repetition by division, the temperature by its reciprocal), out rounded once.
+ * best is the lowest of the tokens with the largest x, taken in front of the temperature; a row of which nothing is left gets best -1 and
+ * lse -inf.  A NaN logit that a mask leaves makes lse NaN and is passed over by best.
+ * Without any penalty the lists of tokens are not looked at.  A row of no sequence (also where cu_q falls or leaves its range there: AT_GRPO_DATA_SEQLENS) has its mask and nothing else.  Tokens outside
+ * [0, V) are passed over (AT_GRPO_DATA_TOKEN_RANGE), a length or list out of range counts as empty (AT_GRPO_DATA_SEQLENS), a
+ * repetition or temperature that is not positive and finite as 1, a presence or frequency that is not finite as 0 and a mask_row out of
+ * range as -1 (AT_GRPO_DATA_RULE).  Workspace: at_grpo_logit_rules_workspace_bytes (0 on invalid arguments; no pointer is read).
+ */
+int at_grpo_logit_rules(const at_grpo_sampling_rules* rules, int32_t n_rows, const void* logits,
+                        int64_t logits_stride, void* out, int64_t out_stride, float* lse, int32_t* best,
+                        int32_t* data_error, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t at_grpo_logit_rules_workspace_bytes(const at_grpo_sampling_rules* rules, int32_t n_rows);
+
+/*
  * Bytes of workspace a call needs.  `batch` may be NULL for AT_GRPO_CALL_GROUP_ADVANTAGE; the
  * id extents are ignored for the other calls.  Only sizes are read from `batch` (H, V, n_heads,
  * dtype, n_tok, n_resp); no pointer in it is dereferenced.  With the other sizes as they are, a batch of

@@ -1,4 +1,4 @@
-"""Plain definitions of what a rollout that drafts its tokens calls beside attention: pages and slots of a step.
+"""Plain definitions of what a rollout that drafts its tokens calls: pages and slots of a step, and the rules of sampling on logits.
 
 Written from the formulas, one sequence and one token at a time; shares no code with the product."""
 from __future__ import annotations
@@ -81,3 +81,49 @@ def plan(page, pages, ring, length, keep, add, state, n_tok, group_seq=(0,), pre
 
 def as_bits(ancestors):
     return np.array(ancestors, dtype=np.uint64).view(np.int64)
+
+
+def sampling_row(logit, prompt, behind, repetition, presence, frequency, temperature, bias, allowed):
+    """One row of logits [V]: `prompt` and `behind` are the tokens in front of the row's, bias {token: value}, allowed [V] of truth values
+    or None.  Returns (out, lse, best, size): size [V] is the sum of the magnitudes of what is rounded on the way to out, for error bounds."""
+    V = len(logit)
+    x = np.array(logit, dtype=np.float64)
+    size = np.zeros(V)
+    count = np.zeros(V)
+    seen = np.zeros(V, dtype=bool)
+    for token in prompt:
+        seen[token] = True
+    for token in behind:
+        seen[token] = True
+        count[token] += 1
+    for v in np.flatnonzero(seen):
+        x[v] = x[v] / repetition if x[v] > 0 else x[v] * repetition
+        size[v] += abs(x[v])
+        if count[v]:
+            size[v] += abs(frequency * count[v])
+            x[v] -= frequency * count[v]
+            size[v] += abs(x[v])
+            x[v] -= presence
+            size[v] += abs(x[v])
+    for v, b in bias.items():
+        x[v] += b
+        size[v] += abs(x[v])
+    if allowed is not None:
+        x[~allowed] = -np.inf
+        size[~allowed] = 0
+    real = ~np.isnan(x) & (x > -np.inf)
+    best = -1
+    for v in np.flatnonzero(real):
+        if best < 0 or x[v] > x[best]:
+            best = int(v)
+    out = x / temperature
+    size = size / temperature + 2 * np.where(np.isfinite(out), np.abs(out), 0)
+    if np.isnan(out).any():
+        lse = np.nan
+    elif best < 0:
+        lse = -np.inf
+    elif out[best] == np.inf:
+        lse = np.inf
+    else:
+        lse = out[best] + np.log(np.exp(out - out[best]).sum())
+    return out, lse, best, size

@@ -43,6 +43,7 @@ EXPORTS = [
     "at_grpo_status_string", "at_grpo_version", "at_grpo_profile_enable", "at_grpo_profile_classes",
     "at_grpo_profile_read", "at_grpo_rope_table", "at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append",
     "at_grpo_prefix_attention", "at_grpo_prefix_attention_workspace_bytes", "at_grpo_kv_plan", "at_grpo_kv_plan_workspace_bytes",
+    "at_grpo_logit_rules", "at_grpo_logit_rules_workspace_bytes",
 ]
 
 
@@ -80,6 +81,12 @@ class _KV(C.Structure):
 class _PagePool(C.Structure):
     _fields_ = [("page_size", C.c_int32), ("n_pages", C.c_int32), ("n_seq", C.c_int32), ("max_pages", C.c_int32), ("n_group", C.c_int32),
                 ("pages", C.c_void_p), ("ring", C.c_void_p), ("group_seq", C.c_void_p), ("prefix_len", C.c_void_p)]
+
+
+class _SamplingRules(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("dtype", "out_dtype", "V", "n_seq", "n_group", "max_tokens", "max_prompt", "n_bias", "n_mask")] + \
+               [(n, C.c_void_p) for n in ("cu_q", "tokens", "length", "group_seq", "prompt", "prompt_len", "drafted", "ancestors", "repetition", "presence",
+                                          "frequency", "temperature", "bias_cu", "bias_token", "bias", "mask_row", "allowed")]
 
 
 class _Batch(C.Structure):
@@ -167,6 +174,10 @@ def load_library():
     lib.at_grpo_kv_plan.restype = C.c_int
     lib.at_grpo_kv_plan_workspace_bytes.argtypes = [i32]
     lib.at_grpo_kv_plan_workspace_bytes.restype = sz
+    lib.at_grpo_logit_rules.argtypes = [C.POINTER(_SamplingRules), i32, vp, C.c_int64, vp, C.c_int64, vp, vp, vp, vp, sz, vp]
+    lib.at_grpo_logit_rules.restype = C.c_int
+    lib.at_grpo_logit_rules_workspace_bytes.argtypes = [C.POINTER(_SamplingRules), i32]
+    lib.at_grpo_logit_rules_workspace_bytes.restype = sz
     _lib = lib
     return lib
 
@@ -184,7 +195,8 @@ def load_binding():
         _group_fn = C.cast(lib.at_grpo_group_advantage, C.c_void_p).value
         _mixed_fn = C.cast(lib.at_grpo_group_advantage_mixed, C.c_void_p).value
         for name in ("at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append", "at_grpo_prefix_attention",
-                     "at_grpo_prefix_attention_workspace_bytes", "at_grpo_kv_plan", "at_grpo_kv_plan_workspace_bytes"):
+                     "at_grpo_prefix_attention_workspace_bytes", "at_grpo_kv_plan", "at_grpo_kv_plan_workspace_bytes",
+                     "at_grpo_logit_rules", "at_grpo_logit_rules_workspace_bytes"):
             _fn[name] = C.cast(getattr(lib, name), C.c_void_p).value
         _binding = binding
     return _binding
@@ -960,3 +972,79 @@ def at_grpo_kv_plan(pool: PagePool, length, add, state, n_tok: int, keep=None, p
     _explain_groups(pool.group_seq, pool.prefix_len, "prefix_len", device)
     _word(data_error, device)
     _refused(res, "at_grpo_kv_plan")
+
+
+@dataclass
+class LogitRules:
+    """Python-side mirror of at_grpo_sampling_rules: what the logits of a batch of sequences go by.  The tensors' contents may change between
+    calls (tokens are appended, settings change); every one may be None."""
+    tokens: Optional[torch.Tensor] = None       # int32 [n_seq, max_tokens]: the sequences' own tokens
+    length: Optional[torch.Tensor] = None       # int32 [n_seq]
+    prompt: Optional[torch.Tensor] = None       # int32 [n_group, max_prompt]
+    prompt_len: Optional[torch.Tensor] = None   # int32 [n_group]
+    group_seq: Optional[torch.Tensor] = None    # int32 [n_group + 1]
+    cu_q: Optional[torch.Tensor] = None         # int32 [n_seq + 1]; None: a row for every sequence
+    drafted: Optional[torch.Tensor] = None      # int32 [rows]: the new tokens, and
+    ancestors: Optional[torch.Tensor] = None    # int64 [rows]: for each the bits of those on its path
+    repetition: Optional[torch.Tensor] = None   # float32 [n_seq]
+    presence: Optional[torch.Tensor] = None
+    frequency: Optional[torch.Tensor] = None
+    temperature: Optional[torch.Tensor] = None
+    bias_cu: Optional[torch.Tensor] = None      # int32 [n_seq + 1]
+    bias_token: Optional[torch.Tensor] = None   # int32 [entries]
+    bias: Optional[torch.Tensor] = None         # float32 [entries]
+    allowed: Optional[torch.Tensor] = None      # int32 [masks, ceil(V / 32)]: a bit for each token
+    mask_row: Optional[torch.Tensor] = None     # int32 [rows]; -1: no mask
+
+
+def at_grpo_logit_rules(rules: LogitRules, logits, want_out: bool = True, want_lse: bool = True, want_best: bool = True, out=None, out_dtype=None,
+                        data_error=None):
+    """The logits [rows, V] by the rules: penalties, biases, masks, temperature.  out: what takes them, which may be the logits themselves; a
+    new tensor of out_dtype (the logits' own, or float32) where none is given.  lse: their log-sum of exponentials; best: the token with the
+    largest, the lowest of several, -1 where a mask leaves none.  Returns dict(out, lse, best, workspace), None for what is not wanted."""
+    if _binding is None:
+        load_binding()
+    device = _tensor_on_gpu("logits", logits)
+    on, stream = _on(device)
+    new = None if out is not None or not want_out else logits.dtype if out_dtype is None else out_dtype
+    with on:
+        ws, res = _with_scratch(lambda ws: _binding.logit_rules(_fn["at_grpo_logit_rules"], _fn["at_grpo_logit_rules_workspace_bytes"], rules, logits, out, new,
+                                                                want_lse, want_best, data_error, ws, stream), device, stream)
+    if type(res) is dict:
+        res["workspace"] = ws
+        return res
+    for name, t in (("logits", logits), ("out", out)):
+        if t is not None and (not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype not in DTYPE or t.device != device or t.shape != logits.shape or
+                              (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1])):
+            raise AtGrpoError(f"{name} must be [rows, V] of float32 or bfloat16 on {device}, with contiguous rows that do not overlap")
+    if new is not None and new not in DTYPE or torch.float32 not in (out.dtype if out is not None else new, logits.dtype) and \
+            (out.dtype if out is not None else new) not in (None, logits.dtype):
+        raise AtGrpoError("out is of the logits' dtype or float32")
+    n = logits.shape[0]
+    if rules.cu_q is not None and (not isinstance(rules.cu_q, torch.Tensor) or rules.cu_q.dim() != 1 or rules.cu_q.numel() < 1):
+        raise AtGrpoError("cu_q must have n_seq + 1 elements")
+    n_seq = n if rules.cu_q is None else rules.cu_q.numel() - 1
+    _vector("cu_q", rules.cu_q, n_seq + 1, torch.int32, device)
+    for names, m, dt in ((("drafted", "mask_row"), n, torch.int32), (("ancestors",), n, torch.int64), (("length",), n_seq, torch.int32),
+                         (("repetition", "presence", "frequency", "temperature"), n_seq, torch.float32), (("bias_cu",), n_seq + 1, torch.int32)):
+        for name in names:
+            _vector(name, getattr(rules, name), m, dt, device)
+    for name, m in (("tokens", n_seq), ("prompt", None), ("allowed", None)):
+        t = getattr(rules, name)
+        if t is not None and (not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != torch.int32 or t.device != device or not t.is_contiguous() or
+                              (m is not None and t.shape[0] != m)):
+            raise AtGrpoError(f"{name} must be a contiguous int32 matrix on {device}" + (" with a row for each sequence" if m is not None else ""))
+    _explain_groups(rules.group_seq, rules.prompt_len, "prompt_len", device)
+    for name, needed in (("tokens", ("length",)), ("prompt", ("prompt_len", "group_seq")), ("ancestors", ("drafted",)),
+                         ("bias_cu", ("bias_token", "bias")), ("allowed", ("mask_row",))):
+        if getattr(rules, name) is not None and any(getattr(rules, x) is None for x in needed):
+            raise AtGrpoError(f"{name} needs {' and '.join(needed)}")
+    if rules.prompt is not None and rules.prompt.shape[0] != rules.group_seq.numel() - 1:
+        raise AtGrpoError("prompt must have a row for each group")
+    if rules.allowed is not None and rules.allowed.shape[1] != (logits.shape[1] + 31) // 32:
+        raise AtGrpoError("allowed must have a bit for each token: ceil(V / 32) columns")
+    if rules.bias_cu is not None:
+        for name, dt in (("bias_token", torch.int32), ("bias", torch.float32)):
+            _vector(name, getattr(rules, name), rules.bias.numel(), dt, device)
+    _word(data_error, device)
+    _refused(res, "at_grpo_logit_rules")

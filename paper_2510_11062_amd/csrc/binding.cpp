@@ -7,6 +7,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
@@ -498,6 +499,134 @@ PyObject* kv_plan(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   END_HANDLE_TH_ERRORS
 }
 
+enum RuleField {
+  R_TOKENS, R_LENGTH, R_PROMPT, R_PROMPT_LEN, R_GROUP_SEQ, R_CU_Q, R_DRAFTED, R_ANCESTORS, R_REPETITION, R_PRESENCE, R_FREQUENCY, R_TEMPERATURE, R_BIAS_CU,
+  R_BIAS_TOKEN, R_BIAS, R_ALLOWED, R_MASK_ROW, RULE_FIELDS
+};
+const char* const kRuleFields[RULE_FIELDS] = {"tokens", "length", "prompt", "prompt_len", "group_seq", "cu_q", "drafted", "ancestors", "repetition", "presence",
+                                              "frequency", "temperature", "bias_cu", "bias_token", "bias", "allowed", "mask_row"};
+PyObject *g_rule[RULE_FIELDS], *g_best;
+
+// Rows [n, V] with contiguous elements, as far apart as they are long or farther.
+const at::Tensor* logit_rows(PyObject* o) {
+  const at::Tensor* t = as_tensor(o);
+  return t && t->dim() == 2 && t->is_cuda() && known(t->scalar_type()) && t->size(0) <= 0x7fffffff && t->size(1) <= 0x7fffffff &&
+                 (t->numel() == 0 || ((t->stride(1) == 1 || t->size(1) == 1) && (t->size(0) == 1 || t->stride(0) >= t->size(1))))
+             ? t
+             : nullptr;
+}
+
+// The fields of a LogitRules for n rows of V logits.
+bool sampling_rules(THPObjectPtr (&held)[RULE_FIELDS], int64_t n, int64_t V, at::Device device, at_grpo_sampling_rules* r) {
+  const auto field = [&](int i) { return held[i].get(); };
+  const auto there = [&](int i) { return field(i) != Py_None; };
+  int64_t n_seq = n;
+  if (there(R_CU_Q)) {
+    const at::Tensor* t = as_tensor(field(R_CU_Q));
+    if (!t || t->dim() != 1 || t->size(0) < 1 || t->size(0) > 0x7fffffff) return false;
+    n_seq = t->size(0) - 1;
+  }
+  r->n_seq = static_cast<int32_t>(n_seq);
+  const void *cu, *len, *groups, *prompt_len, *drafted, *ancestors, *bias_cu, *bias_token, *bias, *mask_row;
+  if (!vector(field(R_CU_Q), n_seq + 1, at::kInt, device, &cu) || !vector(field(R_DRAFTED), n, at::kInt, device, &drafted) ||
+      !vector(field(R_ANCESTORS), n, at::kLong, device, &ancestors) || !vector(field(R_MASK_ROW), n, at::kInt, device, &mask_row))
+    return false;
+  r->cu_q = static_cast<const int32_t*>(cu);
+  r->drafted = static_cast<const int32_t*>(drafted);
+  r->ancestors = static_cast<const uint64_t*>(ancestors);
+  r->mask_row = static_cast<const int32_t*>(mask_row);
+  const float** const settings[4] = {&r->repetition, &r->presence, &r->frequency, &r->temperature};
+  for (int i = 0; i < 4; ++i) {
+    const void* p;
+    if (!vector(field(R_REPETITION + i), n_seq, at::kFloat, device, &p)) return false;
+    *settings[i] = static_cast<const float*>(p);
+  }
+  if (there(R_TOKENS)) {
+    const at::Tensor* t = matrix(field(R_TOKENS), n_seq, at::kInt, device);
+    if (!t || !there(R_LENGTH) || !vector(field(R_LENGTH), n_seq, at::kInt, device, &len)) return false;
+    r->tokens = data<const int32_t>(*t);
+    r->length = static_cast<const int32_t*>(len);
+    r->max_tokens = static_cast<int32_t>(t->size(1));
+  }
+  if (there(R_PROMPT)) {
+    if (!there(R_GROUP_SEQ) || !groups_of(field(R_GROUP_SEQ), field(R_PROMPT_LEN), device, &groups, &prompt_len, &r->n_group)) return false;
+    const at::Tensor* t = matrix(field(R_PROMPT), r->n_group, at::kInt, device);
+    if (!t) return false;
+    r->group_seq = static_cast<const int32_t*>(groups);
+    r->prompt_len = static_cast<const int32_t*>(prompt_len);
+    r->prompt = r->n_group ? data<const int32_t>(*t) : nullptr;
+    r->max_prompt = static_cast<int32_t>(t->size(1));
+  }
+  if (there(R_BIAS_CU)) {
+    const at::Tensor* t = as_tensor(field(R_BIAS));
+    const int64_t m = t && t->dim() == 1 ? t->size(0) : -1;
+    if (m < 0 || m > 0x7fffffff || !there(R_BIAS_TOKEN) || !vector(field(R_BIAS_CU), n_seq + 1, at::kInt, device, &bias_cu) ||
+        !vector(field(R_BIAS_TOKEN), m, at::kInt, device, &bias_token) || !vector(field(R_BIAS), m, at::kFloat, device, &bias))
+      return false;
+    r->bias_cu = static_cast<const int32_t*>(bias_cu);
+    r->bias_token = static_cast<const int32_t*>(bias_token);
+    r->bias = static_cast<const float*>(bias);
+    r->n_bias = static_cast<int32_t>(m);
+  }
+  if (there(R_ALLOWED)) {
+    const at::Tensor* t = matrix(field(R_ALLOWED), -1, at::kInt, device);
+    if (!t || t->size(1) != (V + 31) / 32 || !there(R_MASK_ROW)) return false;
+    r->allowed = t->size(0) ? data<const uint32_t>(*t) : nullptr;
+    r->n_mask = static_cast<int32_t>(t->size(0));
+  }
+  return true;
+}
+
+// logit_rules(function's address, its workspace query's, LogitRules, logits, out or None, the dtype of a new one or None, want_lse, want_best,
+//             data_error, workspace or None, stream)
+// Where the workspace is none or too small: (bytes,).
+PyObject* logit_rules(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+  HANDLE_TH_ERRORS
+  if (n_args != 11) {
+    PyErr_SetString(PyExc_TypeError, "logit_rules takes 11 arguments");
+    return nullptr;
+  }
+  THPObjectPtr held[RULE_FIELDS];
+  const at::Tensor *logits = logit_rows(v[3]), *given = v[4] == Py_None ? nullptr : logit_rows(v[4]);
+  if (!logits || !fields_of(v[2], g_rule, held) || (v[4] != Py_None && !given)) Py_RETURN_NONE;
+  const int64_t n = logits->size(0), V = logits->size(1);
+  if (given && (given->sizes() != logits->sizes() || given->device() != logits->device())) Py_RETURN_NONE;
+  const bool want_lse = PyObject_IsTrue(v[6]) == 1, want_best = PyObject_IsTrue(v[7]) == 1;
+  void* stream = PyLong_AsVoidPtr(v[10]);
+  if (PyErr_Occurred()) return nullptr;
+  const void* word;
+  at_grpo_sampling_rules r{};
+  r.dtype = r.out_dtype = code(logits->scalar_type());
+  r.V = static_cast<int32_t>(V);
+  if (!vector(v[8], 1, at::kInt, logits->device(), &word) || !sampling_rules(held, n, V, logits->device(), &r)) Py_RETURN_NONE;
+  at::Tensor out, lse, best;
+  if (given) {
+    out = *given;
+  } else if (v[5] != Py_None) {
+    if (!THPDtype_Check(v[5]) || !known(reinterpret_cast<THPDtype*>(v[5])->scalar_type)) Py_RETURN_NONE;
+    const WithoutPythonLock others_run;
+    out = at::empty({n, V}, logits->options().dtype(reinterpret_cast<THPDtype*>(v[5])->scalar_type));
+  }
+  if (out.defined()) r.out_dtype = code(out.scalar_type());
+  const size_t bytes = reinterpret_cast<decltype(&at_grpo_logit_rules_workspace_bytes)>(PyLong_AsVoidPtr(v[1]))(&r, static_cast<int32_t>(n));
+  if (bytes == 0) Py_RETURN_NONE;
+  const at::Tensor* ws = as_tensor(v[9]);
+  if (!ws || static_cast<size_t>(ws->numel()) < bytes) return Py_BuildValue("(n)", static_cast<Py_ssize_t>(bytes));
+  {
+    const WithoutPythonLock others_run;
+    if (want_lse) lse = at::empty({n}, logits->options().dtype(at::kFloat));
+    if (want_best) best = at::empty({n}, logits->options().dtype(at::kInt));
+  }
+  const int status = reinterpret_cast<decltype(&at_grpo_logit_rules)>(PyLong_AsVoidPtr(v[0]))(
+      &r, static_cast<int32_t>(n), logits->data_ptr(), logits->stride(0), data<void>(out), out.defined() ? out.stride(0) : 0, data<float>(lse),
+      data<int32_t>(best), static_cast<int32_t*>(const_cast<void*>(word)), ws->data_ptr(), static_cast<size_t>(ws->numel()), stream);
+  if (status != AT_GRPO_OK) return PyLong_FromLong(status);
+  THPObjectPtr dict(PyDict_New());
+  if (!dict || !put(dict.get(), g_out, std::move(out)) || !put(dict.get(), g_lse, std::move(lse)) || !put(dict.get(), g_best, std::move(best))) return nullptr;
+  return dict.release();
+  END_HANDLE_TH_ERRORS
+}
+
 template <typename F>
 PyCFunction fast(F f) {
   return reinterpret_cast<PyCFunction>(reinterpret_cast<void*>(f));
@@ -510,6 +639,7 @@ PyMethodDef g_methods[] = {{"group_advantage", fast(group_advantage), METH_FASTC
                            {"kv_append", fast(kv_append), METH_FASTCALL, nullptr},
                            {"prefix_attention", fast(prefix_attention), METH_FASTCALL, nullptr},
                            {"kv_plan", fast(kv_plan), METH_FASTCALL, nullptr},
+                           {"logit_rules", fast(logit_rules), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_binding", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -524,8 +654,10 @@ PyMODINIT_FUNC PyInit__binding() {
     if (!(g_planned[k] = PyUnicode_InternFromString(kPlanned[k]))) return nullptr;
   for (int k = 0; k < POOL_FIELDS; ++k)
     if (!(g_pool[k] = PyUnicode_InternFromString(kPoolFields[k]))) return nullptr;
+  for (int k = 0; k < RULE_FIELDS; ++k)
+    if (!(g_rule[k] = PyUnicode_InternFromString(kRuleFields[k]))) return nullptr;
   const std::pair<PyObject**, const char*> more[] = {{&g_q, "q"}, {&g_k, "k"}, {&g_dq, "dq"}, {&g_dk, "dk"}, {&g_dqw, "dq_weight"},
-                                                     {&g_dkw, "dk_weight"}, {&g_out, "out"}, {&g_lse, "lse"}};
+                                                     {&g_dkw, "dk_weight"}, {&g_out, "out"}, {&g_lse, "lse"}, {&g_best, "best"}};
   for (const auto& [name, text] : more)
     if (!(*name = PyUnicode_InternFromString(text))) return nullptr;
   return PyModule_Create(&g_module);

@@ -2,6 +2,7 @@
 import pytest
 
 from paper_2510_11062_amd import api
+from tests import test_rollout_abi
 
 EINVAL, EUNSUPPORTED, EWORKSPACE = 1, 2, 3
 AT = iter(range(1 << 40, 1 << 50, 1 << 30))      # addresses far from each other
@@ -48,3 +49,52 @@ def test_plan_workspace():
     assert lib.at_grpo_kv_plan_workspace_bytes(-1) == 0
     sizes = [lib.at_grpo_kv_plan_workspace_bytes(n) for n in (0, 1, 100, 5000, 1 << 20)]
     assert sizes == sorted(sizes) and sizes[0] > 0 and sizes[-1] >= 8 << 20
+
+
+def rules_args(**over):
+    f = {n: 0 for n, _ in api._SamplingRules._fields_}
+    f.update(dtype=1, out_dtype=1, V=1000, n_seq=4, n_group=1, max_tokens=50, max_prompt=60, n_bias=5, n_mask=2)
+    f.update({n: next(AT) for n, t in api._SamplingRules._fields_ if t is api.C.c_void_p})
+    f.update(n_rows=9, logits=next(AT), stride=1000, out=next(AT), out_stride=1000, lse=next(AT), best=next(AT), workspace=next(AT), bytes=1 << 20)
+    f.update(over)
+    return f
+
+
+def call_rules(f):
+    r = api._SamplingRules(*(f[n] for n, _ in api._SamplingRules._fields_))
+    return api.load_library().at_grpo_logit_rules(api.C.byref(r), f["n_rows"], f["logits"], f["stride"], f["out"], f["out_stride"], f["lse"], f["best"], None,
+                                                  f["workspace"], f["bytes"], None)
+
+
+@pytest.mark.parametrize("over,status", [
+    (dict(n_rows=-1), EINVAL), (dict(V=0), EINVAL), (dict(n_seq=-1), EINVAL), (dict(n_group=-1), EINVAL), (dict(max_tokens=-1), EINVAL), (dict(max_prompt=-1), EINVAL),
+    (dict(n_bias=-1), EINVAL), (dict(n_mask=-1), EINVAL), (dict(dtype=2), EUNSUPPORTED), (dict(dtype=0), EUNSUPPORTED), (dict(out_dtype=2), EUNSUPPORTED),
+    (dict(V=2 ** 31 - 1), EUNSUPPORTED), (dict(V=1 << 30, n_rows=1 << 20, stride=1 << 30, out_stride=1 << 30), EUNSUPPORTED),
+    (dict(cu_q=None), EINVAL), (dict(logits=None), EINVAL), (dict(out=None, lse=None, best=None), EINVAL), (dict(stride=999), EINVAL), (dict(out_stride=999), EINVAL),
+    (dict(length=None), EINVAL), (dict(group_seq=None), EINVAL), (dict(prompt_len=None), EINVAL), (dict(drafted=None), EINVAL), (dict(bias_token=None), EINVAL),
+    (dict(bias=None), EINVAL), (dict(mask_row=None), EINVAL), (dict(logits=(1 << 51) + 1), EINVAL), (dict(out=(1 << 51) + 1), EINVAL),
+    (dict(workspace=None), EWORKSPACE), (dict(bytes=16), EWORKSPACE), (dict(workspace=(1 << 51) + 8), EWORKSPACE)])
+def test_rules(over, status):
+    assert call_rules(rules_args(**over)) == status
+
+
+@pytest.mark.parametrize("apart,stride,out_dtype", [(2, 1000, 1), (0, 1001, 1), (0, 1000, 0), (-2, 1000, 1), (17998, 1000, 1)])
+def test_rules_outputs_that_meet_the_logits(apart, stride, out_dtype):
+    f = rules_args(out_stride=stride, out_dtype=out_dtype)
+    f["out"] = f["logits"] + apart
+    assert call_rules(f) == EINVAL
+
+
+def test_rules_of_no_rows():
+    assert call_rules(rules_args(n_rows=0)) == 0
+    r = api._SamplingRules(1, 1, 1000, 4)
+    lib = api.load_library()
+    assert lib.at_grpo_logit_rules_workspace_bytes(api.C.byref(r), -1) == 0 and lib.at_grpo_logit_rules_workspace_bytes(None, 5) == 0
+    sizes = [lib.at_grpo_logit_rules_workspace_bytes(api.C.byref(r), n) for n in (0, 1, 100, 10 ** 6)]
+    assert sizes == sorted(sizes) and sizes[0] > 0
+
+
+@pytest.mark.parametrize("compiler,std", [("gcc", "-std=c99"), ("g++", "-std=c++17")])
+def test_struct_layout(tmp_path, monkeypatch, compiler, std):
+    monkeypatch.setattr(test_rollout_abi, "MIRRORS", {"at_grpo_page_pool": api._PagePool, "at_grpo_sampling_rules": api._SamplingRules})
+    test_rollout_abi.test_struct_layout(tmp_path, compiler, std)
