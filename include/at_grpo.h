@@ -78,7 +78,7 @@ enum {
   AT_GRPO_DATA_AGENT_RANGE = 16, /* resp_agent / head_of_agent entry out of range     */
   AT_GRPO_DATA_PAGE = 32,        /* page id outside the cache, or a token behind its page table */
   AT_GRPO_DATA_POSITION = 64,    /* position outside the rotation table               */
-  AT_GRPO_DATA_TREE = 128,       /* a drafted token whose parent does not stand in front of it */
+  AT_GRPO_DATA_TREE = 128,       /* a parent that does not stand in front of its token, a tree of more than 64 */
   AT_GRPO_DATA_POOL = 256,       /* a pool that has too few pages, or whose state no pool can have */
   AT_GRPO_DATA_RULE = 512        /* a penalty, temperature, bias list or mask that is none */
 };
@@ -557,6 +557,18 @@ int at_grpo_kv_plan(const at_grpo_page_pool* pool, int32_t n_tok, const int32_t*
                     uint64_t* ancestors, int32_t* data_error, void* workspace, size_t workspace_bytes,
                     void* hip_stream);
 size_t at_grpo_kv_plan_workspace_bytes(int32_t n_seq);
+
+/*
+ * Attention of trees of drafted tokens: as at_grpo_prefix_attention, with other visible tokens.  New token j of a sequence is its own token
+ * length - (new tokens) + j, and row t's token sees the prefix, the own tokens in front of the new ones, and new token j where bit j of
+ * ancestors[t] is set: its path, as at_grpo_kv_plan writes it, or any other choice; itself only where its own bit says so.  Bits behind the last
+ * new token are passed over; a sequence has at most 64 new tokens, and those behind the 64th are seen by nobody (AT_GRPO_DATA_TREE).
+ * ancestors [n_tok].  A row that sees nothing gets out 0 and lse -inf; everything else, refusals and workspace among it, is as there.
+ */
+int at_grpo_tree_attention(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* q,
+                           const uint64_t* ancestors, float scale, int32_t max_q, const at_grpo_rows* out, float* lse,
+                           int32_t* data_error, void* workspace, size_t workspace_bytes, void* hip_stream);
+size_t at_grpo_tree_attention_workspace_bytes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q);
 
 /*
  * The rules of sampling.  Row t of the logits belongs to sequence s, cu_q[s] <= t < cu_q[s + 1] (cu_q NULL: row s).  What stands in

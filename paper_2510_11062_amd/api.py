@@ -43,7 +43,7 @@ EXPORTS = [
     "at_grpo_status_string", "at_grpo_version", "at_grpo_profile_enable", "at_grpo_profile_classes",
     "at_grpo_profile_read", "at_grpo_rope_table", "at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append",
     "at_grpo_prefix_attention", "at_grpo_prefix_attention_workspace_bytes", "at_grpo_kv_plan", "at_grpo_kv_plan_workspace_bytes",
-    "at_grpo_logit_rules", "at_grpo_logit_rules_workspace_bytes",
+    "at_grpo_logit_rules", "at_grpo_logit_rules_workspace_bytes", "at_grpo_tree_attention", "at_grpo_tree_attention_workspace_bytes",
 ]
 
 
@@ -170,6 +170,10 @@ def load_library():
         getattr(lib, name).restype = C.c_int
     lib.at_grpo_prefix_attention_workspace_bytes.argtypes = [kv, i32, i32, i32]
     lib.at_grpo_prefix_attention_workspace_bytes.restype = sz
+    lib.at_grpo_tree_attention.argtypes = [kv, i32, i32, rows, vp, f32, i32, rows, vp, vp, vp, sz, vp]
+    lib.at_grpo_tree_attention.restype = C.c_int
+    lib.at_grpo_tree_attention_workspace_bytes.argtypes = [kv, i32, i32, i32]
+    lib.at_grpo_tree_attention_workspace_bytes.restype = sz
     lib.at_grpo_kv_plan.argtypes = [C.POINTER(_PagePool), i32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.at_grpo_kv_plan.restype = C.c_int
     lib.at_grpo_kv_plan_workspace_bytes.argtypes = [i32]
@@ -196,7 +200,7 @@ def load_binding():
         _mixed_fn = C.cast(lib.at_grpo_group_advantage_mixed, C.c_void_p).value
         for name in ("at_grpo_qk_norm_rope", "at_grpo_qk_norm_rope_bwd", "at_grpo_kv_append", "at_grpo_prefix_attention",
                      "at_grpo_prefix_attention_workspace_bytes", "at_grpo_kv_plan", "at_grpo_kv_plan_workspace_bytes",
-                     "at_grpo_logit_rules", "at_grpo_logit_rules_workspace_bytes"):
+                     "at_grpo_logit_rules", "at_grpo_logit_rules_workspace_bytes", "at_grpo_tree_attention", "at_grpo_tree_attention_workspace_bytes"):
             _fn[name] = C.cast(getattr(lib, name), C.c_void_p).value
         _binding = binding
     return _binding
@@ -972,6 +976,34 @@ def at_grpo_kv_plan(pool: PagePool, length, add, state, n_tok: int, keep=None, p
     _explain_groups(pool.group_seq, pool.prefix_len, "prefix_len", device)
     _word(data_error, device)
     _refused(res, "at_grpo_kv_plan")
+
+
+def at_grpo_tree_attention(kv: KVBatch, q, ancestors, scale: Optional[float] = None, max_q: int = 64, out=None, want_lse: bool = False, data_error=None):
+    """Attention of trees of drafted tokens: the queries q [n, Hq, D] of a sequence's new tokens (at most 64) over its group's prefix, its own tokens
+    in front of the new ones, and those of the new ones that the bits of ancestors int64 [n] name (as at_grpo_kv_plan gives them).  1 /
+    sqrt(D) where no scale is given; max_q: an upper bound of the new tokens of one sequence.  out may not share memory with q.
+    Returns dict(out, lse, workspace)."""
+    if _binding is None:
+        load_binding()
+    device = _tensor_on_gpu("q", q)
+    on, stream = _on(device)
+    with on:
+        ws, res = _with_scratch(lambda ws: _binding.tree_attention(_fn["at_grpo_tree_attention"], _fn["at_grpo_tree_attention_workspace_bytes"], kv, q, scale,
+                                                                   ancestors, max_q, out, want_lse, data_error, ws, stream), device, stream)
+    if type(res) is dict:
+        res["workspace"] = ws
+        return res
+    kv.__post_init__()
+    kv._rows("q", q, None)
+    if ancestors is None:
+        raise AtGrpoError("ancestors are needed")
+    _vector("ancestors", ancestors, q.shape[0], torch.int64, device)
+    if out is not None:
+        kv._rows("out", out, q, q.shape[1])
+    _word(data_error, device)
+    if res is None:
+        raise AtGrpoError("at_grpo_tree_attention: heads, head size, page size, tokens or max_q that it does not cover")
+    _refused(res, "at_grpo_tree_attention")
 
 
 @dataclass

@@ -343,11 +343,13 @@ PyObject* kv_append(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
 
 // prefix_attention(function's address, its workspace query's address, KVBatch, q, scale or None, causal, max_q, out, want_lse, data_error,
 //                  workspace or None, stream)
+// tree_attention: the same with ancestors in place of causal
 // Where the workspace is none or too small: (bytes,).
-PyObject* prefix_attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
+template <bool TREE>
+PyObject* attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   HANDLE_TH_ERRORS
   if (n_args != 12) {
-    PyErr_SetString(PyExc_TypeError, "prefix_attention takes 12 arguments");
+    PyErr_SetString(PyExc_TypeError, "prefix_attention and tree_attention take 12 arguments");
     return nullptr;
   }
   Cache kv;
@@ -355,13 +357,14 @@ PyObject* prefix_attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
   at_grpo_rows rq, ro;
   if (!cache_of(v[2], &kv) || !cache_rows(kv, v[3], nullptr, 0, &rq, &q)) Py_RETURN_NONE;
   const double scale = v[4] == Py_None ? 1.0 / std::sqrt(static_cast<double>(q->size(2))) : PyFloat_AsDouble(v[4]);
-  const int causal = PyObject_IsTrue(v[5]) == 1;
+  const int causal = !TREE && PyObject_IsTrue(v[5]) == 1;
   const long long max_q = PyLong_AsLongLong(v[6]);
   const bool want_lse = PyObject_IsTrue(v[8]) == 1;
   void* stream = PyLong_AsVoidPtr(v[11]);
   if (PyErr_Occurred()) return nullptr;
-  const void* word;
+  const void *word, *ancestors = nullptr;
   if (max_q < 1 || max_q > 0x7fffffff || !vector(v[9], 1, at::kInt, q->device(), &word)) Py_RETURN_NONE;
+  if (TREE && (v[5] == Py_None || !vector(v[5], q->size(0), at::kLong, q->device(), &ancestors))) Py_RETURN_NONE;
   const int32_t n = static_cast<int32_t>(q->size(0)), heads = static_cast<int32_t>(q->size(1)), most = static_cast<int32_t>(max_q);
   const size_t bytes = reinterpret_cast<decltype(&at_grpo_prefix_attention_workspace_bytes)>(PyLong_AsVoidPtr(v[1]))(&kv.c, n, heads, most);
   if (bytes == 0) Py_RETURN_NONE;
@@ -373,9 +376,14 @@ PyObject* prefix_attention(PyObject*, PyObject* const* v, Py_ssize_t n_args) {
     const WithoutPythonLock others_run;
     lse = at::empty({q->size(0), q->size(1)}, q->options().dtype(at::kFloat));
   }
-  const int status = reinterpret_cast<decltype(&at_grpo_prefix_attention)>(PyLong_AsVoidPtr(v[0]))(
-      &kv.c, n, heads, &rq, static_cast<float>(scale), causal, most, &ro, want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr,
-      static_cast<int32_t*>(const_cast<void*>(word)), ws->data_ptr(), static_cast<size_t>(ws->numel()), stream);
+  float* const sums = want_lse ? static_cast<float*>(lse.data_ptr()) : nullptr;
+  int32_t* const flags = static_cast<int32_t*>(const_cast<void*>(word));
+  void* const fn = PyLong_AsVoidPtr(v[0]);
+  const size_t held = static_cast<size_t>(ws->numel());
+  const int status = TREE ? reinterpret_cast<decltype(&at_grpo_tree_attention)>(fn)(&kv.c, n, heads, &rq, static_cast<const uint64_t*>(ancestors),
+                                                                                  static_cast<float>(scale), most, &ro, sums, flags, ws->data_ptr(), held, stream)
+                          : reinterpret_cast<decltype(&at_grpo_prefix_attention)>(fn)(&kv.c, n, heads, &rq, static_cast<float>(scale), causal, most, &ro, sums,
+                                                                                    flags, ws->data_ptr(), held, stream);
   if (status != AT_GRPO_OK) return PyLong_FromLong(status);
   THPObjectPtr dict(PyDict_New());
   if (!dict || !put(dict.get(), g_out, std::move(out)) || !put(dict.get(), g_lse, std::move(lse))) return nullptr;
@@ -637,7 +645,8 @@ PyMethodDef g_methods[] = {{"group_advantage", fast(group_advantage), METH_FASTC
                            {"qk_norm_rope_bwd", fast(qk_norm_rope_bwd), METH_FASTCALL, nullptr},
                            {"check_kv", check_kv, METH_O, nullptr},
                            {"kv_append", fast(kv_append), METH_FASTCALL, nullptr},
-                           {"prefix_attention", fast(prefix_attention), METH_FASTCALL, nullptr},
+                           {"prefix_attention", fast(attention<false>), METH_FASTCALL, nullptr},
+                           {"tree_attention", fast(attention<true>), METH_FASTCALL, nullptr},
                            {"kv_plan", fast(kv_plan), METH_FASTCALL, nullptr},
                            {"logit_rules", fast(logit_rules), METH_FASTCALL, nullptr},
                            {nullptr, nullptr, 0, nullptr}};

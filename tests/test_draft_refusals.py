@@ -98,3 +98,26 @@ def test_rules_of_no_rows():
 def test_struct_layout(tmp_path, monkeypatch, compiler, std):
     monkeypatch.setattr(test_rollout_abi, "MIRRORS", {"at_grpo_page_pool": api._PagePool, "at_grpo_sampling_rules": api._SamplingRules})
     test_rollout_abi.test_struct_layout(tmp_path, compiler, std)
+
+
+def test_tree_attention():
+    lib = api.load_library()
+    kv = dict(dtype=1, Hk=2, D=64, page_size=16, n_pages=100, n_seq=4, max_pages=8, n_group=1, max_prefix_pages=9)
+    ptr = {n: next(AT) for n in ("k", "v", "pages", "length", "cu_q", "group_seq", "prefix_len", "prefix_pages")}
+
+    def call(ancestors=None, Hq=4, n_tok=9, scale=0.1, max_q=8, bytes=1 << 40, **over):
+        sizes, ptrs = dict(kv, **{k: x for k, x in over.items() if k in kv}), dict(ptr, **{k: x for k, x in over.items() if k in ptr})
+        c = api._KV(*sizes.values(), *ptrs.values())
+        q, out = api._Rows(next(AT), 256, 64), api._Rows(next(AT), 256, 64)
+        if over.get("in_place"):
+            out = q
+        return lib.at_grpo_tree_attention(api.C.byref(c), n_tok, Hq, api.C.byref(q), ancestors, scale, max_q, api.C.byref(out), None, None, next(AT), bytes, None)
+
+    words = next(AT)
+    assert call(None) == EINVAL and call(words, n_tok=0) == 0 and call(words, in_place=True) == EINVAL and call(words, bytes=100) == EWORKSPACE
+    for over, status in ((dict(Hq=3), EINVAL), (dict(scale=0.0), EINVAL), (dict(max_q=0), EINVAL), (dict(k=None), EINVAL), (dict(length=None), EINVAL),
+                         (dict(cu_q=None), EINVAL), (dict(prefix_pages=None), EINVAL), (dict(D=12), EUNSUPPORTED), (dict(D=264), EUNSUPPORTED), (dict(dtype=2), EUNSUPPORTED),
+                         (dict(page_size=20), EUNSUPPORTED), (dict(n_tok=2 ** 31 - 1), EUNSUPPORTED)):
+        assert call(words, **over) == status, over
+    c = api._KV(*kv.values(), *[None] * 8)
+    assert lib.at_grpo_tree_attention_workspace_bytes(api.C.byref(c), 9, 4, 8) > 0 and lib.at_grpo_tree_attention_workspace_bytes(api.C.byref(c), 9, 3, 8) == 0
