@@ -2,10 +2,13 @@
 // its best token on the way (gfx950).
 //
 // Memory bounds it: a row is read once and written once, 2 V elements, and everything else is lists that are short beside it.  A workgroup
-// has 8192 tokens of a row.  Which of them occur in front of the row's token it finds out by itself: it goes through the lists (from the
-// cache, where the row's other workgroups read them too) and counts those of its tokens in LDS, while its logits are on their way.  Then
-// every logit is in a register, the rules are applied there, and the row's largest and its sum of exponentials come from the same
-// registers.  A second kernel joins the parts of a row.
+// has chunks of 8192 tokens of a row.  Which of these occur in front of the row's token it finds out by itself: it goes through the lists (whose
+// first entries its threads keep) and counts those of its tokens in LDS, while the chunk's logits and mask bits are on their way.  Then eight
+// logits at a time are in a lane's registers; the rules are applied there, and the row's largest and its sum of exponentials come from the
+// same registers.  A second kernel joins the parts of a row.
+//
+// Rows of 151936 in bf16: 1339 under masks alone, read and not written, 86 us (4.7 TB/s, a large copy 4.9); 682 rewritten without lists 87 us
+// (5.0 TB/s), with prompts, own tokens and drafted paths 103, with biases too 114: the lists' atomics, barriers and branches.
 #include "kv_common.hpp"
 
 #include <math.h>
@@ -16,8 +19,11 @@ namespace atg {
 
 namespace {
 
-constexpr int kRuleThreads = 256, kRuleSteps = 4, kStepTokens = 8 * kRuleThreads, kRuleChunk = kRuleSteps * kStepTokens;
-constexpr uint32_t kInPrompt = 0x80000000u;      // of a token's word in LDS; the rest counts it behind the prompt
+constexpr int kRuleThreads = 256, kRuleSteps = 4, kStepTokens = 8 * kRuleThreads, kRuleChunk = kRuleSteps * kStepTokens, kMostChunks = 8;
+// A token's word in LDS: whether the prompt has it, the number of its bias among the sequence's, from 1 on, or 0, and how often it occurs behind
+// the prompt.  Where lists may be longer than that counts the biases go through LDS first, and the count has all other bits.
+constexpr uint32_t kInPrompt = 0x80000000u;
+constexpr int kBiasShift = 16, kMostBiases = 0x7fff, kMostTokens = 0xffff, kNearBiases = 512;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 // Of a workgroup's tokens: the largest x, where it is first, and sum exp((x - reference(top)) to_out).
@@ -36,14 +42,14 @@ __device__ __forceinline__ float moved(float sum, float of, float to, float to_l
 
 struct RuleArgs {
   at_grpo_sampling_rules r;
-  int n_rows, chunks;
+  int n_rows, chunks, splits, per;      // workgroups of a row, chunks that each of them goes through
   const void* logits;
   int64_t logits_stride;
   void* out;
   int64_t out_stride;
   float* lse;
   int32_t *best, *data_error;
-  RulePart* parts;      // workspace: [n_rows][chunks], or null where neither lse nor best is asked for
+  RulePart* parts;      // workspace: [n_rows][splits], or null where neither lse nor best is asked for
 };
 
 // What belongs to a row.
@@ -136,7 +142,6 @@ template <>
 struct Eight<bf16_t> {
   Words4 w;
   __device__ __forceinline__ void load(const bf16_t* p) { w = *reinterpret_cast<const Words4At2*>(p); }
-  __device__ __forceinline__ void set(int j, bf16_t x) { w[j >> 1] = j & 1 ? (w[j >> 1] & 0xffffu) | static_cast<uint32_t>(x.bits) << 16 : x.bits; }
   __device__ __forceinline__ float at(int j) const { return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16); }
 };
 template <>
@@ -146,7 +151,6 @@ struct Eight<float> {
     w[0] = reinterpret_cast<const Words4At4*>(p)[0];
     w[1] = reinterpret_cast<const Words4At4*>(p)[1];
   }
-  __device__ __forceinline__ void set(int j, float x) { w[j >> 2][j & 3] = __float_as_uint(x); }
   __device__ __forceinline__ float at(int j) const { return __uint_as_float(w[j >> 2][j & 3]); }
 };
 __device__ __forceinline__ void store_eight(bf16_t* p, const float* y) {
@@ -158,22 +162,39 @@ __device__ __forceinline__ void store_eight(float* p, const float* y) {
     reinterpret_cast<Words4At4*>(p)[i] = Words4{__float_as_uint(y[4 * i]), __float_as_uint(y[4 * i + 1]), __float_as_uint(y[4 * i + 2]), __float_as_uint(y[4 * i + 3])};
 }
 
-// f(token - base, i) for the entries i of a list that name one of a workgroup's tokens.
-template <typename F>
-__device__ __forceinline__ void go_through(const int32_t* list, int n, int base, int count, int V, bool look, int* error, F f) {
-  for (int i0 = threadIdx.x; i0 < n; i0 += 4 * kRuleThreads) {
-    int token[4];
+// The entries of a list, the first K of each thread in registers.
+template <int K>
+struct List {
+  const int32_t* from;
+  int n, held[K];
+  __device__ __forceinline__ List(const int32_t* list, int count) : from(list), n(count) {
 #pragma unroll
-    for (int k = 0; k < 4; ++k) token[k] = i0 + k * kRuleThreads < n ? list[i0 + k * kRuleThreads] : base - 1;
+    for (int k = 0; k < K; ++k) held[k] = static_cast<int>(threadIdx.x) + k * kRuleThreads < n ? list[threadIdx.x + k * kRuleThreads] : -1;
+  }
+  // f(token - base, i) for the entries i that name one of `count` tokens from base on.
+  template <typename F>
+  __device__ __forceinline__ void each(int base, int count, int V, bool look, int* error, F f) const {
+    auto one = [&](int token, int i) {
+      if (static_cast<unsigned>(token - base) < static_cast<unsigned>(count)) f(token - base, i);
+      if (look && i < n && static_cast<unsigned>(token) >= static_cast<unsigned>(V)) *error |= AT_GRPO_DATA_TOKEN_RANGE;
+    };
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int at = token[k] - base;
-      if (static_cast<unsigned>(at) < static_cast<unsigned>(count)) f(at, i0 + k * kRuleThreads);
-      if (look && i0 + k * kRuleThreads < n && static_cast<unsigned>(token[k]) >= static_cast<unsigned>(V)) *error |= AT_GRPO_DATA_TOKEN_RANGE;
+    for (int k = 0; k < K; ++k) one(held[k], threadIdx.x + k * kRuleThreads);
+    for (int i0 = threadIdx.x + K * kRuleThreads; i0 < n; i0 += 4 * kRuleThreads) {
+      int token[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) token[k] = i0 + k * kRuleThreads < n ? from[i0 + k * kRuleThreads] : -1;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) one(token[k], i0 + k * kRuleThreads);
     }
   }
-}
+};
 
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float x;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+  return x;
+}
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
@@ -190,143 +211,213 @@ __device__ __forceinline__ int wave_min(int x) {
   return x;
 }
 
-// LISTS: there are lists to go through; BIAS: biases among them.
-template <typename T, typename O, bool LISTS, bool BIAS>
-__global__ __launch_bounds__(kRuleThreads) void k_rules(RuleArgs a) {
+// x / d, rounded once, for x of any kind: the product with the reciprocal `one_over` (itself rounded once), corrected by what is left over.
+__device__ __forceinline__ float divided(float x, float d, float one_over) {
+  const float q = x * one_over;
+  return __builtin_amdgcn_div_fixupf(__builtin_fmaf(__builtin_fmaf(-q, d, x), one_over, q), d, x);
+}
+
+// What lists there are to go through: none, those of tokens, of biases too, of any length.
+enum Lists { NONE, TOKENS, BIASES, LONG };
+
+template <typename T, typename O, int LISTS>
+__global__ __launch_bounds__(kRuleThreads, LISTS == LONG ? 2 : 4) void k_rules(RuleArgs a) {
 #pragma clang fp contract(off)
-  __shared__ __attribute__((aligned(16))) uint32_t words[LISTS ? kRuleChunk : 4];
+  __shared__ __attribute__((aligned(16))) uint32_t words[LISTS != NONE ? kRuleChunk : 4];
+  __shared__ float bias_near[LISTS == BIASES ? kNearBiases : 1];      // values of the first biases
   __shared__ float tops[kRuleThreads / 64], sums[kRuleThreads / 64];
   __shared__ int firsts[kRuleThreads / 64];
   const uint32_t block = flat_block();
-  const int row = static_cast<int>(block / static_cast<uint32_t>(a.chunks)), chunk = static_cast<int>(block - static_cast<uint32_t>(row) * a.chunks);
+  const int row = static_cast<int>(block / static_cast<uint32_t>(a.splits)), split = static_cast<int>(block - static_cast<uint32_t>(row) * a.splits);
   if (row >= a.n_rows) return;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.r.V, base = chunk * kRuleChunk, n = min(kRuleChunk, V - base);
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, V = a.r.V, chunk0 = split * a.per, chunk1 = min(a.chunks, chunk0 + a.per);
+  const T* const logits = static_cast<const T*>(a.logits) + row * a.logits_stride;
+  // The whole steps of a chunk, 2048 tokens each, are asked for ahead; what is left of a row behind them is read token by token.
   Eight<T> raw[kRuleSteps];
-  const T* from = static_cast<const T*>(a.logits) + row * a.logits_stride + base + 8 * tid;
+  auto whole_steps = [&](int chunk) { return chunk < chunk1 ? min(kRuleSteps, (V - chunk * kRuleChunk) / kStepTokens) : 0; };
+  int bits[kRuleSteps];      // of the row's mask: 8 tokens from a multiple of 8 are a byte
+  auto load = [&](int chunk, int i) { raw[i].load(logits + chunk * kRuleChunk + i * kStepTokens + 8 * tid); };
+  const int whole0 = whole_steps(chunk0);
 #pragma unroll
-  for (int i = 0; i < kRuleSteps; ++i) {
-    if ((i + 1) * kStepTokens <= n) {
-      raw[i].load(from + i * kStepTokens);
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) raw[i].set(j, i * kStepTokens + 8 * tid + j < n ? from[i * kStepTokens + j] : T{});
-    }
-  }
+  for (int i = 0; i < kRuleSteps; ++i)
+    if (i < whole0) load(chunk0, i);
   int error = 0;
   const RowRules rules = rules_of(a, row, &error);
-  const bool look = chunk == 0;
-  auto clear = [&] {
-#pragma unroll
-    for (int i = 0; i < kRuleChunk / (4 * kRuleThreads); ++i) *reinterpret_cast<uint4*>(words + 4 * (tid + i * kRuleThreads)) = make_uint4(0, 0, 0, 0);
-  };
-  auto own_words = [&](int i, uint32_t (&w)[8]) {
-    const uint4 lo = *reinterpret_cast<const uint4*>(words + i * kStepTokens + 8 * tid), hi = *reinterpret_cast<const uint4*>(words + i * kStepTokens + 8 * tid + 4);
+  const List<LISTS != NONE ? 4 : 1> prompt(rules.prompt, LISTS != NONE ? rules.n_prompt : 0), own(rules.own, LISTS != NONE ? rules.n_own : 0);
+  const List<LISTS >= BIASES ? 2 : 1> biased(rules.bias_token, LISTS >= BIASES ? rules.n_bias : 0);
+  if constexpr (LISTS == BIASES)
+    for (int i = tid; i < min(rules.n_bias, kNearBiases); i += kRuleThreads) bias_near[i] = rules.bias[i];
+  const bool on_path = LISTS != NONE && tid < rules.n_drafted && (rules.path >> (tid & 63) & 1);
+  const int drafted = on_path ? rules.drafted[tid] : -1;
+  // A thread's own words of a step, which it leaves as 0 for the next chunk.  Those of its first four tokens lie in one half of the step's, those of
+  // the others in the other, so that neighbours' lie side by side and no bank is met twice.
+  auto take_words = [&](int of, uint32_t (&w)[8]) {      // of: the first one's place in the chunk
+    uint4* const at = reinterpret_cast<uint4*>(words + (of - 4 * tid));
+    const uint4 lo = at[0], hi = at[kStepTokens / 8];
+    at[0] = at[kStepTokens / 8] = make_uint4(0, 0, 0, 0);
     w[0] = lo.x, w[1] = lo.y, w[2] = lo.z, w[3] = lo.w, w[4] = hi.x, w[5] = hi.y, w[6] = hi.z, w[7] = hi.w;
   };
-  float bias[BIAS ? kRuleSteps : 1][8];
-  if constexpr (BIAS) {      // of several entries for a token the last: the largest number
-    clear();
-    __syncthreads();
-    go_through(rules.bias_token, rules.n_bias, base, n, V, look, &error, [&](int at, int i) { atomicMax(words + at, static_cast<uint32_t>(i) + 1); });
-    __syncthreads();
+  auto word_of = [&](int at) {
+    const int in = at & (kStepTokens - 1);
+    return words + (at - in) + (in >> 2 & 1) * (kStepTokens / 2) + (in >> 3 << 2) + (in & 3);
+  };
+  if constexpr (LISTS != NONE) {
 #pragma unroll
     for (int i = 0; i < kRuleSteps; ++i) {
-      uint32_t w[8];
-      own_words(i, w);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) bias[i][j] = w[j] ? rules.bias[w[j] - 1] : 0.f;
+      uint32_t unused[8];
+      take_words(i * kStepTokens + 8 * tid, unused);
     }
-    __syncthreads();
   }
-  if constexpr (LISTS) {
-    clear();
-    __syncthreads();
-    go_through(rules.prompt, rules.n_prompt, base, n, V, look, &error, [&](int at, int) { atomicOr(words + at, kInPrompt); });
-    go_through(rules.own, rules.n_own, base, n, V, look, &error, [&](int at, int) { atomicAdd(words + at, 1u); });
-    if (tid < rules.n_drafted && (rules.path >> tid & 1)) {
-      const int token = rules.drafted[tid], at = token - base;
-      if (static_cast<unsigned>(at) < static_cast<unsigned>(n)) atomicAdd(words + at, 1u);
-      if (look && static_cast<unsigned>(token) >= static_cast<unsigned>(V)) error |= AT_GRPO_DATA_TOKEN_RANGE;
-    }
-    __syncthreads();
-  }
-  if (look) raise_data_error(a.data_error, error);
-
-  float z[kRuleSteps][8];
-  float top = -INFINITY;
+  auto load_bits = [&](int chunk, int i) { bits[i] = rules.allowed ? rules.allowed[(chunk * kRuleChunk + i * kStepTokens) / 8 + tid] : 0xff; };
 #pragma unroll
-  for (int i = 0; i < kRuleSteps; ++i) {
-    const int at = i * kStepTokens + 8 * tid;
-    uint32_t bits = 0xff;
-    if (rules.allowed) bits = at < n ? rules.allowed[(base + at) >> 3] : 0;      // 8 tokens from a multiple of 8: a byte
-    if ((i + 1) * kStepTokens > n) bits &= at + 8 <= n ? 0xffu : at < n ? (1u << (n - at)) - 1 : 0u;      // behind the last token: as if masked
-#pragma unroll
-    for (int j = 0; j < 8; ++j) z[i][j] = raw[i].at(j);
-    if constexpr (LISTS) {
+  for (int i = 0; i < kRuleSteps; ++i)
+    if (i < whole0) load_bits(chunk0, i);
+  const float one_over = 1.f / rules.repetition, to_log2 = rules.to_out * kLog2e;
+  float top = -INFINITY, scaled = 0.f, sum = 0.f;      // of the wavefront's tokens, its multiple as exponents have it, and of this thread's
+  int first = 0x7fffffff;
+  // The rules on eight tokens from `token` on, of which the row has `have`; `at` is their place in the chunk.
+  auto step = [&](float (&z)[8], const float* bias, int bits, int at, int token, int have, auto is_whole) {
+    constexpr bool whole = decltype(is_whole)::value;
+    if constexpr (LISTS != NONE) {
       uint32_t w[8];
-      own_words(i, w);
-      if ((w[0] | w[1] | w[2] | w[3]) | (w[4] | w[5] | w[6] | w[7])) {
+      take_words(at, w);
+      if (__any((w[0] | w[1] | w[2] | w[3]) | (w[4] | w[5] | w[6] | w[7]))) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const uint32_t count = w[j] & ~kInPrompt;
-          const float x = z[i][j], y = w[j] ? (x > 0.f ? x / rules.repetition : x * rules.repetition) : x;
-          z[i][j] = count ? (y - rules.frequency * static_cast<float>(count)) - rules.presence : y;
-        }
+        for (int j = 0; j < 8; ++j)
+          if (w[j]) {
+            float x = z[j];
+            const uint32_t count = LISTS == BIASES ? w[j] & kMostTokens : w[j] & ~kInPrompt;
+            if (LISTS != BIASES || count || w[j] >= kInPrompt) x = x > 0.f ? divided(x, rules.repetition, one_over) : x * rules.repetition;
+            if (count) x = (x - rules.frequency * static_cast<float>(count)) - rules.presence;
+            if constexpr (LISTS == BIASES) {
+              const int entry = w[j] >> kBiasShift & kMostBiases;
+              if (entry) x += entry <= kNearBiases ? bias_near[entry - 1] : rules.bias[entry - 1];
+            }
+            z[j] = x;
+          }
       }
     }
+    if constexpr (LISTS == LONG) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      if constexpr (BIAS) z[i][j] += bias[i][j];
-      z[i][j] = bits >> j & 1 ? z[i][j] : -INFINITY;
-      top = fmaxf(top, z[i][j]);
+      for (int j = 0; j < 8; ++j) z[j] += bias[j];
     }
-  }
-  if (a.out) {
-    O* to = static_cast<O*>(a.out) + row * a.out_stride + base + 8 * tid;
+    if (rules.allowed || !whole) {
+      if (!whole) bits &= have >= 8 ? 0xff : have > 0 ? (1 << have) - 1 : 0;           // behind the last token: as if masked
 #pragma unroll
-    for (int i = 0; i < kRuleSteps; ++i) {
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t on = static_cast<uint32_t>(bits << (31 - j) >> 31);
+        z[j] = __uint_as_float((__float_as_uint(z[j]) & on) | (0xff800000u & ~on));
+      }
+    }
+    if (a.out) {
+      O* const to = static_cast<O*>(a.out) + row * a.out_stride + token;
       float y[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) y[j] = z[i][j] * rules.to_out;
-      if ((i + 1) * kStepTokens <= n) {
-        store_eight(to + i * kStepTokens, y);
+      for (int j = 0; j < 8; ++j) y[j] = z[j] * rules.to_out;
+      if constexpr (whole) {
+        store_eight(to, y);
       } else {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (i * kStepTokens + 8 * tid + j < n) to[i * kStepTokens + j] = from_f32<O>(y[j]);
+          if (j < have) to[j] = from_f32<O>(y[j]);
       }
     }
-  }
-  if (!a.parts) return;
-  top = wave_max(top);
-  if (lane == 0) tops[wave] = top;
-  const float to_log2 = rules.to_out * kLog2e, ref = reference(top);
-  if (a.lse) {
-    float sum = 0.f;
+    if (!a.parts) return;
+    // Four instructions; those that fmaxf makes of signalling NaN bring it to fifteen.  Here one may come out as NaN, and is looked at as a larger one is.
+    if (__any(!(max3(max3(max3(z[0], z[1], z[2]), z[3], z[4]), z[5], max3(z[6], z[7], z[7])) <= top))) {      // seldom, once a wavefront has seen some of its tokens
+      const float now = wave_max(fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7]))));
+      if (now > top) {
+        sum = moved(sum, top, now, to_log2);
+        top = now;
+        scaled = reference(top) * to_log2;
+        first = 0x7fffffff;
+#pragma unroll
+        for (int j = 7; j >= 0; --j) first = z[j] == now ? token + j : first;
+      }
+    }
+    if (a.lse) {
+      if (fabsf(scaled) < 1e30f) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], to_log2, -scaled));
+      } else {      // numbers near the ends of the range: their multiples may be infinite, their differences not
+        const float ref = reference(top);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f((z[j] - ref) * to_log2);
+      }
+    }
+  };
+  for (int chunk = chunk0; chunk < chunk1; ++chunk) {
+    const int base = chunk * kRuleChunk, n = min(kRuleChunk, V - base);
+    const bool look = chunk == 0;
+    float bias[LISTS == LONG ? kRuleSteps : 1][8];
+    if constexpr (LISTS != NONE) __syncthreads();
+    if constexpr (LISTS == LONG) {      // of several entries for a token the last: the largest number
+      biased.each(base, n, V, look, &error, [&](int at, int i) { atomicMax(word_of(at), static_cast<uint32_t>(i) + 1); });
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < kRuleSteps; ++i) {
+        uint32_t w[8];
+        take_words(i * kStepTokens + 8 * tid, w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) bias[i][j] = w[j] ? rules.bias[w[j] - 1] : 0.f;
+      }
+      __syncthreads();
+    }
+    if constexpr (LISTS == BIASES) {
+      biased.each(base, n, V, look, &error, [&](int at, int i) { atomicMax(word_of(at), static_cast<uint32_t>(i + 1) << kBiasShift); });
+      __syncthreads();
+    }
+    if constexpr (LISTS != NONE) {
+      prompt.each(base, n, V, look, &error, [&](int at, int) { atomicOr(word_of(at), kInPrompt); });
+      own.each(base, n, V, look, &error, [&](int at, int) { atomicAdd(word_of(at), 1u); });
+      if (static_cast<unsigned>(drafted - base) < static_cast<unsigned>(n)) atomicAdd(word_of(drafted - base), 1u);
+      if (look && on_path && static_cast<unsigned>(drafted) >= static_cast<unsigned>(V)) error |= AT_GRPO_DATA_TOKEN_RANGE;
+      __syncthreads();
+    }
+
+    const int whole = whole_steps(chunk), whole_next = whole_steps(chunk + 1);
 #pragma unroll
     for (int i = 0; i < kRuleSteps; ++i)
+      if (i < whole) {
+        float z[8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f((z[i][j] - ref) * to_log2);
-    sum = wave_sum_all(sum);
-    if (lane == 0) sums[wave] = sum;
+        for (int j = 0; j < 8; ++j) z[j] = raw[i].at(j);
+        const int allowed = bits[i];
+        if (i < whole_next) {
+          load(chunk + 1, i);
+          load_bits(chunk + 1, i);
+        }
+        const int at = i * kStepTokens + 8 * tid;
+        step(z, bias[LISTS == LONG ? i : 0], allowed, at, base + at, 8, std::true_type{});
+      }
+    if (whole < kRuleSteps && whole * kStepTokens < n) {      // the row's last tokens
+      const int at = whole * kStepTokens + 8 * tid, token = base + at, have = V - token;
+      float z[8], b[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        z[j] = j < have ? to_f32(logits[token + j]) : 0.f;
+        if constexpr (LISTS == LONG) b[j] = whole == 0 ? bias[0][j] : whole == 1 ? bias[1][j] : whole == 2 ? bias[2][j] : bias[3][j];
+      }
+      step(z, b, rules.allowed && have > 0 ? rules.allowed[token >> 3] : 0xff, at, token, have, std::false_type{});
+    }
   }
-  __syncthreads();
-  const float all = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-  int first = 0x7fffffff;
-  if (a.best && top == all && all > -INFINITY) {
-#pragma unroll
-    for (int i = kRuleSteps - 1; i >= 0; --i)
-#pragma unroll
-      for (int j = 7; j >= 0; --j) first = z[i][j] == all ? base + i * kStepTokens + 8 * tid + j : first;
-    first = wave_min(first);
+  if (chunk0 == 0) raise_data_error(a.data_error, error);
+  if (!a.parts) return;
+  sum = wave_sum_all(sum);
+  first = wave_min(first);
+  if (lane == 0) {
+    tops[wave] = top;
+    sums[wave] = sum;
+    firsts[wave] = first;
   }
-  if (lane == 0) firsts[wave] = first;
   __syncthreads();
   if (tid == 0) {
-    RulePart p{all, 0.f, rules.to_out, min(min(firsts[0], firsts[1]), min(firsts[2], firsts[3]))};
-    if (a.lse)
-      for (int w = 0; w < kRuleThreads / 64; ++w) p.sum += moved(sums[w], tops[w], all, to_log2);
-    a.parts[static_cast<int64_t>(row) * a.chunks + chunk] = p;
+    RulePart p{fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), 0.f, rules.to_out, 0x7fffffff};
+    for (int w = 0; w < kRuleThreads / 64; ++w) {
+      p.sum += moved(sums[w], tops[w], p.top, to_log2);
+      if (tops[w] == p.top) p.best = min(p.best, firsts[w]);
+    }
+    a.parts[static_cast<int64_t>(row) * a.splits + split] = p;
   }
 }
 
@@ -335,14 +426,14 @@ __global__ __launch_bounds__(256) void k_rules_join(RuleArgs a) {
   const int64_t row = static_cast<int64_t>(flat_block()) * 4 + (threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   if (row >= a.n_rows) return;
-  const RulePart* const parts = a.parts + row * a.chunks;
+  const RulePart* const parts = a.parts + row * a.splits;
   float top = -INFINITY;
-  for (int c = lane; c < a.chunks; c += 64) top = fmaxf(top, parts[c].top);
+  for (int c = lane; c < a.splits; c += 64) top = fmaxf(top, parts[c].top);
   top = wave_max(top);
   const float to_out = parts[0].to_out;
   float sum = 0.f;
   int first = 0x7fffffff;
-  for (int c = lane; c < a.chunks; c += 64) {
+  for (int c = lane; c < a.splits; c += 64) {
     const RulePart p = parts[c];
     sum += moved(p.sum, p.top, top, to_out * kLog2e);
     if (p.top == top) first = min(first, p.best);
@@ -370,9 +461,9 @@ size_t rule_parts(const at_grpo_sampling_rules* r, int32_t n_rows, void* workspa
 }
 
 template <typename T, typename O>
-void launch_rules(const RuleArgs& a, bool lists, bool bias, hipStream_t s) {
-  const dim3 grid = grid_of(static_cast<int64_t>(a.chunks) * a.n_rows);
-  const auto kernel = bias ? k_rules<T, O, true, true> : lists ? k_rules<T, O, true, false> : k_rules<T, O, false, false>;
+void launch_rules(const RuleArgs& a, int lists, hipStream_t s) {
+  const dim3 grid = grid_of(static_cast<int64_t>(a.splits) * a.n_rows);
+  const auto kernel = lists == LONG ? k_rules<T, O, LONG> : lists == BIASES ? k_rules<T, O, BIASES> : lists == TOKENS ? k_rules<T, O, TOKENS> : k_rules<T, O, NONE>;
   hipLaunchKernelGGL(kernel, grid, dim3(kRuleThreads), 0, s, a);
 }
 
@@ -404,20 +495,30 @@ extern "C" int at_grpo_logit_rules(const at_grpo_sampling_rules* rules, int32_t 
     const bool itself = out == logits && r.out_dtype == r.dtype && (n_rows == 1 || out_stride == logits_stride);
     if (!itself && in0 < out1 && out0 < in1) return AT_GRPO_EINVAL;
   }
-  RuleArgs a{r, n_rows, static_cast<int>(ceil_div(r.V, kRuleChunk)), logits, logits_stride, out, out_stride, lse, best, data_error, nullptr};
+  const int chunks = static_cast<int>(ceil_div(r.V, kRuleChunk));
+  RuleArgs a{r, n_rows, chunks, chunks, 1, logits, logits_stride, out, out_stride, lse, best, data_error, nullptr};
   const bool penalties = r.repetition || r.presence || r.frequency;
   if (!penalties) a.r.tokens = a.r.prompt = a.r.drafted = nullptr, a.r.ancestors = nullptr;
-  const bool lists = a.r.tokens || a.r.prompt || a.r.ancestors, bias = r.bias_cu && r.n_bias > 0;
+  const bool tokens = a.r.tokens || a.r.prompt || a.r.ancestors, bias = r.bias_cu && r.n_bias > 0;
   if (!bias) a.r.bias_cu = nullptr;
+  const int64_t most = (a.r.tokens ? r.max_tokens : 0) + (a.r.ancestors ? int64_t{64} : 0);
+  const int lists = !bias ? tokens ? TOKENS : NONE : r.n_bias <= kMostBiases && most <= kMostTokens ? BIASES : LONG;
+  // As many chunks a workgroup as leave two rounds of four workgroups a compute unit: what belongs to a row is looked up once for them and a chunk's
+  // logits come beside the work on the one in front.  682 rows of 151936 with all rules: a chunk each 146 us, three 124, five 119, seven 114,
+  // ten 160 (not two rounds); 1339 rows under masks alone: 103, 88, 89, 86.
+  const int64_t share = ceil_div(static_cast<int64_t>(chunks) * n_rows, int64_t{8} * device_cu_count());
+  a.per = static_cast<int>(share < kMostChunks ? share : kMostChunks);
+  a.splits = static_cast<int>(ceil_div(chunks, a.per));
+  a.per = static_cast<int>(ceil_div(chunks, a.splits));
   if (lse || best) {
     const size_t bytes = rule_parts(rules, n_rows, workspace, &a.parts);
     if (!workspace || (at(workspace) & 255) || workspace_bytes < bytes) return AT_GRPO_EWORKSPACE;
   }
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   ProfScope ps(PROF_RULES, s);
-  if (r.dtype == AT_GRPO_F32) launch_rules<float, float>(a, lists, bias, s);
-  else if (r.out_dtype == AT_GRPO_F32) launch_rules<bf16_t, float>(a, lists, bias, s);
-  else launch_rules<bf16_t, bf16_t>(a, lists, bias, s);
+  if (r.dtype == AT_GRPO_F32) launch_rules<float, float>(a, lists, s);
+  else if (r.out_dtype == AT_GRPO_F32) launch_rules<bf16_t, float>(a, lists, s);
+  else launch_rules<bf16_t, bf16_t>(a, lists, s);
   ATG_LAUNCH_CHECK();
   if (a.parts) {
     hipLaunchKernelGGL(k_rules_join, grid_of(ceil_div(n_rows, 4)), dim3(256), 0, s, a);

@@ -320,6 +320,16 @@ def test_counts_of_long_lists(gpu_device):
     r.tokens = [np.concatenate([np.full(70000, 8999), rs.integers(0, 9000, 30000)]), np.arange(9000)]
     r.frequency = np.array([0.001, 0.5])
     compare(apply(r, gpu_device), r.want())
+    # with biases, whose numbers and the counts then have a word each: lists of any length, and of the most that share one
+    r.bias = [[(8999, 1.0), (5, 2.0), (8999, -4.0)], [(v, float(v % 5)) for v in range(0, 9000, 7)]]
+    compare(apply(r, gpu_device), r.want())
+    for n in (65535, 65536):
+        r.tokens = [np.full(n, 8999), np.arange(100)]
+        compare(api.at_grpo_logit_rules(r.device(gpu_device, spare=0), to_dev(r.logits, r.dtype, gpu_device)), r.want(), what=f"{n}")
+    r.tokens = [np.arange(50), np.arange(100)]
+    for n in (32766, 32767, 32768):
+        r.bias = [[(v, float(v % 5)) for v in rs.integers(0, 9000, n - 1)], [(3, 2.0)]]
+        compare(apply(r, gpu_device), r.want(), what=f"{n} biases")
 
 
 @pytest.mark.gpu
@@ -432,6 +442,36 @@ def test_many_rows(gpu_device):
     assert torch.equal(o["best"].long(), logits.argmax(1))
     assert float((o["out"].double() - x).abs().max()) <= 4 * U32 * float(x.abs().max())
     assert float((o["lse"].double() - torch.logsumexp(x, 1)).abs().max()) <= U32 * (8 * float(x.abs().max()) + 60)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("biases", [0, 20])
+def test_several_chunks_a_workgroup(gpu_device, dtype, biases):
+    """Rows enough that a workgroup has more than one chunk of them: some of them against the oracle, all against the same rows few at a time."""
+    rs = np.random.default_rng(18)
+    V, new = 50003, [1 + i % 3 for i in range(1000)]
+    r = draw(rs, dtype, 300, 1000, new, (400, 600), biases=biases)      # lists of the first 300 tokens ..
+    n = sum(new)
+    spread = lambda v: int(v) * 165 % V                                 # .. spread over all
+    r.tokens, r.prompt = [[spread(v) for v in x] for x in r.tokens], [[spread(v) for v in x] for x in r.prompt]
+    r.drafted = np.array([spread(v) for v in r.drafted])
+    r.bias = None if r.bias is None else [[(spread(v), b) for v, b in x] for x in r.bias]
+    r.allowed = rs.random((3, V)) < 0.7
+    logits = torch.randn(n, V, generator=torch.Generator().manual_seed(3)).to(r.dtype)
+    r.logits = np.zeros((n, 1))
+    rules, dev_logits = r.device(gpu_device), logits.to(gpu_device)
+    o = api.at_grpo_logit_rules(rules, dev_logits)
+    start = r.start()
+    for s in (0, 1, 2, 399, 400, 998, 999):
+        rows = slice(start[s], start[s + 1])
+        part = Rows(logits[rows].double().numpy(), r.dtype, np.array(new[s:s + 1]), r.tokens[s:s + 1], (1,), r.prompt[:1] if s < 400 else r.prompt[1:], r.drafted[rows],
+                    r.parent[rows], r.repetition[s:s + 1], r.presence[s:s + 1], r.frequency[s:s + 1], r.temperature[s:s + 1],
+                    None if r.bias is None else r.bias[s:s + 1], r.allowed, r.mask_row[rows])
+        few = apply(part, gpu_device)
+        compare({k: o[k][rows] for k in ("out", "lse", "best")}, part.want(), what=f"sequence {s}")
+        assert torch.equal(few["out"], o["out"][rows]) and torch.equal(few["best"], o["best"][rows]), s
+        assert float((few["lse"] - o["lse"][rows]).abs().max()) <= 40 * U32 * float(few["lse"].abs().max().clamp(min=1))      # sums in another order
 
 
 @pytest.mark.gpu
