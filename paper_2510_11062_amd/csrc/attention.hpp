@@ -41,6 +41,9 @@ constexpr int kMostGroups = 1024;     // workgroups of a launch
 constexpr int kCachedUnits = 512;     // units whose sizes are kept in LDS
 // A run's beginning and end (queries, first loads, adding up) take about as long as 128 tokens and count as that.
 constexpr int kRunCost = 16, kMinShare = 16;
+// A tree's run has two tiles that not all see, and few rows to a tile: 6.8 us beside 2.2 to 2.5 for 64 tokens.  220 candidates with 16 drafted tokens
+// 275 us with 16, 265 with 32, 278 with 56; two prompts of 40000 tokens 249, 219 and 225.
+constexpr int kTreeRunCost = 32;
 constexpr int kPageSlots = 1024;     // page ids of a chunk in LDS at a time
 constexpr int kMaxRows = 128;        // rows of the largest tile
 constexpr int kWideRows = 128;       // of the tiles below that four wavefronts share by rows
@@ -66,7 +69,7 @@ struct Args {
   int n_tok, Hq, share;      // share: Hq / Hk
   Divisor by_share;
   int coarse, rise, quantum; // of the costs below; rise: by how much from one causal tile to the next
-  int causal;
+  int causal, run_cost;      // run_cost: of a run's beginning and end
   float scale;
   Rows q, out;
   float* lse;                // [n_tok, Hq] or null
@@ -141,7 +144,7 @@ struct Cost {
 __device__ __forceinline__ Cost cost_of(const Unit& u, bool steps, const Args& a, int rows) {
   if (u.len == 0 || u.ntok == 0) return Cost{0, 0};
   const bool rises = steps && a.rise && u.ntok <= u.len;
-  const int first = (((rises ? end_of(u, true, a, 0, rows) : u.len) + 7) >> 3 >> a.coarse) + kRunCost;
+  const int first = (((rises ? end_of(u, true, a, 0, rows) : u.len) + 7) >> 3 >> a.coarse) + a.run_cost;
   return Cost{(first + a.quantum - 1) & -a.quantum, rises ? a.rise : 0};
 }
 __device__ __forceinline__ int head_cost(const Unit& u, bool steps, const Args& a, int rows) {
@@ -365,6 +368,13 @@ __device__ __forceinline__ float element(const f32x4& v, int e) { return v[e]; }
 template <typename V>
 __device__ __forceinline__ float element(const V& v, int e) {
   return __uint_as_float(e & 1 ? dword(v, e >> 1) & 0xffff0000u : dword(v, e >> 1) << 16);
+}
+// The largest of three, NaN passed over as fmaxf does.  Of numbers that no signalling NaN is among, as a matrix instruction's are: fmaxf takes an
+// instruction more for each to make sure.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float x;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
+  return x;
 }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 // 0 in place of infinities and NaN
@@ -1061,6 +1071,7 @@ __device__ __forceinline__ int swizzle_v(int r) { return D >= 128 ? 2 * (r & 7) 
 
 template <int D, bool EXACT, bool TREE>
 __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv, Args a) {
+  constexpr int BUFFERS = 2, AHEAD = 1;
   constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES, VG = DT > 4 ? 2 : 1, DB = DT / VG;
   extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
   WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * TB);
@@ -1086,6 +1097,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 
   // Page ids of tokens page0 << page_shift .. in LDS: a unit's all, where they fit, for all its runs.
   int page0 = 0, staged = -1;
+  const int* const pages = lds.pages;
   bool holes = false;
   auto stage = [&](const int32_t* table, int first_token, int to) {
     page0 = first_token >> kv.page_shift;
@@ -1104,13 +1116,13 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
     holes = __syncthreads_or(missing);
   };
   // A tile of tokens t .. into a buffer; rows behind the last token are the last.
-  auto request = [&](int hk, int t, int to, int buffer) {
+  auto request = [&](int hk, int t, int to, int buffer, const int* pages, int page0) {
     const char* const kbase = static_cast<const char*>(kv.k) + ((static_cast<int64_t>(hk) * dim * 2) << kv.page_shift);
     const char* const vbase = static_cast<const char*>(kv.v) + ((static_cast<int64_t>(hk) * dim * 2) << kv.page_shift);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int row = (wave * NL + i) * LROWS + lane / PIECES, piece = lane & (PIECES - 1), token = min(t + row, to - 1);
-      const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(max(0, lds.pages[(token >> kv.page_shift) - page0]))) * page_bytes;
+      const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(max(0, pages[(token >> kv.page_shift) - page0]))) * page_bytes;
       const uint32_t in = static_cast<uint32_t>(token & in_page) * (2 * dim);
       const int of_k = piece ^ swizzle_k<D>(row), of_v = piece ^ swizzle_v<D>(row);
       if (EXACT || 8 * of_k < dim) direct_load_v(kbase + (at + (in + 16 * of_k)), lds0 + buffer * 2 * TB + i * 1024);
@@ -1124,25 +1136,23 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 #pragma unroll
     for (int c = 0; c < KC; ++c) q[c] = EXACT || 16 * c + 8 * g < dim ? *reinterpret_cast<const uint4*>(from + 16 * c) : make_uint4(0, 0, 0, 0);
   };
-  int buffer = 0;
-  bool requested = false;      // the run's first tile, by the run in front of it
+  int buffer = 0, requested = 0;      // of the run's first tiles, by the run in front of it
+  auto behind = [&](int tiles) { return buffer + tiles < BUFFERS ? buffer + tiles : buffer + tiles - BUFFERS; };
   TileRun w = tile_run(run, a);
   load_q(run.x, w);
   for (;;) {
     const Unit u = run.x;
     const bool steps = run.steps, own = run.own, fits = ((u.len - 1) >> kv.page_shift) < kPageSlots;
-    const int rows = u.ntok * a.share, r = w.r0 + 32 * wave + m, tq = min(r, rows - 1) / a.by_share, h = w.hk * a.share + min(r, rows - 1) - tq * a.share;
+    const int rows = u.ntok * a.share;
     const int first = u.len - u.ntok + 1, k1 = w.k1;      // a causal query sees the own tokens in front of `first + its number among the new tokens`
-    const int limit = steps ? min(k1, first + tq) : k1;
+    // What is needed at a run's end alone, or for few tiles, is computed there: the loop has no register left.
+    auto token_of = [&] { return min(w.r0 + 32 * wave + m, rows - 1) / a.by_share; };
+    const int limit = steps ? min(k1, first + token_of()) : k1;
     // a first row sees least: the tile's, and the wavefront's; in a tree, what is in front of it
     const bool tree = TREE && own;
     const int all_see = tree ? first - 1 : steps ? first + w.r0 / a.by_share : k1;
     const int wave_sees = tree ? first - 1 : steps ? first + min(w.r0 + 32 * wave, rows - 1) / a.by_share : k1;
-    uint64_t path = 0;
-    if constexpr (TREE) {
-      if (tree) path = a.ancestors[u.tok0 + tq];
-      if (tree && u.ntok > kMostTree) raise_data_error(a.data_error, AT_GRPO_DATA_TREE);
-    }
+    if (tree && u.ntok > kMostTree) raise_data_error(a.data_error, AT_GRPO_DATA_TREE);
     const bool direct = kv.n_group == 0 && run.from() == 0 && run.to() == run.cost, first_part = run.from() == 0;
     const int group = run.number;
     const int32_t* const table = own ? kv.pages + static_cast<int64_t>(u.row) * kv.max_pages : kv.prefix_pages + static_cast<int64_t>(u.row) * kv.max_prefix_pages;
@@ -1161,6 +1171,8 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
     float top = -INFINITY, ref = 0.f, sum = 0.f;
+    const bool idle = TREE && w.r0 + 32 * wave >= rows;      // no rows: it loads and waits with the others
+    int next_requested = 0;
 
     for (int from = w.k0; from < k1;) {
       int to = k1;
@@ -1169,22 +1181,32 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
         stage(table, from, to);
         staged = -1;
       }
-      if (!requested) request(w.hk, from, to, buffer);
-      requested = false;
-      for (int t = from; t < to; t += kWideTok, buffer ^= 1) {
+      const int tiles = (to - from + kWideTok - 1) / kWideTok;
+      int asked = requested;      // tiles of these, in buffers behind each other
+      for (; asked < min(AHEAD, tiles); ++asked) request(w.hk, from + asked * kWideTok, to, behind(asked), pages, page0);
+      requested = 0;
+      for (int t = from, number = 0; t < to; t += kWideTok, ++number, buffer = behind(1)) {
         asm volatile("" ::: "memory");
         wait_loads_but<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        // the next tile, or the next run's first: its buffer is free, since who has passed this barrier has read the tile in front
-        if (t + kWideTok < to) request(w.hk, t + kWideTok, to, buffer ^ 1);
-        else if (ahead && to == k1) request(next.hk, next.k0, next.k1, buffer ^ 1);
+        // the tile that comes AHEAD from here, or the next run's first: its buffer is free, since who has passed this barrier has read the tile in front
+        if (asked < tiles) {
+          request(w.hk, from + asked * kWideTok, to, behind(asked - number), pages, page0);
+          ++asked;
+        } else if (ahead && to == k1 && next.k0 + next_requested * kWideTok < next.k1) {
+          request(next.hk, next.k0 + next_requested * kWideTok, next.k1, behind(tiles - number + next_requested), pages, page0);
+          ++next_requested;
+        }
+        uint64_t path = 0;
+        if constexpr (TREE)
+          if (tree && t + kWideTok > all_see) path = a.ancestors[u.tok0 + token_of()];
         const char* const kt = smem + buffer * 2 * TB;
         char* const vt = smem + buffer * 2 * TB + TB;
         if (holes || t + kWideTok > to) {      // what stands for a token behind the last or of no page counts as 0
           for (int i = tid; i < kWideTok * PIECES; i += 256) {
             const int token = t + i / PIECES;
-            if (token >= to || lds.pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
+            if (token >= to || pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
           }
           lds_barrier();
           asm volatile("" ::: "memory");
@@ -1209,6 +1231,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[x & 1][i] = *reinterpret_cast<const bf16x8*>(kt + (read_k ^ ((2 * x + (i >> 1)) << 5)) + (i & 1) * 32 * 2 * D);
         };
+        if (!idle) {
         read_k_group(0);
 #pragma unroll
         for (int x = 0; x < KC / 2; ++x) {
@@ -1217,6 +1240,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 #pragma unroll
           for (int i = 0; i < 4; ++i)
             s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 1][i], __builtin_bit_cast(bf16x8, q[2 * x + (i >> 1)]), s[i & 1], 0, 0, 0);
+        }
         }
         if (more && t + kWideTok >= k1) load_q(run.x, next);      // the last scores of this run are on their way
         auto read_v_group = [&](int k) {      // 16 tokens, all blocks of 32 elements or half of them
@@ -1227,18 +1251,18 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
             f[k & 1][x] = __builtin_bit_cast(bf16x8, make_uint4(lo.x, lo.y, hi.x, hi.y));
           }
         };
-        read_v_group(0);
+        if (!idle) read_v_group(0);
         uint64_t sees = ~uint64_t{0};      // of the tile's tokens
         if constexpr (TREE)
-          if (tree) sees = tree_bits(path, t - (first - 1));
-        if (t + kWideTok > min(to, wave_sees) || holes) {
+          if (tree && t + kWideTok > all_see) sees = tree_bits(path, t - (first - 1));
+        if (!idle && (t + kWideTok > min(to, wave_sees) || holes)) {
 #pragma unroll
           for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int b = 0; b < 4; ++b) {      // four tokens that start at a multiple of four share a page
               const int t4 = t + 32 * y + 8 * b + 4 * g;
               int left = limit - t4;
-              if (holes) left = lds.pages[(min(t4, to - 1) >> kv.page_shift) - page0] < 0 ? 0 : left;
+              if (holes) left = pages[(min(t4, to - 1) >> kv.page_shift) - page0] < 0 ? 0 : left;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 bool on = i < left;
@@ -1247,11 +1271,12 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
               }
             }
         }
+        if (!idle) {
         float high = -INFINITY;
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) high = fmaxf(high, s[y][i]);
+          for (int i = 0; i < 16; i += 2) high = max3(high, s[y][i], s[y][i + 1]);
         high *= to_log2;
         if (__any(high > top + kSlack)) {
           high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
@@ -1262,6 +1287,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 #pragma unroll
           for (int x = 0; x < DT; ++x) acc[x] *= keep;
         }
+        }
         bool apart = false;
         if (partly) {
           lds_barrier();
@@ -1270,7 +1296,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
         }
         if (apart) {
 #pragma unroll 1
-          for (int i = 0; i < kWideTok * PIECES; ++i) {
+          for (int i = 0; i < (idle ? 0 : kWideTok * PIECES); ++i) {
             const int token = i / PIECES, c = i & (PIECES - 1);      // elements 8 c ..
             const uint4 x = *reinterpret_cast<const uint4*>(vt + (token * PIECES + (c ^ swizzle_v<D>(token))) * 16);
             if (!__any(not_finite<bf16_t>(largest_bits(0u, x)))) continue;
@@ -1288,8 +1314,9 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
           }
           lds_barrier();
           asm volatile("" ::: "memory");
-          read_v_group(0);
+          if (!idle) read_v_group(0);
         }
+        if (!idle) {
         uint4 w[2];
         auto weigh = [&](int ks) {
           float p[8];
@@ -1320,12 +1347,15 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
             }
           }
         }
+        }
       }
       from = to;
     }
 
     sum += __shfl_xor(sum, 32, 64);
+    const int r = w.r0 + 32 * wave + m;
     if (r < rows) {
+      const int tq = token_of(), h = w.hk * a.share + r - tq * a.share;
       const float f = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), x = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
       const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h;
       if (direct) {
@@ -1354,11 +1384,8 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
       }
     }
     if (!more) break;
-    requested = ahead;
-    if (w.k0 >= w.k1) {      // no tile, at which they were asked for
-      load_q(run.x, next);
-      requested = false;
-    }
+    requested = next_requested;
+    if (w.k0 >= w.k1) load_q(run.x, next);      // no tile, at which they were asked for
     w = next;
   }
 }
@@ -1894,7 +1921,7 @@ Scratch lay_out(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, WsAlloc& ws) {
 typedef void (*Kernel)(KvView, Args);
 struct Choice {
   Kernel kernel;
-  int rows, per_unit, lds;
+  int rows, per_unit, lds, run_cost = kRunCost;
 };
 
 // Rows of a prefix (or, without prefixes, of a sequence) on average, and of a sequence at most.
@@ -1916,7 +1943,8 @@ Choice choose_of(int rows_p, int rows_o, bool decode) {
   // of 256, messages of 40 tokens: tiles of 32 rows 394 us, of 16 284.
   constexpr int kMost = sizeof(T) == 2 || D == 256 ? 1 : 2;
   if constexpr (sizeof(T) == 2)
-    if (rows_o > 16) return {k_attend_wide<D, EXACT, TREE>, kWideRows, kWidePerUnit<D>, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds))};
+    if (rows_o > 16)
+      return {k_attend_wide<D, EXACT, TREE>, kWideRows, kWidePerUnit<D>, 4 * kWideTok * D * 2 + static_cast<int>(sizeof(WideLds)), TREE ? kTreeRunCost : kRunCost};
   return {k_attend<T, D, kMost, EXACT, TREE>, 16 * kMost, kPerUnit<D, kMost>, 0};
 }
 
@@ -1946,7 +1974,8 @@ int make_plan(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q, Pl
   const int64_t rows_p = kv->n_group ? ceil_div(all_rows, kv->n_group) : 0, rows_o = static_cast<int64_t>(max_q) * share;
   auto small = [](int64_t x) { return static_cast<int>(x < 1 << 20 ? x : 1 << 20); };
   const auto eights_of = [&](int64_t pages) { return static_cast<double>(pages) * kv->page_size / 8; };
-  const double fixed = 8 + kRunCost + kMinShare;
+  constexpr int run_cost = TREE ? kTreeRunCost : kRunCost;
+  const double fixed = 8 + run_cost + kMinShare;
   // Few rows a sequence, as many sequences as LDS has places for, their blocks counted in 26 bits and all costs in 30.
   const double decode_most = kv->Hk * ((all_rows / 16 + kv->n_group + kv->n_seq) * (eights_of(kv->max_prefix_pages) + fixed) + kv->n_seq * (eights_of(kv->max_pages) + fixed));
   out->decode = rows_o <= 16 && kv->n_seq <= kDecodeSeqs && static_cast<int64_t>(kv->n_seq + 1) * kv->max_pages * kv->page_size < 1 << 30 &&
@@ -1961,7 +1990,7 @@ int make_plan(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q, Pl
   }
   // Costs are added up in 32 bits.  Those of tokens are counted in larger blocks where need be; what each run costs beside them (kRunCost, and
   // up to 1 by rounding up) does not shrink.
-  const double runs = kv->Hk * static_cast<double>(tiles_p + tiles_o), beside = runs * (kRunCost + 1);
+  const double runs = kv->Hk * static_cast<double>(tiles_p + tiles_o), beside = runs * (run_cost + 1);
   double tokens = kv->Hk * (tiles_p * eights_of(kv->max_prefix_pages) + tiles_o * eights_of(kv->max_pages));
   if (beside > 1 << 30) return AT_GRPO_EUNSUPPORTED;
   out->most = tokens + runs * fixed;
@@ -2000,7 +2029,7 @@ int attend(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* 
   const Choice& k = plan.choice;
   const bool decode = plan.decode;
   const unsigned blocks = device_cu_count() * k.per_unit < kMostGroups ? device_cu_count() * k.per_unit : kMostGroups;
-  Args args{n_tok, Hq, share, divisor(share), plan.coarse, 0, 1, causal != 0, scale, rows_of(q), rows_of(out), lse, ancestors, data_error, scratch.units, scratch.part_lse, scratch.part_out};
+  Args args{n_tok, Hq, share, divisor(share), plan.coarse, 0, 1, causal != 0, k.run_cost, scale, rows_of(q), rows_of(out), lse, ancestors, data_error, scratch.units, scratch.part_lse, scratch.part_out};
   args.rise = k.rows / (8 * share) >> args.coarse;
   // Where there are workgroups enough, costs are whole shares, so that a run begins with a workgroup: one group of four by
   // k_attend 13.2 us, then 8.0.
