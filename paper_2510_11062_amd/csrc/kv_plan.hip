@@ -3,9 +3,15 @@
 // A sequence holds ceil(tokens / page) pages, so a step takes or gives the difference of two such counts, and where in the ring a
 // sequence's pages come from is a sum over the sequences in front of it, as is the place of its tokens among the new ones.  There is next
 // to nothing to read (20 bytes a sequence, 28 written a token): what a call takes is launches and loads one behind the other.
+//   k_plan             up to 2048 sequences, in one launch: every workgroup adds up all sequences by itself, keeps the sums in LDS, and writes its
+//                      share of the tokens, the sequences and the pages moved; a new page's id it reads where it stands in the ring.  Where an output is its
+//                      input itself it may only be written once every workgroup has read that: by a single workgroup then, while the tokens are few
+// Otherwise two:
 //   k_plan_sequences   a workgroup for 1024 sequences.  Each adds up all sequences, since every one has to know whether the pool suffices, and
 //                      those in front of its own; then pages are moved, a thread for each
 //   k_plan_tokens      a thread for each new token and for each sequence's length, which the first still reads
+// Four candidates 4.3 us (two launches 7.5 and 2.2), 1339 with 11000 drafted tokens 10.3 (10.5 and 6.2), 512 prompts of 374000 tokens 14.6 (11.5 and 5.6,
+// and the gap between them).
 #include "kv_common.hpp"
 
 namespace atg {
@@ -229,6 +235,179 @@ __global__ __launch_bounds__(256) void k_plan_tokens(PlanArgs a) {
   raise_data_error(a.data_error, error);
 }
 
+// ---- in one launch ------------------------------------------------------------------------------------
+constexpr int kPlanAlone = 8 * kPlanBlock;
+
+template <int BLOCK>
+struct PlanLds {
+  static constexpr int kSeqs = 2 * BLOCK;
+  int cu[kSeqs], take[kSeqs], give[kSeqs], group[kSeqs];      // in front of each sequence; the last group that begins there or in front
+  int keep[kSeqs], used[kSeqs];
+  int wave_take[BLOCK / 64], wave_give[BLOCK / 64], wave_group[BLOCK / 64], wave_wrong[BLOCK / 64], wave_falls[BLOCK / 64];
+  int64_t wave_add[BLOCK / 64];
+  int parents[BLOCK + kMostDrafted];
+};
+
+// BLOCK threads for 2 BLOCK sequences.
+template <int BLOCK>
+__global__ __launch_bounds__(BLOCK) void k_plan(PlanArgs a, int64_t per) {
+  __shared__ PlanLds<BLOCK> lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int first = a.state[0], count = a.state[1];
+  for (int s = tid; s < 2 * BLOCK; s += BLOCK) lds.group[s] = -1;
+  Step of[2];
+  int take = 0, give = 0, wrong = 0;
+  int64_t add = 0;
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {      // two sequences side by side a thread
+    const int s = 2 * tid + k;
+    of[k] = s < a.n_seq ? step_of(a, s) : Step{};
+    take += max(0, of[k].will - of[k].used);
+    give += max(0, of[k].used - of[k].will);
+    add += of[k].add;
+    wrong |= of[k].wrong;
+  }
+  __syncthreads();
+  // Where groups begin: of several that begin with a sequence the last, which is the one that has it.
+  int falls = 0, error = 0;
+  for (int g = tid; g < a.n_group; g += BLOCK) {
+    const int s0 = a.group_seq[g], s1 = a.group_seq[g + 1], n = a.prefix_len[g];
+    falls |= s0 < 0 || s1 < s0 || s1 > a.n_seq;
+    if (n < 0 || n > 1 << 30) error |= AT_GRPO_DATA_SEQLENS;
+    if (s0 >= 0 && s0 < a.n_seq) atomicMax(&lds.group[s0], g);
+  }
+  if (falls) error |= AT_GRPO_DATA_SEQLENS;
+  __syncthreads();
+  const int own_group[2] = {lds.group[2 * tid], max(lds.group[2 * tid], lds.group[2 * tid + 1])};
+  int take_up = take, give_up = give, group_up = own_group[1];      // up to this thread
+  int64_t add_up = add;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int t = __shfl_up(take_up, o, 64), g = __shfl_up(give_up, o, 64), m = __shfl_up(group_up, o, 64);
+    const int64_t d = __shfl_up(add_up, o, 64);
+    if (lane >= o) {
+      take_up += t;
+      give_up += g;
+      add_up += d;
+      group_up = max(group_up, m);
+    }
+  }
+  wrong = __any(wrong);
+  falls = __any(falls);
+  if (lane == 63) {
+    lds.wave_take[wave] = take_up;
+    lds.wave_give[wave] = give_up;
+    lds.wave_add[wave] = add_up;
+    lds.wave_group[wave] = group_up;
+    lds.wave_wrong[wave] = wrong;
+    lds.wave_falls[wave] = falls;
+  }
+  __syncthreads();
+  Sums all{};
+  int take0 = take_up - take, give0 = give_up - give, group0 = -1;
+  int64_t add0 = add_up - add;
+  falls = 0;
+#pragma unroll
+  for (int w = 0; w < BLOCK / 64; ++w) {
+    if (w < wave) {
+      take0 += lds.wave_take[w];
+      give0 += lds.wave_give[w];
+      add0 += lds.wave_add[w];
+      group0 = max(group0, lds.wave_group[w]);
+    }
+    all.taken += lds.wave_take[w];
+    all.given += lds.wave_give[w];
+    all.added += lds.wave_add[w];
+    all.wrong |= lds.wave_wrong[w];
+    falls |= lds.wave_falls[w];
+  }
+  // of the lanes in front in the wavefront
+  const int lane_before = __shfl_up(group_up, 1, 64);
+  if (lane > 0) group0 = max(group0, lane_before);
+  const int refused = verdict_of(a, first, count, all);
+  if (blockIdx.x == 0) raise_data_error(a.data_error, error | (tid == 0 ? refused : 0));
+  const int total = refused ? 0 : static_cast<int>(all.added);
+#pragma unroll
+  for (int k = 0; k < 2; ++k) {
+    const int s = 2 * tid + k;
+    lds.cu[s] = refused ? 0 : static_cast<int>(add0);
+    lds.take[s] = take0;
+    lds.give[s] = give0;
+    lds.keep[s] = of[k].keep;
+    lds.used[s] = of[k].used;
+    add0 += of[k].add;
+    take0 += max(0, of[k].will - of[k].used);
+    give0 += max(0, of[k].used - of[k].will);
+  }
+  __syncthreads();      // every thread has read which groups begin where
+  lds.group[2 * tid] = max(group0, own_group[0]);
+  lds.group[2 * tid + 1] = max(group0, own_group[1]);
+  __syncthreads();
+
+  const int64_t step = static_cast<int64_t>(gridDim.x) * BLOCK, here = static_cast<int64_t>(blockIdx.x) * BLOCK + tid;
+  // the tokens
+  const int64_t t0 = blockIdx.x * per, t1 = min<int64_t>(total, t0 + per);
+  for (int64_t begin = t0; begin < t1; begin += BLOCK) {
+    if (a.parent) {
+      __syncthreads();
+      for (int i = tid; i < BLOCK + kMostDrafted; i += BLOCK) {
+        const int64_t t = begin - kMostDrafted + i;
+        lds.parents[i] = t >= 0 && t < total ? a.parent[t] : -1;
+      }
+      __syncthreads();
+    }
+    const int64_t at = begin + tid;
+    if (at >= t1) continue;
+    const int t = static_cast<int>(at), s = last_below(lds.cu, a.n_seq, t), j = t - lds.cu[s], place = lds.keep[s] + j, page = place >> a.shift;
+    int depth = j, wrong_parent = 0;
+    const int g = lds.group[s];
+    int64_t id = 0;
+    if (a.slot) {
+      const int from_ring = page - lds.used[s];
+      id = from_ring < 0 ? a.pages[static_cast<int64_t>(s) * a.max_pages + page] : a.ring[ring_at(a, first, lds.take[s] + from_ring)];
+    }
+    int prefix = 0;
+    if (a.position && !falls && g >= 0 && s < a.group_seq[g + 1]) {
+      prefix = a.prefix_len[g];
+      if (prefix < 0 || prefix > 1 << 30) prefix = 0;
+    }
+    if (a.parent) {
+      const uint64_t bits = path_of(lds.parents + kMostDrafted + tid, j, &wrong_parent);
+      depth = __popcll(bits) - 1;
+      if (a.ancestors) a.ancestors[t] = bits;
+      raise_data_error(a.data_error, wrong_parent);
+    }
+    if (a.seq) a.seq[t] = s;
+    if (a.position) a.position[t] = prefix + lds.keep[s] + depth;
+    if (a.slot) a.slot[t] = (id << a.shift) + (place & ((1 << a.shift) - 1));
+  }
+  // pages moved
+  if (!refused) {
+    for (int64_t m = here; m < all.taken; m += step) {
+      const int s = last_below(lds.take, a.n_seq, static_cast<int>(m));
+      a.pages[static_cast<int64_t>(s) * a.max_pages + lds.used[s] + m - lds.take[s]] = a.ring[ring_at(a, first, static_cast<int>(m))];
+    }
+    const int end = all.given ? ring_at(a, first, count) : 0;
+    for (int64_t m = here; m < all.given; m += step) {
+      const int s = last_below(lds.give, a.n_seq, static_cast<int>(m));
+      const int will = (lds.keep[s] + (s + 1 < a.n_seq ? lds.cu[s + 1] : total) - lds.cu[s] + (1 << a.shift) - 1) >> a.shift;
+      a.ring[ring_at(a, end, static_cast<int>(m))] = a.pages[static_cast<int64_t>(s) * a.max_pages + will + m - lds.give[s]];
+    }
+  }
+  // the sequences: behind everything that has read their lengths, where there is one workgroup
+  __syncthreads();
+  for (int64_t s = here; s < a.n_seq; s += step) {
+    a.cu_q[s] = lds.cu[s];
+    if (refused) a.length_out[s] = a.length[s];
+    else a.length_out[s] = lds.keep[s] + (s + 1 < a.n_seq ? lds.cu[s + 1] : total) - lds.cu[s];
+  }
+  if (here == 0) {
+    a.cu_q[a.n_seq] = total;
+    a.state_out[0] = refused ? first : ring_at(a, first, all.taken);
+    a.state_out[1] = refused ? count : count - all.taken + all.given;
+  }
+}
+
 struct Span {
   const void* at;
   size_t bytes;
@@ -290,6 +469,18 @@ extern "C" int at_grpo_kv_plan(const at_grpo_page_pool* pool, int32_t n_tok, con
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < bytes) return AT_GRPO_EWORKSPACE;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   ProfScope ps(PROF_PLAN, s);
+  // One launch for few sequences; in place by one workgroup, which has a share of at most 8192 tokens.  The smaller workgroup for few of both: four
+  // candidates 6.7 us by 1024 threads, 4.3 by 256.
+  const bool in_place = length_out == length || state_out == state;
+  const bool small = pool->n_seq <= 512 && n_tok <= 1024;
+  const int block = small ? 256 : kPlanBlock;
+  if (pool->n_seq <= 2 * kPlanBlock && (!in_place || n_tok <= kPlanAlone)) {
+    const int64_t per = in_place ? (n_tok > block ? n_tok : block) : block * (1 + n_tok / (int64_t{block} * 512));
+    const int64_t blocks = n_tok ? ceil_div(n_tok, per) : 1;
+    hipLaunchKernelGGL(small ? k_plan<256> : k_plan<kPlanBlock>, dim3(static_cast<unsigned>(blocks)), dim3(block), 0, s, a, per);
+    ATG_LAUNCH_CHECK();
+    return AT_GRPO_OK;
+  }
   hipLaunchKernelGGL(k_plan_sequences, dim3(static_cast<unsigned>(S ? ceil_div(S, kPlanBlock) : 1)), dim3(kPlanBlock), 0, s, a);
   ATG_LAUNCH_CHECK();
   const int64_t threads = static_cast<int64_t>(T > S ? T : S);

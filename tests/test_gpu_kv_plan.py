@@ -95,6 +95,13 @@ CASES = {
     "many, kept in part": (8, [s % 70 for s in range(5000)], 128, 25000, 4000, [s % 70 * (s % 3) // 2 for s in range(5000)], [(s * 7) % 30 for s in range(5000)],
                            [0, 2500, 1], [8, 9, 10]),
     "no pages": (16, [0, 0], 0, 3, 1, None, [0, 0], [], []),
+    # on both sides of what a workgroup of either size, one launch, and one workgroup in place take
+    "512": (16, [s % 90 for s in range(512)], 128, 4000, 70, [s % 90 - s % 2 * (s % 90 // 3) for s in range(512)], [s % 3 for s in range(512)], [7] * 70, list(range(70))),
+    "513": (16, [s % 90 for s in range(513)], 128, 4000, 70, None, [1 + s % 7 for s in range(513)], [0, 500, 13], [5, 6, 7]),
+    "1025 tokens": (8, [3, 9, 20], 1600, 500, 2, None, [1000, 0, 25], [3], [11]),
+    "2048": (8, [s % 50 for s in range(2048)], 128, 20000, 9000, [s % 50 * 2 // 3 for s in range(2048)], [s % 9 for s in range(2048)], [1] * 2048, list(range(2048))),
+    "2049": (8, [s % 50 for s in range(2049)], 128, 20000, 9000, None, [s % 9 for s in range(2049)], [1] * 2049, list(range(2049))),
+    "large prompts": (64, [0] * 40, 20000, 12000, 11, None, [500 * s for s in range(40)], [], []),
 }
 
 
