@@ -908,11 +908,14 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
       // A tile of the stream: tokens token .. of a sequence (or of the prefix: -1), of which there are `last`; where its page ids are listed.
       struct Tile {
         int seq, token, last, slot0;
+        int q0, q1;      // the sequence's queries
       };
       auto tile_at = [&](int t) {
-        Tile x{-1, t, u.prefix, -page0};
+        Tile x{-1, t, u.prefix, -page0, 0, 0};
         if (t >= own0) {
           x.seq = seq_at(t);
+          x.q0 = kv.cu_q ? kv.cu_q[x.seq] : x.seq;
+          x.q1 = kv.cu_q ? kv.cu_q[x.seq + 1] : x.seq + 1;
           x.token = t - begin_of(x.seq);
           x.last = __builtin_amdgcn_readfirstlane(length_of(lds, x.seq));
           x.slot0 = slot0_of(x.seq);
@@ -996,7 +999,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
               if constexpr (TREE) sees[n] = ~0u;
             }
             if (tile.seq >= 0) {
-              const int q0 = kv.cu_q ? kv.cu_q[tile.seq] : tile.seq, q1 = kv.cu_q ? kv.cu_q[tile.seq + 1] : tile.seq + 1;      // the sequence's queries
+              const int q0 = tile.q0, q1 = tile.q1;
 #pragma unroll
               for (int n = 0; n < NR; ++n) {
                 const bool of_it = row_tok[n] >= q0 && row_tok[n] < q1;
@@ -1733,12 +1736,17 @@ struct RowParts {
 // Rows behind prefixes: a wavefront for four heads of a token, so that what belongs to the token is looked up once.  3840 tokens of 32 heads of 128
 // 50 us; a wavefront for each row 111.
 template <typename T>
-__global__ __launch_bounds__(256) void k_join_heads(KvView kv, Args a, int tile_rows) {
-  const int lane = threadIdx.x & 63, per_token = (a.Hq + 3) / 4;
+__global__ __launch_bounds__(256) void k_join_heads(KvView kv, Args a, int tile_rows, int heads) {
+  const int lane = threadIdx.x & 63, per_token = (a.Hq + heads - 1) / heads;
   const int64_t unit = static_cast<int64_t>(flat_block()) * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (unit >= static_cast<int64_t>(a.n_tok) * per_token) return;
-  const int t = static_cast<int>(unit / per_token), h0 = 4 * static_cast<int>(unit - static_cast<int64_t>(t) * per_token);
+  const int t = static_cast<int>(unit / per_token), h0 = heads * static_cast<int>(unit - static_cast<int64_t>(t) * per_token);
   const UnitsOf units = units_of(kv, a, t);
+  if (heads == 1) {
+    const RowParts of(a, units, t, h0, tile_rows);
+    join_row(a, kv.D, of.parts(), true, true, of, static_cast<T*>(a.out.data) + t * a.out.ts + h0 * a.out.hs, a.lse ? a.lse + of.unit : nullptr);
+    return;
+  }
   const RowParts of_slot(a, units, t, min(h0 + (lane >> 4), a.Hq - 1), tile_rows);
   T* const to = static_cast<T*>(a.out.data) + t * a.out.ts;
   if (!__any(of_slot.parts() > 8)) {
@@ -2054,8 +2062,11 @@ int attend(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* 
     // twelve sequences of fp32 behind 300 22.4 (21.3); 3840 rows 39.6 (38.5), 84.1 (85.5) and 38.4 (29.0).
     hipLaunchKernelGGL(bf16 ? k_join<bf16_t> : k_join<float>, dim3(static_cast<unsigned>(outputs)), dim3(256), 0, s, view, args, k.rows);
   } else {
-    const int64_t waves = static_cast<int64_t>(n_tok) * ceil_div(Hq, 4);
-    hipLaunchKernelGGL(bf16 ? k_join_heads<bf16_t> : k_join_heads<float>, grid_of(ceil_div(waves, 4)), dim3(256), 0, s, view, args, k.rows);
+    // Few rows of trees, with many parts each: a wavefront for a row.  Two prompts of 40000 tokens, 6400 rows 216 us whole, then 211, 3500 rows 117 and
+    // 110; 45000 rows 221 and 254.
+    const int heads = TREE && outputs <= 16384 ? 1 : 4;
+    const int64_t waves = static_cast<int64_t>(n_tok) * ceil_div(Hq, heads);
+    hipLaunchKernelGGL(bf16 ? k_join_heads<bf16_t> : k_join_heads<float>, grid_of(ceil_div(waves, 4)), dim3(256), 0, s, view, args, k.rows, heads);
   }
   ATG_LAUNCH_CHECK();
   return AT_GRPO_OK;

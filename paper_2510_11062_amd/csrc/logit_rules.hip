@@ -62,9 +62,7 @@ struct RowRules {
   const uint8_t* allowed;                             // bits, or null
 };
 
-__device__ __forceinline__ float setting(const float* of, int s, float otherwise, bool positive, int* error) {
-  if (!of) return otherwise;
-  const float x = of[s];
+__device__ __forceinline__ float checked(float x, float otherwise, bool positive, int* error) {
   const bool fine = fabsf(x) < INFINITY && (!positive || x > 0.f);
   if (!fine) *error |= AT_GRPO_DATA_RULE;
   return fine ? x : otherwise;
@@ -75,59 +73,81 @@ __device__ __forceinline__ RowRules rules_of(const RuleArgs& a, int row, int* er
   RowRules x{};
   x.repetition = 1.f;
   x.to_out = 1.f;
-  if (r.allowed) {
-    const int m = r.mask_row[row];
-    if (m < -1 || m >= r.n_mask) *error |= AT_GRPO_DATA_RULE;
-    else if (m >= 0) x.allowed = reinterpret_cast<const uint8_t*>(r.allowed + static_cast<int64_t>(m) * ((r.V + 31) >> 5));
-  }
+  // Everything that can be asked for at once is, and looked at behind that: one after the other these loads are what a short call takes.
+  const int m = r.allowed ? r.mask_row[row] : -1;
+  if (r.ancestors) x.path = r.ancestors[row];
   int s = row, t0 = row, t1 = row + 1;
+  bool of_one = true;
   if (r.cu_q) {
     s = wave_upper_bound(r.cu_q, r.n_seq + 1, row) - 1;
-    if (s < 0 || s >= r.n_seq) return x;      // of no sequence
-    t0 = r.cu_q[s];
-    t1 = r.cu_q[s + 1];
-    if (t0 < 0 || t0 > row || t1 <= row || t1 > a.n_rows) {
-      *error |= AT_GRPO_DATA_SEQLENS;
-      return x;
+    of_one = s >= 0 && s < r.n_seq;
+    s = of_one ? s : 0;
+    if (of_one) {
+      t0 = r.cu_q[s];
+      t1 = r.cu_q[s + 1];
     }
   }
-  x.repetition = setting(r.repetition, s, 1.f, true, error);
-  x.presence = setting(r.presence, s, 0.f, false, error);
-  x.frequency = setting(r.frequency, s, 0.f, false, error);
-  x.to_out = 1.f / setting(r.temperature, s, 1.f, true, error);
+  float repetition = 1.f, presence = 0.f, frequency = 0.f, temperature = 1.f;
+  int n_own = 0, b0 = 0, b1 = 0, g = -1, n_prompt = 0, s0 = 0, s1 = 0;
+  if (of_one) {
+    if (r.repetition) repetition = r.repetition[s];
+    if (r.presence) presence = r.presence[s];
+    if (r.frequency) frequency = r.frequency[s];
+    if (r.temperature) temperature = r.temperature[s];
+    if (r.tokens) n_own = r.length[s];
+    if (r.bias_cu) {
+      b0 = r.bias_cu[s];
+      b1 = r.bias_cu[s + 1];
+    }
+    if (r.prompt) {
+      g = wave_upper_bound(r.group_seq, r.n_group + 1, s) - 1;
+      if (g >= 0 && g < r.n_group) {
+        n_prompt = r.prompt_len[g];
+        s0 = r.group_seq[g];
+        s1 = r.group_seq[g + 1];
+      }
+    }
+  }
+  if (m < -1 || m >= r.n_mask) {
+    if (r.allowed) *error |= AT_GRPO_DATA_RULE;
+  } else if (m >= 0) {
+    x.allowed = reinterpret_cast<const uint8_t*>(r.allowed + static_cast<int64_t>(m) * ((r.V + 31) >> 5));
+  }
+  if (!of_one) return x;
+  if (t0 < 0 || t0 > row || t1 <= row || t1 > a.n_rows) {      // of no sequence either
+    *error |= AT_GRPO_DATA_SEQLENS;
+    return x;
+  }
+  x.repetition = checked(repetition, 1.f, true, error);
+  x.presence = checked(presence, 0.f, false, error);
+  x.frequency = checked(frequency, 0.f, false, error);
+  x.to_out = 1.f / checked(temperature, 1.f, true, error);
   if (r.tokens) {
     x.own = r.tokens + static_cast<int64_t>(s) * r.max_tokens;
-    x.n_own = r.length[s];
-    if (x.n_own < 0 || x.n_own > r.max_tokens) {
+    x.n_own = n_own;
+    if (n_own < 0 || n_own > r.max_tokens) {
       *error |= AT_GRPO_DATA_SEQLENS;
       x.n_own = 0;
     }
   }
-  if (r.prompt) {
-    const int g = wave_upper_bound(r.group_seq, r.n_group + 1, s) - 1;
-    if (g >= 0 && g < r.n_group) {
-      x.prompt = r.prompt + static_cast<int64_t>(g) * r.max_prompt;
-      x.n_prompt = r.prompt_len[g];
-      if (x.n_prompt < 0 || x.n_prompt > r.max_prompt || r.group_seq[g] < 0 || r.group_seq[g] > s || r.group_seq[g + 1] <= s || r.group_seq[g + 1] > r.n_seq) {
-        *error |= AT_GRPO_DATA_SEQLENS;
-        x.n_prompt = 0;
-      }
+  if (g >= 0 && g < r.n_group) {
+    x.prompt = r.prompt + static_cast<int64_t>(g) * r.max_prompt;
+    x.n_prompt = n_prompt;
+    if (n_prompt < 0 || n_prompt > r.max_prompt || s0 < 0 || s0 > s || s1 <= s || s1 > r.n_seq) {
+      *error |= AT_GRPO_DATA_SEQLENS;
+      x.n_prompt = 0;
     }
   }
   if (r.ancestors) {
-    x.path = r.ancestors[row];
     x.drafted = r.drafted + t0;
     x.n_drafted = min(64, t1 - t0);
   }
-  if (r.bias_cu) {
-    const int b0 = r.bias_cu[s], b1 = r.bias_cu[s + 1];
-    if (b0 < 0 || b1 < b0 || b1 > r.n_bias) {
-      *error |= AT_GRPO_DATA_SEQLENS;
-    } else {
-      x.bias_token = r.bias_token + b0;
-      x.bias = r.bias + b0;
-      x.n_bias = b1 - b0;
-    }
+  if (b0 < 0 || b1 < b0 || b1 > r.n_bias) {
+    *error |= AT_GRPO_DATA_SEQLENS;
+  } else if (r.bias_cu) {
+    x.bias_token = r.bias_token + b0;
+    x.bias = r.bias + b0;
+    x.n_bias = b1 - b0;
   }
   return x;
 }
