@@ -12,6 +12,7 @@
 //   k_attend_wide   more, in bf16: units are the prefix of a group with the queries of all its sequences, and a sequence's own tokens with its
 //                   queries; tiles of 128 rows
 //   k_attend        the same in fp32, and where k_decode's tables end; tiles of 16 or 32 rows
+// and, for trees, k_tree_near where there is little of everything.
 //
 // In the first and the last a wavefront holds a tile's queries, takes 32 tokens at a time (16 in fp32) and keeps everything in registers:
 //   S^T = K Q^T     MFMA 16x16: tokens down, queries across, so that a lane has four consecutive tokens of one query
@@ -474,7 +475,9 @@ __device__ __forceinline__ void set_apart(float* slab, typename Shape<T, D>::VV 
 // The matrix instruction takes bf16 weights with bf16 values, so a weight is rounded to 8 bits there (the sums take it as it is): an error
 // of up to 2^-8 of each term, of the order of the result's own rounding.  Against 64 bits bf16 results are off by 0.0023 (rounded once from
 // 32 bits 0.0017).  Weights in two parts would take twice the products.
-template <typename T, int D, int NR, typename Before>
+// EACH: a row's maximum is raised where its own score asks for it and not where another row's in the wavefront does, so that what one row sees
+// leaves the others' bits as they are.
+template <typename T, int D, bool EACH, int NR, typename Before>
 __device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::SUB], const typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
                                               float to_log2, f32x4 (&acc)[NR][Shape<T, D>::NB][Shape<T, D>::E], float (&top)[NR], float (&ref)[NR],
                                               float (&sum)[NR], Before before) {
@@ -494,6 +497,7 @@ __device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::
     if (__any(high > top[n] + kSlack)) {
       high = fmaxf(high, __shfl_xor(high, 16, 64));
       high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top[n]);
+      if (EACH && !(high > top[n] + kSlack)) high = top[n];
       const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top[n] - now);
       top[n] = high;
       ref[n] = now;
@@ -1025,7 +1029,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
               }
             }
           }
-          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, [&] {
+          weigh_and_add<T, D, TREE>(s, v, to_log2, acc, top, ref, sum, [&] {
             // the one new token of a unit sees its stream whole: that of its sequence alone (in a tree itself only where its bit says so)
             if (tile.seq >= 0 && (TREE || u.ntok > 1))
               set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) {
@@ -1283,6 +1287,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
         high *= to_log2;
         if (__any(high > top + kSlack)) {
           high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
+          if (TREE && !(high > top + kSlack)) high = top;      // as EACH there
           const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top - now);
           top = high;
           ref = now;
@@ -1587,7 +1592,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_attend(KvView kv, Ar
               }
             }
           }
-          weigh_and_add<T, D>(s, v, to_log2, acc, top, ref, sum, [&] {
+          weigh_and_add<T, D, TREE>(s, v, to_log2, acc, top, ref, sum, [&] {
             if (part && t + TOK > all_see)
               set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) {
                 if constexpr (tree) return t + token < limit[n] && (sees[n] >> token & 1);
@@ -1903,6 +1908,214 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int tile_r
   }
 }
 
+// ---- few short sequences ------------------------------------------------------------------------------
+// With few rows and short contexts a call is its loads one behind the other, and a schedule is some of them, as is a second launch.  Here a
+// workgroup has a tile of rows of one sequence for one key head and reads the prefix and the own tokens whole, its four wavefronts in turns:
+// bounds, lengths and page ids are asked for together, then queries and keys.  A group's prefix is read by each of its sequences, from the caches.
+// Lengths are only on the device, so what the tables have room for says whether it is taken; by the other kernels (heads of 128 on 8, bf16):
+//   four candidates behind 197 tokens, 64 rows a group        8.2 us  21.8      120 sequences of up to 2000, 16 rows each        121 us  132
+//   22 behind prompts of 300, 64 rows each                   20     43          60 behind prompts of 1000, 64 rows each          56.8    57.0
+//   220 behind prompts of 300                                95    111          110 of them                                      92.8    93.1
+//   six of up to 3500                                        36.7   37.3        four behind 3500                                 36.6    30.8
+// fp32, heads of 64 on 2: 12 behind 300 tokens 14.2 and 20.5, 12 behind 900 27.9 and 26.7.
+constexpr int kNearSlots = 512, kNearSeqs = 1024, kNearRoom = 2048, kNearRoomF32 = 1024;
+constexpr int64_t kNearWork = 5 << 19;      // tiles of rows and key heads, times the room
+
+struct NearLds {
+  int group, holes[4];
+  int pages[2][kNearSlots];      // of the prefix, and the sequence's
+  float ml[4][64][2];
+  float slab[4][16][128 + 4];
+};
+
+template <typename T>
+__device__ void clear_token(const Args& a, int D, int t);
+
+template <typename T, int D, int NR, bool EXACT>
+__global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_tree_near(KvView kv, Args a) {
+  typedef Shape<T, D> Z;
+  constexpr int E = Z::E, NB = Z::NB, KC = Z::KC, SUB = Z::SUB, TOK = Z::TOK, VJ = 4 * SUB, R = 16 * NR;
+  __shared__ NearLds lds;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), m = lane & 15, g = lane >> 4;
+  const int dim = EXACT ? D : kv.D, hk = blockIdx.y, s = blockIdx.z, last_page = (1 << kv.page_shift) - 1;
+  if (tid == 0) lds.group = -1;
+  const int32_t* const own_table = kv.pages + static_cast<int64_t>(s) * kv.max_pages;
+  int own_id[2], prefix_id[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) own_id[i] = tid + 256 * i < kv.max_pages ? own_table[tid + 256 * i] : 0;
+  const int length = kv.length[s], q0 = kv.cu_q ? kv.cu_q[s] : s, q1 = kv.cu_q ? kv.cu_q[s + 1] : s + 1;
+  bool falls = false;
+  if (kv.cu_q)
+    for (int i = tid; i < kv.n_seq; i += 256) falls |= kv.cu_q[i] < 0 || kv.cu_q[i + 1] < kv.cu_q[i] || kv.cu_q[i + 1] > a.n_tok;
+  int mine = -1;
+  for (int i = tid; i < kv.n_group; i += 256) {
+    const int s0 = kv.group_seq[i], s1 = kv.group_seq[i + 1];
+    falls |= s0 < 0 || s1 < s0 || s1 > kv.n_seq;
+    if (s >= s0 && s < s1) mine = i;
+  }
+  __syncthreads();
+  if (mine >= 0) lds.group = mine;
+  const bool none = __syncthreads_or(falls);
+  // rows of nobody
+  const int workgroups = gridDim.x * gridDim.y * gridDim.z, number = (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
+  const int cu0 = none ? a.n_tok : kv.cu_q ? kv.cu_q[0] : 0, cu1 = none ? a.n_tok : kv.cu_q ? kv.cu_q[kv.n_seq] : a.n_tok;
+  for (int t = number * 4 + wave; t < cu0; t += workgroups * 4) clear_token<T>(a, dim, t);
+  for (int t = cu1 + number * 4 + wave; t < a.n_tok; t += workgroups * 4) clear_token<T>(a, dim, t);
+  const bool speaks = blockIdx.x == 0 && blockIdx.y == 0;      // of what is wrong with the sequence
+  if (none) {
+    if (number == 0 && tid == 0) raise_data_error(a.data_error, AT_GRPO_DATA_SEQLENS);
+    return;
+  }
+  const int group = __builtin_amdgcn_readfirstlane(lds.group), ntok = q1 - q0, rows = ntok * a.share;
+  const int32_t* const prefix_table = kv.prefix_pages + static_cast<int64_t>(max(group, 0)) * kv.max_prefix_pages;
+  int prefix = group >= 0 ? kv.prefix_len[group] : 0, own = length, error = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) prefix_id[i] = group >= 0 && tid + 256 * i < kv.max_prefix_pages ? prefix_table[tid + 256 * i] : 0;
+  if (prefix < 0 || prefix > (kv.max_prefix_pages << kv.page_shift)) {
+    error |= AT_GRPO_DATA_SEQLENS;
+    prefix = 0;
+  }
+  if (own < 0 || own > (kv.max_pages << kv.page_shift)) {
+    error |= AT_GRPO_DATA_SEQLENS;
+    own = 0;
+  }
+  if (ntok > kMostTree) error |= AT_GRPO_DATA_TREE;
+  bool missing = false;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int slot = tid + 256 * i;
+    auto put = [&](int which, int id, int tokens) {
+      if (slot >= (tokens + last_page) >> kv.page_shift) return;
+      const bool no = static_cast<unsigned>(id) >= static_cast<unsigned>(kv.n_pages);
+      lds.pages[which][slot] = no ? -1 : id;
+      missing |= no;
+    };
+    put(0, prefix_id[i], prefix);
+    put(1, own_id[i], own);
+  }
+  if (missing && ntok > 0) error |= AT_GRPO_DATA_PAGE;
+  if (speaks) raise_data_error(a.data_error, error);
+  const bool any = __any(missing);
+  if (lane == 0) lds.holes[wave] = any;
+  __syncthreads();
+  const bool holes = (lds.holes[0] | lds.holes[1] | lds.holes[2] | lds.holes[3]) != 0;
+
+  const uint32_t page_step = static_cast<uint32_t>(kv.Hk * dim) << kv.page_shift;
+  const float to_log2 = a.scale * kLog2e;
+  const T* const kbase = static_cast<const T*>(kv.k) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+  const T* const vbase = static_cast<const T*>(kv.v) + ((static_cast<int64_t>(hk) * dim) << kv.page_shift);
+  const int own0 = (prefix + TOK - 1) & -TOK, end = own0 + own, tree0 = own - ntok;      // own tokens begin a tile; the first new one of them
+  struct Tile {
+    int which, token, last;
+  };
+  auto tile_at = [&](int t) { return t < own0 ? Tile{0, t, prefix} : Tile{1, t - own0, own}; };
+  auto row_of = [&](const Tile& x, int token) {
+    return static_cast<uint64_t>(static_cast<uint32_t>(max(0, lds.pages[x.which][token >> kv.page_shift]))) * page_step + static_cast<uint32_t>((token & last_page) * dim);
+  };
+  typename Z::KV q[NR][KC], k[SUB][KC];
+  typename Z::VV v[NB][VJ];
+  auto load_k = [&](const Tile& x) {      // a token behind the last stands for it
+#pragma unroll
+    for (int y = 0; y < SUB; ++y) {
+      const T* p = kbase + row_of(x, min(x.token + 16 * y + m, x.last - 1));
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const int d = 4 * Z::KE * c + Z::KE * g;
+        typename Z::KV z{};
+        if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(p + d);
+        k[y][c] = z;
+      }
+    }
+  };
+  auto load_v = [&](const Tile& x) {
+#pragma unroll
+    for (int y = 0; y < SUB; ++y) {
+      const T* p = vbase + row_of(x, min(x.token + 16 * y + 4 * g, (x.last - 1) & ~3));
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const int d = 16 * E * b + E * m;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          typename Z::VV z{};
+          if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::VV*>(p + static_cast<int64_t>(j) * dim + d);
+          v[b][4 * y + j] = z;
+        }
+      }
+    }
+  };
+  for (int r0 = blockIdx.x * R; r0 < rows; r0 += gridDim.x * R) {
+    uint64_t path[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      const int r = min(r0 + 16 * n + m, rows - 1), tq = r / a.by_share, h = hk * a.share + r - tq * a.share;
+      const T* from = static_cast<const T*>(a.q.data) + (q0 + tq) * a.q.ts + h * a.q.hs;
+      path[n] = a.ancestors[q0 + tq];
+#pragma unroll
+      for (int c = 0; c < KC; ++c) {
+        const int d = 4 * Z::KE * c + Z::KE * g;
+        typename Z::KV z{};
+        if (EXACT || d < dim) z = *reinterpret_cast<const typename Z::KV*>(from + d);
+        q[n][c] = z;
+      }
+    }
+    f32x4 acc[NR][NB][E];
+    float top[NR], ref[NR], sum[NR];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      top[n] = -INFINITY;
+      ref[n] = 0.f;
+      sum[n] = 0.f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int e = 0; e < E; ++e) acc[n][b][e] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    int t = TOK * wave;
+    if (t < end) {
+      Tile tile = tile_at(t);
+      load_k(tile);
+      asm volatile("" ::: "memory");
+      __builtin_amdgcn_sched_barrier(0);
+      load_v(tile);
+      for (;;) {      // loads are not behind a branch (see k_attend)
+        const bool more = t + 4 * TOK < end;
+        const Tile next = more ? tile_at(t + 4 * TOK) : tile;
+        f32x4 z[NR][SUB];
+        scores<T, D>(k, q, z);
+        load_k(next);
+        uint32_t sees[NR];      // of the tile's tokens
+        const bool partly = tile.which && tile.token + TOK > tree0;
+#pragma unroll
+        for (int n = 0; n < NR; ++n) sees[n] = partly ? static_cast<uint32_t>(tree_bits(path[n], tile.token - tree0)) : ~0u;
+        if (partly || tile.token + TOK > tile.last || holes) {
+#pragma unroll
+          for (int y = 0; y < SUB; ++y) {
+            const int at = 16 * y + 4 * g, t4 = tile.token + at, last = tile.last - t4;
+            const int seen = last > 0 && lds.pages[tile.which][min(t4, tile.last - 1) >> kv.page_shift] >= 0 ? last : 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+#pragma unroll
+              for (int n = 0; n < NR; ++n) z[n][y][i] = i < seen && (sees[n] >> (at + i) & 1) ? z[n][y][i] : -INFINITY;
+#pragma unroll
+              for (int b = 0; b < NB; ++b) v[b][4 * y + i] = i < seen ? v[b][4 * y + i] : typename Z::VV{};
+            }
+          }
+        }
+        weigh_and_add<T, D, true>(z, v, to_log2, acc, top, ref, sum, [&] {
+          if (partly) set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) { return token < tile.last - tile.token && (sees[n] >> token & 1); });
+        });
+        load_v(next);
+        asm volatile("" ::: "memory");
+        if (!more) break;
+        tile = next;
+        t += 4 * TOK;
+      }
+    }
+    finish<T, EXACT>(a, lds, acc, top, sum, RowsOf{q0, hk, r0, rows}, true, -1, 0, 0, dim);
+    lds_barrier();      // what was added up has been read
+  }
+}
+
 // ---- host -------------------------------------------------------------------------------------------
 int check_sizes(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q) {
   ATG_TRY(check_kv_sizes(kv, n_tok));
@@ -1966,10 +2179,27 @@ Choice choose(int D, int rows_p, int rows_o, bool decode) {
   return choose_of<T, 256, false, TREE>(rows_p, rows_o, decode);
 }
 
+// Rows of a sequence at most.
+template <typename T, int D, bool EXACT>
+Choice near_of(int rows_o) {
+  if constexpr (D <= 128)
+    if (rows_o > 16) return {k_tree_near<T, D, 2, EXACT>, 32, 1, 0};
+  return {k_tree_near<T, D, 1, EXACT>, 16, 1, 0};
+}
+template <typename T>
+Choice choose_near(int D, int rows_o) {
+  if (D == 64) return near_of<T, 64, true>(rows_o);
+  if (D == 128) return near_of<T, 128, true>(rows_o);
+  if (D == 256) return near_of<T, 256, true>(rows_o);
+  if (D < 64) return near_of<T, 64, false>(rows_o);
+  if (D < 128) return near_of<T, 128, false>(rows_o);
+  return near_of<T, 256, false>(rows_o);
+}
+
 // Everything that goes by sizes alone.
 struct Plan {
   Choice choice;
-  bool decode;
+  bool near, decode;
   int coarse;
   double most;      // an upper bound of all costs together
 };
@@ -1984,6 +2214,20 @@ int make_plan(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q, Pl
   const auto eights_of = [&](int64_t pages) { return static_cast<double>(pages) * kv->page_size / 8; };
   constexpr int run_cost = TREE ? kTreeRunCost : kRunCost;
   const double fixed = 8 + run_cost + kMinShare;
+  out->near = false;
+  if constexpr (TREE) {
+    const int64_t room = (static_cast<int64_t>(kv->max_pages) + kv->max_prefix_pages) * kv->page_size;
+    const int64_t rows = rows_o < 64 * share ? rows_o : 64 * share, tiles = ceil_div(rows, rows > 16 && kv->D <= 128 ? 32 : 16);
+    out->near = kv->n_seq > 0 && kv->n_seq <= kNearSeqs && kv->n_group <= kNearSeqs && kv->Hk <= 65535 && kv->max_pages <= kNearSlots && kv->max_prefix_pages <= kNearSlots &&
+                room <= (kv->dtype == AT_GRPO_BF16 ? kNearRoom : kNearRoomF32) && tiles * kv->Hk * kv->n_seq * room <= kNearWork;
+    if (out->near) {
+      out->choice = kv->dtype == AT_GRPO_BF16 ? choose_near<bf16_t>(kv->D, small(rows)) : choose_near<float>(kv->D, small(rows));
+      out->decode = false;
+      out->coarse = 0;
+      out->most = static_cast<double>(tiles);
+      return AT_GRPO_OK;
+    }
+  }
   // Few rows a sequence, as many sequences as LDS has places for, their blocks counted in 26 bits and all costs in 30.
   const double decode_most = kv->Hk * ((all_rows / 16 + kv->n_group + kv->n_seq) * (eights_of(kv->max_prefix_pages) + fixed) + kv->n_seq * (eights_of(kv->max_pages) + fixed));
   out->decode = rows_o <= 16 && kv->n_seq <= kDecodeSeqs && static_cast<int64_t>(kv->n_seq + 1) * kv->max_pages * kv->page_size < 1 << 30 &&
@@ -2046,6 +2290,11 @@ int attend(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* 
     args.rise = 0;
   }
   ProfScope ps(PROF_ATTENTION, s);
+  if (plan.near) {
+    hipLaunchKernelGGL(k.kernel, dim3(static_cast<unsigned>(plan.most), kv->Hk, kv->n_seq), dim3(256), 0, s, view, args);
+    ATG_LAUNCH_CHECK();
+    return AT_GRPO_OK;
+  }
   if (k.lds) ATG_TRY(allow_big_lds(k.kernel, k.lds));
   hipLaunchKernelGGL(k.kernel, dim3(blocks), dim3(256), k.lds, s, view, args);
   ATG_LAUNCH_CHECK();

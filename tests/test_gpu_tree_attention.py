@@ -56,6 +56,13 @@ def check(p, out, ref, what=""):
         assert_within(np.where(seen, got, 0), np.where(seen, lse, 0), bl + 2.0 ** -22 * np.abs(np.where(seen, lse, 0)), what + " lse")
 
 
+def wide(kv):
+    """The same batch with page tables that have room for far more than it holds: which kernel is taken goes by that too."""
+    pad = torch.full((kv.pages.shape[0], 600), 1 << 30, dtype=torch.int32, device=kv.pages.device)
+    return api.KVBatch(kv.cache_k, kv.cache_v, torch.cat((kv.pages, pad), 1), kv.length, cu_q=kv.cu_q, group_seq=kv.group_seq, prefix_len=kv.prefix_len,
+                       prefix_pages=kv.prefix_pages)
+
+
 def bits(words, dev):
     return torch.from_numpy(words.view(np.int64).copy()).to(dev)
 
@@ -100,6 +107,7 @@ def test_against_the_oracle(gpu_device, dtype, name):
         assert again["lse"] is None and torch.equal(again["out"], out["out"])
         for max_q in {1, 7, 64, 4096}:      # whichever kernel a bound picks
             check(p, api.at_grpo_tree_attention(kv, q, b, max_q=max_q, want_lse=True), ref, f"{kind} max_q={max_q}")
+            check(p, api.at_grpo_tree_attention(wide(kv), q, b, max_q=max_q, want_lse=True), ref, f"{kind} max_q={max_q}, wide tables")
     assert int(word) == 0
 
 
@@ -120,13 +128,15 @@ def test_an_order_is_a_tree(gpu_device, dtype, name):
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("Hq,new", [(2, [5, 8, 6]), (8, [9, 40, 64])])
 @pytest.mark.parametrize("grouped", [False, True])
-def test_what_is_not_seen_stays_out(gpu_device, dtype, Hq, new, grouped):
+@pytest.mark.parametrize("tables", ["near", "wide"])
+def test_what_is_not_seen_stays_out(gpu_device, dtype, Hq, new, grouped, tables):
     """Infinities and NaN in tokens off a path, keys and values: the results are those without them, bit for bit; where a path has one its
     rows are what the formula says."""
     p = Paged(dtype, 2, 64, 16, [20, 70, 64], new, *(([2], [45]) if grouped else ()), seed=2)
     words = trees(p.rs, new, "paths")
     q = to_dev(p.queries(Hq), p.dtype, gpu_device)
     kv, b = p.device(gpu_device), bits(words, gpu_device)
+    kv = wide(kv) if tables == "wide" else kv
     want = api.at_grpo_tree_attention(kv, q, b, max_q=max(new), want_lse=True)
     for s in range(3):
         at = int(p.length[s] - p.new[s]) + 2      # the third drafted token of the sequence
@@ -159,9 +169,10 @@ def test_more_than_64_new_tokens(gpu_device, dtype, heads):
     word = torch.zeros(1, dtype=torch.int32, device=gpu_device)
     ref = attention(p, q64, words, 0.125)
     for max_q in (1, 64, 80):
-        out = api.at_grpo_tree_attention(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), bits(words, gpu_device), max_q=max_q, want_lse=True, data_error=word.zero_())
-        check(p, out, ref, f"max_q={max_q}")
-        assert int(word) == TREE
+        for kv in (p.device(gpu_device), wide(p.device(gpu_device))):
+            out = api.at_grpo_tree_attention(kv, to_dev(q64, p.dtype, gpu_device), bits(words, gpu_device), max_q=max_q, want_lse=True, data_error=word.zero_())
+            check(p, out, ref, f"max_q={max_q}")
+            assert int(word) == TREE
 
 
 @pytest.mark.gpu
@@ -171,8 +182,9 @@ def test_more_new_tokens_than_tokens(gpu_device, dtype):
     p = Paged(dtype, 2, 64, 16, [5, 40, 0], [9, 40, 20], [1], [17], seed=6)
     words = trees(p.rs, p.new, "paths")
     q64 = p.queries(4)
-    out = api.at_grpo_tree_attention(p.device(gpu_device), to_dev(q64, p.dtype, gpu_device), bits(words, gpu_device), want_lse=True)
-    check(p, out, attention(p, q64, words, 0.125))
+    for kv in (p.device(gpu_device), wide(p.device(gpu_device))):
+        out = api.at_grpo_tree_attention(kv, to_dev(q64, p.dtype, gpu_device), bits(words, gpu_device), want_lse=True)
+        check(p, out, attention(p, q64, words, 0.125))
 
 
 @pytest.mark.gpu
@@ -184,8 +196,8 @@ def test_bad_pages_lengths_and_rows_of_nobody(gpu_device, dtype, new):
     words = trees(p.rs, new, "order")
     q = to_dev(p.queries(4), p.dtype, gpu_device)
     b = bits(words, gpu_device)
-    for change in ("page", "length", "cu_q", "group_seq", "front"):
-        kv = p.device(gpu_device)
+    for change, tables in [(c, t) for c in ("page", "length", "cu_q", "group_seq", "front") for t in ("near", "wide")]:
+        kv = p.device(gpu_device) if tables == "near" else wide(p.device(gpu_device))
         if change == "page":
             kv.pages[1, 2], kv.prefix_pages[0, 1] = 1 << 30, -1
         elif change == "length":
