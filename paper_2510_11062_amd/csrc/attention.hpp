@@ -1917,8 +1917,8 @@ __global__ __launch_bounds__(256) void k_join_runs(KvView kv, Args a, int tile_r
 //   22 behind prompts of 300, 64 rows each                   20     43          60 behind prompts of 1000, 64 rows each          56.8    57.0
 //   220 behind prompts of 300                                95    111          110 of them                                      92.8    93.1
 //   six of up to 3500                                        36.7   37.3        four behind 3500                                 36.6    30.8
-// fp32, heads of 64 on 2: 12 behind 300 tokens 14.2 and 20.5, 12 behind 900 27.9 and 26.7.
-constexpr int kNearSlots = 512, kNearSeqs = 1024, kNearRoom = 2048, kNearRoomF32 = 1024;
+// fp32, heads of 64 on 2: 11 behind 300 tokens 9.7 and 20.5, behind 1500 25.8 and 27.1, 56 behind 1500 42.5 and 42.1, 50 of up to 1900 46 and 38.
+constexpr int kNearSlots = 512, kNearSeqs = 1024, kNearRoom = 2048;
 constexpr int64_t kNearWork = 5 << 19;      // tiles of rows and key heads, times the room
 
 struct NearLds {
@@ -2179,21 +2179,21 @@ Choice choose(int D, int rows_p, int rows_o, bool decode) {
   return choose_of<T, 256, false, TREE>(rows_p, rows_o, decode);
 }
 
-// Rows of a sequence at most.
+// Tiles of 32 rows, or of 16 where these are no more than there are compute units: 11 sequences of fp32, 52 rows each, 14.1 us and 9.7.
 template <typename T, int D, bool EXACT>
-Choice near_of(int rows_o) {
+Choice near_of(bool large) {
   if constexpr (D <= 128)
-    if (rows_o > 16) return {k_tree_near<T, D, 2, EXACT>, 32, 1, 0};
+    if (large) return {k_tree_near<T, D, 2, EXACT>, 32, 1, 0};
   return {k_tree_near<T, D, 1, EXACT>, 16, 1, 0};
 }
 template <typename T>
-Choice choose_near(int D, int rows_o) {
-  if (D == 64) return near_of<T, 64, true>(rows_o);
-  if (D == 128) return near_of<T, 128, true>(rows_o);
-  if (D == 256) return near_of<T, 256, true>(rows_o);
-  if (D < 64) return near_of<T, 64, false>(rows_o);
-  if (D < 128) return near_of<T, 128, false>(rows_o);
-  return near_of<T, 256, false>(rows_o);
+Choice choose_near(int D, bool large) {
+  if (D == 64) return near_of<T, 64, true>(large);
+  if (D == 128) return near_of<T, 128, true>(large);
+  if (D == 256) return near_of<T, 256, true>(large);
+  if (D < 64) return near_of<T, 64, false>(large);
+  if (D < 128) return near_of<T, 128, false>(large);
+  return near_of<T, 256, false>(large);
 }
 
 // Everything that goes by sizes alone.
@@ -2217,11 +2217,13 @@ int make_plan(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q, Pl
   out->near = false;
   if constexpr (TREE) {
     const int64_t room = (static_cast<int64_t>(kv->max_pages) + kv->max_prefix_pages) * kv->page_size;
-    const int64_t rows = rows_o < 64 * share ? rows_o : 64 * share, tiles = ceil_div(rows, rows > 16 && kv->D <= 128 ? 32 : 16);
+    const int64_t rows = rows_o < 64 * share ? rows_o : 64 * share;
+    const bool large = kv->D <= 128 && ceil_div(rows, 16) * kv->Hk * kv->n_seq > device_cu_count();
+    const int64_t tiles = ceil_div(rows, large ? 32 : 16);
     out->near = kv->n_seq > 0 && kv->n_seq <= kNearSeqs && kv->n_group <= kNearSeqs && kv->Hk <= 65535 && kv->max_pages <= kNearSlots && kv->max_prefix_pages <= kNearSlots &&
-                room <= (kv->dtype == AT_GRPO_BF16 ? kNearRoom : kNearRoomF32) && tiles * kv->Hk * kv->n_seq * room <= kNearWork;
+                room <= kNearRoom && tiles * kv->Hk * kv->n_seq * room <= kNearWork;
     if (out->near) {
-      out->choice = kv->dtype == AT_GRPO_BF16 ? choose_near<bf16_t>(kv->D, small(rows)) : choose_near<float>(kv->D, small(rows));
+      out->choice = kv->dtype == AT_GRPO_BF16 ? choose_near<bf16_t>(kv->D, large) : choose_near<float>(kv->D, large);
       out->decode = false;
       out->coarse = 0;
       out->most = static_cast<double>(tiles);
