@@ -611,7 +611,7 @@ typedef struct {
  * lse -inf.  A NaN logit that a mask leaves makes lse NaN and is passed over by best.
  * Without any penalty the lists of tokens are not looked at.  A row of no sequence (also where cu_q falls or leaves its range there: AT_GRPO_DATA_SEQLENS) has its mask and nothing else.  Tokens outside
  * [0, V) are passed over (AT_GRPO_DATA_TOKEN_RANGE), a length or list out of range counts as empty (AT_GRPO_DATA_SEQLENS), a
- * repetition or temperature that is not positive and finite as 1, a presence or frequency that is not finite as 0 and a mask_row out of
+ * repetition or temperature that is not positive and finite, or whose reciprocal is not, as 1, a presence or frequency that is not finite as 0 and a mask_row out of
  * range as -1 (AT_GRPO_DATA_RULE).  Workspace: at_grpo_logit_rules_workspace_bytes (0 on invalid arguments; no pointer is read).
  */
 int at_grpo_logit_rules(const at_grpo_sampling_rules* rules, int32_t n_rows, const void* logits,

@@ -63,7 +63,7 @@ struct RowRules {
 };
 
 __device__ __forceinline__ float checked(float x, float otherwise, bool positive, int* error) {
-  const bool fine = fabsf(x) < INFINITY && (!positive || x > 0.f);
+  const bool fine = fabsf(x) < INFINITY && (!positive || (x > 0.f && 1.f / x < INFINITY));
   if (!fine) *error |= AT_GRPO_DATA_RULE;
   return fine ? x : otherwise;
 }

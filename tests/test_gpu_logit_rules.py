@@ -390,7 +390,7 @@ def test_data_that_is_none(gpu_device, what, bit):
 
 
 @pytest.mark.gpu
-@pytest.mark.parametrize("value", [0.0, -1.0])
+@pytest.mark.parametrize("value", [0.0, -1.0, 1e-40])
 def test_settings_that_are_not_positive(gpu_device, value):
     r = draw(np.random.default_rng(11), "f32", 500, 3)
     for name in ("repetition", "temperature"):
