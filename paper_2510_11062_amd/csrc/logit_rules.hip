@@ -513,7 +513,12 @@ extern "C" int at_grpo_logit_rules(const at_grpo_sampling_rules* rules, int32_t 
   if (out) {      // the logits themselves, or apart from them
     const uintptr_t in0 = at(logits), in1 = in0 + ((n_rows - 1) * logits_stride + r.V) * e, out0 = at(out), out1 = out0 + ((n_rows - 1) * out_stride + r.V) * eo;
     const bool itself = out == logits && r.out_dtype == r.dtype && (n_rows == 1 || out_stride == logits_stride);
-    if (!itself && in0 < out1 && out0 < in1) return AT_GRPO_EINVAL;
+    bool beside = false;      // in rows of one buffer
+    if (n_rows > 1 && logits_stride * e == out_stride * eo) {
+      const int64_t step = logits_stride * e, apart = ((static_cast<int64_t>(out0) - static_cast<int64_t>(in0)) % step + step) % step;
+      beside = apart >= r.V * e && apart + r.V * eo <= step;
+    }
+    if (!itself && !beside && in0 < out1 && out0 < in1) return AT_GRPO_EINVAL;
   }
   const int chunks = static_cast<int>(ceil_div(r.V, kRuleChunk));
   RuleArgs a{r, n_rows, chunks, chunks, 1, logits, logits_stride, out, out_stride, lse, best, data_error, nullptr};

@@ -238,6 +238,13 @@ def test_strides_places_and_the_logits_themselves(gpu_device, dtype, V):
         assert torch.equal(view, want["out"])
         before[:, off_in:off_in + V] = want["out"]
         assert torch.equal(store.nan_to_num(7), before.nan_to_num(7))
+    both = torch.full((4, 2 * V + 3), -5.0, dtype=r.dtype, device=gpu_device)      # beside each other in rows of one buffer
+    for a, b in ((0, V + 3), (V + 1, 0)):
+        both[:, a:a + V] = rows
+        assert torch.equal(api.at_grpo_logit_rules(rules, both[:, a:a + V], out=both[:, b:b + V])["out"], want["out"])
+        assert torch.equal(both[:, a:a + V], rows) and torch.equal(both[:, b:b + V], want["out"])
+    with pytest.raises(api.AtGrpoError):
+        api.at_grpo_logit_rules(rules, both[:, :V], out=both[:, V - 1:2 * V - 1])
     with pytest.raises(api.AtGrpoError):
         flat = torch.zeros(8 * V, dtype=r.dtype, device=gpu_device)
         api.at_grpo_logit_rules(rules, flat[:4 * V].view(4, V), out=flat[1:4 * V + 1].view(4, V))
