@@ -325,7 +325,7 @@ __global__ __launch_bounds__(kRuleThreads, LISTS == LONG ? 2 : 4) void k_rules(R
       if (!whole) bits &= have >= 8 ? 0xff : have > 0 ? (1 << have) - 1 : 0;           // behind the last token: as if masked
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        const uint32_t on = static_cast<uint32_t>(bits << (31 - j) >> 31);
+        const uint32_t on = static_cast<uint32_t>(static_cast<int>(static_cast<uint32_t>(bits) << (31 - j)) >> 31);
         z[j] = __uint_as_float((__float_as_uint(z[j]) & on) | (0xff800000u & ~on));
       }
     }
