@@ -94,6 +94,7 @@ CASES = {
     "many": (16, [s % 70 for s in range(3000)], 128, 12000, 900, None, [s % 5 for s in range(3000)], [3] * 900, [s % 50 for s in range(900)]),
     "many, kept in part": (8, [s % 70 for s in range(5000)], 128, 25000, 4000, [s % 70 * (s % 3) // 2 for s in range(5000)], [(s * 7) % 30 for s in range(5000)],
                            [0, 2500, 1], [8, 9, 10]),
+    "no sequences": (16, [], 16, 5, 2, None, [], [], []),
     "no pages": (16, [0, 0], 0, 3, 1, None, [0, 0], [], []),
     # on both sides of what a workgroup of either size, one launch, and one workgroup in place take
     "512": (16, [s % 90 for s in range(512)], 128, 4000, 70, [s % 90 - s % 2 * (s % 90 // 3) for s in range(512)], [s % 3 for s in range(512)], [7] * 70, list(range(70))),
