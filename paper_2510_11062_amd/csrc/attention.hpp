@@ -1239,15 +1239,15 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
           for (int i = 0; i < 4; ++i) f[x & 1][i] = *reinterpret_cast<const bf16x8*>(kt + (read_k ^ ((2 * x + (i >> 1)) << 5)) + (i & 1) * 32 * 2 * D);
         };
         if (!idle) {
-        read_k_group(0);
+          read_k_group(0);
 #pragma unroll
-        for (int x = 0; x < KC / 2; ++x) {
-          if (x + 1 < KC / 2) read_k_group(x + 1);
-          __builtin_amdgcn_sched_barrier(0);
+          for (int x = 0; x < KC / 2; ++x) {
+            if (x + 1 < KC / 2) read_k_group(x + 1);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 1][i], __builtin_bit_cast(bf16x8, q[2 * x + (i >> 1)]), s[i & 1], 0, 0, 0);
-        }
+            for (int i = 0; i < 4; ++i)
+              s[i & 1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[x & 1][i], __builtin_bit_cast(bf16x8, q[2 * x + (i >> 1)]), s[i & 1], 0, 0, 0);
+          }
         }
         if (more && t + kWideTok >= k1) load_q(run.x, next);      // the last scores of this run are on their way
         auto read_v_group = [&](int k) {      // 16 tokens, all blocks of 32 elements or half of them
@@ -1279,22 +1279,22 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
             }
         }
         if (!idle) {
-        float high = -INFINITY;
+          float high = -INFINITY;
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+          for (int y = 0; y < 2; ++y)
 #pragma unroll
-          for (int i = 0; i < 16; i += 2) high = max3(high, s[y][i], s[y][i + 1]);
-        high *= to_log2;
-        if (__any(high > top + kSlack)) {
-          high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
-          if (TREE && !(high > top + kSlack)) high = top;      // as EACH there
-          const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top - now);
-          top = high;
-          ref = now;
-          sum *= keep;
+            for (int i = 0; i < 16; i += 2) high = max3(high, s[y][i], s[y][i + 1]);
+          high *= to_log2;
+          if (__any(high > top + kSlack)) {
+            high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
+            if (TREE && !(high > top + kSlack)) high = top;      // as EACH there
+            const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top - now);
+            top = high;
+            ref = now;
+            sum *= keep;
 #pragma unroll
-          for (int x = 0; x < DT; ++x) acc[x] *= keep;
-        }
+            for (int x = 0; x < DT; ++x) acc[x] *= keep;
+          }
         }
         bool apart = false;
         if (partly) {
@@ -1325,36 +1325,36 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
           if (!idle) read_v_group(0);
         }
         if (!idle) {
-        uint4 w[2];
-        auto weigh = [&](int ks) {
-          float p[8];
+          uint4 w[2];
+          auto weigh = [&](int ks) {
+            float p[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            p[j] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + j], to_log2, -ref));
-            sum += p[j];
-          }
-          w[ks & 1] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
-        };
-        weigh(0);
+            for (int j = 0; j < 8; ++j) {
+              p[j] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + j], to_log2, -ref));
+              sum += p[j];
+            }
+            w[ks & 1] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
+          };
+          weigh(0);
 #pragma unroll
-        for (int k = 0; k < 4 * VG; ++k) {
-          const int ks = k / VG;
-          __builtin_amdgcn_sched_barrier(0);
-          const bool weighing = k % VG == 0 && ks < 3;
-          if (k + 1 < 4 * VG) read_v_group(k + 1);
-          if (weighing) weigh(ks + 1);      // the next tokens' weights are computed between this step's products
+          for (int k = 0; k < 4 * VG; ++k) {
+            const int ks = k / VG;
+            __builtin_amdgcn_sched_barrier(0);
+            const bool weighing = k % VG == 0 && ks < 3;
+            if (k + 1 < 4 * VG) read_v_group(k + 1);
+            if (weighing) weigh(ks + 1);      // the next tokens' weights are computed between this step's products
 #pragma unroll
-          for (int x = 0; x < DB; ++x)
-            acc[DB * (k % VG) + x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[k & 1][x], __builtin_bit_cast(bf16x8, w[ks & 1]), acc[DB * (k % VG) + x], 0, 0, 0);
-          if (weighing) {
-            __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);      // LDS reads, then a product and some of the weights in turn
+            for (int x = 0; x < DB; ++x)
+              acc[DB * (k % VG) + x] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f[k & 1][x], __builtin_bit_cast(bf16x8, w[ks & 1]), acc[DB * (k % VG) + x], 0, 0, 0);
+            if (weighing) {
+              __builtin_amdgcn_sched_group_barrier(0x100, 2 * DB, 0);      // LDS reads, then a product and some of the weights in turn
 #pragma unroll
-            for (int x = 0; x < DB; ++x) {
-              __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
-              __builtin_amdgcn_sched_group_barrier(0x402, 28 / DB, 0);
+              for (int x = 0; x < DB; ++x) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x402, 28 / DB, 0);
+              }
             }
           }
-        }
         }
       }
       from = to;
