@@ -7,7 +7,8 @@
  * masked averaging per policy (Eq. 2; per-model batches B_m of Sec. 3) and its gradients
  * with respect to the final hidden states and the head weights.  Beside that, of the layers in front of
  * the head: norms and rotation of queries and keys with their gradient, a paged cache of the rollout's keys
- * and values, and attention over it.
+ * and values, and attention over it.  For rollouts that draft their tokens: the plan of a step's pages, attention
+ * of trees of drafted tokens, and the rules of sampling on rows of logits.
  *
  * Conventions common to every call
  *   - Pointers are DEVICE pointers unless the comment says "host".  The caller owns every
@@ -18,7 +19,7 @@
  *     bytes, 256-byte aligned.  Its first int32 is an error word: 0, or the bit-or of
  *     AT_GRPO_DATA_* flags raised by data that is only visible on the device.  Offending
  *     elements are treated as masked out.  Read it after synchronising the stream.  (The calls on queries,
- *     keys and the cache use the first word as scratch: they raise their flags in `data_error`.)
+ *     keys and the cache, on drafted tokens and on logits use the first word as scratch: they raise their flags in `data_error`.)
  *   - Return value: an at_grpo_status.  Argument errors are detected on the host before
  *     anything is launched; nothing is thrown and nothing aborts.
  *   - Matrices are row-major and dense.  `hidden` is [n_tok, H]; each head W is [V, H].
@@ -609,10 +610,10 @@ typedef struct {
  * All arithmetic is fp32, each operation rounded by itself (repetition by division, the temperature by its reciprocal), out rounded once.
  * best is the lowest of the tokens with the largest x, taken in front of the temperature; a row of which nothing is left gets best -1 and
  * lse -inf.  A NaN logit that a mask leaves makes lse NaN and is passed over by best.
- * Without any penalty the lists of tokens are not looked at.  A row of no sequence (also where cu_q falls or leaves its range there: AT_GRPO_DATA_SEQLENS) has its mask and nothing else.  Tokens outside
- * [0, V) are passed over (AT_GRPO_DATA_TOKEN_RANGE), a length or list out of range counts as empty (AT_GRPO_DATA_SEQLENS), a
- * repetition or temperature that is not positive and finite, or whose reciprocal is not, as 1, a presence or frequency that is not finite as 0 and a mask_row out of
- * range as -1 (AT_GRPO_DATA_RULE).  Workspace: at_grpo_logit_rules_workspace_bytes (0 on invalid arguments; no pointer is read).
+ * Without any penalty the lists of tokens are not looked at.  A row of no sequence (also where cu_q falls or leaves its range there:
+ * AT_GRPO_DATA_SEQLENS) has its mask and nothing else.  Tokens outside [0, V) are passed over (AT_GRPO_DATA_TOKEN_RANGE), a length or
+ * list out of range counts as empty (AT_GRPO_DATA_SEQLENS), a repetition or temperature that is not positive and finite, or whose
+ * reciprocal is not, as 1, a presence or frequency that is not finite as 0 and a mask_row out of range as -1 (AT_GRPO_DATA_RULE).  Workspace: at_grpo_logit_rules_workspace_bytes (0 on invalid arguments; no pointer is read).
  */
 int at_grpo_logit_rules(const at_grpo_sampling_rules* rules, int32_t n_rows, const void* logits,
                         int64_t logits_stride, void* out, int64_t out_stride, float* lse, int32_t* best,

@@ -188,7 +188,7 @@ def load_library():
 
 def load_binding():
     """Loads _binding.so (built in-tree with the library) for the calls that go through it: two that group responses, and those on
-    queries, keys and the rollout's cache; raises if it is missing or was built for another torch.  Every other call does without."""
+    queries, keys, the rollout's cache, drafted tokens and rows of logits; raises if it is missing or was built for another torch.  Every other call does without."""
     global _binding, _group_fn, _mixed_fn
     if _binding is None:
         lib = load_library()

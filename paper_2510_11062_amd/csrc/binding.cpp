@@ -2,7 +2,8 @@
 //
 // A grouping call of a training step is 7 to 17 us of kernels, so what the host does around it is what a program waits for: of 16.3
 // us for 64 responses, seven outputs made one by one from Python were 9, the checks and pointers of the arguments 3.  A rollout's token
-// takes 4 us of rotation, 4 of appending and 14 of attention a layer; made from Python, the first two took 18 and 24, now 6 and 6.5.  Everything else in
+// takes 4 us of rotation, 4 of appending and 14 of attention a layer; made from Python, the first two took 18 and 24, now 6 and 6.5.  The plan of
+// a step is 4 us of kernel with up to seven outputs, rules on the logits of four candidates 12, and both go this way too.  Everything else in
 // api.py stays Python: those calls' kernels are longer than what the host does in front of them.
 #include <Python.h>
 

@@ -7,8 +7,8 @@
 // logits at a time are in a lane's registers; the rules are applied there, and the row's largest and its sum of exponentials come from the
 // same registers.  A second kernel joins the parts of a row.
 //
-// Rows of 151936 in bf16: 1339 under masks alone, read and not written, 86 us (4.7 TB/s, a large copy 4.9); 682 rewritten without lists 87 us
-// (5.0 TB/s), with prompts, own tokens and drafted paths 103, with biases too 114: the lists' atomics, barriers and branches.
+// Rows of 151936 in bf16: 1339 under masks alone, read and not written, 80 to 86 us (4.8 to 5.1 TB/s, a large copy 4.9); 682 rewritten without lists 87 us
+// (5.0 TB/s), with prompts, own tokens and drafted paths 103, with biases too 110 to 114: the lists' atomics, barriers and branches.
 #include "kv_common.hpp"
 
 #include <math.h>
