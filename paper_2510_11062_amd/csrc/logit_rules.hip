@@ -35,6 +35,9 @@ struct RulePart {
 // What exponents are taken relative to.  x itself, not its multiple by log2e: a row of the type's lowest values would be infinite so.
 __device__ __forceinline__ float reference(float top) { return fabsf(top) < INFINITY ? top : 0.f; }
 
+// The temperature's reciprocal for exponents to the base 2: finite, since differences of 0 are multiplied by it.
+__device__ __forceinline__ float exponents(float to_out) { return fminf(to_out * kLog2e, 0x1.fffffep127f); }
+
 // A sum relative to `of` as one relative to `to`.  An empty one stays: its reference says nothing.
 __device__ __forceinline__ float moved(float sum, float of, float to, float to_log2) {
   return sum == 0.f ? 0.f : sum * __builtin_amdgcn_exp2f((reference(of) - reference(to)) * to_log2);
@@ -292,7 +295,7 @@ __global__ __launch_bounds__(kRuleThreads, LISTS == LONG ? 2 : 4) void k_rules(R
 #pragma unroll
   for (int i = 0; i < kRuleSteps; ++i)
     if (i < whole0) load_bits(chunk0, i);
-  const float one_over = 1.f / rules.repetition, to_log2 = rules.to_out * kLog2e;
+  const float one_over = 1.f / rules.repetition, to_log2 = exponents(rules.to_out);
   float top = -INFINITY, scaled = 0.f, sum = 0.f;      // of the wavefront's tokens, its multiple as exponents have it, and of this thread's
   int first = 0x7fffffff;
   // The rules on eight tokens from `token` on, of which the row has `have`; `at` is their place in the chunk.
@@ -455,7 +458,7 @@ __global__ __launch_bounds__(256) void k_rules_join(RuleArgs a) {
   int first = 0x7fffffff;
   for (int c = lane; c < a.splits; c += 64) {
     const RulePart p = parts[c];
-    sum += moved(p.sum, p.top, top, to_out * kLog2e);
+    sum += moved(p.sum, p.top, top, exponents(to_out));
     if (p.top == top) first = min(first, p.best);
   }
   sum = wave_sum_all(sum);

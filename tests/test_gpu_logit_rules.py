@@ -412,6 +412,43 @@ def test_settings_that_are_not_positive(gpu_device, value):
 
 
 @pytest.mark.gpu
+@pytest.mark.parametrize("V", [500, 9000])
+def test_a_temperature_at_the_end_of_the_range(gpu_device, V):
+    """Its reciprocal is finite, and times log2 e it is not.  out: the reciprocal's rounding and the product's, neither of which is of small
+    numbers; lse: ln of a count (two roundings and the exponential's unit), or the largest itself."""
+    logits = torch.full((2, V), -1.0)
+    logits[0, 3::7], logits[1], logits[1, V - 2] = 0.0, 0.0, 1.0
+    temperature, word = torch.full((2,), 3.5e-39), torch.zeros(1, dtype=torch.int32, device=gpu_device)
+    rules = api.LogitRules(temperature=temperature.to(gpu_device))
+    o = api.at_grpo_logit_rules(rules, logits.to(gpu_device), data_error=word)
+    want = logits.double() / temperature.double()[:, None]
+    assert int(word) == 0 and o["best"].tolist() == [3, V - 2]
+    assert ((o["out"].cpu().double() - want).abs() <= 2.01 * U32 * want.abs()).all()
+    n = np.log(len(range(3, V, 7)))
+    assert abs(float(o["lse"][0]) - n) <= 8 * U32 * n and abs(float(o["lse"][1]) - float(want[1].max())) <= 3.01 * U32 * float(want[1].max())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("biases", [False, True])
+def test_quotients_past_the_range(gpu_device, biases):
+    """A repetition so small that what occurs in front is multiplied out of the range: infinite, no NaN."""
+    V, r = 700, np.float32(1e-38)
+    logits = torch.zeros(2, V)
+    logits[:, 5], logits[0, 9], logits[1, 9] = 2.0, 10.0, -10.0
+    dev, i32 = gpu_device, lambda x: torch.tensor(x, dtype=torch.int32, device=gpu_device)
+    more = dict(bias_cu=i32([0, 1, 1]), bias_token=i32([600]), bias=torch.zeros(1, device=dev)) if biases else {}
+    rules = api.LogitRules(tokens=i32([[5, 9], [5, 9]]), length=i32([2, 2]), repetition=torch.full((2,), float(r)).to(dev), **more)
+    word = torch.zeros(1, dtype=torch.int32, device=dev)
+    o = api.at_grpo_logit_rules(rules, logits.to(dev), data_error=word)
+    out, two = o["out"].cpu(), 2 / float(r)
+    assert int(word) == 0 and o["best"].tolist() == [9, 5] and float(out[0, 9]) == float("inf") == float(o["lse"][0])
+    assert all(abs(float(out[t, 5]) - two) <= 1.01 * U32 * two for t in (0, 1)) and abs(float(o["lse"][1]) - two) <= 3.01 * U32 * two
+    assert abs(float(out[1, 9]) + 10 * float(r)) <= 1.01 * U32 * 10 * float(r)
+    rest = [v for v in range(V) if v not in (5, 9)]
+    assert (out[:, rest] == 0).all()
+
+
+@pytest.mark.gpu
 def test_rows_of_no_sequence(gpu_device):
     """In front of the first and behind the last: their masks and nothing else."""
     r = draw(np.random.default_rng(12), "f32", 700, 3, [2, 1, 2], (3,))
