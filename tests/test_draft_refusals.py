@@ -69,7 +69,8 @@ def call_rules(f):
 @pytest.mark.parametrize("over,status", [
     (dict(n_rows=-1), EINVAL), (dict(V=0), EINVAL), (dict(n_seq=-1), EINVAL), (dict(n_group=-1), EINVAL), (dict(max_tokens=-1), EINVAL), (dict(max_prompt=-1), EINVAL),
     (dict(n_bias=-1), EINVAL), (dict(n_mask=-1), EINVAL), (dict(dtype=2), EUNSUPPORTED), (dict(dtype=0), EUNSUPPORTED), (dict(out_dtype=2), EUNSUPPORTED),
-    (dict(V=2 ** 31 - 1), EUNSUPPORTED), (dict(V=1 << 30, n_rows=1 << 20, stride=1 << 30, out_stride=1 << 30), EUNSUPPORTED),
+    (dict(V=2 ** 31 - 1), EUNSUPPORTED), (dict(max_tokens=2 ** 31 - 1), EUNSUPPORTED), (dict(max_prompt=2 ** 31 - 1), EUNSUPPORTED),
+    (dict(n_bias=2 ** 31 - 1), EUNSUPPORTED), (dict(V=1 << 30, n_rows=1 << 20, stride=1 << 30, out_stride=1 << 30), EUNSUPPORTED),
     (dict(cu_q=None), EINVAL), (dict(logits=None), EINVAL), (dict(out=None, lse=None, best=None), EINVAL), (dict(stride=999), EINVAL), (dict(out_stride=999), EINVAL),
     (dict(length=None), EINVAL), (dict(group_seq=None), EINVAL), (dict(prompt_len=None), EINVAL), (dict(drafted=None), EINVAL), (dict(bias_token=None), EINVAL),
     (dict(bias=None), EINVAL), (dict(mask_row=None), EINVAL), (dict(logits=(1 << 51) + 1), EINVAL), (dict(out=(1 << 51) + 1), EINVAL),
