@@ -25,6 +25,9 @@ constexpr int kRuleThreads = 256, kRuleSteps = 4, kStepTokens = 8 * kRuleThreads
 constexpr uint32_t kInPrompt = 0x80000000u;
 constexpr int kBiasShift = 16, kMostBiases = 0x7fff, kMostTokens = 0xffff, kNearBiases = 512;
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+// Up to where the largest's multiple is subtracted from the others': rounded, it is off by half a unit of its last place, which is in every exponent
+// then.  Here that is at most 2^-5, and never more than half a unit of the log-sum; at 2^32 it is past 127, where sums are infinite or 0.
+constexpr float kMostScaled = 0x1p20f;
 
 // Of a workgroup's tokens: the largest x, where it is first, and sum exp((x - reference(top)) to_out).
 struct RulePart {
@@ -359,10 +362,10 @@ __global__ __launch_bounds__(kRuleThreads, LISTS == LONG ? 2 : 4) void k_rules(R
       }
     }
     if (a.lse) {
-      if (fabsf(scaled) < 1e30f) {
+      if (fabsf(scaled) < kMostScaled) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f(__builtin_fmaf(z[j], to_log2, -scaled));
-      } else {      // numbers near the ends of the range: their multiples may be infinite, their differences not
+      } else {      // differences first: 0 for the largest itself, also where multiples are infinite
         const float ref = reference(top);
 #pragma unroll
         for (int j = 0; j < 8; ++j) sum += __builtin_amdgcn_exp2f((z[j] - ref) * to_log2);
