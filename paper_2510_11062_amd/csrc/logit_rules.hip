@@ -216,11 +216,9 @@ struct List {
   }
 };
 
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float x;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
-  return x;
-}
+// The largest of three, or NaN where one of them is NaN of either kind: v_maximum3_f32.  v_max3_f32 passes NaN over, and what it has seen in front of
+// a signalling one with it.
+__device__ __forceinline__ float maximum3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 __device__ __forceinline__ float wave_max(float x) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
@@ -349,9 +347,12 @@ __global__ __launch_bounds__(kRuleThreads, LISTS == LONG ? 2 : 4) void k_rules(R
       }
     }
     if (!a.parts) return;
-    // Four instructions; those that fmaxf makes of signalling NaN bring it to fifteen.  Here one may come out as NaN, and is looked at as a larger one is.
-    if (__any(!(max3(max3(max3(z[0], z[1], z[2]), z[3], z[4]), z[5], max3(z[6], z[7], z[7])) <= top))) {      // seldom, once a wavefront has seen some of its tokens
-      const float now = wave_max(fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7]))));
+    // Four instructions; fmaxf, which has to quiet signalling NaN first, takes fifteen.  A NaN comes out as one, and is looked at as a larger one is.
+    if (__any(!(maximum3(maximum3(maximum3(z[0], z[1], z[2]), z[3], z[4]), z[5], maximum3(z[6], z[7], z[7])) <= top))) {      // seldom, once a wavefront has seen some of its tokens
+      float high = -INFINITY;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) high = z[j] > high ? z[j] : high;      // NaN of either kind is passed over; of several fmaxf the compiler makes v_max3_f32
+      const float now = wave_max(high);
       if (now > top) {
         sum = moved(sum, top, now, to_log2);
         top = now;

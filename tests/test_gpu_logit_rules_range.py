@@ -1,8 +1,9 @@
-"""Log-sums where the largest logit over the temperature is far from the range of exponents."""
+"""Log-sums and best tokens where the largest logit over the temperature is far from the range of exponents, and beside NaN of either kind."""
 import numpy as np
 import pytest
 import torch
 
+from oracle import draft_oracle as oracle
 from paper_2510_11062_amd import api
 from tests.rollout_case import DTYPES, U32, rounded, to_dev
 from tests.test_gpu_logit_rules import Rows, apply, compare, draw
@@ -74,3 +75,53 @@ def test_small_temperatures_in_many_rows(gpu_device, dtype, n, V):
         bound = U32 * (2.02 * most + 8 * most + 50 + V / 8192 + 8 * lse.abs())
         off = (o["lse"][rows].double() - lse).abs()
         assert bool((off <= bound).all()), f"{float((off / bound).max())} times the bound"
+
+
+# ---- NaN ------------------------------------------------------------------------------------------------
+# bits of a NaN that signals (the first bit of its mantissa is 0), and of one that does not
+SIGNALLING = {"bf16": [0x7f81, 0x7fa0, -0x007f], "f32": [0x7f800001, 0x7fa00000, -0x007fffff]}
+QUIET = {"bf16": [0x7fc0, -0x0040], "f32": [0x7fc00000, -0x00400000]}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["signalling", "quiet"])
+@pytest.mark.parametrize("V", [40, 2048, 8200])
+def test_the_best_beside_nan(gpu_device, dtype, kind, V):
+    """A NaN is passed over by best, wherever among eight neighbours it and the largest stand, and whatever rules there are; lse is NaN, or where a
+    mask takes the NaN out what is left has it."""
+    ints = torch.int16 if dtype == "bf16" else torch.int32
+    rs = np.random.default_rng(V)
+    for bits in (SIGNALLING if kind == "signalling" else QUIET)[dtype]:
+        for first in (0, V // 16 * 8, V - 8):
+            at = [(first + i, first + j) for i in range(8) for j in range(8) if i != j]
+            logits = to_dev(rounded(rs.normal(size=(len(at), V)), DTYPES[dtype]), DTYPES[dtype], gpu_device)
+            rows = torch.arange(len(at), device=gpu_device)
+            nan, best = (torch.tensor(x, device=gpu_device) for x in zip(*at))
+            logits[rows, best] = 100.0
+            plain = logits.clone()
+            logits.view(ints)[rows, nan] = bits
+            assert bool(torch.isnan(logits[rows, nan]).all()) and bool((logits.view(ints)[rows, nan] == bits).all())
+            n = len(at)
+            zeros = torch.zeros(n, 1, dtype=torch.int32, device=gpu_device)
+            one = torch.ones(n, dtype=torch.int32, device=gpu_device)
+            lists = dict(tokens=zeros + (first + 9) % V, length=one, presence=torch.full((n,), 0.5, device=gpu_device))
+            biases = dict(bias_cu=torch.arange(n + 1, dtype=torch.int32, device=gpu_device), bias_token=one * ((first + 11) % V),
+                          bias=torch.full((n,), -0.5, device=gpu_device))
+            for rules in (api.LogitRules(), api.LogitRules(**lists), api.LogitRules(**lists, **biases), api.LogitRules(**biases)):
+                o = api.at_grpo_logit_rules(rules, logits)
+                assert torch.equal(o["best"].long(), best), (first, bits)
+                assert bool(torch.isnan(o["lse"]).all()) and bool(torch.isnan(o["out"][rows, nan]).all())
+                assert int(torch.isnan(o["out"]).sum()) == n
+            # masked
+            words = torch.full((n, (V + 31) // 32), -1, dtype=torch.int32, device=gpu_device)
+            words[rows, nan // 32] = (-1 ^ (1 << (nan % 32))).to(torch.int32)
+            rules = api.LogitRules(allowed=words, mask_row=rows.to(torch.int32))
+            got, want = api.at_grpo_logit_rules(rules, logits), api.at_grpo_logit_rules(rules, plain)
+            assert all(torch.equal(got[name], want[name]) for name in ("out", "lse", "best")) and torch.equal(got["best"].long(), best)
+
+
+def test_the_oracle_passes_nan_over():
+    out, lse, best, _ = oracle.sampling_row(np.array([1.0, np.nan, 5.0]), [], [], 1, 0, 0, 1, {}, None)
+    assert best == 2 and np.isnan(lse) and np.isnan(out[1])
+    assert oracle.sampling_row(np.array([1.0, np.nan, 5.0]), [], [], 1, 0, 0, 1, {}, np.array([True, False, True]))[1] == pytest.approx(5 + np.log1p(np.exp(-4)))
