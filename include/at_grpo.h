@@ -525,7 +525,7 @@ typedef struct {
   int32_t page_size;             /* a power of two, 8 .. 65536                                           */
   int32_t n_pages;               /* of the cache: what the ring has room for                             */
   int32_t n_seq, max_pages;      /* rows and columns of pages; n_seq * max_pages < 2^31, max_pages * page_size <= 2^30 */
-  int32_t n_group;               /* 0: no prefixes                                                       */
+  int32_t n_group;               /* 0: no prefixes; at most 2^30 - 2^8                                   */
   int32_t* pages;                /* [n_seq, max_pages]                                                   */
   int32_t* ring;                 /* [n_pages]                                                            */
   const int32_t* group_seq;      /* [n_group + 1], not falling, as in at_grpo_kv                         */
@@ -585,7 +585,7 @@ size_t at_grpo_tree_attention_workspace_bytes(const at_grpo_kv* kv, int32_t n_to
  */
 typedef struct {
   int32_t dtype, out_dtype;      /* of the logits; of out: the same, or AT_GRPO_F32                      */
-  int32_t V, n_seq, n_group;
+  int32_t V, n_seq, n_group;     /* V <= 2^30; sequences, groups and entries of a list: at most 2^31 - 2^16 */
   int32_t max_tokens, max_prompt; /* columns of tokens and prompt                                        */
   int32_t n_bias, n_mask;        /* entries of all bias lists; rows of allowed                           */
   const int32_t* cu_q;           /* [n_seq + 1], not falling; NULL: n_rows == n_seq                      */

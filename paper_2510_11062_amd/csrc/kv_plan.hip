@@ -441,9 +441,9 @@ extern "C" int at_grpo_kv_plan(const at_grpo_page_pool* pool, int32_t n_tok, con
                                void* hip_stream) {
   if (!pool || n_tok < 0 || pool->n_pages <= 0 || pool->n_seq < 0 || pool->max_pages < 0 || pool->n_group < 0) return AT_GRPO_EINVAL;
   if (pool->page_size < 8 || pool->page_size > 65536 || (pool->page_size & (pool->page_size - 1))) return AT_GRPO_EUNSUPPORTED;
-  // places, pages of all sequences and threads of a launch are counted in 32 bits
+  // places, pages of all sequences, groups (a thread's next is up to 1024 further) and threads of a launch are counted in 32 bits
   if (static_cast<int64_t>(pool->max_pages) * pool->page_size > 1 << 30 || static_cast<int64_t>(pool->n_seq) * pool->max_pages > 0x7fffffff ||
-      n_tok > 0x7fffff00 || pool->n_seq > 0x3fffff00)
+      n_tok > 0x7fffff00 || pool->n_seq > 0x3fffff00 || pool->n_group > 0x3fffff00)
     return AT_GRPO_EUNSUPPORTED;
   const size_t S = pool->n_seq, T = n_tok, word = sizeof(int32_t);
   if (!pool->ring || !state || !state_out || !cu_q || (S > 0 && (!length || !add || !length_out || (pool->max_pages > 0 && !pool->pages)))) return AT_GRPO_EINVAL;

@@ -477,8 +477,9 @@ int check_rules(const at_grpo_sampling_rules* r, int32_t n_rows) {
     return AT_GRPO_EINVAL;
   if (r->dtype != AT_GRPO_F32 && r->dtype != AT_GRPO_BF16) return AT_GRPO_EUNSUPPORTED;
   if (r->out_dtype != r->dtype && r->out_dtype != AT_GRPO_F32) return AT_GRPO_EUNSUPPORTED;
-  // tokens, places in lists and the workgroups of a launch are counted in 32 bits; places go past a list's end by less than 2^16
-  if (r->max_tokens > 0x7fff0000 || r->max_prompt > 0x7fff0000 || r->n_bias > 0x7fff0000) return AT_GRPO_EUNSUPPORTED;
+  // tokens, places in lists, sequences, groups and the workgroups of a launch are counted in 32 bits; places go past a list's end by less than 2^16
+  const int32_t most = 0x7fff0000;
+  if (r->max_tokens > most || r->max_prompt > most || r->n_bias > most || r->n_seq > most || r->n_group > most) return AT_GRPO_EUNSUPPORTED;
   return r->V <= 0x40000000 && ceil_div(r->V, kRuleChunk) * n_rows < 0x7f000000 ? AT_GRPO_OK : AT_GRPO_EUNSUPPORTED;
 }
 
