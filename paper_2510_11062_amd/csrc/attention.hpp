@@ -1078,7 +1078,6 @@ __device__ __forceinline__ int swizzle_v(int r) { return D >= 128 ? 2 * (r & 7) 
 
 template <int D, bool EXACT, bool TREE>
 __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv, Args a) {
-  constexpr int BUFFERS = 2, AHEAD = 1;
   constexpr int KC = D / 16, DT = D / 32, TB = kWideTok * D * 2, NL = TB / 4096, PIECES = D / 8, LROWS = 64 / PIECES, VG = DT > 4 ? 2 : 1, DB = DT / VG;
   extern __shared__ __attribute__((aligned(1024))) char smem[];      // two tiles of keys and values, then the rest
   WideLds& lds = *reinterpret_cast<WideLds*>(smem + 4 * TB);
@@ -1104,7 +1103,6 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 
   // Page ids of tokens page0 << page_shift .. in LDS: a unit's all, where they fit, for all its runs.
   int page0 = 0, staged = -1;
-  const int* const pages = lds.pages;
   bool holes = false;
   auto stage = [&](const int32_t* table, int first_token, int to) {
     page0 = first_token >> kv.page_shift;
@@ -1123,13 +1121,13 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
     holes = __syncthreads_or(missing);
   };
   // A tile of tokens t .. into a buffer; rows behind the last token are the last.
-  auto request = [&](int hk, int t, int to, int buffer, const int* pages, int page0) {
+  auto request = [&](int hk, int t, int to, int buffer) {
     const char* const kbase = static_cast<const char*>(kv.k) + ((static_cast<int64_t>(hk) * dim * 2) << kv.page_shift);
     const char* const vbase = static_cast<const char*>(kv.v) + ((static_cast<int64_t>(hk) * dim * 2) << kv.page_shift);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       const int row = (wave * NL + i) * LROWS + lane / PIECES, piece = lane & (PIECES - 1), token = min(t + row, to - 1);
-      const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(max(0, pages[(token >> kv.page_shift) - page0]))) * page_bytes;
+      const uint64_t at = static_cast<uint64_t>(static_cast<uint32_t>(max(0, lds.pages[(token >> kv.page_shift) - page0]))) * page_bytes;
       const uint32_t in = static_cast<uint32_t>(token & in_page) * (2 * dim);
       const int of_k = piece ^ swizzle_k<D>(row), of_v = piece ^ swizzle_v<D>(row);
       if (EXACT || 8 * of_k < dim) direct_load_v(kbase + (at + (in + 16 * of_k)), lds0 + buffer * 2 * TB + i * 1024);
@@ -1143,8 +1141,8 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 #pragma unroll
     for (int c = 0; c < KC; ++c) q[c] = EXACT || 16 * c + 8 * g < dim ? *reinterpret_cast<const uint4*>(from + 16 * c) : make_uint4(0, 0, 0, 0);
   };
-  int buffer = 0, requested = 0;      // of the run's first tiles, by the run in front of it
-  auto behind = [&](int tiles) { return buffer + tiles < BUFFERS ? buffer + tiles : buffer + tiles - BUFFERS; };
+  int buffer = 0;
+  bool requested = false;      // the run's first tile, by the run in front of it
   TileRun w = tile_run(run, a);
   load_q(run.x, w);
   for (;;) {
@@ -1179,7 +1177,6 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
       for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
     float top = -INFINITY, ref = 0.f, sum = 0.f;
     const bool idle = TREE && w.r0 + 32 * wave >= rows;      // no rows: it loads and waits with the others
-    int next_requested = 0;
 
     for (int from = w.k0; from < k1;) {
       int to = k1;
@@ -1188,23 +1185,17 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
         stage(table, from, to);
         staged = -1;
       }
-      const int tiles = (to - from + kWideTok - 1) / kWideTok;
-      int asked = requested;      // tiles of these, in buffers behind each other
-      for (; asked < min(AHEAD, tiles); ++asked) request(w.hk, from + asked * kWideTok, to, behind(asked), pages, page0);
-      requested = 0;
-      for (int t = from, number = 0; t < to; t += kWideTok, ++number, buffer = behind(1)) {
+      if (!requested) request(w.hk, from, to, buffer);
+      requested = false;
+      for (int t = from; t < to; t += kWideTok, buffer ^= 1) {
         asm volatile("" ::: "memory");
         wait_loads_but<0>();
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
-        // the tile that comes AHEAD from here, or the next run's first: its buffer is free, since who has passed this barrier has read the tile in front
-        if (asked < tiles) {
-          request(w.hk, from + asked * kWideTok, to, behind(asked - number), pages, page0);
-          ++asked;
-        } else if (ahead && to == k1 && next.k0 + next_requested * kWideTok < next.k1) {
-          request(next.hk, next.k0 + next_requested * kWideTok, next.k1, behind(tiles - number + next_requested), pages, page0);
-          ++next_requested;
-        }
+        // The next tile, or the next run's first: its buffer is free, since who has passed this barrier has read the tile in front.  Asked for in one
+        // place: in two it takes 12 registers more (trees, heads of 128: 116 bytes of them in memory and not 28).
+        const bool inside = t + kWideTok < to;
+        if (inside || (ahead && to == k1)) request(inside ? w.hk : next.hk, inside ? t + kWideTok : next.k0, inside ? to : next.k1, buffer ^ 1);
         uint64_t path = 0;
         if constexpr (TREE)
           if (tree && t + kWideTok > all_see) path = a.ancestors[u.tok0 + token_of()];
@@ -1213,7 +1204,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
         if (holes || t + kWideTok > to) {      // what stands for a token behind the last or of no page counts as 0
           for (int i = tid; i < kWideTok * PIECES; i += 256) {
             const int token = t + i / PIECES;
-            if (token >= to || pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
+            if (token >= to || lds.pages[(token >> kv.page_shift) - page0] < 0) *reinterpret_cast<uint4*>(vt + i * 16) = make_uint4(0, 0, 0, 0);
           }
           lds_barrier();
           asm volatile("" ::: "memory");
@@ -1269,7 +1260,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
             for (int b = 0; b < 4; ++b) {      // four tokens that start at a multiple of four share a page
               const int t4 = t + 32 * y + 8 * b + 4 * g;
               int left = limit - t4;
-              if (holes) left = pages[(min(t4, to - 1) >> kv.page_shift) - page0] < 0 ? 0 : left;
+              if (holes) left = lds.pages[(min(t4, to - 1) >> kv.page_shift) - page0] < 0 ? 0 : left;
 #pragma unroll
               for (int i = 0; i < 4; ++i) {
                 bool on = i < left;
@@ -1392,8 +1383,11 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
       }
     }
     if (!more) break;
-    requested = next_requested;
-    if (w.k0 >= w.k1) load_q(run.x, next);      // no tile, at which they were asked for
+    requested = ahead;
+    if (w.k0 >= w.k1) {      // no tile, at which they were asked for
+      load_q(run.x, next);
+      requested = false;
+    }
     w = next;
   }
 }
@@ -2200,6 +2194,7 @@ Choice choose_near(int D, bool large) {
 struct Plan {
   Choice choice;
   bool near, decode;
+  int64_t tiles;    // of k_tree_near: the most of a sequence and key head
   int coarse;
   double most;      // an upper bound of all costs together
 };
@@ -2215,6 +2210,7 @@ int make_plan(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q, Pl
   constexpr int run_cost = TREE ? kTreeRunCost : kRunCost;
   const double fixed = 8 + run_cost + kMinShare;
   out->near = false;
+  out->tiles = 0;
   if constexpr (TREE) {
     const int64_t room = (static_cast<int64_t>(kv->max_pages) + kv->max_prefix_pages) * kv->page_size;
     const int64_t rows = rows_o < 64 * share ? rows_o : 64 * share;
@@ -2226,7 +2222,8 @@ int make_plan(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, int32_t max_q, Pl
       out->choice = kv->dtype == AT_GRPO_BF16 ? choose_near<bf16_t>(kv->D, large) : choose_near<float>(kv->D, large);
       out->decode = false;
       out->coarse = 0;
-      out->most = static_cast<double>(tiles);
+      out->tiles = tiles;
+      out->most = 0;
       return AT_GRPO_OK;
     }
   }
@@ -2293,7 +2290,7 @@ int attend(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* 
   }
   ProfScope ps(PROF_ATTENTION, s);
   if (plan.near) {
-    hipLaunchKernelGGL(k.kernel, dim3(static_cast<unsigned>(plan.most), kv->Hk, kv->n_seq), dim3(256), 0, s, view, args);
+    hipLaunchKernelGGL(k.kernel, dim3(static_cast<unsigned>(plan.tiles), kv->Hk, kv->n_seq), dim3(256), 0, s, view, args);
     ATG_LAUNCH_CHECK();
     return AT_GRPO_OK;
   }
