@@ -370,13 +370,9 @@ template <typename V>
 __device__ __forceinline__ float element(const V& v, int e) {
   return __uint_as_float(e & 1 ? dword(v, e >> 1) & 0xffff0000u : dword(v, e >> 1) << 16);
 }
-// The largest of three, NaN passed over as fmaxf does.  Of numbers that no signalling NaN is among, as a matrix instruction's are: fmaxf takes an
-// instruction more for each to make sure.
-__device__ __forceinline__ float max3(float a, float b, float c) {
-  float x;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(x) : "v"(a), "v"(b), "v"(c));
-  return x;
-}
+// The largest of three, or NaN: v_maximum3_f32, where fmaxf takes an instruction more for each number that might be a signalling NaN.  Not in asm: what a matrix
+// instruction writes may be read only some cycles later, and the compiler waits for its own instructions alone.
+__device__ __forceinline__ float maximum3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 __device__ __forceinline__ bool not_finite(float x) { return (__float_as_uint(x) & 0x7f800000u) == 0x7f800000u; }
 // 0 in place of infinities and NaN
 __device__ __forceinline__ uint32_t finite_halves(uint32_t x) {
@@ -1274,7 +1270,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
 #pragma unroll
           for (int y = 0; y < 2; ++y)
 #pragma unroll
-            for (int i = 0; i < 16; i += 2) high = max3(high, s[y][i], s[y][i + 1]);
+            for (int i = 0; i < 16; i += 2) high = maximum3(high, s[y][i], s[y][i + 1]);
           high *= to_log2;
           if (__any(high > top + kSlack)) {
             high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
