@@ -52,6 +52,11 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 // The running maximum is raised where a score passes it by more than this (in powers of two): weights of at most 2^8 lose nothing in
 // fp32 sums, nor in bf16, whose error is relative, and most tokens then leave the sums as they are.
 constexpr float kSlack = 8.f;
+// Up to where a row's exponents are its scores' multiples less the largest's, in one instruction: that multiple is rounded, and half a unit of its last
+// place, here at most 2^-5, is in every exponent.  From 2^32 on it is past 127, where all weights are infinite or 0.
+// Differences for all rows would take an instruction a score: trees of 24 conversations, heads of 64, 81.6 us, by this branch 80.8, by neither 77.8; elsewhere
+// a tile's check costs up to 1 %, 0.1 to 0.6 us of calls of 8 to 20.
+constexpr float kFar = 0x1p20f;
 
 // x / d for 0 <= x < 2^31 by a product: ceil(2^(31 + k) / d) with 2^k >= d is off by less than one part in 2^31.
 struct Divisor {
@@ -467,6 +472,32 @@ __device__ __forceinline__ void set_apart(float* slab, typename Shape<T, D>::VV 
   }
 }
 
+// What a row's weights are relative to: `top`, its largest score at some time (-inf: none yet), and `lead`, that times log2 e and the scale.  Raises them to `high`,
+// the largest of a tile; returns what sums up to there are multiplied by.
+template <bool EACH>
+__device__ __forceinline__ float raise_top(float high, float to_log2, float& top, float& lead) {
+  if (EACH && !(high * to_log2 > lead + kSlack)) high = top;
+  top = fmaxf(high, top);
+  const float now = top * to_log2, keep = __builtin_amdgcn_exp2f(lead - (now == -INFINITY ? 0.f : now));
+  lead = now;
+  return keep;
+}
+// Far from 0 the scores of a tile become differences from the largest before their exponents are taken, so that it has none, and any larger one raises it.
+// `less` is what they are less by, `lead` 0 then.
+__device__ __forceinline__ bool is_far(float top, float lead) { return fabsf(lead) > kFar && top > -INFINITY; }
+__device__ __forceinline__ float raise_far(float high, float to_log2, float& top, float& lead, float& less) {
+  const bool far = is_far(top, lead);
+  const float now = far ? fmaxf(high, top) : top, keep = far ? __builtin_amdgcn_exp2f((top - now) * to_log2) : 1.f;
+  top = now;
+  less = far ? now : 0.f;
+  lead = far ? 0.f : lead;
+  return keep;
+}
+// The largest score's multiple; a number where the product is none.
+__device__ __forceinline__ float top_log2(float top, float to_log2) {
+  return top == -INFINITY ? top : fminf(fmaxf(top * to_log2, -0x1.fffffep127f), 0x1.fffffep127f);
+}
+
 // The tile's weights into the sums, and their products with its values into the accumulators; `before` the products, once these are scaled.
 // The matrix instruction takes bf16 weights with bf16 values, so a weight is rounded to 8 bits there (the sums take it as it is): an error
 // of up to 2^-8 of each term, of the order of the result's own rounding.  Against 64 bits bf16 results are off by 0.0023 (rounded once from
@@ -474,9 +505,9 @@ __device__ __forceinline__ void set_apart(float* slab, typename Shape<T, D>::VV 
 // EACH: a row's maximum is raised where its own score asks for it and not where another row's in the wavefront does, so that what one row sees
 // leaves the others' bits as they are.
 template <typename T, int D, bool EACH, int NR, typename Before>
-__device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::SUB], const typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB],
-                                              float to_log2, f32x4 (&acc)[NR][Shape<T, D>::NB][Shape<T, D>::E], float (&top)[NR], float (&ref)[NR],
-                                              float (&sum)[NR], Before before) {
+__device__ __forceinline__ void weigh_and_add(const typename Shape<T, D>::VV (&v)[Shape<T, D>::NB][4 * Shape<T, D>::SUB], f32x4 (&s)[NR][Shape<T, D>::SUB],
+                                              float to_log2, f32x4 (&acc)[NR][Shape<T, D>::NB][Shape<T, D>::E], float (&top)[NR], float (&sum)[NR],
+                                              Before before) {
   typedef Shape<T, D> Z;
   constexpr int E = Z::E, NB = Z::NB, SUB = Z::SUB;
   constexpr bool kBf16 = sizeof(T) == 2;
@@ -489,26 +520,34 @@ __device__ __forceinline__ void weigh_and_add(const f32x4 (&s)[NR][Shape<T, D>::
     for (int y = 0; y < SUB; ++y)
 #pragma unroll
       for (int i = 0; i < 4; ++i) high = fmaxf(high, s[n][y][i]);
-    high *= to_log2;
-    if (__any(high > top[n] + kSlack)) {
-      high = fmaxf(high, __shfl_xor(high, 16, 64));
-      high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top[n]);
-      if (EACH && !(high > top[n] + kSlack)) high = top[n];
-      const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top[n] - now);
-      top[n] = high;
-      ref[n] = now;
-      sum[n] *= keep;
+    float lead = top[n] * to_log2;
+    const auto keep = [&](float x) {
+      sum[n] *= x;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[n][b][e] *= keep;
+        for (int e = 0; e < E; ++e) acc[n][b][e] *= x;
+    };
+    const auto of_row = [&] {
+      const float x = fmaxf(high, __shfl_xor(high, 16, 64));
+      return fmaxf(x, __shfl_xor(x, 32, 64));
+    };
+    if (__any(high * to_log2 > lead + kSlack)) keep(raise_top<EACH>(of_row(), to_log2, top[n], lead));
+    if (__any(is_far(top[n], lead))) {
+      float less;
+      keep(raise_far(of_row(), to_log2, top[n], lead, less));
+#pragma unroll
+      for (int y = 0; y < SUB; ++y)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][y][i] -= less;
     }
+    const float minus = top[n] == -INFINITY ? 0.f : lead;
     float p[4 * SUB];
 #pragma unroll
     for (int y = 0; y < SUB; ++y)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        p[4 * y + i] = __builtin_amdgcn_exp2f(fmaf(s[n][y][i], to_log2, -ref[n]));
+        p[4 * y + i] = __builtin_amdgcn_exp2f(fmaf(s[n][y][i], to_log2, -minus));
         sum[n] += p[4 * y + i];
       }
     if constexpr (kBf16) {
@@ -557,7 +596,7 @@ __device__ __forceinline__ void finish(const Args& a, L& lds, const f32x4 (&acc)
     sum[n] += __shfl_xor(sum[n], 16, 64);
     sum[n] += __shfl_xor(sum[n], 32, 64);
     if (g == 0) {
-      lds.ml[wave][16 * n + m][0] = top[n];
+      lds.ml[wave][16 * n + m][0] = top_log2(top[n], a.scale * kLog2e);
       lds.ml[wave][16 * n + m][1] = sum[n];
     }
   }
@@ -966,11 +1005,10 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
       };
 
       f32x4 acc[NR][NB][E];
-      float top[NR], ref[NR], sum[NR];
+      float top[NR], sum[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         top[n] = -INFINITY;
-        ref[n] = 0.f;
         sum[n] = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -1025,7 +1063,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_decode(KvView kv, Ar
               }
             }
           }
-          weigh_and_add<T, D, TREE>(s, v, to_log2, acc, top, ref, sum, [&] {
+          weigh_and_add<T, D, TREE>(v, s, to_log2, acc, top, sum, [&] {
             // the one new token of a unit sees its stream whole: that of its sequence alone (in a tree itself only where its bit says so)
             if (tile.seq >= 0 && (TREE || u.ntok > 1))
               set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) {
@@ -1171,7 +1209,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
     for (int t = 0; t < DT; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) acc[t][i] = 0.f;
-    float top = -INFINITY, ref = 0.f, sum = 0.f;
+    float top = -INFINITY, sum = 0.f;
     const bool idle = TREE && w.r0 + 32 * wave >= rows;      // no rows: it loads and waits with the others
 
     for (int from = w.k0; from < k1;) {
@@ -1265,23 +1303,29 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
               }
             }
         }
+        float lead = 0.f;
         if (!idle) {
           float high = -INFINITY;
 #pragma unroll
           for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) high = maximum3(high, s[y][i], s[y][i + 1]);
-          high *= to_log2;
-          if (__any(high > top + kSlack)) {
-            high = fmaxf(fmaxf(high, __shfl_xor(high, 32, 64)), top);
-            if (TREE && !(high > top + kSlack)) high = top;      // as EACH there
-            const float now = high == -INFINITY ? 0.f : high, keep = __builtin_amdgcn_exp2f(top - now);
-            top = high;
-            ref = now;
-            sum *= keep;
+          lead = top * to_log2;
+          const auto keep = [&](float f) {
+            sum *= f;
 #pragma unroll
-            for (int x = 0; x < DT; ++x) acc[x] *= keep;
+            for (int x = 0; x < DT; ++x) acc[x] *= f;
+          };
+          if (__any(high * to_log2 > lead + kSlack)) keep(raise_top<TREE>(fmaxf(high, __shfl_xor(high, 32, 64)), to_log2, top, lead));
+          if (__any(is_far(top, lead))) {
+            float less;
+            keep(raise_far(fmaxf(high, __shfl_xor(high, 32, 64)), to_log2, top, lead, less));
+#pragma unroll
+            for (int y = 0; y < 2; ++y)
+#pragma unroll
+              for (int i = 0; i < 16; ++i) s[y][i] -= less;
           }
+          lead = top == -INFINITY ? 0.f : lead;
         }
         bool apart = false;
         if (partly) {
@@ -1317,7 +1361,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
             float p[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-              p[j] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + j], to_log2, -ref));
+              p[j] = __builtin_amdgcn_exp2f(fmaf(s[ks >> 1][8 * (ks & 1) + j], to_log2, -lead));
               sum += p[j];
             }
             w[ks & 1] = make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7]));
@@ -1351,7 +1395,7 @@ __global__ __launch_bounds__(256, kWidePerUnit<D>) void k_attend_wide(KvView kv,
     const int r = w.r0 + 32 * wave + m;
     if (r < rows) {
       const int tq = token_of(), h = w.hk * a.share + r - tq * a.share;
-      const float f = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), x = sum == 0.f ? -INFINITY : (ref + __builtin_amdgcn_logf(sum)) * kLn2;
+      const float f = sum == 0.f ? 0.f : __builtin_amdgcn_rcpf(sum), x = sum == 0.f ? -INFINITY : (top_log2(top, to_log2) + __builtin_amdgcn_logf(sum)) * kLn2;
       const int64_t by_query = static_cast<int64_t>(own && kv.n_group ? a.n_tok : 0) * a.Hq + static_cast<int64_t>(u.tok0 + tq) * a.Hq + h;
       if (direct) {
         if (a.lse && g == 0) a.lse[by_query] = x;
@@ -1524,11 +1568,10 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_attend(KvView kv, Ar
       }
       if (tree && u.ntok > kMostTree) raise_data_error(a.data_error, AT_GRPO_DATA_TREE);
       f32x4 acc[NR][NB][E];
-      float top[NR], ref[NR], sum[NR];
+      float top[NR], sum[NR];
 #pragma unroll
       for (int n = 0; n < NR; ++n) {
         top[n] = -INFINITY;
-        ref[n] = 0.f;
         sum[n] = 0.f;
 #pragma unroll
         for (int b = 0; b < NB; ++b)
@@ -1582,7 +1625,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_attend(KvView kv, Ar
               }
             }
           }
-          weigh_and_add<T, D, TREE>(s, v, to_log2, acc, top, ref, sum, [&] {
+          weigh_and_add<T, D, TREE>(v, s, to_log2, acc, top, sum, [&] {
             if (part && t + TOK > all_see)
               set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) {
                 if constexpr (tree) return t + token < limit[n] && (sees[n] >> token & 1);
@@ -2049,11 +2092,10 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_tree_near(KvView kv,
       }
     }
     f32x4 acc[NR][NB][E];
-    float top[NR], ref[NR], sum[NR];
+    float top[NR], sum[NR];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
       top[n] = -INFINITY;
-      ref[n] = 0.f;
       sum[n] = 0.f;
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -2091,7 +2133,7 @@ __global__ __launch_bounds__(256, (kPerUnit<D, NR>)) void k_tree_near(KvView kv,
             }
           }
         }
-        weigh_and_add<T, D, true>(z, v, to_log2, acc, top, ref, sum, [&] {
+        weigh_and_add<T, D, true>(v, z, to_log2, acc, top, sum, [&] {
           if (partly) set_apart<T, D>(lds.slab[wave][0], v, acc, [&](int n, int token) { return token < tile.last - tile.token && (sees[n] >> token & 1); });
         });
         load_v(next);
