@@ -500,7 +500,7 @@ int at_grpo_kv_append(const at_grpo_kv* kv, const at_grpo_norm_rope* layer, int3
  * Weights are divided by their sum at the end: the values of V times 2^8 times the visible tokens have to stay in fp32's
  * range.
  * max_q (host): an upper bound of the new tokens of one sequence; it picks the kernel, results do not depend on
- * it but for rounding.  scale > 0.  Scores and sums are fp32; bf16 weights are rounded to bf16 for the product
+ * it but for rounding.  scale > 0, finite times log2 e.  Scores and sums are fp32; bf16 weights are rounded to bf16 for the product
  * with v.  Workspace: at_grpo_prefix_attention_workspace_bytes (0 on invalid arguments; no pointer in kv is read).
  * More than some 6 * 10^7 pairs of a key head with a sequence, group or tile of 16 to 128 rows are
  * AT_GRPO_EUNSUPPORTED.

@@ -2301,7 +2301,7 @@ int attend(const at_grpo_kv* kv, int32_t n_tok, int32_t Hq, const at_grpo_rows* 
            const at_grpo_rows* out, float* lse, int32_t* data_error, void* workspace, size_t workspace_bytes, void* hip_stream) {
   Plan plan;
   ATG_TRY(make_plan<TREE>(kv, n_tok, Hq, max_q, &plan));
-  if (!(scale > 0.f) || !isfinite(scale)) return AT_GRPO_EINVAL;
+  if (!(scale > 0.f) || !isfinite(scale * kLog2e)) return AT_GRPO_EINVAL;
   KvView view;
   ATG_TRY(check_kv(kv, n_tok, &view));
   if (n_tok == 0) return AT_GRPO_OK;
