@@ -2,7 +2,8 @@
 //
 // A sequence holds ceil(tokens / page) pages, so a step takes or gives the difference of two such counts, and where in the ring a
 // sequence's pages come from is a sum over the sequences in front of it, as is the place of its tokens among the new ones.  There is next
-// to nothing to read (20 bytes a sequence, 28 written a token): what a call takes is launches and loads one behind the other.
+// to nothing to move (12 bytes a sequence read, 16 with `keep`, and 8 written; a token's parent read, 4, and up to 24 written): what a call takes is launches and loads
+// one behind the other.
 //   k_plan             up to 2048 sequences, in one launch: every workgroup adds up all sequences by itself, keeps the sums in LDS, and writes its
 //                      share of the tokens, the sequences and the pages moved; a new page's id it reads where it stands in the ring.  Where an output is its
 //                      input itself it may only be written once every workgroup has read that: by a single workgroup then, while the tokens are few
