@@ -81,7 +81,7 @@ enum {
   AT_GRPO_DATA_POSITION = 64,    /* position outside the rotation table               */
   AT_GRPO_DATA_TREE = 128,       /* a parent that does not stand in front of its token, a tree of more than 64 */
   AT_GRPO_DATA_POOL = 256,       /* a pool that has too few pages, or whose state no pool can have */
-  AT_GRPO_DATA_RULE = 512        /* a penalty, temperature, bias list or mask that is none */
+  AT_GRPO_DATA_RULE = 512        /* a penalty, temperature or row of masks that is none */
 };
 
 /* Bits of clip_mask[t] (Eq. 2's clip, decided in log space on d = logp - old_logp, one fp32
